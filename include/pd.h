@@ -27,7 +27,8 @@
  *  - A zero outer extent (rows == 0, M == 0, N == 0, batch == 0) is PD_OK and
  *    launches nothing; a zero reduction extent (cols == 0, K == 0) is
  *    PD_ERR_BAD_SHAPE.
- *  - Results are deterministic: no atomics, fixed reduction trees.
+ *  - Results are deterministic: fixed reduction trees, and no atomics but integer
+ *    sums in shared memory, which do not depend on their order.
  *  - The current device must be compute capability 10.x, else PD_ERR_UNSUPPORTED.
  *  - There is no CPU fallback of any kind.
  */
@@ -370,6 +371,138 @@ pd_status pd_encoder_layer_fwd_profiled(const pd_encoder_layer_desc* desc,
                                         const pd_encoder_layer_weights* weights, const void* x, void* y,
                                         void* workspace, size_t workspace_bytes, cudaStream_t stream,
                                         float* stage_ms);
+
+/* ---- a paged key/value cache, and the operators of a decoder that reads it ----
+ * (no counterpart in the paper, whose models are run on whole sequences: these
+ * are what its layer operators "bmm", "softmax", "rmsnorm", "layernorm", "add"
+ * become when a model answers token by token.)
+ *
+ * The cache holds, for every token of every sequence, heads_kv keys and values of
+ * head_dim bf16 elements, in pages of page_size tokens.  Element (page, slot,
+ * head, d) of either cache lies at
+ *   page * page_stride + slot * slot_stride + head * head_stride + d
+ * elements from its base; both caches have the same strides, multiples of 8
+ * elements, so [pages, slots, heads, d] and [pages, heads, slots, d] both fit.
+ * block_table: int32 [batch, max_pages], dense: entry [b, i] is the page that
+ * holds the tokens i * page_size ... of sequence b.
+ * cu_q: int32 [batch + 1], ascending from 0: the new tokens of sequence b are the
+ * rows cu_q[b] ... cu_q[b+1] - 1 of the packed token tensors, of which `tokens`
+ * rows exist.  kv_len: int32 [batch]: tokens of sequence b in the cache, the new
+ * ones included, so that new token i of n sits at position kv_len[b] - n + i.
+ * All three live on the device and are read by the kernels: nothing about a
+ * batch's lengths passes through the host, and a captured graph can be replayed
+ * with other lengths.
+ *  - Rows of the token tensors from cu_q[batch] on are padding: not read as
+ *    tokens, and left as they were in outputs.
+ *  - Only what a query may see is read: pages that no key in view lies on may
+ *    have any entry (an evicted page, -1), and slots behind kv_len, or in front
+ *    of the window, may hold anything, NaN included.  An entry outside
+ *    [0, num_pages) is never followed: keys and values there count as zeros.
+ *  - What is visible to any query of a sequence has to be finite.
+ *  - The sequences' pages may be shared for reading (a common prefix). */
+typedef struct {
+  int32_t batch, tokens;               /* sequences; rows of the token tensors */
+  int32_t heads_q, heads_kv, head_dim; /* heads_q a multiple of heads_kv */
+  int32_t num_pages, page_size, max_pages;
+  int32_t max_q_len;   /* upper bounds of the new tokens and the cached tokens of a sequence, for sizing the */
+  int32_t max_kv_len;  /* launch: new tokens beyond max_q_len are not computed; longer caches only take longer */
+  int32_t window;      /* keys a query sees, its own position included; 0: all before it */
+  int32_t sinks;       /* first tokens of the sequence that stay visible whatever the window */
+  float scale;         /* of the scores, before the softmax; above 0 */
+  int64_t ld_q, ld_out;                           /* elements from token to token; head h at column h * head_dim */
+  int64_t page_stride, slot_stride, head_stride;  /* of both caches, in elements */
+} pd_paged_attention_desc;
+
+/* Appends the new tokens' keys and values to the cache:
+ *   k_cache[page, slot, h, :] = k_new[t, h, :]   (and v) for position p of token t,
+ *   page = block_table[b, p / page_size], slot = p % page_size.
+ * k_new, v_new: bf16 [tokens, heads_kv, head_dim] with ld_new elements from token to
+ * token (a column block of a packed projection); desc: batch, tokens, heads_kv,
+ * head_dim (a multiple of 8, at most 1024), num_pages, page_size (any), max_pages
+ * and the cache strides are used, the rest is ignored.  All pointers 16-byte
+ * aligned (the int32 arrays 4-byte), ld_new a multiple of 8, else
+ * PD_ERR_ALIGNMENT.  A token whose position lies in front of 0, beyond max_pages
+ * pages or on a page outside [0, num_pages) is dropped; tokens of different
+ * sequences must not map to the same slot.  tokens = 0 or batch = 0 is a no-op. */
+pd_status pd_kv_cache_append(const pd_paged_attention_desc* desc, const void* k_new, const void* v_new, int64_t ld_new,
+                             void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* cu_q,
+                             const int32_t* kv_len, cudaStream_t stream);
+
+/* Causal attention of the new tokens over the paged cache, which already holds
+ * their own keys and values (operators "bmm", "softmax", "bmm" again):
+ *   out[t, h] = sum_j softmax_j(scale * q[t, h] . k[j]) v[j]
+ * over the keys j visible from position p of token t: j <= p and, when window > 0,
+ * j > p - window or j < sinks; head h reads the cache head h / (heads_q / heads_kv).
+ * A query that sees nothing (position in front of 0) gets zeros.  q, out: bf16,
+ * strides in desc; out must not overlap an input.  head_dim 64 or 128,
+ * heads_q / heads_kv at most 64, page_size a power of two from 8 to 4096 (else
+ * PD_ERR_UNSUPPORTED).  Base pointers 16-byte aligned, strides multiples of 8
+ * elements (else PD_ERR_ALIGNMENT).  Scores, softmax statistics and sums are
+ * fp32; the exponentials are rounded to bf16 for the second product, which
+ * accumulates in fp32.
+ * workspace: 256-byte aligned, pd_attention_paged_workspace_bytes(desc) bytes (it
+ * depends on the desc alone and may be 0, as it is for an invalid desc), else PD_ERR_WORKSPACE_TOO_SMALL; when few rows meet long caches the keys
+ * are split over CTAs, whose partial sums a second kernel joins.  Two calls that
+ * may run at the same time need a workspace each. */
+size_t pd_attention_paged_workspace_bytes(const pd_paged_attention_desc* desc);
+pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc, const void* q, const void* k_cache,
+                                 const void* v_cache, const int32_t* block_table, const int32_t* cu_q,
+                                 const int32_t* kv_len, void* out, void* workspace, size_t workspace_bytes,
+                                 cudaStream_t stream);
+
+/* What stands between two blocks of a layer, in one pass over memory (operators
+ * "rmsnorm", "layernorm", "add"): the norm after the block that produced y, its
+ * gate, the scaled residual sum, and the norm before the next block:
+ *   h[i,:] = alpha * x[i,:] + gate[i / gate_rows, :] * Post(y[i,:])
+ *   n[i,:] = Pre(h[i,:])
+ * Post and Pre are each PD_NORM_NONE (identity), PD_NORM_RMS
+ * (v / sqrt(mean v^2 + eps) * gamma) or PD_NORM_LAYER ((v - mean) / sqrt(var + eps) *
+ * gamma + beta, biased variance); gamma and beta are fp32 [cols], NULL for ones and
+ * zeros (and ignored by a norm that has no use for them).
+ * x, h: [rows, cols] of x_dtype; y, n: [rows, cols] of y_dtype; gate: [ceil(rows /
+ * gate_rows), cols] of y_dtype, or NULL for ones; all contiguous.  gate_rows >= 1:
+ * rows that share a gate (1: a gate for every row; rows: one for all).  All sums
+ * are fp32, n is computed from h before h is rounded.  h may alias x, n may
+ * alias y; nothing else may overlap.  h or n may be NULL when it is not wanted
+ * (not both); n is not computed for PD_NORM_NONE as Pre unless it is asked for.
+ * Pointers aligned to their elements (else PD_ERR_ALIGNMENT); 16-byte alignment
+ * and cols % 8 == 0, cols <= 32768 take the path that holds a row in registers. */
+enum { PD_NORM_NONE = 0, PD_NORM_RMS = 1, PD_NORM_LAYER = 2 };
+typedef struct {
+  int64_t rows, cols, gate_rows;
+  pd_dtype x_dtype, y_dtype;
+  int32_t post_norm, pre_norm;
+  float alpha, eps;
+} pd_norm_gate_residual_desc;
+pd_status pd_norm_gate_residual_norm(const pd_norm_gate_residual_desc* desc, const void* y, const void* x,
+                                     const void* gate, const float* post_gamma, const float* post_beta,
+                                     const float* pre_gamma, const float* pre_beta, void* h, void* n,
+                                     cudaStream_t stream);
+
+/* Draws one token per row of logits (operator "softmax", and what follows it when a
+ * model answers).  Row i, with T = temperature[i], is turned into weights
+ *   w[j] = exp((logits[i,j] - max) / T)
+ * which are ranked by logit, equal ones by index.  Kept are, one filter after the
+ * other: the first top_k[i]; of these the shortest leading run whose weight
+ * reaches top_p[i] of theirs; of these the ones with w[j] >= min_p[i].
+ * tokens[i] is the first index, in index order, at which the running sum of the
+ * kept weights exceeds u[i] of their total; probs[i] = its weight over that total.
+ *  - temperature, top_k, top_p, min_p: device vectors of one value a row, or NULL:
+ *    1, and no filter.  T <= 0 or NaN: the largest logit (lowest index).
+ *    top_k <= 0, top_p >= 1 (or NaN) and min_p <= 0 (or NaN) switch that filter off; the first rank
+ *    is always kept (top_p <= 0; min_p above 1 counts as 1).
+ *  - u: fp32 in [0, 1) (clamped into it; NaN counts as 0).
+ *  - -inf and NaN logits are never drawn; a row of nothing else gives token -1,
+ *    probability 0.  +inf logits share the whole weight.
+ *  - Weights are summed as integers in units of 2^-44 of the largest one, so
+ *    results do not depend on any order of summation; a token lighter
+ *    than half a unit (z more than 31 below the largest) is never drawn.
+ * logits: [rows, vocab] of `dtype` with row stride ld >= vocab elements, aligned to
+ * its elements; 1 <= vocab <= 327680 (else PD_ERR_UNSUPPORTED).  tokens: int32
+ * [rows]; probs: fp32 [rows] or NULL.  rows = 0 is a no-op. */
+pd_status pd_sample(const void* logits, pd_dtype dtype, int64_t rows, int64_t vocab, int64_t ld,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                    const float* u, int32_t* tokens, float* probs, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -25,7 +25,8 @@ EXPORTS = (
     "pd_softmax", "pd_layernorm", "pd_rmsnorm", "pd_bias_gelu_residual", "pd_gemm_bf16", "pd_set_gemm_tile_mode", "pd_attention_fwd",
     "pd_encoder_layer_workspace_bytes", "pd_encoder_layer_workspace_layout", "pd_encoder_layer_fwd", "pd_encoder_layer_stage_count",
     "pd_encoder_layer_stage_name", "pd_encoder_layer_fwd_profiled", "pd_encoder_layer_static_scratch_bytes",
-    "pd_encoder_layer_fwd_static",
+    "pd_encoder_layer_fwd_static", "pd_kv_cache_append", "pd_attention_paged_workspace_bytes",
+    "pd_attention_paged_fwd", "pd_norm_gate_residual_norm", "pd_sample",
 )
 
 
@@ -46,6 +47,19 @@ class EncoderLayerWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in (
         "w_qkv", "w_o", "w_ffn1", "w_ffn2", "b_qkv", "b_o", "b_ffn1", "b_ffn2",
         "ln1_gamma", "ln1_beta", "ln2_gamma", "ln2_beta")]
+
+
+class PagedAttentionDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "tokens", "heads_q", "heads_kv", "head_dim", "num_pages", "page_size", "max_pages", "max_q_len",
+        "max_kv_len", "window", "sinks")] + [("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+            "ld_q", "ld_out", "page_stride", "slot_stride", "head_stride")]
+
+
+class NormGateResidualDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "cols", "gate_rows")] + [
+        (n, ctypes.c_int32) for n in ("x_dtype", "y_dtype", "post_norm", "pre_norm")] + [
+            (n, ctypes.c_float) for n in ("alpha", "eps")]
 
 
 def _load() -> ctypes.CDLL:
@@ -101,6 +115,16 @@ def _load() -> ctypes.CDLL:
     lib.pd_encoder_layer_stage_name.restype = ctypes.c_char_p
     lib.pd_encoder_layer_fwd_profiled.argtypes = lib.pd_encoder_layer_fwd.argtypes + [ctypes.POINTER(ctypes.c_float)]
     lib.pd_encoder_layer_fwd_profiled.restype = st
+    paged = ctypes.POINTER(PagedAttentionDesc)
+    lib.pd_kv_cache_append.argtypes = [paged, vp, vp, i64, vp, vp, vp, vp, vp, vp]; lib.pd_kv_cache_append.restype = st
+    lib.pd_attention_paged_workspace_bytes.argtypes = [paged]
+    lib.pd_attention_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.pd_attention_paged_fwd.argtypes = [paged, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.pd_attention_paged_fwd.restype = st
+    lib.pd_norm_gate_residual_norm.argtypes = [ctypes.POINTER(NormGateResidualDesc)] + [vp] * 10
+    lib.pd_norm_gate_residual_norm.restype = st
+    lib.pd_sample.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.pd_sample.restype = st
     return lib
 
 
@@ -427,3 +451,195 @@ def pd_debug_set_wait_limit_ns(limit_ns: int) -> None:
 def pd_debug_withhold_loads(on: bool) -> None:
     """Test switch: the single-CTA contraction kernel's producer issues no load, so a bounded wait runs out."""
     _check(_lib.pd_debug_withhold_loads(int(bool(on))), "pd_debug_withhold_loads")
+
+
+# ---- a paged key/value cache and the operators of a decoder that reads it ----------------------------------------
+# These bindings run on the device of their first tensor, whichever is current, and on that device's current stream
+# unless one is given; every tensor has to live there.
+
+def _on(device: torch.device, t, dtypes, name: str, *, contiguous: bool = True) -> int | None:
+    """Address of ``t`` (None for None) after checking its device, type and, unless told otherwise, density."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise TypeError(f"{name} must be a tensor on {device}")
+    if t.dtype not in (dtypes if isinstance(dtypes, tuple) else (dtypes,)):
+        raise TypeError(f"{name} must be {dtypes}, got {t.dtype}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _cuda_device(t, name: str) -> torch.device:
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError(f"{name} must be a CUDA tensor")
+    return t.device
+
+
+def _stream_on(device: torch.device, stream) -> int:
+    if stream is not None and stream.device != device:
+        raise ValueError(f"stream must belong to {device}")
+    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+
+def _token_stride(t: torch.Tensor, name: str) -> int:
+    """Elements from token to token of [tokens, heads, head_dim] whose heads lie side by side."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim]")
+    _, heads, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the heads of a token must lie side by side")
+    return t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def _paged_desc(device, k_cache, v_cache, block_table, cu_q, kv_len) -> tuple[PagedAttentionDesc, list[int]]:
+    ptrs = [_on(device, k_cache, torch.bfloat16, "k_cache", contiguous=False),
+            _on(device, v_cache, torch.bfloat16, "v_cache", contiguous=False),
+            _on(device, block_table, torch.int32, "block_table"), _on(device, cu_q, torch.int32, "cu_q"),
+            _on(device, kv_len, torch.int32, "kv_len")]
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or any(
+            k_cache.shape[i] > 1 and k_cache.stride(i) != v_cache.stride(i) for i in range(4)):
+        raise ValueError("k_cache and v_cache must be [pages, page_size, heads, head_dim] with the same strides")
+    if k_cache.shape[3] > 1 and k_cache.stride(3) != 1:
+        raise ValueError("the elements of a cached head must be contiguous")
+    if block_table.dim() != 2 or cu_q.dim() != 1 or kv_len.dim() != 1:
+        raise ValueError("block_table must be [batch, max_pages], cu_q [batch + 1], kv_len [batch]")
+    batch = kv_len.shape[0]
+    if block_table.shape[0] != batch or cu_q.shape[0] != batch + 1:
+        raise ValueError("block_table must be [batch, max_pages], cu_q [batch + 1], kv_len [batch]")
+    d = PagedAttentionDesc()
+    d.batch, d.max_pages = batch, block_table.shape[1]
+    d.num_pages, d.page_size, d.heads_kv, d.head_dim = k_cache.shape
+    # strides of extents of one are never used; the library still asks for legal ones
+    tight = (d.page_size * d.heads_kv * d.head_dim, d.heads_kv * d.head_dim, d.head_dim)
+    d.page_stride, d.slot_stride, d.head_stride = (
+        k_cache.stride(i) if k_cache.shape[i] > 1 else tight[i] for i in range(3))
+    return d, ptrs
+
+
+def pd_kv_cache_append(k_new, v_new, k_cache, v_cache, block_table, cu_q, kv_len, stream=None) -> None:
+    """Writes the new tokens' keys and values (bf16 [tokens, heads_kv, head_dim], column blocks of a packed projection
+    will do) to their slots of the caches (bf16 [pages, page_size, heads_kv, head_dim], any page, slot and head
+    strides).  ``kv_len`` counts the new tokens already."""
+    device = _cuda_device(k_new, "k_new")
+    d, (kc, vc, table, cu, lens) = _paged_desc(device, k_cache, v_cache, block_table, cu_q, kv_len)
+    k = _on(device, k_new, torch.bfloat16, "k_new", contiguous=False)
+    v = _on(device, v_new, torch.bfloat16, "v_new", contiguous=False)
+    if tuple(k_new.shape[1:]) != (d.heads_kv, d.head_dim) or v_new.shape != k_new.shape:
+        raise ValueError("k_new and v_new must be [tokens, heads_kv, head_dim]")
+    ld = _token_stride(k_new, "k_new")
+    if ld != _token_stride(v_new, "v_new"):
+        raise ValueError("k_new and v_new must have the same token stride")
+    d.tokens = k_new.shape[0]
+    with torch.cuda.device(device):
+        _check(_lib.pd_kv_cache_append(ctypes.byref(d), k, v, ld, kc, vc, table, cu, lens, _stream_on(device, stream)),
+               "pd_kv_cache_append")
+
+
+def pd_attention_paged_workspace_bytes(desc: PagedAttentionDesc) -> int:
+    return int(_lib.pd_attention_paged_workspace_bytes(ctypes.byref(desc)))
+
+
+def pd_attention_paged_fwd(q, k_cache, v_cache, block_table, cu_q, kv_len, *, max_q_len: int, max_kv_len: int,
+                           window: int = 0, sinks: int = 0, scale: float | None = None, out=None, workspace=None,
+                           stream=None) -> torch.Tensor:
+    """Causal attention of the packed new tokens q (bf16 [tokens, heads_q, head_dim]) over the paged caches, which hold
+    their keys and values already; ``window`` > 0 limits a query to that many last keys, plus the first ``sinks``.
+    ``scale`` defaults to head_dim ** -0.5.  Rows of q behind the last sequence are left as they are in ``out``."""
+    device = _cuda_device(q, "q")
+    d, (kc, vc, table, cu, lens) = _paged_desc(device, k_cache, v_cache, block_table, cu_q, kv_len)
+    qp = _on(device, q, torch.bfloat16, "q", contiguous=False)
+    d.ld_q = _token_stride(q, "q")
+    d.tokens, d.heads_q = q.shape[0], q.shape[1]
+    if q.shape[2] != d.head_dim:
+        raise ValueError("q and the caches must have the same head_dim")
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=device)
+    op = _on(device, out, torch.bfloat16, "out", contiguous=False)
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    d.ld_out = _token_stride(out, "out")
+    d.max_q_len, d.max_kv_len, d.window, d.sinks = max_q_len, max_kv_len, window, sinks
+    d.scale = d.head_dim ** -0.5 if scale is None else scale
+    if workspace is None:
+        nbytes = int(_lib.pd_attention_paged_workspace_bytes(ctypes.byref(d)))
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    else:
+        _on(device, workspace, torch.uint8, "workspace")
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    with torch.cuda.device(device):
+        _check(_lib.pd_attention_paged_fwd(ctypes.byref(d), qp, kc, vc, table, cu, lens, op, ws, ws_bytes,
+                                           _stream_on(device, stream)), "pd_attention_paged_fwd")
+    return out
+
+
+_NORMS = {"none": 0, "rms": 1, "layer": 2}
+_PD_DTYPES = {torch.bfloat16: PD_BF16, torch.float32: PD_F32}
+
+
+def pd_norm_gate_residual_norm(y, x, *, gate=None, gate_rows: int | None = None, alpha: float = 1.0, eps: float = 1e-5,
+                               post_norm: str = "rms", post_gamma=None, post_beta=None, pre_norm: str = "rms",
+                               pre_gamma=None, pre_beta=None, h=None, n=None, stream=None):
+    """h = alpha * x + gate * post_norm(y), n = pre_norm(h); returns (h, n).
+
+    y, n: bf16 or fp32 [rows, cols] (the block's output, the next block's input); x, h: bf16 or fp32 (the residual
+    stream).  Norms: "none", "rms", "layer"; gamma and beta fp32 [cols] or None.  gate: y's type, [groups, cols] (or
+    [cols]), one row for every ``gate_rows`` rows (default: rows / groups rounded up)."""
+    device = _cuda_device(y, "y")
+    floats = (torch.bfloat16, torch.float32)
+    yp, xp = _on(device, y, floats, "y"), _on(device, x, floats, "x")
+    if y.dim() != 2 or x.shape != y.shape:
+        raise ValueError("y and x must be [rows, cols]")
+    rows, cols = y.shape
+    vectors = []
+    for name, t in (("post_gamma", post_gamma), ("post_beta", post_beta), ("pre_gamma", pre_gamma), ("pre_beta", pre_beta)):
+        vectors.append(_on(device, t, torch.float32, name))
+        if t is not None and t.numel() != cols:
+            raise ValueError(f"{name} must have {cols} elements")
+    gp = _on(device, gate, y.dtype, "gate")
+    if gate is not None:
+        if gate.dim() not in (1, 2) or gate.shape[-1] != cols:
+            raise ValueError("gate must be [groups, cols] or [cols]")
+        groups = gate.shape[0] if gate.dim() == 2 else 1
+        if gate_rows is None:
+            gate_rows = max(1, -(-rows // max(groups, 1)))
+        if gate_rows < 1 or -(-rows // gate_rows) > groups:
+            raise ValueError("gate has too few rows")
+    h = torch.empty_like(x) if h is None else h
+    n = torch.empty_like(y) if n is None else n
+    hp, np_ = _on(device, h, x.dtype, "h"), _on(device, n, y.dtype, "n")
+    if h.shape != x.shape or n.shape != y.shape:
+        raise ValueError("h and n must be [rows, cols]")
+    d = NormGateResidualDesc(rows, cols, gate_rows or 1, _PD_DTYPES[x.dtype], _PD_DTYPES[y.dtype], _NORMS[post_norm],
+                             _NORMS[pre_norm], alpha, eps)
+    with torch.cuda.device(device):
+        _check(_lib.pd_norm_gate_residual_norm(ctypes.byref(d), yp, xp, gp, *vectors, hp, np_,
+                                               _stream_on(device, stream)), "pd_norm_gate_residual_norm")
+    return h, n
+
+
+def pd_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=None, stream=None):
+    """Draws a token per row of logits (bf16 or fp32 [rows, vocab], rows of any stride) with the random numbers u
+    (fp32 [rows] in [0, 1)); temperature, top_p, min_p: fp32 [rows], top_k: int32 [rows], None for no such filter.
+    Returns (tokens int32 [rows], probs fp32 [rows])."""
+    device = _cuda_device(logits, "logits")
+    lp = _on(device, logits, (torch.bfloat16, torch.float32), "logits", contiguous=False)
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [rows, vocab] with contiguous rows")
+    rows, vocab = logits.shape
+    per_row = []
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("u", u, torch.float32)):
+        per_row.append(_on(device, t, dtype, name))
+        if t is not None and t.numel() != rows:
+            raise ValueError(f"{name} must have one value per row")
+    tokens = torch.empty(rows, dtype=torch.int32, device=device) if tokens is None else tokens
+    probs = torch.empty(rows, dtype=torch.float32, device=device) if probs is None else probs
+    tp, pp = _on(device, tokens, torch.int32, "tokens"), _on(device, probs, torch.float32, "probs")
+    if tokens.numel() != rows or probs.numel() != rows:
+        raise ValueError("tokens and probs must have one value per row")
+    ld = logits.stride(0) if rows > 1 else vocab
+    with torch.cuda.device(device):
+        _check(_lib.pd_sample(lp, _PD_DTYPES[logits.dtype], rows, vocab, ld, *per_row, tp, pp,
+                              _stream_on(device, stream)), "pd_sample")
+    return tokens, probs

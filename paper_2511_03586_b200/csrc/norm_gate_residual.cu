@@ -1,0 +1,308 @@
+// Norm after a block, gate, scaled residual sum and norm before the next block in one pass:
+//
+//   h[i,j] = alpha * x[i,j] + gate[i / gate_rows, j] * Post(y[i,:])[j]
+//   n[i,j] = Pre(h[i,:])[j]
+//
+// with Post and Pre nothing, RMSNorm or LayerNorm (biased variance, eps inside the root).  HBM-bound: x and y are read
+// once, h and n written once (8 bytes per element for bf16 streams, 12 with an fp32 residual stream), and the row
+// stays in registers from the first load to the last store.  Statistics are fp32; LayerNorm's second moment is taken
+// about the mean (no E[v^2] - mean^2 cancellation), which costs a reduction more than RMSNorm; each reduction is a
+// warp shuffle tree and, for rows that several warps share, one barrier.  Only h and n are rounded, and n is computed
+// from the unrounded h.
+//
+// A thread holds UNITS groups of 8 elements.  Rows of up to 512 columns take a warp, longer ones a CTA.
+#include <cmath>
+
+#include "pd_common.cuh"
+
+namespace pd {
+namespace {
+
+struct NormParams {
+  const void *y, *x, *gate;
+  const float *post_gamma, *post_beta, *pre_gamma, *pre_beta;
+  void *h, *n;
+  int64_t rows, gate_rows;
+  int cols, post_norm, pre_norm;
+  float alpha, eps;
+};
+
+struct Raw8f { float4 a, b; };
+// 8 elements as they lie in memory, and as floats
+__device__ __forceinline__ uint4 load_raw8(const __nv_bfloat16* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ Raw8f load_raw8(const float* p) {
+  return {__ldcs(reinterpret_cast<const float4*>(p)), __ldcs(reinterpret_cast<const float4*>(p) + 1)};
+}
+__device__ __forceinline__ void widen8(const uint4& r, float (&v)[8]) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void widen8(const Raw8f& r, float (&v)[8]) {
+  v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w; v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<uint32_t*>(&t);
+  }
+  __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+  __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+}
+__device__ __forceinline__ void load_vec8(const float* p, float (&v)[8]) {  // a parameter vector: stays cached
+  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ uint4 load_gate8(const __nv_bfloat16* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ Raw8f load_gate8(const float* p) {
+  return {__ldg(reinterpret_cast<const float4*>(p)), __ldg(reinterpret_cast<const float4*>(p) + 1)};
+}
+
+// Sums of two values over the row's threads.
+template <int NW>
+__device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*scratch)[NW], int slot) {
+  a = warp_sum(a);
+  b = warp_sum(b);
+  if constexpr (NW == 1) return make_float2(a, b);
+  if ((threadIdx.x & 31) == 0) scratch[slot][threadIdx.x >> 5] = make_float2(a, b);
+  __syncthreads();
+  float2 r = scratch[slot][0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) { r.x += scratch[slot][w].x; r.y += scratch[slot][w].y; }
+  return r;
+}
+
+// v <- norm(v) over the row that THREADS threads hold, elements beyond the row left alone.
+template <int UNITS, int THREADS>
+__device__ __forceinline__ void norm_row(float (&v)[UNITS][8], int t, int units, int kind, float inv_cols, float eps,
+                                         const float* gamma, const float* beta, float2 (*scratch)[THREADS / 32], int& slot) {
+  constexpr int NW = THREADS / 32;
+  if (kind == PD_NORM_NONE) return;
+  float shift = 0.f;
+  if (kind == PD_NORM_LAYER) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)
+      if (t + i * THREADS < units)
+        sum += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
+    shift = block_sum2<NW>(sum, 0.f, scratch, slot).x * inv_cols;
+    slot ^= 1;
+  }
+  float sum = 0.f, q = 0.f;
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i)
+    if (t + i * THREADS < units)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float d = v[i][j] - shift;
+        v[i][j] = d;
+        sum += d;
+        q = fmaf(d, d, q);
+      }
+  const float2 m = block_sum2<NW>(sum, q, scratch, slot);
+  slot ^= 1;
+  const float rest = kind == PD_NORM_LAYER ? m.x * inv_cols : 0.f;
+  const float rstd = rsqrtf(fmaxf(m.y * inv_cols - rest * rest, 0.f) + eps);
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    const int c = t + i * THREADS;
+    if (c < units) {
+      float gm[8];
+      if (gamma) {
+        load_vec8(gamma + 8 * c, gm);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - rest) * (rstd * gm[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - rest) * rstd;
+      }
+      if (kind == PD_NORM_LAYER && beta) {
+        load_vec8(beta + 8 * c, gm);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] += gm[j];
+      }
+    }
+  }
+}
+
+template <typename TX, typename TY, int UNITS, int THREADS_PER_ROW, int THREADS_PER_CTA>
+__global__ void __launch_bounds__(THREADS_PER_CTA)
+norm_gate_residual_rows_in_registers(const NormParams p) {
+  constexpr int ROWS = THREADS_PER_CTA / THREADS_PER_ROW;
+  __shared__ float2 scratch[2][THREADS_PER_ROW / 32];
+  const int t = threadIdx.x % THREADS_PER_ROW;
+  const int units = p.cols >> 3;
+  const float inv_cols = 1.0f / (float)p.cols;
+  griddep_wait();
+  griddep_launch_dependents();
+  int slot = 0;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS_PER_ROW; row < p.rows;
+       row += (int64_t)gridDim.x * ROWS) {
+    const TY* y = static_cast<const TY*>(p.y) + row * p.cols;
+    const TX* x = static_cast<const TX*>(p.x) + row * p.cols;
+    decltype(load_raw8(y)) ry[UNITS];
+    decltype(load_raw8(x)) rx[UNITS];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)
+      if (t + i * THREADS_PER_ROW < units) ry[i] = load_raw8(y + 8 * (t + i * THREADS_PER_ROW));
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)
+      if (t + i * THREADS_PER_ROW < units) rx[i] = load_raw8(x + 8 * (t + i * THREADS_PER_ROW));
+    float v[UNITS][8];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) widen8(ry[i], v[i]);
+    norm_row<UNITS, THREADS_PER_ROW>(v, t, units, p.post_norm, inv_cols, p.eps, p.post_gamma, p.post_beta, scratch, slot);
+    const TY* gate = p.gate ? static_cast<const TY*>(p.gate) + (row / p.gate_rows) * p.cols : nullptr;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int c = t + i * THREADS_PER_ROW;
+      if (c < units) {
+        float xv[8];
+        widen8(rx[i], xv);
+        if (gate) {
+          float gv[8];
+          widen8(load_gate8(gate + 8 * c), gv);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = fmaf(v[i][j], gv[j], p.alpha * xv[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = fmaf(p.alpha, xv[j], v[i][j]);
+        }
+        if (p.h) store8(static_cast<TX*>(p.h) + row * p.cols + 8 * c, v[i]);
+      }
+    }
+    if (p.n) {
+      norm_row<UNITS, THREADS_PER_ROW>(v, t, units, p.pre_norm, inv_cols, p.eps, p.pre_gamma, p.pre_beta, scratch, slot);
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int c = t + i * THREADS_PER_ROW;
+        if (c < units) store8(static_cast<TY*>(p.n) + row * p.cols + 8 * c, v[i]);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float widen(float v) { return v; }
+
+// Any length and alignment: a CTA per row that reads the row again for every statistic (from L2).
+template <typename TX, typename TY>
+__global__ void __launch_bounds__(256) norm_gate_residual_generic(const NormParams p) {
+  __shared__ float2 scratch[2][8];
+  griddep_wait();
+  griddep_launch_dependents();
+  int slot = 0;
+  const float inv_cols = 1.0f / (float)p.cols;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const TY* y = static_cast<const TY*>(p.y) + row * p.cols;
+    const TX* x = static_cast<const TX*>(p.x) + row * p.cols;
+    const TY* gate = p.gate ? static_cast<const TY*>(p.gate) + (row / p.gate_rows) * p.cols : nullptr;
+    auto stats = [&](int kind, auto&& value, float& mean, float& rstd) {
+      mean = 0.f;
+      rstd = 1.f;
+      if (kind == PD_NORM_NONE) return;
+      float shift = 0.f;
+      if (kind == PD_NORM_LAYER) {
+        float s = 0.f;
+        for (int j = threadIdx.x; j < p.cols; j += 256) s += value(j);
+        shift = block_sum2<8>(s, 0.f, scratch, slot).x * inv_cols;
+        slot ^= 1;
+      }
+      float s = 0.f, q = 0.f;
+      for (int j = threadIdx.x; j < p.cols; j += 256) {
+        const float d = value(j) - shift;
+        s += d;
+        q = fmaf(d, d, q);
+      }
+      const float2 m = block_sum2<8>(s, q, scratch, slot);
+      slot ^= 1;
+      const float rest = kind == PD_NORM_LAYER ? m.x * inv_cols : 0.f;
+      mean = shift + rest;
+      rstd = rsqrtf(fmaxf(m.y * inv_cols - rest * rest, 0.f) + p.eps);
+    };
+    auto affine = [&](int kind, float v, float mean, float rstd, const float* gamma, const float* beta, int j) {
+      if (kind == PD_NORM_NONE) return v;
+      v = (v - mean) * (rstd * (gamma ? gamma[j] : 1.f));
+      return kind == PD_NORM_LAYER && beta ? v + beta[j] : v;
+    };
+    float post_mean, post_rstd, pre_mean = 0.f, pre_rstd = 1.f;
+    stats(p.post_norm, [&](int j) { return widen(y[j]); }, post_mean, post_rstd);
+    auto h = [&](int j) {
+      const float v = affine(p.post_norm, widen(y[j]), post_mean, post_rstd, p.post_gamma, p.post_beta, j);
+      return fmaf(v, gate ? widen(gate[j]) : 1.f, p.alpha * widen(x[j]));
+    };
+    if (p.n) stats(p.pre_norm, h, pre_mean, pre_rstd);
+    for (int j = threadIdx.x; j < p.cols; j += 256) {
+      const float v = h(j);
+      const float n = affine(p.pre_norm, v, pre_mean, pre_rstd, p.pre_gamma, p.pre_beta, j);
+      if (p.h) store_out1(static_cast<TX*>(p.h), row * p.cols + j, v);
+      if (p.n) store_out1(static_cast<TY*>(p.n), row * p.cols + j, n);
+    }
+  }
+}
+
+template <typename TX, typename TY, int UNITS, int THREADS, int CTA = THREADS>
+void launch_rows(const NormParams& p, cudaStream_t s) {
+  constexpr int kRows = CTA / THREADS;
+  const int64_t ctas = (p.rows + kRows - 1) / kRows;
+  const int grid = (int)(ctas < 0x7fffffff ? ctas : 0x7fffffff);
+  launch_pdl(norm_gate_residual_rows_in_registers<TX, TY, UNITS, THREADS, CTA>, dim3(grid), dim3(CTA), 0, s, p);
+}
+
+template <typename TX, typename TY>
+pd_status launch(const NormParams& p, cudaStream_t s) {
+  const bool vec_ok = p.cols % 8 == 0 && p.cols <= 32768 && aligned16(p.y) && aligned16(p.x) && aligned16(p.gate) &&
+                      aligned16(p.h) && aligned16(p.n) && aligned16(p.post_gamma) && aligned16(p.post_beta) &&
+                      aligned16(p.pre_gamma) && aligned16(p.pre_beta);
+  logf("norm gate residual norm %lld x %d: %s", (long long)p.rows, p.cols,
+       !vec_ok ? "scalar path (unaligned, ragged or very long rows)" : p.cols <= 512 ? "one warp per row, row in registers"
+       : "one CTA per row, row in registers");
+  if (!vec_ok) {
+    const int64_t cap = (int64_t)sm_count() * 8;
+    launch_pdl(norm_gate_residual_generic<TX, TY>, dim3((unsigned)(p.rows < cap ? p.rows : cap)), dim3(256), 0, s, p);
+  } else if (p.cols <= 256) launch_rows<TX, TY, 1, 32, 64>(p, s);
+  else if (p.cols <= 512) launch_rows<TX, TY, 2, 32, 64>(p, s);
+  else if (p.cols <= 1024) launch_rows<TX, TY, 2, 64>(p, s);
+  else if (p.cols <= 2048) launch_rows<TX, TY, 2, 128>(p, s);
+  else if (p.cols <= 4096) launch_rows<TX, TY, 2, 256>(p, s);
+  else if (p.cols <= 8192) launch_rows<TX, TY, 2, 512>(p, s);
+  else if (p.cols <= 16384) launch_rows<TX, TY, 4, 512>(p, s);
+  else launch_rows<TX, TY, 4, 1024>(p, s);
+  return check_launch();
+}
+
+}  // namespace
+}  // namespace pd
+
+extern "C" pd_status pd_norm_gate_residual_norm(const pd_norm_gate_residual_desc* desc, const void* y, const void* x,
+                                                const void* gate, const float* post_gamma, const float* post_beta,
+                                                const float* pre_gamma, const float* pre_beta, void* h, void* n,
+                                                cudaStream_t stream) {
+  if (!desc || !y || !x || (!h && !n)) return PD_ERR_NULL_POINTER;
+  const pd_norm_gate_residual_desc& d = *desc;
+  if (d.rows < 0 || d.cols <= 0 || d.cols > 0x7fffffff || !(d.eps >= 0.f) || !std::isfinite(d.alpha)) return PD_ERR_BAD_SHAPE;
+  if (gate && d.gate_rows < 1) return PD_ERR_BAD_SHAPE;
+  auto is_dtype = [](int t) { return t == PD_BF16 || t == PD_F32; };
+  auto is_norm = [](int k) { return k >= PD_NORM_NONE && k <= PD_NORM_LAYER; };
+  if (!is_dtype(d.x_dtype) || !is_dtype(d.y_dtype) || !is_norm(d.post_norm) || !is_norm(d.pre_norm)) return PD_ERR_BAD_SHAPE;
+  auto bits = [](const void* q) { return reinterpret_cast<uintptr_t>(q); };
+  const uintptr_t xb = bits(x) | bits(h), yb = bits(y) | bits(n) | bits(gate);
+  if ((xb & (d.x_dtype == PD_F32 ? 3u : 1u)) || (yb & (d.y_dtype == PD_F32 ? 3u : 1u)) ||
+      ((bits(post_gamma) | bits(post_beta) | bits(pre_gamma) | bits(pre_beta)) & 3u))
+    return PD_ERR_ALIGNMENT;
+  if (d.rows == 0) return PD_OK;
+  if (pd_status st = pd::require_sm100(); st != PD_OK) return st;
+  pd::NormParams p{y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta, h, n, d.rows, gate ? d.gate_rows : 1,
+                   (int)d.cols, d.post_norm, d.pre_norm, d.alpha, d.eps};
+  if (d.x_dtype == PD_BF16)
+    return d.y_dtype == PD_BF16 ? pd::launch<__nv_bfloat16, __nv_bfloat16>(p, stream) : pd::launch<__nv_bfloat16, float>(p, stream);
+  return d.y_dtype == PD_BF16 ? pd::launch<float, __nv_bfloat16>(p, stream) : pd::launch<float, float>(p, stream);
+}

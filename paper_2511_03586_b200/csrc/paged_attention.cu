@@ -1,0 +1,158 @@
+// Entry point of the attention over the paged cache: argument checks, the choice of kernel and of the number of key
+// splits, and the kernel that joins the splits.
+#include <climits>
+#include <algorithm>
+#include <cmath>
+
+#include "paged_cache.cuh"
+
+namespace pd {
+namespace paged {
+namespace {
+
+// out[row] = sum_z w_z O_z / sum_z w_z,  w_z = 2^(lse_z - max lse): a warp per (token, head), lanes across head_dim.
+// HBM / L2-bound on the partial outputs, 4 bytes per element and split.
+template <int D>
+__global__ void __launch_bounds__(128) paged_attention_join(const Params p) {
+  const int lane = threadIdx.x & 31;
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t rows = (int64_t)p.tokens * p.heads_q;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int t = (int)(row / p.heads_q), h = (int)(row % p.heads_q);
+  // padding tokens, and tokens beyond max_q_len, have no partial results
+  const int b = find_sequence(p.cu_q, p.batch, t);
+  if (b >= p.batch || (unsigned)(t - __ldg(p.cu_q + b)) >= (unsigned)p.max_q_len) return;
+  const int per = D / 32;
+  float lse_max = -INFINITY;
+  for (int z = lane; z < p.splits; z += 32) lse_max = fmaxf(lse_max, p.part_lse[z * rows + row]);
+  lse_max = warp_max(lse_max);
+  float acc[per], sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < per; ++j) acc[j] = 0.f;
+  for (int z = 0; z < p.splits; ++z) {
+    const float lse = p.part_lse[z * rows + row];
+    if (lse == -INFINITY) continue;
+    const float w = ex2(lse - lse_max);
+    sum += w;
+    const float* o = p.part_o + (z * rows + row) * D + lane * per;
+#pragma unroll
+    for (int j = 0; j < per; ++j) acc[j] += w * o[j];
+  }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  uint32_t* out = reinterpret_cast<uint32_t*>(p.out + (int64_t)t * p.ld_out + (int64_t)h * D + lane * per);
+#pragma unroll
+  for (int j = 0; j < per; j += 2) out[j / 2] = pack_bf16(acc[j] * inv, acc[j + 1] * inv);
+}
+
+struct Plan {
+  int rows_per_tile;
+  int splits, min_split_tiles;  // key tiles of 64
+};
+
+bool valid(const pd_paged_attention_desc& d) {
+  return d.batch >= 0 && d.tokens >= 0 && d.heads_q > 0 && d.heads_kv > 0 && d.head_dim > 0 &&
+         d.heads_q % d.heads_kv == 0 && d.num_pages > 0 && d.page_size > 0 && d.max_pages > 0 && d.max_q_len >= 0 &&
+         d.max_kv_len >= 0 && d.window >= 0 && d.sinks >= 0 && std::isfinite(d.scale) && d.scale > 0.f;
+}
+bool supported(const pd_paged_attention_desc& d) {
+  return (d.head_dim == 64 || d.head_dim == 128) && d.heads_q / d.heads_kv <= 64 && d.page_size >= 8 &&
+         d.page_size <= 4096 && (d.page_size & (d.page_size - 1)) == 0 &&
+         (int64_t)d.max_pages * d.page_size <= INT_MAX - 4096 && d.batch <= 65535 && d.heads_kv <= 65535;
+}
+
+// Depends on the desc alone (the workspace size follows from it).
+Plan plan(const pd_paged_attention_desc& d) {
+  constexpr int kSms = 148, kTile = 64;
+  Plan pl{};
+  const int64_t group = d.heads_q / d.heads_kv, rows = d.max_q_len * group;
+  pl.rows_per_tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  const int64_t row_tiles = (rows + pl.rows_per_tile - 1) / pl.rows_per_tile;
+  const int64_t items = row_tiles * d.heads_kv * d.batch;  // CTAs without splitting
+  int64_t keys = d.max_kv_len;
+  if (d.window > 0) keys = std::min<int64_t>(keys, (int64_t)d.window + d.sinks + d.max_q_len);
+  const int64_t tiles = (keys + kTile - 1) / kTile;
+  // Two CTAs fit on an SM; about six waves of them even out ragged lengths.  No share below min_split_tiles.
+  pl.min_split_tiles = 4;
+  int64_t want = items > 0 ? (kSms * 2 * 6 + items - 1) / items : 1;
+  if (items * 2 <= kSms * 2) pl.min_split_tiles = 2;
+  want = std::min<int64_t>(want, (tiles + pl.min_split_tiles - 1) / pl.min_split_tiles);
+  pl.splits = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 256);
+  return pl;
+}
+
+size_t workspace_bytes(const pd_paged_attention_desc& d) {
+  const Plan pl = plan(d);
+  if (pl.splits <= 1) return 0;
+  const size_t rows = (size_t)d.tokens * d.heads_q;
+  return pl.splits * rows * ((size_t)d.head_dim + 1) * sizeof(float);
+}
+
+}  // namespace
+}  // namespace paged
+}  // namespace pd
+
+extern "C" size_t pd_attention_paged_workspace_bytes(const pd_paged_attention_desc* desc) {
+  if (!desc || !pd::paged::valid(*desc) || !pd::paged::supported(*desc)) return 0;
+  if (desc->batch == 0 || desc->tokens == 0 || desc->max_q_len == 0) return 0;
+  return pd::paged::workspace_bytes(*desc);
+}
+
+extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc, const void* q, const void* k_cache,
+                                            const void* v_cache, const int32_t* block_table, const int32_t* cu_q,
+                                            const int32_t* kv_len, void* out, void* workspace, size_t workspace_bytes,
+                                            cudaStream_t stream) {
+  using namespace pd;
+  if (!desc) return PD_ERR_NULL_POINTER;
+  const pd_paged_attention_desc& d = *desc;
+  if (!paged::valid(d)) return PD_ERR_BAD_SHAPE;
+  if (!paged::supported(d)) return PD_ERR_UNSUPPORTED;
+  const int64_t row = (int64_t)d.heads_q * d.head_dim;
+  if (d.ld_q < row || d.ld_out < row || d.page_stride <= 0 || d.slot_stride <= 0 || d.head_stride <= 0)
+    return PD_ERR_BAD_SHAPE;
+  if (d.batch == 0 || d.tokens == 0 || d.max_q_len == 0) return PD_OK;
+  if (!q || !k_cache || !v_cache || !block_table || !cu_q || !kv_len || !out) return PD_ERR_NULL_POINTER;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) ||
+      ((d.ld_q | d.ld_out | d.page_stride | d.slot_stride | d.head_stride) & 7) != 0 ||
+      ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(cu_q) |
+        reinterpret_cast<uintptr_t>(kv_len)) & 3u) != 0)
+    return PD_ERR_ALIGNMENT;
+  const size_t need = paged::workspace_bytes(d);
+  if (need > 0) {
+    if (!workspace) return PD_ERR_NULL_POINTER;
+    if (workspace_bytes < need) return PD_ERR_WORKSPACE_TOO_SMALL;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return PD_ERR_ALIGNMENT;
+  }
+  if (pd_status st = require_sm100(); st != PD_OK) return st;
+
+  const paged::Plan pl = paged::plan(d);
+  paged::Params p{};
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.block_table = block_table; p.cu_q = cu_q; p.kv_len = kv_len;
+  p.status = device_status_ptr();
+  if (!p.status) return PD_ERR_CUDA;
+  p.ld_q = d.ld_q; p.ld_out = d.ld_out;
+  p.batch = d.batch; p.tokens = d.tokens; p.heads_q = d.heads_q; p.heads_kv = d.heads_kv; p.group = d.heads_q / d.heads_kv;
+  p.num_pages = d.num_pages; p.page_size = d.page_size; p.max_pages = d.max_pages;
+  while ((1 << p.page_shift) < d.page_size) ++p.page_shift;
+  p.max_q_len = d.max_q_len; p.window = d.window; p.sinks = d.sinks;
+  p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles;
+  p.scale_log2e = (float)((double)d.scale * 1.4426950408889634);
+  if (pl.splits > 1) {
+    p.part_o = static_cast<float*>(workspace);
+    p.part_lse = p.part_o + (size_t)pl.splits * d.tokens * d.heads_q * d.head_dim;
+  }
+  logf("paged attention batch %d tokens %d (max %d) heads %d/%d x %d: tiles of %d rows, %d key splits", d.batch, d.tokens,
+       d.max_q_len, d.heads_q, d.heads_kv, d.head_dim, pl.rows_per_tile, pl.splits);
+  if (pd_status st = paged::launch_rows(d, p, k_cache, v_cache, pl.rows_per_tile, stream); st != PD_OK) return st;
+  if (pl.splits > 1) {
+    const int64_t rows = (int64_t)d.tokens * d.heads_q;
+    const unsigned grid = (unsigned)((rows + 3) / 4);
+    if (d.head_dim == 64) launch_pdl(paged::paged_attention_join<64>, dim3(grid), dim3(128), 0, stream, p);
+    else launch_pdl(paged::paged_attention_join<128>, dim3(grid), dim3(128), 0, stream, p);
+    return check_launch();
+  }
+  return PD_OK;
+}
