@@ -1,6 +1,5 @@
 // Entry point of the attention over the paged cache: argument checks, the choice of kernel and of the number of key
 // splits, and the kernel that joins the splits.
-#include <climits>
 #include <algorithm>
 #include <cmath>
 
@@ -47,9 +46,11 @@ __global__ void __launch_bounds__(128) paged_attention_join(const Params p) {
 }
 
 struct Plan {
-  int rows_per_tile;
-  int splits, min_split_tiles;  // key tiles of 64
+  int rows_per_tile;            // 16, 32, 64: row kernel; 256: chunk kernel
+  int splits, min_split_tiles;  // in key tiles of the kernel (64, 128)
 };
+
+constexpr int kMaxPositions = 1 << 30;  // of a sequence's table, and rows of a cache head: sums of two stay in 32 bits
 
 bool valid(const pd_paged_attention_desc& d) {
   return d.batch >= 0 && d.tokens >= 0 && d.heads_q > 0 && d.heads_kv > 0 && d.head_dim > 0 &&
@@ -59,24 +60,32 @@ bool valid(const pd_paged_attention_desc& d) {
 bool supported(const pd_paged_attention_desc& d) {
   return (d.head_dim == 64 || d.head_dim == 128) && d.heads_q / d.heads_kv <= 64 && d.page_size >= 8 &&
          d.page_size <= 4096 && (d.page_size & (d.page_size - 1)) == 0 &&
-         (int64_t)d.max_pages * d.page_size <= INT_MAX - 4096 && d.batch <= 65535 && d.heads_kv <= 65535;
+         (int64_t)d.max_pages * d.page_size <= kMaxPositions && (int64_t)d.tokens * (d.heads_q / d.heads_kv) <= kMaxPositions &&
+         d.batch <= 65535 && d.heads_kv <= 65535;
 }
 
 // Depends on the desc alone (the workspace size follows from it).
 Plan plan(const pd_paged_attention_desc& d) {
-  constexpr int kSms = 148, kTile = 64;
+  constexpr int kSms = 148;
   Plan pl{};
-  const int64_t group = d.heads_q / d.heads_kv, rows = d.max_q_len * group;
-  pl.rows_per_tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  const int64_t group = d.heads_q / d.heads_kv, rows = std::min(d.max_q_len, d.tokens) * group;
+  pl.rows_per_tile = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
+  const bool chunk = pl.rows_per_tile == 256;
   const int64_t row_tiles = (rows + pl.rows_per_tile - 1) / pl.rows_per_tile;
   const int64_t items = row_tiles * d.heads_kv * d.batch;  // CTAs without splitting
   int64_t keys = d.max_kv_len;
   if (d.window > 0) keys = std::min<int64_t>(keys, (int64_t)d.window + d.sinks + d.max_q_len);
-  const int64_t tiles = (keys + kTile - 1) / kTile;
-  // Two CTAs fit on an SM; about six waves of them even out ragged lengths.  No share below min_split_tiles.
-  pl.min_split_tiles = 4;
-  int64_t want = items > 0 ? (kSms * 2 * 6 + items - 1) / items : 1;
-  if (items * 2 <= kSms * 2) pl.min_split_tiles = 2;
+  const int64_t tile = chunk ? 128 : 64, tiles = (keys + tile - 1) / tile;
+  // Row kernel: two CTAs fit on an SM; about six waves of them even out ragged lengths.  Chunk kernel: one CTA per SM, and
+  // splits only to fill the SMs.  No share below min_split_tiles.
+  int64_t want;
+  if (chunk) {
+    pl.min_split_tiles = 4;
+    want = items > 0 ? kSms / items : 1;
+  } else {
+    pl.min_split_tiles = items <= kSms ? 2 : 4;
+    want = items > 0 ? (kSms * 2 * 6 + items - 1) / items : 1;
+  }
   want = std::min<int64_t>(want, (tiles + pl.min_split_tiles - 1) / pl.min_split_tiles);
   pl.splits = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 256);
   return pl;
@@ -137,7 +146,7 @@ extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc,
   p.batch = d.batch; p.tokens = d.tokens; p.heads_q = d.heads_q; p.heads_kv = d.heads_kv; p.group = d.heads_q / d.heads_kv;
   p.num_pages = d.num_pages; p.page_size = d.page_size; p.max_pages = d.max_pages;
   while ((1 << p.page_shift) < d.page_size) ++p.page_shift;
-  p.max_q_len = d.max_q_len; p.window = d.window; p.sinks = d.sinks;
+  p.max_q_len = std::min(d.max_q_len, d.tokens); p.window = std::min(d.window, paged::kMaxPositions); p.sinks = d.sinks;
   p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles;
   p.scale_log2e = (float)((double)d.scale * 1.4426950408889634);
   if (pl.splits > 1) {
@@ -146,7 +155,9 @@ extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc,
   }
   logf("paged attention batch %d tokens %d (max %d) heads %d/%d x %d: tiles of %d rows, %d key splits", d.batch, d.tokens,
        d.max_q_len, d.heads_q, d.heads_kv, d.head_dim, pl.rows_per_tile, pl.splits);
-  if (pd_status st = paged::launch_rows(d, p, k_cache, v_cache, pl.rows_per_tile, stream); st != PD_OK) return st;
+  const pd_status launched = pl.rows_per_tile == 256 ? paged::launch_chunk(d, p, k_cache, v_cache, stream)
+                                                     : paged::launch_rows(d, p, k_cache, v_cache, pl.rows_per_tile, stream);
+  if (launched != PD_OK) return launched;
   if (pl.splits > 1) {
     const int64_t rows = (int64_t)d.tokens * d.heads_q;
     const unsigned grid = (unsigned)((rows + 3) / 4);

@@ -305,7 +305,7 @@ pd_status launch(const pd_paged_attention_desc& d, const Params& p, const CUtens
   using C = RowsConfig<D, WR, WK>;
   static PerDeviceFlag smem_allowed;
   if (pd_status st = allow_dynamic_smem(paged_attention_rows_kernel<D, WR, WK>, C::kSmem, smem_allowed); st != PD_OK) return st;
-  const int64_t row_tiles = ((int64_t)d.max_q_len * p.group + C::kRows - 1) / C::kRows;
+  const int64_t row_tiles = ((int64_t)p.max_q_len * p.group + C::kRows - 1) / C::kRows;
   if (row_tiles * p.splits > 0x7fffffff) return PD_ERR_BAD_SHAPE;
   launch_pdl(paged_attention_rows_kernel<D, WR, WK>, dim3((unsigned)(row_tiles * p.splits), d.heads_kv, d.batch),
              dim3(C::kThreads), C::kSmem, s, tk, tv, p);

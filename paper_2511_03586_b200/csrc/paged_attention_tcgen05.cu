@@ -1,0 +1,403 @@
+// Attention over the paged cache for chunks of tokens, on the tcgen05 tensor cores:
+//
+//   out[t, h] = sum_j softmax_j(scale * q[t, h] . k[j]) v[j],   j visible from token t's position
+//
+// A CTA takes two consecutive tiles ("slots") of 128 rows of one cache head (a row is a token and one of the query heads
+// that share the cache head) and walks the key tiles of 128 keys that any of them sees; both slots read the same K and V
+// tiles, which halves what comes from L2.  While one slot's scores are being exponentiated the other slot's products
+// run.
+//
+//   warps 0-3, 4-7 : softmax of slot 0 / 1, one thread per row.  Read the row's 128 scores from tensor memory once, mask
+//                    them in tiles that are not in view as a whole, and form p = 2^(s * scale * log2 e - m).  m is a
+//                    reference that is raised only when a score exceeds it by more than 2^8 (then the output accumulator
+//                    and the row sum are rescaled through tensor memory); sums stay fp32, p is rounded to bf16 and goes
+//                    back over the scores' columns, where the second product reads it as its A operand.  At the end the
+//                    same warps divide by the sum and write the rows.
+//   warps 8, 9     : MMA issuers of slot 0 / 1 (the warp walks the loop, one elected lane issues): S = Q K^T
+//                    (128 x 128 x D), O += P V (128 x D x 128).  The next S overwrites P's columns, so it is issued when
+//                    the product that reads P has completed.
+//   warp 10        : producer: looks the pages up and copies K and V tiles by TMA, one box per page, into a ring of four
+//                    32 KiB (head_dim 128) stages, K and V in turn.
+//
+// Values of keys in nobody's view may be anything (stale slots of a page, NaN) and would poison the product with
+// probability 0 * NaN: in the tiles that hold such keys the issuers overwrite them with zeros first.
+// With `splits` > 1 the key tiles are shared out over that many CTAs, whose partial outputs paged_attention_join joins.
+#include "paged_cache.cuh"
+
+namespace pd {
+namespace paged {
+namespace {
+
+constexpr int kTile = 128;             // keys per tile, and rows per slot
+constexpr int kSlots = 2;
+constexpr int kSoftmaxWarps = 4;       // per slot
+constexpr int kIssuer0 = kSlots * kSoftmaxWarps;
+constexpr int kProducer = kIssuer0 + kSlots;
+constexpr int kThreads = 32 * (kProducer + 1);
+constexpr int kStages = 4;
+constexpr int kHalf = kTile * 128;     // 64 columns of a tile: 128 lines of 128 bytes
+constexpr float kRaise = 8.f;          // powers of two by which a score may exceed the row's reference
+
+template <int D>
+struct ChunkConfig {
+  static constexpr int kTensor = kTile * D * 2;  // a Q, K or V tile
+  static constexpr int kSmem = kSlots * kTensor + kStages * kTensor + 1024 /*barriers*/ + 1024 /*alignment*/;
+  // tensor-memory columns: scores (and probabilities) of slot s at 128 s, output of slot s at 256 + D s
+  static constexpr uint32_t kColO = 256, kCols = 512;
+};
+
+// The view of one slot: keys [lo, hi) and sinks [0, sink_hi) are seen by some of its rows.
+struct SlotView {
+  int lo, hi, sink_hi;
+  int first_pos, last_pos;
+  bool active;
+  __device__ __forceinline__ bool needs(int key0) const {
+    return active && ((key0 < hi && key0 + kTile > lo) || key0 < sink_hi);
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                             const Params p) {
+  using C = ChunkConfig<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t sQ = base, ring = sQ + kSlots * C::kTensor, bars = ring + kStages * C::kTensor;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 32u + 8u * s; };
+  auto q_full = [&](int s) { return bars + 64u + 8u * s; };
+  auto s_full = [&](int s) { return bars + 80u + 8u * s; };
+  auto p_full = [&](int s) { return bars + 96u + 8u * s; };
+  auto o_full = [&](int s) { return bars + 112u + 8u * s; };   // every product of the tile's output has completed
+  auto drained = [&](int s) { return bars + 128u + 8u * s; };
+  uint8_t* ctrl = smem_raw + (bars - smem_u32(smem_raw)) + 512;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kSlots); }
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(q_full(s), kSoftmaxWarps); mbar_init(s_full(s), 1); mbar_init(p_full(s), kSoftmaxWarps);
+      mbar_init(o_full(s), 1); mbar_init(drained(s), 1);
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == kProducer) {
+    tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::kCols);
+    tmem_relinquish_alloc_permit();
+    if (lane == 0) { prefetch_tensormap(&tmap_k); prefetch_tensormap(&tmap_v); }
+  }
+  tcgen05_fence_before_sync();
+  __syncthreads();
+  tcgen05_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  griddep_wait();
+  griddep_launch_dependents();
+
+  const int split = blockIdx.x % p.splits;
+  const int pairs = gridDim.x / p.splits;
+  const int pair = pairs - 1 - blockIdx.x / p.splits;  // the last rows see the most keys: they go first
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  const Sequence seq = load_sequence(p, b);
+  const int all_rows = seq.n * p.group, row0 = pair * kSlots * kTile;
+  if (row0 < all_rows) {
+    const int last_row = min(row0 + kSlots * kTile, all_rows) - 1;
+    const KeyTiles kt = key_tiles(p, seq.pos0 + row0 / p.group, seq.pos0 + last_row / p.group, seq.length, kTile);
+    int begin, end;
+    split_range(p, kt.n, split, begin, end);
+    auto slot_view = [&](int s) {
+      SlotView v;
+      const int r0 = row0 + s * kTile;
+      v.active = r0 < all_rows;
+      v.first_pos = seq.pos0 + r0 / p.group;
+      v.last_pos = seq.pos0 + (min(r0 + kTile, all_rows) - 1) / p.group;
+      const KeyTiles t = key_tiles(p, v.first_pos, v.last_pos, seq.length, kTile);
+      v.lo = t.lo; v.hi = t.hi; v.sink_hi = t.sink_hi;
+      return v;
+    };
+
+    if (warp == kProducer) {
+      // ------------------------------------------------------------------ producer
+      const int box = min(p.page_size, kTile);
+      const int per_tile = kTile / box, per_batch = 32 / per_tile;
+      int page = 0, n = 0;  // n: ring slots requested so far
+      bool ok = true;
+      for (int i = begin; i < end && ok; ++i) {
+        const int in_batch = (i - begin) % per_batch;
+        if (in_batch == 0) {
+          const int ti = i + lane / per_tile;
+          page = ti < end ? page_of(p, b, kt.tile_index(ti) * kTile + (lane % per_tile) * box) : 0;
+        }
+        const int slot = (kt.tile_index(i) * kTile) & (p.page_size - 1);
+        for (int kv = 0; kv < 2; ++kv, ++n) {
+          const int stage = n % kStages;
+          if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer)) { ok = false; break; }
+          if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensor);
+          __syncwarp();
+          for (int j = 0; j < per_tile; ++j) {
+            const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + j);
+            if (elect_one()) {
+#pragma unroll
+              for (int h = 0; h < D / 64; ++h)
+                tma_load_4d(ring + stage * C::kTensor + h * kHalf + j * box * 128, kv == 0 ? &tmap_k : &tmap_v, full(stage),
+                            h * 64, slot, kvh, pg);
+            }
+            __syncwarp();
+          }
+        }
+      }
+      if (!ok) {
+        // leave no copy in flight: give the last request of every stage a short time to land
+        volatile int never = 0;
+        for (int back = 1; back <= kStages && back <= n; ++back)
+          mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
+      }
+    } else if (warp >= kIssuer0) {
+      // --------------------------------------------------------------- MMA issuers
+      const int s = warp - kIssuer0;
+      const SlotView view = slot_view(s);
+      constexpr uint32_t idesc_s = make_idesc_bf16(kTile, kTile, false, false);
+      constexpr uint32_t idesc_o = make_idesc_bf16(kTile, D, false, true);  // V is MN-major
+      const uint64_t q_desc = make_smem_desc(sQ + s * C::kTensor, 0, 1024);
+      const uint32_t t_s = tmem + s * kTile, t_o = tmem + C::kColO + s * D;
+      bool ok = true, first = true;
+      uint32_t done = 0;  // tiles this slot has worked on
+      if (view.active) ok = mbar_wait_warp(q_full(s), 0, abort_flag, p.status, kTimeoutChunkMma);
+      for (int i = begin; i < end && ok; ++i) {
+        const int key0 = kt.tile_index(i) * kTile, n = 2 * (i - begin);
+        const bool need = view.needs(key0);
+        // ---- scores
+        if (!mbar_wait_warp(full(n % kStages), (n / kStages) & 1u, abort_flag, p.status, kTimeoutChunkMma)) { ok = false; break; }
+        if (need) {
+          // P of the slot's previous tile lies in the columns that S is about to overwrite
+          if (!first && !mbar_wait_warp(o_full(s), (done - 1) & 1u, abort_flag, p.status, kTimeoutChunkMma)) { ok = false; break; }
+          tcgen05_fence_after_sync();
+          const uint64_t k_desc = make_smem_desc(ring + (n % kStages) * C::kTensor, 0, 1024);
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint64_t step = (uint64_t)((ks >> 2) * (kHalf >> 4) + (ks & 3) * 2);
+              mma_bf16_ss(t_s, q_desc + step, k_desc + step, idesc_s, ks != 0 ? 1u : 0u);
+            }
+            mma_commit(s_full(s));
+          }
+          __syncwarp();
+        }
+        if (elect_one()) mma_commit(empty(n % kStages));
+        __syncwarp();
+        // ---- output
+        const int m = n + 1;
+        if (!mbar_wait_warp(full(m % kStages), (m / kStages) & 1u, abort_flag, p.status, kTimeoutChunkMma)) { ok = false; break; }
+        if (need) {
+          const uint32_t v_tile = ring + (m % kStages) * C::kTensor;
+          const bool edge = key0 + kTile > kt.hi || (key0 < kt.lo && key0 + kTile > kt.sink_hi);
+          if (edge) {
+            // keys in nobody's view: zeros (both issuers write the same ones; neither's product reads before its own are in)
+            for (int k = lane; k < kTile; k += 32) {
+              const int key = key0 + k;
+              if (!((key < kt.hi && key >= kt.lo) || key < kt.sink_hi)) {
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c)
+                  st_shared_v4(v_tile + (c >> 3) * kHalf + k * 128 + (c & 7) * 16, make_uint4(0, 0, 0, 0));
+              }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          if (!mbar_wait_warp(p_full(s), done & 1u, abort_flag, p.status, kTimeoutChunkMma)) { ok = false; break; }
+          tcgen05_fence_after_sync();
+          const uint64_t v_desc = make_smem_desc(v_tile, kHalf, 1024);
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = 0; ks < kTile / 16; ++ks)
+              mma_bf16_ts(t_o, t_s + 8 * ks, v_desc + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o, (first && ks == 0) ? 0u : 1u);
+            mma_commit(o_full(s));
+          }
+          __syncwarp();
+          first = false;
+          ++done;
+        }
+        if (elect_one()) mma_commit(empty(m % kStages));
+        __syncwarp();
+      }
+      if (!ok) {
+        // products in flight still read shared and tensor memory: give them a short time to end
+        if (elect_one()) mma_commit(drained(s));
+        __syncwarp();
+        volatile int never = 0;
+        mbar_wait(drained(s), 0, &never, nullptr, 0, 20000000ull);
+      }
+    } else {
+      // ------------------------------------------------------------------- softmax
+      const int s = warp >> 2, quarter = warp & 3;
+      const int r = quarter * 32 + lane, row = row0 + s * kTile + r;
+      const SlotView view = slot_view(s);
+      const bool valid = row < all_rows;
+      const int t = valid ? row / p.group : 0, head = kvh * p.group + (valid ? row % p.group : 0);
+      const int pos = seq.pos0 + t;
+      if (view.active) {
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)(seq.q0 + t) * p.ld_q + (int64_t)head * D);
+        const uint32_t dst = sQ + s * C::kTensor + (uint32_t)r * 128u;
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c)
+          st_shared_v4(dst + (c >> 3) * kHalf + (uint32_t)(((c & 7) ^ (r & 7)) << 4), valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0));
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full(s));
+      }
+      const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16);
+      const uint32_t t_s = t_lane + s * kTile, t_o = t_lane + C::kColO + s * D;
+      float m = -INFINITY, l = 0.f;
+      uint32_t done = 0;
+      bool ok = true;
+      for (int i = begin; i < end; ++i) {
+        const int key0 = kt.tile_index(i) * kTile;
+        if (!view.needs(key0)) continue;
+        if (!mbar_wait_warp(s_full(s), done & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) { ok = false; break; }
+        tcgen05_fence_after_sync();
+        uint32_t x[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(t_s + 32 * c, x[c]);
+        tmem_ld_wait();
+        const bool whole = key0 + kTile - 1 <= view.first_pos && key0 + kTile <= seq.length &&
+                           (p.window == 0 || key0 > view.last_pos - p.window || key0 + kTile <= p.sinks);
+        if (!whole) {
+          // columns [low, high) and [0, sink) of the tile are in this row's view
+          const int high = min(pos + 1, seq.length) - key0;
+          const int low = p.window > 0 ? pos - p.window + 1 - key0 : 0;
+          const int sink = p.window > 0 ? p.sinks - key0 : 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const int k = 32 * c + j;
+              if (!(k < high && (k >= low || k < sink))) x[c][j] = 0xff800000u;  // -inf
+            }
+        }
+        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) mx4[c] = fmaxf(mx4[c], __uint_as_float(x[c][j]));
+        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2e;
+        const bool raise = mx > m + kRaise;  // also the first finite score of a row (m = -inf)
+        if (__any_sync(0xffffffffu, raise)) {
+          const float alpha = raise ? ex2(m - mx) : 1.f;
+          if (raise) m = mx;
+          l *= alpha;
+          if (done > 0) {
+            // (the products into O so far completed before this tile's scores were begun)
+#pragma unroll 1
+            for (int c = 0; c < D; c += 8) {
+              uint32_t o[8];
+              tmem_ld_32x32b_x8(t_o + c, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+              tmem_st_32x32b_x8(t_o + c, o);
+            }
+          }
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e), nref2 = pack_f32x2(-ref, -ref);
+        uint64_t sum2[2] = {0, 0};
+#pragma unroll
+        for (int c = 0; c < 4; c += 2) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int j = 0; j < 64; j += 2) {
+            const uint32_t(&v)[32] = x[c + (j >> 5)];
+            float a0, a1;
+            unpack_f32x2(fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2, nref2), a0, a1);
+            const float e0 = ex2(a0), e1 = ex2(a1);
+            sum2[(j >> 1) & 1] = add_f32x2(sum2[(j >> 1) & 1], pack_f32x2(e0, e1));
+            pk[j / 2] = pack_bf16(e0, e1);
+          }
+          tmem_st_32x32b_x32(t_s + 16 * c, pk);
+        }
+        float s0, s1;
+        unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
+        l += s0 + s1;
+        tmem_st_wait();
+        tcgen05_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(s));
+        ++done;
+      }
+      // ---- the row's output
+      if (ok && done > 0) ok = mbar_wait_warp(o_full(s), (done - 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax);
+      if (ok && view.active && *abort_flag == 0) {
+        tcgen05_fence_after_sync();
+        const float inv = l > 0.f ? 1.f / l : 0.f;  // nothing seen: zeros
+        const int64_t tok = seq.q0 + t;
+        const int64_t at = ((int64_t)split * p.tokens + tok) * p.heads_q + head;
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          if (done > 0) {
+            tmem_ld_32x32b_x32(t_o + c, o);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = 0;
+          }
+          if (valid && p.splits == 1) {
+            uint4* dst = reinterpret_cast<uint4*>(p.out + tok * p.ld_out + (int64_t)head * D + c);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                w[j] = pack_bf16(__uint_as_float(o[8 * u + 2 * j]) * inv, __uint_as_float(o[8 * u + 2 * j + 1]) * inv);
+              dst[u] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          } else if (valid && l > 0.f) {
+            float4* dst = reinterpret_cast<float4*>(p.part_o + at * D + c);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+              dst[u] = make_float4(__uint_as_float(o[4 * u]) * inv, __uint_as_float(o[4 * u + 1]) * inv,
+                                   __uint_as_float(o[4 * u + 2]) * inv, __uint_as_float(o[4 * u + 3]) * inv);
+          }
+        }
+        if (valid && p.splits > 1) p.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
+      }
+    }
+  }
+
+  // ------------------------------------------------------------------------ teardown
+  __syncwarp();
+  tcgen05_fence_before_sync();
+  __syncthreads();
+  if (warp == kProducer) {
+    tcgen05_fence_after_sync();
+    tmem_dealloc(tmem, C::kCols);
+  }
+}
+
+template <int D>
+pd_status launch(const pd_paged_attention_desc& d, const Params& p, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t s) {
+  using C = ChunkConfig<D>;
+  static PerDeviceFlag smem_allowed;
+  if (pd_status st = allow_dynamic_smem(paged_attention_chunk_kernel<D>, C::kSmem, smem_allowed); st != PD_OK) return st;
+  const int64_t pairs = ((int64_t)p.max_q_len * p.group + kSlots * kTile - 1) / (kSlots * kTile);
+  if (pairs * p.splits > 0x7fffffff) return PD_ERR_BAD_SHAPE;
+  launch_pdl(paged_attention_chunk_kernel<D>, dim3((unsigned)(pairs * p.splits), d.heads_kv, d.batch), dim3(kThreads),
+             C::kSmem, s, tk, tv, p);
+  return check_launch();
+}
+
+}  // namespace
+
+pd_status launch_chunk(const pd_paged_attention_desc& d, const Params& p, const void* k_cache, const void* v_cache, cudaStream_t s) {
+  CUtensorMap tk, tv;
+  const int box = d.page_size < kTile ? d.page_size : kTile;
+  if (!make_cache_map(&tk, k_cache, d, box) || !make_cache_map(&tv, v_cache, d, box)) return PD_ERR_UNSUPPORTED;
+  return d.head_dim == 64 ? launch<64>(d, p, tk, tv, s) : launch<128>(d, p, tk, tv, s);
+}
+
+}  // namespace paged
+}  // namespace pd

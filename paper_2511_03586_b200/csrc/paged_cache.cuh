@@ -137,6 +137,8 @@ inline bool make_cache_map(CUtensorMap* map, const void* cache, const pd_paged_a
 // Launchers (each in its own file).  `rows_per_tile` of the row kernel: 16, 32 or 64.
 pd_status launch_rows(const pd_paged_attention_desc& d, Params& p, const void* k_cache, const void* v_cache,
                       int rows_per_tile, cudaStream_t s);
+pd_status launch_chunk(const pd_paged_attention_desc& d, const Params& p, const void* k_cache, const void* v_cache,
+                       cudaStream_t s);
 
 }  // namespace paged
 }  // namespace pd
