@@ -455,89 +455,101 @@ def pd_debug_withhold_loads(on: bool) -> None:
 
 # ---- a paged key/value cache and the operators of a decoder that reads it ----------------------------------------
 # These bindings run on the device of their first tensor, whichever is current, and on that device's current stream
-# unless one is given; every tensor has to live there.
+# unless one is given; every tensor has to live there.  A decode step calls them with little work each, so the checks
+# are kept to attribute reads: device indices instead of device objects, raw stream handles, no context manager unless
+# the device has to be switched (with these the host side of a call went from 19-32 us to HOST_US).
 
-def _on(device: torch.device, t, dtypes, name: str, *, contiguous: bool = True) -> int | None:
+def _device(t, name: str) -> int:
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError(f"{name} must be a CUDA tensor")
+    return t.get_device()
+
+
+def _on(device: int, t, dtype, name: str, dense: bool = True) -> int | None:
     """Address of ``t`` (None for None) after checking its device, type and, unless told otherwise, density."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.device != device:
-        raise TypeError(f"{name} must be a tensor on {device}")
-    if t.dtype not in (dtypes if isinstance(dtypes, tuple) else (dtypes,)):
-        raise TypeError(f"{name} must be {dtypes}, got {t.dtype}")
-    if contiguous and not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        raise TypeError(f"{name} must be a tensor on cuda:{device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if dense and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _cuda_device(t, name: str) -> torch.device:
-    if not (isinstance(t, torch.Tensor) and t.is_cuda):
-        raise TypeError(f"{name} must be a CUDA tensor")
-    return t.device
-
-
-def _stream_on(device: torch.device, stream) -> int:
-    if stream is not None and stream.device != device:
-        raise ValueError(f"stream must belong to {device}")
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+def _call(fn, device: int, stream, *args) -> None:
+    """fn(*args, stream) with ``device`` current."""
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(device)
+    elif stream.device_index != device:
+        raise ValueError(f"stream must belong to cuda:{device}")
+    else:
+        handle = stream.cuda_stream
+    if torch.cuda.current_device() == device:
+        status = fn(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, handle)
+    if status != PD_OK:
+        raise PdError(status, fn.__name__)
 
 
 def _token_stride(t: torch.Tensor, name: str) -> int:
     """Elements from token to token of [tokens, heads, head_dim] whose heads lie side by side."""
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens, heads, head_dim]")
-    _, heads, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+    tokens, heads, d = t.shape
+    token_stride, head_stride, stride = t.stride()
+    if (d > 1 and stride != 1) or (heads > 1 and head_stride != d):
         raise ValueError(f"{name}: the heads of a token must lie side by side")
-    return t.stride(0) if t.shape[0] > 1 else heads * d
+    return token_stride if tokens > 1 else heads * d
 
 
-def _paged_desc(device, k_cache, v_cache, block_table, cu_q, kv_len) -> tuple[PagedAttentionDesc, list[int]]:
-    ptrs = [_on(device, k_cache, torch.bfloat16, "k_cache", contiguous=False),
-            _on(device, v_cache, torch.bfloat16, "v_cache", contiguous=False),
-            _on(device, block_table, torch.int32, "block_table"), _on(device, cu_q, torch.int32, "cu_q"),
-            _on(device, kv_len, torch.int32, "kv_len")]
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or any(
-            k_cache.shape[i] > 1 and k_cache.stride(i) != v_cache.stride(i) for i in range(4)):
+def _paged_desc(device: int, k_cache, v_cache, block_table, cu_q, kv_len):
+    """The cache's part of the desc, and the addresses of the five tensors."""
+    kc, vc = _on(device, k_cache, torch.bfloat16, "k_cache", False), _on(device, v_cache, torch.bfloat16, "v_cache", False)
+    table, cu = _on(device, block_table, torch.int32, "block_table"), _on(device, cu_q, torch.int32, "cu_q")
+    lens = _on(device, kv_len, torch.int32, "kv_len")
+    shape, strides, other = k_cache.shape, k_cache.stride(), v_cache.stride()
+    if len(shape) != 4 or v_cache.shape != shape:
         raise ValueError("k_cache and v_cache must be [pages, page_size, heads, head_dim] with the same strides")
-    if k_cache.shape[3] > 1 and k_cache.stride(3) != 1:
+    num_pages, page_size, heads, head_dim = shape
+    if strides != other and any(n > 1 and a != b for n, a, b in zip(shape, strides, other)):
+        raise ValueError("k_cache and v_cache must be [pages, page_size, heads, head_dim] with the same strides")
+    if head_dim > 1 and strides[3] != 1:
         raise ValueError("the elements of a cached head must be contiguous")
     if block_table.dim() != 2 or cu_q.dim() != 1 or kv_len.dim() != 1:
         raise ValueError("block_table must be [batch, max_pages], cu_q [batch + 1], kv_len [batch]")
-    batch = kv_len.shape[0]
-    if block_table.shape[0] != batch or cu_q.shape[0] != batch + 1:
+    batch, max_pages = block_table.shape
+    if kv_len.shape[0] != batch or cu_q.shape[0] != batch + 1:
         raise ValueError("block_table must be [batch, max_pages], cu_q [batch + 1], kv_len [batch]")
-    d = PagedAttentionDesc()
-    d.batch, d.max_pages = batch, block_table.shape[1]
-    d.num_pages, d.page_size, d.heads_kv, d.head_dim = k_cache.shape
+    d = PagedAttentionDesc(batch, 0, 0, heads, head_dim, num_pages, page_size, max_pages)
     # strides of extents of one are never used; the library still asks for legal ones
-    tight = (d.page_size * d.heads_kv * d.head_dim, d.heads_kv * d.head_dim, d.head_dim)
-    d.page_stride, d.slot_stride, d.head_stride = (
-        k_cache.stride(i) if k_cache.shape[i] > 1 else tight[i] for i in range(3))
-    return d, ptrs
+    d.page_stride = strides[0] if num_pages > 1 else page_size * heads * head_dim
+    d.slot_stride = strides[1] if page_size > 1 else heads * head_dim
+    d.head_stride = strides[2] if heads > 1 else head_dim
+    return d, kc, vc, table, cu, lens
 
 
 def pd_kv_cache_append(k_new, v_new, k_cache, v_cache, block_table, cu_q, kv_len, stream=None) -> None:
     """Writes the new tokens' keys and values (bf16 [tokens, heads_kv, head_dim], column blocks of a packed projection
     will do) to their slots of the caches (bf16 [pages, page_size, heads_kv, head_dim], any page, slot and head
     strides).  ``kv_len`` counts the new tokens already."""
-    device = _cuda_device(k_new, "k_new")
-    d, (kc, vc, table, cu, lens) = _paged_desc(device, k_cache, v_cache, block_table, cu_q, kv_len)
-    k = _on(device, k_new, torch.bfloat16, "k_new", contiguous=False)
-    v = _on(device, v_new, torch.bfloat16, "v_new", contiguous=False)
-    if tuple(k_new.shape[1:]) != (d.heads_kv, d.head_dim) or v_new.shape != k_new.shape:
-        raise ValueError("k_new and v_new must be [tokens, heads_kv, head_dim]")
+    device = _device(k_new, "k_new")
+    d, kc, vc, table, cu, lens = _paged_desc(device, k_cache, v_cache, block_table, cu_q, kv_len)
+    k, v = _on(device, k_new, torch.bfloat16, "k_new", False), _on(device, v_new, torch.bfloat16, "v_new", False)
     ld = _token_stride(k_new, "k_new")
+    if k_new.shape[1:] != k_cache.shape[2:] or v_new.shape != k_new.shape:
+        raise ValueError("k_new and v_new must be [tokens, heads_kv, head_dim]")
     if ld != _token_stride(v_new, "v_new"):
         raise ValueError("k_new and v_new must have the same token stride")
     d.tokens = k_new.shape[0]
-    with torch.cuda.device(device):
-        _check(_lib.pd_kv_cache_append(ctypes.byref(d), k, v, ld, kc, vc, table, cu, lens, _stream_on(device, stream)),
-               "pd_kv_cache_append")
+    _call(_lib.pd_kv_cache_append, device, stream, d, k, v, ld, kc, vc, table, cu, lens)
 
 
 def pd_attention_paged_workspace_bytes(desc: PagedAttentionDesc) -> int:
-    return int(_lib.pd_attention_paged_workspace_bytes(ctypes.byref(desc)))
+    return int(_lib.pd_attention_paged_workspace_bytes(desc))
 
 
 def pd_attention_paged_fwd(q, k_cache, v_cache, block_table, cu_q, kv_len, *, max_q_len: int, max_kv_len: int,
@@ -546,35 +558,50 @@ def pd_attention_paged_fwd(q, k_cache, v_cache, block_table, cu_q, kv_len, *, ma
     """Causal attention of the packed new tokens q (bf16 [tokens, heads_q, head_dim]) over the paged caches, which hold
     their keys and values already; ``window`` > 0 limits a query to that many last keys, plus the first ``sinks``.
     ``scale`` defaults to head_dim ** -0.5.  Rows of q behind the last sequence are left as they are in ``out``."""
-    device = _cuda_device(q, "q")
-    d, (kc, vc, table, cu, lens) = _paged_desc(device, k_cache, v_cache, block_table, cu_q, kv_len)
-    qp = _on(device, q, torch.bfloat16, "q", contiguous=False)
+    device = _device(q, "q")
+    d, kc, vc, table, cu, lens = _paged_desc(device, k_cache, v_cache, block_table, cu_q, kv_len)
+    qp = _on(device, q, torch.bfloat16, "q", False)
     d.ld_q = _token_stride(q, "q")
-    d.tokens, d.heads_q = q.shape[0], q.shape[1]
-    if q.shape[2] != d.head_dim:
+    tokens, heads_q, head_dim = q.shape
+    d.tokens, d.heads_q = tokens, heads_q
+    if head_dim != d.head_dim:
         raise ValueError("q and the caches must have the same head_dim")
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=device)
-    op = _on(device, out, torch.bfloat16, "out", contiguous=False)
-    if out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    d.ld_out = _token_stride(out, "out")
-    d.max_q_len, d.max_kv_len, d.window, d.sinks = max_q_len, max_kv_len, window, sinks
-    d.scale = d.head_dim ** -0.5 if scale is None else scale
-    if workspace is None:
-        nbytes = int(_lib.pd_attention_paged_workspace_bytes(ctypes.byref(d)))
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+        out = torch.empty((tokens, heads_q, head_dim), dtype=torch.bfloat16, device=q.device)
+        op, d.ld_out = out.data_ptr(), heads_q * head_dim
     else:
-        _on(device, workspace, torch.uint8, "workspace")
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-    with torch.cuda.device(device):
-        _check(_lib.pd_attention_paged_fwd(ctypes.byref(d), qp, kc, vc, table, cu, lens, op, ws, ws_bytes,
-                                           _stream_on(device, stream)), "pd_attention_paged_fwd")
+        op = _on(device, out, torch.bfloat16, "out", False)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+        d.ld_out = _token_stride(out, "out")
+    d.max_q_len, d.max_kv_len, d.window, d.sinks = max_q_len, max_kv_len, window, sinks
+    d.scale = head_dim ** -0.5 if scale is None else scale
+    if workspace is None:
+        ws_bytes = _lib.pd_attention_paged_workspace_bytes(d)
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device) if ws_bytes else None
+        ws = workspace.data_ptr() if ws_bytes else None
+    else:
+        ws, ws_bytes = _on(device, workspace, torch.uint8, "workspace"), workspace.numel()
+    _call(_lib.pd_attention_paged_fwd, device, stream, d, qp, kc, vc, table, cu, lens, op, ws, ws_bytes)
     return out
 
 
 _NORMS = {"none": 0, "rms": 1, "layer": 2}
 _PD_DTYPES = {torch.bfloat16: PD_BF16, torch.float32: PD_F32}
+
+
+def _vector(device: int, t, cols: int, name: str) -> int | None:
+    ptr = _on(device, t, torch.float32, name)
+    if t is not None and t.numel() != cols:
+        raise ValueError(f"{name} must have {cols} elements")
+    return ptr
+
+
+def _float_type(t, name: str) -> int:
+    code = _PD_DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be torch.bfloat16 or torch.float32, got {t.dtype}")
+    return code
 
 
 def pd_norm_gate_residual_norm(y, x, *, gate=None, gate_rows: int | None = None, alpha: float = 1.0, eps: float = 1e-5,
@@ -585,17 +612,18 @@ def pd_norm_gate_residual_norm(y, x, *, gate=None, gate_rows: int | None = None,
     y, n: bf16 or fp32 [rows, cols] (the block's output, the next block's input); x, h: bf16 or fp32 (the residual
     stream).  Norms: "none", "rms", "layer"; gamma and beta fp32 [cols] or None.  gate: y's type, [groups, cols] (or
     [cols]), one row for every ``gate_rows`` rows (default: rows / groups rounded up)."""
-    device = _cuda_device(y, "y")
-    floats = (torch.bfloat16, torch.float32)
-    yp, xp = _on(device, y, floats, "y"), _on(device, x, floats, "x")
+    device = _device(y, "y")
+    if post_norm not in _NORMS or pre_norm not in _NORMS:
+        raise ValueError(f"norms must be among {tuple(_NORMS)}")
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a tensor")
+    y_code, x_code = _float_type(y, "y"), _float_type(x, "x")
+    yp, xp = _on(device, y, y.dtype, "y"), _on(device, x, x.dtype, "x")
     if y.dim() != 2 or x.shape != y.shape:
         raise ValueError("y and x must be [rows, cols]")
     rows, cols = y.shape
-    vectors = []
-    for name, t in (("post_gamma", post_gamma), ("post_beta", post_beta), ("pre_gamma", pre_gamma), ("pre_beta", pre_beta)):
-        vectors.append(_on(device, t, torch.float32, name))
-        if t is not None and t.numel() != cols:
-            raise ValueError(f"{name} must have {cols} elements")
+    vectors = (_vector(device, post_gamma, cols, "post_gamma"), _vector(device, post_beta, cols, "post_beta"),
+               _vector(device, pre_gamma, cols, "pre_gamma"), _vector(device, pre_beta, cols, "pre_beta"))
     gp = _on(device, gate, y.dtype, "gate")
     if gate is not None:
         if gate.dim() not in (1, 2) or gate.shape[-1] != cols:
@@ -605,16 +633,17 @@ def pd_norm_gate_residual_norm(y, x, *, gate=None, gate_rows: int | None = None,
             gate_rows = max(1, -(-rows // max(groups, 1)))
         if gate_rows < 1 or -(-rows // gate_rows) > groups:
             raise ValueError("gate has too few rows")
-    h = torch.empty_like(x) if h is None else h
-    n = torch.empty_like(y) if n is None else n
+    if h is None:
+        h = torch.empty_like(x)
+    elif h.shape != x.shape:
+        raise ValueError("h must be [rows, cols]")
+    if n is None:
+        n = torch.empty_like(y)
+    elif n.shape != y.shape:
+        raise ValueError("n must be [rows, cols]")
     hp, np_ = _on(device, h, x.dtype, "h"), _on(device, n, y.dtype, "n")
-    if h.shape != x.shape or n.shape != y.shape:
-        raise ValueError("h and n must be [rows, cols]")
-    d = NormGateResidualDesc(rows, cols, gate_rows or 1, _PD_DTYPES[x.dtype], _PD_DTYPES[y.dtype], _NORMS[post_norm],
-                             _NORMS[pre_norm], alpha, eps)
-    with torch.cuda.device(device):
-        _check(_lib.pd_norm_gate_residual_norm(ctypes.byref(d), yp, xp, gp, *vectors, hp, np_,
-                                               _stream_on(device, stream)), "pd_norm_gate_residual_norm")
+    d = NormGateResidualDesc(rows, cols, gate_rows or 1, x_code, y_code, _NORMS[post_norm], _NORMS[pre_norm], alpha, eps)
+    _call(_lib.pd_norm_gate_residual_norm, device, stream, d, yp, xp, gp, *vectors, hp, np_)
     return h, n
 
 
@@ -622,24 +651,23 @@ def pd_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None
     """Draws a token per row of logits (bf16 or fp32 [rows, vocab], rows of any stride) with the random numbers u
     (fp32 [rows] in [0, 1)); temperature, top_p, min_p: fp32 [rows], top_k: int32 [rows], None for no such filter.
     Returns (tokens int32 [rows], probs fp32 [rows])."""
-    device = _cuda_device(logits, "logits")
-    lp = _on(device, logits, (torch.bfloat16, torch.float32), "logits", contiguous=False)
+    device = _device(logits, "logits")
+    code, lp = _float_type(logits, "logits"), logits.data_ptr()
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [rows, vocab] with contiguous rows")
     rows, vocab = logits.shape
-    per_row = []
+    if u is None:
+        raise TypeError("u must be a tensor")
+    if tokens is None:
+        tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    if probs is None:
+        probs = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    ptrs = []
     for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("u", u, torch.float32)):
-        per_row.append(_on(device, t, dtype, name))
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("u", u, torch.float32),
+                           ("tokens", tokens, torch.int32), ("probs", probs, torch.float32)):
+        ptrs.append(_on(device, t, dtype, name))
         if t is not None and t.numel() != rows:
             raise ValueError(f"{name} must have one value per row")
-    tokens = torch.empty(rows, dtype=torch.int32, device=device) if tokens is None else tokens
-    probs = torch.empty(rows, dtype=torch.float32, device=device) if probs is None else probs
-    tp, pp = _on(device, tokens, torch.int32, "tokens"), _on(device, probs, torch.float32, "probs")
-    if tokens.numel() != rows or probs.numel() != rows:
-        raise ValueError("tokens and probs must have one value per row")
-    ld = logits.stride(0) if rows > 1 else vocab
-    with torch.cuda.device(device):
-        _check(_lib.pd_sample(lp, _PD_DTYPES[logits.dtype], rows, vocab, ld, *per_row, tp, pp,
-                              _stream_on(device, stream)), "pd_sample")
+    _call(_lib.pd_sample, device, stream, lp, code, rows, vocab, logits.stride(0) if rows > 1 else vocab, *ptrs)
     return tokens, probs
