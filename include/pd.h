@@ -490,7 +490,8 @@ pd_status pd_norm_gate_residual_norm(const pd_norm_gate_residual_desc* desc, con
  * tokens[i] is the first index, in index order, at which the running sum of the
  * kept weights exceeds u[i] of their total; probs[i] = its weight over that total.
  *  - temperature, top_k, top_p, min_p: device vectors of one value a row, or NULL:
- *    1, and no filter.  T <= 0 or NaN: the largest logit (lowest index).
+ *    1, and no filter.  T <= 0 or NaN: the largest logit (lowest index);
+ *    otherwise T is taken into [1e-30, 1e30].
  *    top_k <= 0, top_p >= 1 (or NaN) and min_p <= 0 (or NaN) switch that filter off; the first rank
  *    is always kept (top_p <= 0; min_p above 1 counts as 1).
  *  - u: fp32 in [0, 1) (clamped into it; NaN counts as 0).

@@ -5,14 +5,12 @@
 //   the running kept weight exceeds u times its total.
 //
 // The row is never sorted as a whole.  A cut is "the first rank at which a running sum reaches a target", and a histogram
-// over value (bins of 1/64 in (max - logit) / T) says which bin holds it; the logits of that bin, a few hundred of a
-// hundred thousand, are gathered and sorted by (value, index), and the cut is the last kept one of them.
+// over value (bins of 1/32 in (max - logit) / T) says which bin holds it; the logits of that bin, a few hundred of a
+// hundred thousand, are gathered in one CTA, where the same search goes on over (value, index) until it is down to one.
 //   top-k            : histogram of counts; everything down to the bin of rank k is gathered, and the rest (top-p, min-p,
 //                      the draw) happens on that short list.
-//   top-p, no top-k  : the total weight exactly; then a histogram of approximate weights (one 32-bit atomic per logit in
-//                      units of 2^-31 of the total, none for logits that are too light to come before the cut), whose
-//                      error is bounded, so that one or two bins surely hold the cut; then the exact weight above them.
-//   neither          : exact sums alone.
+//   top-p, no top-k  : the histogram is of weights; the logits of the bin that holds the cut are gathered.
+//   neither          : sums alone.
 // The token is then found by prefix sums over warps' shares, and by a scan of one warp's share.
 // Rows whose candidates do not fit the list (thousands of equal logits, a very large k) take histograms of exact weights
 // over ever finer ranges of values instead, until a bin is a single value.
@@ -38,10 +36,9 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 2048;           // bins of 1/64 in z = (max - logit) / T, up to z = 32 (weight 2^-46: zero units)
-constexpr float kBinsPerUnit = 64.f;
-constexpr int kList = 2048;           // candidates that are sorted
-constexpr int kSlowBins = 1024;       // bins of a step of the search without a list
+constexpr int kBins = 1024;           // bins of 1/32 in z = (max - logit) / T, up to z = 32 (weight 2^-46: zero units)
+constexpr float kBinsPerUnit = 32.f;
+constexpr int kList = 2048;           // candidates that one CTA takes
 constexpr int kTable = 512;
 constexpr int kFixed = 44;            // weights in units of 2^-44
 constexpr int kMaxCluster = 8;
@@ -69,66 +66,69 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float((a & 0x80000000u) ? a ^ 0x80000000u : ~a);
 }
 
-// A float (not subnormal) as a double, by its bits: conversion instructions run at a quarter of the rate of additions.
-__device__ __forceinline__ double as_double(float v) {
-  const uint32_t b = __float_as_uint(v);
-  const uint32_t hi = (b & 0x80000000u) | (((b & 0x7fffffffu) >> 3) + 0x38000000u);
-  return (b << 1) != 0 ? __hiloint2double((int)hi, (int)(b << 29)) : 0.0;
-}
-
 struct Row {
   float max;
+  float floor;       // logits at or below it weigh nothing (half a unit is at z = -31.2): they are raised to it
   double max_d;
   double per_step;   // kTable / (T ln 2): (logit - max) in 512ths of a factor of two
   float bin_scale;   // kBinsPerUnit / T
-  float exp_scale;   // log2(e) / T
-  const double* table;
-  // weight of logit v in units of 2^-44
-  __device__ __forceinline__ u64 weight(float v) const {
-    if (v == max) return 1ull << kFixed;
-    constexpr double kLn2 = 0.69314718055994530942;
+  const double* table;  // 2^(44 + i / 512)
+
+  __device__ void set(float row_max, float temperature) {
+    max = row_max;
+    max_d = (double)row_max;
+    double t = (double)temperature;
+    constexpr double kFloor = 33.0;
+    floor = fminf(__double2float_rd(max_d - kFloor * t), value_of(key_of(row_max) + 1));  // at most the float below max
+    // where T is far below the spacing of floats, everything but the largest weighs nothing anyway
+    if (!(max_d - (double)floor <= 2.0 * kFloor * t)) t = (max_d - (double)floor) / kFloor;
+    const double inv_t = 1.0 / t;
+    per_step = inv_t * (kTable / 0.69314718055994530942);
+    bin_scale = (float)((double)kBinsPerUnit * inv_t);
+  }
+  // 2^52 plus the weight of logit v in units of 2^-44: a whole number whose low bits are the weight.
+  // Without branches, and with what the conversion, the double-precision and the integer pipe can each bear (integer
+  // operations were the limit when the float was widened by its bits and the exceptions were selected at the end).
+  __device__ __forceinline__ double biased_weight(float v) const {
     constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits hold the rounded integer
-    const double y = (as_double(v) - max_d) * per_step;
-    if (!(y > -32.0 / kLn2 * kTable) || v == -INFINITY) return 0;
+    const double y = ((double)fmaxf(v, floor) - max_d) * per_step;
     const double r = y + kMagic;
-    const int n = (int)__double2loint(r);
-    constexpr double c = kLn2 / kTable;
+    const int n = __double2loint(r);
+    constexpr double c = 0.69314718055994530942 / kTable;
     const double f = y - (r - kMagic);
     double q = fma(c * c * c / 6.0, f, c * c / 2.0);
     q = fma(q, f, c);
     q = fma(q, f, 1.0);
-    q *= table[n & (kTable - 1)];  // in [0.99, 2)
-    q = __hiloint2double(__double2hiint(q) + (((n >> 9) + kFixed) << 20), __double2loint(q));  // times 2^(n / 512 + 44)
-    const double whole = q + 4503599627370496.0;  // 2^52: rounds to an integer
-    return (u64)__double_as_longlong(whole) & ((1ull << 52) - 1);
+    q *= table[n & (kTable - 1)];
+    q = __hiloint2double(__double2hiint(q) + ((n << 11) & 0xfff00000), __double2loint(q));  // times 2^(n >> 9)
+    return q + kBias;  // rounds to an integer
   }
-  // bin: a monotone function of v (each rounding is monotone); kBins for weights of zero
+  static constexpr double kBias = 4503599627370496.0;  // 2^52
+  static constexpr int kBiasHigh = 0x43300000;         // its upper word
+  // the weight as an integer, and as a double (sums of up to 2^9 of them are exact)
+  __device__ __forceinline__ u64 weight(float v) const {
+    const double w = biased_weight(v);
+    return (u64)(uint32_t)(__double2hiint(w) - kBiasHigh) << 32 | (uint32_t)__double2loint(w);
+  }
+  __device__ __forceinline__ double weight_d(float v) const { return biased_weight(v) - kBias; }
+  // bin: a monotone function of v (each rounding is monotone); at least kBins for weights of zero
   __device__ __forceinline__ int bin(float v) const {
-    if (v == max) return 0;
-    const float t = (max - v) * bin_scale;
-    return t < (float)kBins ? (int)t : kBins;
-  }
-  // approximate weight relative to the largest: the exponent is at most 47, so its rounding (two steps of 2^-24) is below
-  // 47 * 2^-23 = 6e-6, and the exponential's own error 2^-22; together below 1e-5 of the weight
-  __device__ __forceinline__ float approx(float v) const {
-    float e;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v == max ? 0.f : (v - max) * exp_scale));
-    return e;
+    const float t = fminf((max - v) * bin_scale, (float)kBins);  // (NaN, from 0 * inf: kBins)
+    return __float_as_int(t + 8388608.f) & 0xffff;               // 2^23: rounds to an integer
   }
 };
 static_assert(kTable == 512 && kTable == kThreads, "weight() shifts by 9, and every thread fills an entry");
-constexpr double kApproxError = 2e-5;  // twice approx()'s bound
 
 struct SlowSearch {
   // own histogram (weights in two halves), then the cluster's sums of the bins this CTA owns (first level, later levels)
-  uint32_t count[kSlowBins], lo[kSlowBins], hi[kSlowBins];
-  uint32_t sum_count[2][kSlowBins];
-  u64 sum_weight[2][kSlowBins];
+  uint32_t count[kBins], lo[kBins], hi[kBins];
+  uint32_t sum_count[2][kBins];
+  u64 sum_weight[2][kBins];
 };
 struct FastSearch {
-  uint32_t hist[kBins];  // own histogram
-  uint32_t sum[kBins];   // the cluster's
-  u64 list[kList];       // candidates as (key, index), in CTA 0
+  uint32_t hist[2 * kBins];  // own histogram: counts, or the lower and the upper halves of weights
+  u64 sum[kBins];            // the cluster's
+  u64 list[kList];           // candidates as (key, index), in CTA 0
 };
 
 struct Shared {
@@ -137,12 +137,11 @@ struct Shared {
     SlowSearch slow;
     FastSearch fast;
   };
-  // filled by the cluster's CTAs, entry r by CTA r (peer_max and peer_weight in every CTA, the rest in CTA 0 alone)
+  // filled by the cluster's CTAs, entry r by CTA r (the first two in every CTA, share_weight in CTA 0 alone)
   float peer_max[kMaxCluster];
-  u64 peer_weight[kMaxCluster];
   uint32_t peer_candidates[kMaxCluster];
   u64 share_weight[kMaxCluster * kWarps];  // kept weight of every warp's share, candidates not included at first
-  uint32_t candidates;
+  uint32_t candidates, own_candidates;
   uint32_t first_max;
   // search without a list: published to the cluster
   u64 slice_weight[2];
@@ -152,9 +151,10 @@ struct Shared {
   // scratch of one CTA
   u64 warp_weight[kWarps];
   uint32_t warp_count[kWarps];
+  u64 warp_high[kWarps];
   float warp_max[kWarps];
   // result of a search step
-  int found_bin, found_bin2;
+  int found_bin;
   u64 found_weight_before, found_weight;
   uint32_t found_count_before, found_count;
   uint32_t range[2];
@@ -196,11 +196,11 @@ __device__ __forceinline__ void add_to_bin(Shared& sh, int b, u64 w) {
   if (hi) atomicAdd(&sh.slow.hi[b], hi);
 }
 
-// Sums the cluster's histograms: CTA r gets the bins [r, r + 1) * kSlowBins / n, and every CTA the sums over these slices of
+// Sums the cluster's histograms: CTA r gets the bins [r, r + 1) * kBins / n, and every CTA the sums over these slices of
 // bins.  `level` 0 keeps the sums of the first histogram for a second search.
 __device__ void sum_bins(cg::cluster_group& cluster, Shared& sh, int level, int n, int rank) {
   cluster.sync();  // every histogram is complete
-  const int own = kSlowBins / n;
+  const int own = kBins / n;
   u64 tw = 0;
   uint32_t tc = 0;
   for (int i = threadIdx.x; i < own; i += kThreads) {
@@ -232,7 +232,7 @@ __device__ void sum_bins(cg::cluster_group& cluster, Shared& sh, int level, int 
 // Finds the first bin at which the running count (by_count) or weight reaches `target`, and leaves it in sh.found_*; the
 // last non-empty bin when the total stays below.  Collective over the CTA; every CTA of the cluster finds the same.
 __device__ void find_bin(cg::cluster_group& cluster, Shared& sh, int level, int n, bool by_count, u64 target) {
-  const int own = kSlowBins / n;
+  const int own = kBins / n;
   __syncthreads();  // the previous search's result and scratch have been read
   u64 before_w = 0;
   uint32_t before_c = 0;
@@ -255,10 +255,10 @@ __device__ void find_bin(cg::cluster_group& cluster, Shared& sh, int level, int 
   const Shared* peer = cluster.map_shared_rank(&sh, owner < 0 ? 0 : owner);
   // thread i takes `per` consecutive bins of the owner's slice
   const int per = (own + kThreads - 1) / kThreads;
-  u64 w[kSlowBins / kThreads], tw = 0;
-  uint32_t c[kSlowBins / kThreads], tc = 0;
+  u64 w[kBins / kThreads], tw = 0;
+  uint32_t c[kBins / kThreads], tc = 0;
 #pragma unroll
-  for (int j = 0; j < kSlowBins / kThreads; ++j) {
+  for (int j = 0; j < kBins / kThreads; ++j) {
     const int i = threadIdx.x * per + j;
     const bool in = j < per && i < own;
     w[j] = in ? peer->slow.sum_weight[level][i] : 0;
@@ -277,7 +277,7 @@ __device__ void find_bin(cg::cluster_group& cluster, Shared& sh, int level, int 
   uint32_t rc = c0 + sc - tc;
   // candidate bins: every non-empty bin whose predecessor sum is below the target; the last of them is the answer
 #pragma unroll
-  for (int j = 0; j < kSlowBins / kThreads; ++j) {
+  for (int j = 0; j < kBins / kThreads; ++j) {
     if (c[j] > 0 && (by_count ? (u64)rc : rw) < target) atomicMax(&sh.found_bin, (int)threadIdx.x * per + j);
     rw += w[j];
     rc += c[j];
@@ -286,7 +286,7 @@ __device__ void find_bin(cg::cluster_group& cluster, Shared& sh, int level, int 
   rw = w0 + sw - tw;
   rc = c0 + sc - tc;
 #pragma unroll
-  for (int j = 0; j < kSlowBins / kThreads; ++j) {
+  for (int j = 0; j < kBins / kThreads; ++j) {
     if (j < per && sh.found_bin == (int)threadIdx.x * per + j) {
       sh.found_weight_before = rw;
       sh.found_count_before = rc;
@@ -323,7 +323,7 @@ __device__ SlowCut search(cg::cluster_group& cluster, Shared& sh, const Row& row
     uint32_t lo = key_of(row.max), hi = key_of(-INFINITY);
     while (lo < hi) {
       const uint32_t mid = lo + (hi - lo) / 2;
-      if (row.bin(value_of(mid)) / 2 >= b) hi = mid; else lo = mid + 1;
+      if (row.bin(value_of(mid)) >= b) hi = mid; else lo = mid + 1;
     }
     sh.range[threadIdx.x] = lo;
   }
@@ -332,8 +332,8 @@ __device__ SlowCut search(cg::cluster_group& cluster, Shared& sh, const Row& row
   for (;;) {
     const uint32_t width = hi - lo;
     int shift = 0;
-    while ((width - 1) >> shift >= (uint32_t)kSlowBins) ++shift;
-    for (int i = threadIdx.x; i < kSlowBins; i += kThreads) sh.slow.count[i] = sh.slow.lo[i] = sh.slow.hi[i] = 0;
+    while ((width - 1) >> shift >= (uint32_t)kBins) ++shift;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.slow.count[i] = sh.slow.lo[i] = sh.slow.hi[i] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < len; i += kThreads) {
       const uint32_t k = key_of(vals[i]);
@@ -368,10 +368,15 @@ __device__ __forceinline__ float widen<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ float widen<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
 
-// NaN counts as -inf, -0 and subnormal logits as +0.
-__device__ __forceinline__ float clean(float v) {
-  if (v != v) return -INFINITY;
-  return fabsf(v) < 1.17549435e-38f ? 0.f : v;
+// NaN counts as -inf, -0 as +0.
+__device__ __forceinline__ float clean(float v) { return v != v ? -INFINITY : v + 0.0f; }
+// Two kinds of rows are mapped to ordinary ones, in shared memory, once their maximum is known.  With logits of +inf, these
+// become 0 and all others -inf.  Where 33 T below the maximum is out of range, every finite logit is near -2^128:
+// logits and T are scaled by a power of two.
+enum class Remap { kNone, kInfinite, kScale };
+constexpr float kRemapScale = 0x1p-64f;
+__device__ __forceinline__ float remapped(float v, Remap how) {
+  return how == Remap::kNone ? v : how == Remap::kScale ? v * kRemapScale : v == INFINITY ? 0.f : -INFINITY;
 }
 
 // Copies the slice to shared memory as floats; returns this thread's maximum.
@@ -382,7 +387,7 @@ __device__ __forceinline__ float load_slice(const T* src, float* vals, int len) 
   int done = 0;
   if ((reinterpret_cast<uintptr_t>(src) & 15u) == 0) {
     done = len / kVec * kVec;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 8;
     for (int base = threadIdx.x * kVec; base < done; base += kAhead * kThreads * kVec) {
       uint4 r[kAhead];
 #pragma unroll
@@ -418,6 +423,7 @@ __device__ __forceinline__ float load_slice(const T* src, float* vals, int len) 
     vals[i] = v;
     mx = fmaxf(mx, v);
   }
+  if (threadIdx.x < 3 && len + threadIdx.x < (len + 3) / 4 * 4) vals[len + threadIdx.x] = -INFINITY;  // for_share's last group
   return mx;
 }
 
@@ -429,21 +435,22 @@ __device__ __forceinline__ u64 block_scan_u64(Shared& sh, u64 v) {
   v = warp_scan_u64(v);
   if (lane == 31) sh.warp_weight[warp] = v;
   __syncthreads();
-  for (int k = 0; k < warp; ++k) v += sh.warp_weight[k];
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) v += k < warp ? sh.warp_weight[k] : 0;
   return v;
 }
 
-// Sorts list[0 ... size) ascending; size a power of two.
-__device__ void sort_list(u64* list, int size) {
-  for (int run = 2; run <= size; run <<= 1)
-    for (int step = run >> 1; step > 0; step >>= 1) {
-      for (int i = threadIdx.x; i < size / 2; i += kThreads) {
-        const int a = 2 * i - (i & (step - 1)), b = a + step;
-        const u64 x = list[a], y = list[b];
-        if ((x > y) == ((a & run) == 0)) { list[a] = y; list[b] = x; }
-      }
-      __syncthreads();
-    }
+// f(v, i) for the logits of this warp's share: groups of four to a lane, the last group padded with -inf.
+template <typename F>
+__device__ __forceinline__ void for_share(const float* vals, int begin, int end, F&& f) {
+#pragma unroll 2
+  for (int i = begin + 4 * (int)(threadIdx.x & 31); i < end; i += 128) {
+    const float4 v = *reinterpret_cast<const float4*>(vals + i);
+    f(v.x, i);
+    f(v.y, i + 1);
+    f(v.z, i + 2);
+    f(v.w, i + 3);
+  }
 }
 
 // Writes a row's result.
@@ -459,130 +466,183 @@ __device__ __forceinline__ u64 draw_target(const SampleParams& p, int64_t row, u
 }
 
 // Sums the cluster's histograms into every CTA's fast.sum: CTA r adds up bins [r, r + 1) * kBins / n and hands them out.
+template <bool WEIGHTS>
 __device__ void sum_histograms(cg::cluster_group& cluster, Shared& sh, int n, int rank) {
   cluster.sync();  // every histogram is complete
   const int own = kBins / n;
   for (int i = threadIdx.x; i < own; i += kThreads) {
     const int b = rank * own + i;
-    uint32_t part[kMaxCluster], c = 0;
+    u64 part[kMaxCluster], sum = 0;
 #pragma unroll
-    for (int r = 0; r < kMaxCluster; ++r) part[r] = r < n ? cluster.map_shared_rank(&sh, r)->fast.hist[b] : 0;
+    for (int r = 0; r < kMaxCluster; ++r) {
+      const uint32_t* hist = r < n ? cluster.map_shared_rank(&sh, r)->fast.hist : nullptr;
+      part[r] = r < n ? hist[b] : 0;
+      if (WEIGHTS) part[r] += r < n ? (u64)hist[kBins + b] << 32 : 0;
+    }
 #pragma unroll
-    for (int r = 0; r < kMaxCluster; ++r) c += part[r];
+    for (int r = 0; r < kMaxCluster; ++r) sum += part[r];
 #pragma unroll
     for (int r = 0; r < kMaxCluster; ++r)
-      if (r < n) cluster.map_shared_rank(&sh, r)->fast.sum[b] = c;
+      if (r < n) cluster.map_shared_rank(&sh, r)->fast.sum[b] = sum;
   }
   cluster.sync();  // the sums are in, and nobody reads a histogram any more
 }
 
-// sh.found_bin, found_bin2: the first bins whose running sum reaches t1 and t2 (kBins - 1 if none does);
-// found_count: the running sum through found_bin2.
-__device__ void locate(Shared& sh, u64 t1, u64 t2) {
-  constexpr int kPer = kBins / kThreads;
-  uint32_t c[kPer];
-  u64 sum = 0;
+// The first bin at which the running sum reaches target(total): sh.found_bin, the sum before and through it
+// (found_weight_before, found_weight); the last bin if the total stays below.
+template <typename F>
+__device__ void locate(Shared& sh, F&& target_of) {
+  constexpr int kEach = kBins / kThreads;
+  u64 c[kEach], sum = 0;
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) { c[j] = sh.fast.sum[threadIdx.x * kPer + j]; sum += c[j]; }
+  for (int j = 0; j < kEach; ++j) { c[j] = sh.fast.sum[threadIdx.x * kEach + j]; sum += c[j]; }
   const u64 upto = block_scan_u64(sh, sum);
   if (threadIdx.x == kThreads - 1) {
-    sh.found_bin = sh.found_bin2 = kBins - 1;
-    sh.found_count = (uint32_t)upto;
+    sh.total = upto;
+    sh.found_bin = kBins - 1;
+    sh.found_weight_before = upto - c[kEach - 1];
+    sh.found_weight = upto;
   }
   __syncthreads();
+  const u64 target = target_of(sh.total);
   u64 run = upto - sum;
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
+  for (int j = 0; j < kEach; ++j) {
     const u64 before = run;
     run += c[j];
-    if (before < t1 && run >= t1) sh.found_bin = threadIdx.x * kPer + j;
-    if (before < t2 && run >= t2) { sh.found_bin2 = threadIdx.x * kPer + j; sh.found_count = (uint32_t)run; }
+    if (before < target && run >= target) {
+      sh.found_bin = threadIdx.x * kEach + j;
+      sh.found_weight_before = before;
+      sh.found_weight = run;
+    }
   }
   __syncthreads();
-}
-
-// CTA 0: sorts its n candidates by (key, index) in place and pads them to a power of two.
-__device__ void sort_candidates(Shared& sh, int n) {
-  int size = 2;
-  while (size < n) size <<= 1;
-  for (int i = n + threadIdx.x; i < size; i += kThreads) sh.fast.list[i] = ~0ull;
-  __syncthreads();
-  sort_list(sh.fast.list, size);
 }
 
 __device__ __forceinline__ u64 candidate(float v, int index) { return (u64)key_of(v) << 32 | (uint32_t)index; }
 __device__ __forceinline__ float candidate_value(u64 c) { return value_of((uint32_t)(c >> 32)); }
 
-// Hands a candidate to CTA 0.
-__device__ __forceinline__ void add_candidate(Shared* first, float v, int index) {
-  const uint32_t at = atomicAdd(&first->candidates, 1u);
-  if (at < (uint32_t)kList) first->fast.list[at] = candidate(v, index);
+// Candidates are collected in the CTA first (over the histograms, which have served by then): one trip to CTA 0 per
+// candidate would stall its warp for a microsecond each.
+__device__ __forceinline__ u64* own_list(Shared& sh) { return reinterpret_cast<u64*>(sh.fast.hist); }
+static_assert(2 * kBins * sizeof(uint32_t) + kBins * sizeof(u64) >= kList * sizeof(u64), "a whole list fits over the histograms");
+// Walks this warp's share as for_share does; the logits for which f(v) is true become candidates.  They are noted as bits
+// and appended once for every 16 groups, since an append costs an atomic's round trip.
+template <typename F>
+__device__ __forceinline__ void collect_share(Shared& sh, const float* vals, int start, int begin, int end, F&& f) {
+  const int lane = threadIdx.x & 31;
+  for (int base = begin; base < end; base += 16 * 128) {
+    u64 bits = 0;
+#pragma unroll 2
+    for (int g = 0; g < 16; ++g) {
+      const int i = base + g * 128 + 4 * lane;
+      if (base + g * 128 >= end) break;
+      if (i < end) {
+        const float4 v = *reinterpret_cast<const float4*>(vals + i);
+        const uint32_t four = (f(v.x) ? 1u : 0u) | (f(v.y) ? 2u : 0u) | (f(v.z) ? 4u : 0u) | (f(v.w) ? 8u : 0u);
+        bits |= (u64)four << (4 * g);
+      }
+    }
+    const uint32_t mine = __popcll(bits);
+    const uint32_t upto = warp_scan_u32(mine);
+    uint32_t at = 0;
+    if (lane == 31 && upto > 0) at = atomicAdd(&sh.own_candidates, upto);
+    at = __shfl_sync(0xffffffffu, at, 31) + upto - mine;
+    for (; bits != 0; bits &= bits - 1, ++at) {
+      const int b = __ffsll((long long)bits) - 1, i = base + (b >> 2) * 128 + 4 * lane + (b & 3);
+      if (at < (uint32_t)kList) own_list(sh)[at] = candidate(vals[i], start + i);
+    }
+  }
+}
+// Hands the CTA's candidates to CTA 0; the next cluster barrier makes them visible there.
+__device__ void push_candidates(Shared& sh, Shared* first) {
+  __syncthreads();
+  const uint32_t n = sh.own_candidates;
+  if (threadIdx.x == 0) sh.range[0] = atomicAdd(&first->candidates, n);
+  __syncthreads();
+  const uint32_t base = sh.range[0];
+  for (uint32_t i = threadIdx.x; i < n; i += kThreads)
+    if (base + i < (uint32_t)kList) first->fast.list[base + i] = own_list(sh)[min(i, (uint32_t)kList - 1)];
 }
 
-// CTA 0, after top-k: the first `k` of the n sorted candidates are what is left of the row; top-p, min-p and the draw.
-__device__ void finish_list(const SampleParams& p, Shared& sh, const Row& row, int64_t i_row, int n, int k, float top_p,
-                            u64 min_weight) {
-  constexpr int kPer = kList / kThreads;
-  sort_candidates(sh, n);
-  n = min(n, k);
-  u64* list = sh.fast.list;
-  // the kept run: ranks whose predecessors weigh less than top_p of all; then min-p
-  u64 w[kPer], sum = 0;
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const int i = threadIdx.x * kPer + j;
-    w[j] = i < n ? row.weight(candidate_value(list[i])) : 0;
-    sum += w[j];
-  }
-  u64 upto = block_scan_u64(sh, sum);
-  if (threadIdx.x == kThreads - 1) sh.total = upto;
-  __syncthreads();
-  u64 need = ~0ull;
-  if (top_p < 1.f) need = max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)sh.total), 1ull);
-  u64 before = upto - sum;
-  // what is kept goes on as (index, rank), the rest is pushed to the end
-  u64 entry[kPer];
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const int i = threadIdx.x * kPer + j;
-    const bool kept = i < n && before < need && w[j] >= min_weight;
-    entry[j] = kept ? (list[i] << 32) | (list[i] >> 32) : ~0ull;  // (index, key)
-    before += w[j];
-  }
-  __syncthreads();
-  int size = 2;
-  while (size < n) size <<= 1;
+// CTA 0: of the candidates c (entry j of thread t is candidate 512 j + t) the one at which the running sum of `amount`, in
+// ascending order, reaches `target`, which is at most the sum of all.  Histograms over ever finer ranges, 512 bins at a
+// time; candidates differ (by index, if not by value), so the last range holds one.
+constexpr int kPer = kList / kThreads;
+__device__ u64 select_candidate(Shared& sh, const u64 (&c)[kPer], const u64 (&amount)[kPer], u64 target) {
+  uint32_t* lo_sum = sh.fast.hist;  // (the histograms and the CTA's own list have served)
+  uint32_t* hi_sum = sh.fast.hist + kThreads;
+  uint32_t* count = sh.fast.hist + 2 * kThreads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  u64 lo = ~0ull, hi = 0;
 #pragma unroll
   for (int j = 0; j < kPer; ++j)
-    if ((int)threadIdx.x * kPer + j < size) list[threadIdx.x * kPer + j] = entry[j];
-  __syncthreads();
-  sort_list(list, size);
-  sum = 0;
+    if (amount[j] > 0) { lo = min(lo, c[j]); hi = max(hi, c[j]); }
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const int i = threadIdx.x * kPer + j;
-    entry[j] = i < size ? list[i] : ~0ull;
-    w[j] = entry[j] != ~0ull ? row.weight(value_of((uint32_t)entry[j])) : 0;
-    sum += w[j];
+  for (int o = 16; o > 0; o >>= 1) {
+    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
-  upto = block_scan_u64(sh, sum);
-  if (threadIdx.x == kThreads - 1) sh.total = upto;
   __syncthreads();
-  const u64 target = draw_target(p, i_row, sh.total);
-  before = upto - sum;
+  if (lane == 0) { sh.warp_weight[warp] = lo; sh.warp_high[warp] = hi; }
+  __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    if (before <= target && target < before + w[j]) write_token(p, i_row, (uint32_t)(entry[j] >> 32), w[j], sh.total);
-    before += w[j];
+  for (int w = 0; w < kWarps; ++w) { lo = min(lo, sh.warp_weight[w]); hi = max(hi, sh.warp_high[w]); }
+  u64 before = 0;
+  for (;;) {
+    const u64 span = hi - lo;
+    const int shift = max(64 - __clzll((long long)span) - 9, 0);  // span >> shift < 512
+    lo_sum[threadIdx.x] = hi_sum[threadIdx.x] = count[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (amount[j] > 0 && c[j] >= lo && c[j] <= hi) {
+        const int b = (int)((c[j] - lo) >> shift);
+        const uint32_t add = (uint32_t)amount[j], old = atomicAdd(&lo_sum[b], add);
+        atomicAdd(&hi_sum[b], (uint32_t)(amount[j] >> 32) + (old + add < old ? 1u : 0u));
+        atomicAdd(&count[b], 1u);
+      }
+    __syncthreads();
+    const u64 mine = ((u64)hi_sum[threadIdx.x] << 32) + lo_sum[threadIdx.x];
+    const u64 upto = before + block_scan_u64(sh, mine);
+    if (upto - mine < target && target <= upto) {
+      sh.found_bin = threadIdx.x;
+      sh.found_weight_before = upto - mine;
+      sh.found_count = count[threadIdx.x];
+    }
+    __syncthreads();
+    const u64 first = lo + ((u64)sh.found_bin << shift);
+    if (shift == 0) return first;
+    hi = min(hi, first + ((1ull << shift) - 1));
+    lo = first;
+    before = sh.found_weight_before;
+    if (sh.found_count == 1) {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (amount[j] > 0 && c[j] >= lo && c[j] <= hi) sh.found_weight = c[j];
+      __syncthreads();
+      return sh.found_weight;
+    }
   }
+}
+
+// CTA 0: adds the kept candidates, those up to `last` of at least min_weight, to the sums of their shares.
+__device__ __forceinline__ void add_to_shares(Shared& sh, const SampleParams& p, int share, const u64 (&c)[kPer],
+                                              const u64 (&w)[kPer], u64 last, u64 min_weight) {
+#pragma unroll
+  for (int j = 0; j < kPer; ++j)
+    if (c[j] <= last && w[j] >= min_weight) {
+      const int index = (int)(uint32_t)c[j], cta = index / p.slice;
+      atomicAdd(&sh.share_weight[cta * kWarps + (index - cta * p.slice) / share], w[j]);
+    }
 }
 
 // CTA 0, top-p without top-k or no cut at all: share_weight holds the kept weight of every warp's share up to the
 // candidates, `last` the last kept (key, index), ~0 for no cut.  Finds the share that the draw falls into and scans it
 // (its logits are read again from global memory: the other CTAs are gone).
 template <typename T>
-__device__ void finish_shares(const SampleParams& p, Shared& sh, const Row& row, int64_t i_row, int n, int share, u64 last,
-                              u64 min_weight) {
+__device__ void finish_shares(const SampleParams& p, Shared& sh, const Row& row, Remap remap, int64_t i_row, int n, int share,
+                              u64 last, u64 min_weight) {
   __syncthreads();
   const u64 mine = threadIdx.x < n * kWarps ? sh.share_weight[threadIdx.x] : 0;
   const u64 upto = block_scan_u64(sh, mine);
@@ -604,7 +664,7 @@ __device__ void finish_shares(const SampleParams& p, Shared& sh, const Row& row,
     const int i = base + threadIdx.x;
     u64 w = 0;
     if (i < end) {
-      const float v = clean(widen<T>(src[i]));
+      const float v = remapped(clean(widen<T>(src[i])), remap);
       if (candidate(v, i) <= last) w = row.weight(v);
       if (w < min_weight) w = 0;
     }
@@ -624,12 +684,12 @@ __device__ void slow_path(cg::cluster_group& cluster, const SampleParams& p, Sha
   cut.key = 0xffffffffu;  // nothing cut off
   cut.ties = 0;
   cluster.sync();  // the list's memory is free
-  for (int i = threadIdx.x; i < kSlowBins; i += kThreads) sh.slow.count[i] = sh.slow.lo[i] = sh.slow.hi[i] = 0;
+  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.slow.count[i] = sh.slow.lo[i] = sh.slow.hi[i] = 0;
   __syncthreads();
   for (int i = threadIdx.x; i < len; i += kThreads) {
     const float v = vals[i];
-    const int b = row.bin(v) / 2;
-    if (b < kSlowBins) add_to_bin(sh, b, row.weight(v));
+    const int b = row.bin(v);
+    if (b < kBins) add_to_bin(sh, b, row.weight(v));
   }
   sum_bins(cluster, sh, 0, n, rank);
   u64 kept_total = 0;
@@ -746,9 +806,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   const int n = (int)cluster_size(), rank = (int)cluster_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t i_row = blockIdx.x / n;
-  sh.table[threadIdx.x] = exp2(threadIdx.x / (double)kTable);
-  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.fast.hist[i] = 0;
-  if (threadIdx.x == 0) { sh.candidates = 0; sh.first_max = 0xffffffffu; }
+  sh.table[threadIdx.x] = exp2(kFixed + threadIdx.x / (double)kTable);
+  for (int i = threadIdx.x; i < 2 * kBins; i += kThreads) sh.fast.hist[i] = 0;
+  if (threadIdx.x == 0) { sh.candidates = sh.own_candidates = 0; sh.first_max = 0xffffffffu; }
   griddep_wait();
   griddep_launch_dependents();
 
@@ -757,6 +817,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   const float top_p = p.top_p ? __ldg(p.top_p + i_row) : 1.f;
   const float min_p = p.min_p ? __ldg(p.min_p + i_row) : 0.f;
   if (!(temperature > 0.f)) { temperature = 1.f; top_k = 1; }
+  temperature = fminf(fmaxf(temperature, 1e-30f), 1e30f);
   // (NaN and values below 0 filter nothing; a weight of zero units is never kept)
   const u64 min_weight = min_p > 0.f ? max((u64)ceil((double)fminf(min_p, 1.f) * (double)(1ull << kFixed)), 1ull) : 1ull;
 
@@ -772,17 +833,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   cluster.sync();
   Row row;
   row.table = sh.table;
-  row.max = -INFINITY;
-  for (int r = 0; r < n; ++r) row.max = fmaxf(row.max, sh.peer_max[r]);
-  const double inv_t = 1.0 / (double)temperature;
-  row.max_d = row.max == INFINITY ? 0.0 : as_double(row.max);
-  row.per_step = inv_t * (kTable / 0.69314718055994530942);
-  row.bin_scale = (float)((double)kBinsPerUnit * inv_t);
-  row.exp_scale = (float)(inv_t * 1.4426950408889634);
-  if (row.max == INFINITY) {  // everything else weighs nothing
-    row.max_d = 1e39;
-    row.per_step = 1e300;
+  float row_max = -INFINITY;
+  for (int r = 0; r < n; ++r) row_max = fmaxf(row_max, sh.peer_max[r]);
+  const Remap remap = row_max == INFINITY ? Remap::kInfinite
+                      : row_max > -INFINITY && (double)row_max - 33.0 * (double)temperature < -3.4028234e38 ? Remap::kScale
+                                                                                                            : Remap::kNone;
+  if (remap != Remap::kNone) {
+    for (int i = threadIdx.x; i < (len + 3) / 4 * 4; i += kThreads) vals[i] = remapped(vals[i], remap);
+    row_max = remapped(row_max, remap);
+    if (remap == Remap::kScale) temperature *= kRemapScale;
+    __syncthreads();
   }
+  row.set(row_max, temperature);
   Shared* first = cluster.map_shared_rank(&sh, 0);
 
   // everything below is uniform over the cluster: the same row, the same parameters, the same sums
@@ -803,136 +865,110 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   const int share = ((p.slice + kWarps - 1) / kWarps + 31) / 32 * 32;  // of a warp, contiguous
   const int w_begin = min(warp * share, len), w_end = min(w_begin + share, len);
   if (top_k > 1 && top_k < p.vocab) {
-    for (int i = threadIdx.x; i < len; i += kThreads) {
-      const int b = row.bin(vals[i]);
+    for_share(vals, w_begin, w_end, [&](float v, int) {
+      const int b = row.bin(v);
       if (b < kBins) atomicAdd(&sh.fast.hist[b], 1u);
-    }
-    sum_histograms(cluster, sh, n, rank);
-    locate(sh, 1, (u64)top_k);
-    const int bin = sh.found_bin2;
-    const uint32_t count = sh.found_count;
+    });
+    sum_histograms<false>(cluster, sh, n, rank);
+    locate(sh, [&](u64) { return (u64)top_k; });
+    const int bin = sh.found_bin;
+    const uint32_t count = (uint32_t)sh.found_weight;
     if (count > (uint32_t)kList) {
       slow_path<T>(cluster, p, sh, row, vals, i_row, start, len, n, rank, top_k, top_p, min_weight);
       return;
     }
-    for (int i = threadIdx.x; i < len; i += kThreads)
-      if (row.bin(vals[i]) <= bin) add_candidate(first, vals[i], start + i);
+    collect_share(sh, vals, start, w_begin, w_end, [&](float v) { return row.bin(v) <= bin; });
+    push_candidates(sh, first);
     cluster.sync();
-    if (rank == 0) finish_list(p, sh, row, i_row, (int)count, top_k, top_p, min_weight);
+    if (rank != 0) return;
+    u64 c[kPer], w[kPer], one[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = j * kThreads + threadIdx.x;
+      one[j] = i < (int)count ? 1 : 0;
+      c[j] = one[j] ? sh.fast.list[i] : ~0ull;
+    }
+    u64 last = select_candidate(sh, c, one, (u64)min((uint32_t)top_k, count));
+    u64 sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      w[j] = c[j] <= last ? row.weight(candidate_value(c[j])) : 0;
+      sum += w[j];
+    }
+    if (threadIdx.x < kMaxCluster * kWarps) sh.share_weight[threadIdx.x] = 0;
+    sum = block_scan_u64(sh, sum);
+    if (top_p < 1.f) {
+      if (threadIdx.x == kThreads - 1) sh.total = sum;
+      __syncthreads();
+      last = select_candidate(sh, c, w, max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)sh.total), 1ull));
+    }
+    add_to_shares(sh, p, share, c, w, last, min_weight);
+    finish_shares<T>(p, sh, row, remap, i_row, n, share, last, min_weight);
     return;
   }
   if (top_p < 1.f) {
-    u64 sum = 0;
-    for (int i = threadIdx.x; i < len; i += kThreads) sum += row.weight(vals[i]);
-    sum = warp_sum_u64(sum);
-    if (lane == 0) sh.warp_weight[warp] = sum;
-    __syncthreads();
-    if (threadIdx.x < n) {
-      sum = 0;
-      for (int w = 0; w < kWarps; ++w) sum += sh.warp_weight[w];
-      cluster.map_shared_rank(&sh, threadIdx.x)->peer_weight[rank] = sum;
-    }
-    cluster.sync();
-    u64 total = 0;
-    for (int r = 0; r < n; ++r) total += sh.peer_weight[r];
-    const u64 need = max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)total), 1ull);
-    // Units of 2^-31 of the total.  The logits lighter than `light` weigh less than the tail behind the cut, all together.
-    const double total_rel = (double)total / (double)(1ull << kFixed);  // in weights of the largest
-    const float unit = (float)(2147483648.0 / total_rel);
-    const float light = (float)(0.5 * (1.0 - (double)need / (double)total) * total_rel / p.vocab);
-    for (int i = threadIdx.x; i < len; i += kThreads) {
-      const float v = vals[i], e = row.approx(v);
+    for_share(vals, w_begin, w_end, [&](float v, int) {
       const int b = row.bin(v);
-      if (b < kBins && e >= light) atomicAdd(&sh.fast.hist[b], (uint32_t)(e * unit));
-    }
-    sum_histograms(cluster, sh, n, rank);
-    // every weight is off by less than a unit and kApproxError of itself
-    const u64 slack = (u64)p.vocab + (u64)(2147483648.0 * kApproxError);
-    const u64 need_units = (u64)((double)need / (double)total * 2147483648.0);
-    locate(sh, need_units > slack ? need_units - slack : 1, need_units + slack);
-    // (the cut lies above `light` in any case)
-    const int low = need_units > slack ? sh.found_bin : 0;
-    const int high = min(sh.found_bin2, light > 0.f ? (int)(kBinsPerUnit * (1.f - ::logf(light))) : kBins - 1);
-    u64 above = 0, kept = 0;
-    uint32_t mine = 0;
-    for (int i = w_begin + lane; i < w_end; i += 32) {
-      const float v = vals[i];
-      const int b = row.bin(v);
-      if (b < low) {
-        const u64 w = row.weight(v);
-        above += w;
-        if (w >= min_weight) kept += w;
-      } else if (b <= high) {
-        add_candidate(first, v, start + i);
-        ++mine;
+      const double w = row.biased_weight(v);
+      if (b < kBins) {
+        const uint32_t lo = (uint32_t)__double2loint(w), old = atomicAdd(&sh.fast.hist[b], lo);
+        const uint32_t hi = (uint32_t)(__double2hiint(w) - Row::kBiasHigh) + (old + lo < old ? 1u : 0u);
+        if (hi) atomicAdd(&sh.fast.hist[kBins + b], hi);
       }
-    }
-    above = warp_sum_u64(above);
-    kept = warp_sum_u64(kept);
-    mine = __reduce_add_sync(0xffffffffu, mine);
-    if (lane == 0) {
-      first->share_weight[rank * kWarps + warp] = kept;
-      sh.warp_weight[warp] = above;
-      sh.warp_count[warp] = mine;
-    }
-    __syncthreads();
-    if (threadIdx.x < n) {
-      above = 0;
-      mine = 0;
-      for (int w = 0; w < kWarps; ++w) { above += sh.warp_weight[w]; mine += sh.warp_count[w]; }
-      Shared* peer = cluster.map_shared_rank(&sh, threadIdx.x);
-      peer->peer_weight[rank] = above;
-      peer->peer_candidates[rank] = mine;
-    }
+    });
+    sum_histograms<true>(cluster, sh, n, rank);
+    u64 need = 0;
+    locate(sh, [&](u64 total) { return need = max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)total), 1ull); });
+    const int bin = sh.found_bin;
+    const u64 before = sh.found_weight_before;
+    double kept = 0.0;
+    if (min_weight <= 1)
+      collect_share(sh, vals, start, w_begin, w_end, [&](float v) {
+        const int b = row.bin(v);
+        kept += row.weight_d(b < bin ? v : row.floor);
+        return b == bin;
+      });
+    else
+      collect_share(sh, vals, start, w_begin, w_end, [&](float v) {
+        const int b = row.bin(v);
+        const double w = row.weight_d(b < bin ? v : row.floor);
+        kept += w >= (double)min_weight ? w : 0.0;
+        return b == bin;
+      });
+    push_candidates(sh, first);
+    const u64 kept_sum = warp_sum_u64((u64)kept);
+    if (lane == 0) first->share_weight[rank * kWarps + warp] = kept_sum;
+    if (threadIdx.x < n) cluster.map_shared_rank(&sh, threadIdx.x)->peer_candidates[rank] = sh.own_candidates;
     cluster.sync();
     uint32_t count = 0;
-    u64 before = 0;
-    for (int r = 0; r < n; ++r) { count += sh.peer_candidates[r]; before += sh.peer_weight[r]; }
+    for (int r = 0; r < n; ++r) count += sh.peer_candidates[r];
     if (count > (uint32_t)kList) {
       slow_path<T>(cluster, p, sh, row, vals, i_row, start, len, n, rank, top_k, top_p, min_weight);
       return;
     }
     if (rank != 0) return;
     // the last candidate whose predecessors weigh less than `need`
-    sort_candidates(sh, (int)count);
-    constexpr int kPer = kList / kThreads;
-    u64 w[kPer];
-    sum = 0;
+    u64 c[kPer], w[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const int i = threadIdx.x * kPer + j;
-      w[j] = i < (int)count ? row.weight(candidate_value(sh.fast.list[i])) : 0;
-      sum += w[j];
+      const int i = j * kThreads + threadIdx.x;
+      c[j] = i < (int)count ? sh.fast.list[i] : ~0ull;
+      w[j] = i < (int)count ? row.weight(candidate_value(c[j])) : 0;
     }
-    if (threadIdx.x == 0) sh.token = 0;
-    before += block_scan_u64(sh, sum) - sum;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = threadIdx.x * kPer + j;
-      if (i < (int)count && before < need) {
-        atomicMax(&sh.token, (uint32_t)i);
-        if (w[j] >= min_weight) {
-          const int index = (int)(uint32_t)sh.fast.list[i];
-          const int cta = index / p.slice;
-          atomicAdd(&sh.share_weight[cta * kWarps + (index - cta * p.slice) / share], w[j]);
-        }
-      }
-      before += w[j];
-    }
-    __syncthreads();
-    const u64 last = sh.fast.list[sh.token];
-    finish_shares<T>(p, sh, row, i_row, n, share, last, min_weight);
+    const u64 last = select_candidate(sh, c, w, need - before);
+    add_to_shares(sh, p, share, c, w, last, min_weight);
+    finish_shares<T>(p, sh, row, remap, i_row, n, share, last, min_weight);
     return;
   }
-  u64 kept = 0;
-  for (int i = w_begin + lane; i < w_end; i += 32) {
-    const u64 w = row.weight(vals[i]);
-    if (w >= min_weight) kept += w;
-  }
-  kept = warp_sum_u64(kept);
-  if (lane == 0) first->share_weight[rank * kWarps + warp] = kept;
+  double kept = 0.0;
+  for_share(vals, w_begin, w_end, [&](float v, int) {
+    const double w = row.weight_d(v);
+    kept += w >= (double)min_weight ? w : 0.0;
+  });
+  const u64 kept_sum = warp_sum_u64((u64)kept);
+  if (lane == 0) first->share_weight[rank * kWarps + warp] = kept_sum;
   cluster.sync();
-  if (rank == 0) finish_shares<T>(p, sh, row, i_row, n, share, ~0ull, min_weight);
+  if (rank == 0) finish_shares<T>(p, sh, row, remap, i_row, n, share, ~0ull, min_weight);
 }
 
 // Slices of at most 16384 logits (64 KiB: two CTAs to an SM) where 8 CTAs allow it, and as many CTAs per row as it takes
