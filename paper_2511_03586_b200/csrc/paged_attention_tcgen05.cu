@@ -11,17 +11,24 @@
 //                    them in tiles that are not in view as a whole, and form p = 2^(s * scale * log2 e - m).  m is a
 //                    reference that is raised only when a score exceeds it by more than 2^8 (then the output accumulator
 //                    and the row sum are rescaled through tensor memory); sums stay fp32, p is rounded to bf16 and goes
-//                    back over the scores' columns, where the second product reads it as its A operand.  At the end the
-//                    same warps divide by the sum and write the rows.
-//   warps 8, 9     : MMA issuers of slot 0 / 1 (the warp walks the loop, one elected lane issues): S = Q K^T
-//                    (128 x 128 x D), O += P V (128 x D x 128).  The next S overwrites P's columns, so it is issued when
-//                    the product that reads P has completed.
-//   warp 10        : producer: looks the pages up and copies K and V tiles by TMA, one box per page, into a ring of four
+//                    to tensor memory, where the second product reads it as its A operand.  At the end the same warps
+//                    divide by the sum and write the rows.
+//   warp 8         : MMA issuer (the warp walks the loop, one elected lane issues): S = Q K^T (128 x 128 x D) and
+//                    O += P V (128 x D x 128) of the slots in turn.  One issuer with a fixed turn keeps the slots half a
+//                    period apart, so that one's exponentials have the special-function unit to themselves while the
+//                    other's products run; with an issuer per slot they fell into step (2000 clk of exponentials and 2000
+//                    of waiting per tile where either takes 1000 alone).
+//   warp 9         : producer: looks the pages up and copies K and V tiles by TMA, one box per page, into a ring of four
 //                    32 KiB (head_dim 128) stages, K and V in turn.
+// Tensor memory, head_dim 128: two score buffers of 128 columns and two outputs of 128 fill it; P overwrites its own
+// scores, and the next S waits until the product that reads P has completed.  head_dim 64 leaves room for P of its own: the
+// next S is issued as soon as the scores have been read.
 //
 // Values of keys in nobody's view may be anything (stale slots of a page, NaN) and would poison the product with
-// probability 0 * NaN: in the tiles that hold such keys the issuers overwrite them with zeros first.
+// probability 0 * NaN: in the tiles that hold such keys the issuer overwrites them with zeros first.
 // With `splits` > 1 the key tiles are shared out over that many CTAs, whose partial outputs paged_attention_join joins.
+#include <type_traits>
+
 #include "paged_cache.cuh"
 
 namespace pd {
@@ -31,19 +38,53 @@ namespace {
 constexpr int kTile = 128;             // keys per tile, and rows per slot
 constexpr int kSlots = 2;
 constexpr int kSoftmaxWarps = 4;       // per slot
-constexpr int kIssuer0 = kSlots * kSoftmaxWarps;
-constexpr int kProducer = kIssuer0 + kSlots;
-constexpr int kThreads = 32 * (kProducer + 1);
+constexpr int kIssuer = kSlots * kSoftmaxWarps, kProducer = kIssuer + 1;
+constexpr int kThreads = 384;          // (warps 10 and 11 only complete the third warpgroup, see kRegs*)
+// Registers: 168 a thread at launch (384 x 168 = 64512); the softmax warpgroups, which hold a row of scores, take what the
+// third gives up: 256 x 208 + 128 x 88 = 64512.
+constexpr int kRegsSoftmax = 208, kRegsRest = 88;
 constexpr int kStages = 4;
 constexpr int kHalf = kTile * 128;     // 64 columns of a tile: 128 lines of 128 bytes
 constexpr float kRaise = 8.f;          // powers of two by which a score may exceed the row's reference
+
+// 2^a for two exponents of at most kRaise on the FMA pipe: 2^round(a) * P(a - round(a)), P the degree-3 fit printed by
+// fit_exp2_poly.py (relative error 7.5e-5, far below the rounding to bf16).
+constexpr uint32_t kPolyPairMask = 0xA888u;  // bit k: pair k of every sixteen (five sixteenths)
+__device__ __forceinline__ void exp2_poly(uint64_t a2, float& e0, float& e1) {
+  constexpr float c0 = 9.999280572e-01f, c1 = 6.932609677e-01f, c2 = 2.426111251e-01f, c3 = 5.517166853e-02f;
+  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it leaves round(a) in the low mantissa bits
+  float a0, a1;
+  unpack_f32x2(a2, a0, a1);
+  a2 = pack_f32x2(fmaxf(a0, -125.0f), fmaxf(a1, -125.0f));  // (below, the exponent field would wrap)
+  const uint64_t t2 = add_f32x2(a2, pack_f32x2(kMagic, kMagic));
+  const uint64_t f2 = fma_f32x2(add_f32x2(t2, pack_f32x2(-kMagic, -kMagic)), pack_f32x2(-1.0f, -1.0f), a2);
+  uint64_t p2 = fma_f32x2(pack_f32x2(c3, c3), f2, pack_f32x2(c2, c2));
+  p2 = fma_f32x2(p2, f2, pack_f32x2(c1, c1));
+  p2 = fma_f32x2(p2, f2, pack_f32x2(c0, c0));
+  uint32_t t0, t1, p0, p1;
+  unpack_b32x2(t2, t0, t1);
+  unpack_b32x2(p2, p0, p1);
+  e0 = __uint_as_float(p0 + (t0 << 23));
+  e1 = __uint_as_float(p1 + (t1 << 23));
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// the lowest n bits, n clamped to [0, 32]
+__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; }
 
 template <int D>
 struct ChunkConfig {
   static constexpr int kTensor = kTile * D * 2;  // a Q, K or V tile
   static constexpr int kSmem = kSlots * kTensor + kStages * kTensor + 1024 /*barriers*/ + 1024 /*alignment*/;
-  // tensor-memory columns: scores (and probabilities) of slot s at 128 s, output of slot s at 256 + D s
+  // tensor-memory columns: scores of slot s at 128 s, output of slot s at 256 + D s; probabilities (two keys to a column)
+  // over the scores, or, where there is room, at 384 + 64 s
+  static constexpr bool kOwnP = D == 64;
   static constexpr uint32_t kColO = 256, kCols = 512;
+  static constexpr __host__ __device__ uint32_t col_p(int s) { return kOwnP ? 384 + 64 * s : 128 * s; }
 };
 
 // The view of one slot: keys [lo, hi) and sinks [0, sink_hi) are seen by some of its rows.
@@ -70,18 +111,20 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
   auto s_full = [&](int s) { return bars + 80u + 8u * s; };
   auto p_full = [&](int s) { return bars + 96u + 8u * s; };
   auto o_full = [&](int s) { return bars + 112u + 8u * s; };   // every product of the tile's output has completed
-  auto drained = [&](int s) { return bars + 128u + 8u * s; };
+  auto s_empty = [&](int s) { return bars + 128u + 8u * s; };  // the scores have been read (own P only)
+  const uint32_t drained = bars + 144u;
   uint8_t* ctrl = smem_raw + (bars - smem_u32(smem_raw)) + 512;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kSlots); }
+    for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(q_full(s), kSoftmaxWarps); mbar_init(s_full(s), 1); mbar_init(p_full(s), kSoftmaxWarps);
-      mbar_init(o_full(s), 1); mbar_init(drained(s), 1);
+      mbar_init(o_full(s), 1); mbar_init(s_empty(s), kSoftmaxWarps);
     }
+    mbar_init(drained, 1);
     *abort_flag = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
@@ -120,118 +163,9 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
       return v;
     };
 
-    if (warp == kProducer) {
-      // ------------------------------------------------------------------ producer
-      const int box = min(p.page_size, kTile);
-      const int per_tile = kTile / box, per_batch = 32 / per_tile;
-      int page = 0, n = 0;  // n: ring slots requested so far
-      bool ok = true;
-      for (int i = begin; i < end && ok; ++i) {
-        const int in_batch = (i - begin) % per_batch;
-        if (in_batch == 0) {
-          const int ti = i + lane / per_tile;
-          page = ti < end ? page_of(p, b, kt.tile_index(ti) * kTile + (lane % per_tile) * box) : 0;
-        }
-        const int slot = (kt.tile_index(i) * kTile) & (p.page_size - 1);
-        for (int kv = 0; kv < 2; ++kv, ++n) {
-          const int stage = n % kStages;
-          if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer)) { ok = false; break; }
-          if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensor);
-          __syncwarp();
-          for (int j = 0; j < per_tile; ++j) {
-            const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + j);
-            if (elect_one()) {
-#pragma unroll
-              for (int h = 0; h < D / 64; ++h)
-                tma_load_4d(ring + stage * C::kTensor + h * kHalf + j * box * 128, kv == 0 ? &tmap_k : &tmap_v, full(stage),
-                            h * 64, slot, kvh, pg);
-            }
-            __syncwarp();
-          }
-        }
-      }
-      if (!ok) {
-        // leave no copy in flight: give the last request of every stage a short time to land
-        volatile int never = 0;
-        for (int back = 1; back <= kStages && back <= n; ++back)
-          mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
-      }
-    } else if (warp >= kIssuer0) {
-      // --------------------------------------------------------------- MMA issuers
-      const int s = warp - kIssuer0;
-      const SlotView view = slot_view(s);
-      constexpr uint32_t idesc_s = make_idesc_bf16(kTile, kTile, false, false);
-      constexpr uint32_t idesc_o = make_idesc_bf16(kTile, D, false, true);  // V is MN-major
-      const uint64_t q_desc = make_smem_desc(sQ + s * C::kTensor, 0, 1024);
-      const uint32_t t_s = tmem + s * kTile, t_o = tmem + C::kColO + s * D;
-      bool ok = true, first = true;
-      uint32_t done = 0;  // tiles this slot has worked on
-      if (view.active) ok = mbar_wait_warp(q_full(s), 0, abort_flag, p.status, kTimeoutChunkMma);
-      for (int i = begin; i < end && ok; ++i) {
-        const int key0 = kt.tile_index(i) * kTile, n = 2 * (i - begin);
-        const bool need = view.needs(key0);
-        // ---- scores
-        if (!mbar_wait_warp(full(n % kStages), (n / kStages) & 1u, abort_flag, p.status, kTimeoutChunkMma)) { ok = false; break; }
-        if (need) {
-          // P of the slot's previous tile lies in the columns that S is about to overwrite
-          if (!first && !mbar_wait_warp(o_full(s), (done - 1) & 1u, abort_flag, p.status, kTimeoutChunkMma)) { ok = false; break; }
-          tcgen05_fence_after_sync();
-          const uint64_t k_desc = make_smem_desc(ring + (n % kStages) * C::kTensor, 0, 1024);
-          if (elect_one()) {
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-              const uint64_t step = (uint64_t)((ks >> 2) * (kHalf >> 4) + (ks & 3) * 2);
-              mma_bf16_ss(t_s, q_desc + step, k_desc + step, idesc_s, ks != 0 ? 1u : 0u);
-            }
-            mma_commit(s_full(s));
-          }
-          __syncwarp();
-        }
-        if (elect_one()) mma_commit(empty(n % kStages));
-        __syncwarp();
-        // ---- output
-        const int m = n + 1;
-        if (!mbar_wait_warp(full(m % kStages), (m / kStages) & 1u, abort_flag, p.status, kTimeoutChunkMma)) { ok = false; break; }
-        if (need) {
-          const uint32_t v_tile = ring + (m % kStages) * C::kTensor;
-          const bool edge = key0 + kTile > kt.hi || (key0 < kt.lo && key0 + kTile > kt.sink_hi);
-          if (edge) {
-            // keys in nobody's view: zeros (both issuers write the same ones; neither's product reads before its own are in)
-            for (int k = lane; k < kTile; k += 32) {
-              const int key = key0 + k;
-              if (!((key < kt.hi && key >= kt.lo) || key < kt.sink_hi)) {
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c)
-                  st_shared_v4(v_tile + (c >> 3) * kHalf + k * 128 + (c & 7) * 16, make_uint4(0, 0, 0, 0));
-              }
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-          }
-          if (!mbar_wait_warp(p_full(s), done & 1u, abort_flag, p.status, kTimeoutChunkMma)) { ok = false; break; }
-          tcgen05_fence_after_sync();
-          const uint64_t v_desc = make_smem_desc(v_tile, kHalf, 1024);
-          if (elect_one()) {
-#pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-              mma_bf16_ts(t_o, t_s + 8 * ks, v_desc + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o, (first && ks == 0) ? 0u : 1u);
-            mma_commit(o_full(s));
-          }
-          __syncwarp();
-          first = false;
-          ++done;
-        }
-        if (elect_one()) mma_commit(empty(m % kStages));
-        __syncwarp();
-      }
-      if (!ok) {
-        // products in flight still read shared and tensor memory: give them a short time to end
-        if (elect_one()) mma_commit(drained(s));
-        __syncwarp();
-        volatile int never = 0;
-        mbar_wait(drained(s), 0, &never, nullptr, 0, 20000000ull);
-      }
-    } else {
+    // (each role's code is compiled for the registers that its branch sets)
+    if (warp < kIssuer) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
       // ------------------------------------------------------------------- softmax
       const int s = warp >> 2, quarter = warp & 3;
       const int r = quarter * 32 + lane, row = row0 + s * kTile + r;
@@ -250,7 +184,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
         if (lane == 0) mbar_arrive(q_full(s));
       }
       const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16);
-      const uint32_t t_s = t_lane + s * kTile, t_o = t_lane + C::kColO + s * D;
+      const uint32_t t_s = t_lane + s * kTile, t_p = t_lane + C::col_p(s), t_o = t_lane + C::kColO + s * D;
       float m = -INFINITY, l = 0.f;
       uint32_t done = 0;
       bool ok = true;
@@ -263,6 +197,11 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(t_s + 32 * c, x[c]);
         tmem_ld_wait();
+        if (C::kOwnP) {
+          tcgen05_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(s_empty(s));
+        }
         const bool whole = key0 + kTile - 1 <= view.first_pos && key0 + kTile <= seq.length &&
                            (p.window == 0 || key0 > view.last_pos - p.window || key0 + kTile <= p.sinks);
         if (!whole) {
@@ -271,26 +210,31 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
           const int low = p.window > 0 ? pos - p.window + 1 - key0 : 0;
           const int sink = p.window > 0 ? p.sinks - key0 : 0;
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t seen = below(high - 32 * c) & (~below(low - 32 * c) | below(sink - 32 * c));
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const int k = 32 * c + j;
-              if (!(k < high && (k >= low || k < sink))) x[c][j] = 0xff800000u;  // -inf
-            }
+            for (int j = 0; j < 32; ++j)
+              if (!((seen >> j) & 1u)) x[c][j] = 0xff800000u;  // -inf
+          }
         }
         float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < 32; j += 2)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) mx4[c] = fmaxf(mx4[c], __uint_as_float(x[c][j]));
+          for (int c = 0; c < 4; ++c) mx4[c] = max3(mx4[c], __uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1]));
         const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2e;
+        if (C::kOwnP && done > 0 && !mbar_wait_warp(o_full(s), (done - 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) {
+          ok = false;  // (P and O: the previous product has to be through with them)
+          break;
+        }
         const bool raise = mx > m + kRaise;  // also the first finite score of a row (m = -inf)
         if (__any_sync(0xffffffffu, raise)) {
           const float alpha = raise ? ex2(m - mx) : 1.f;
           if (raise) m = mx;
           l *= alpha;
           if (done > 0) {
-            // (the products into O so far completed before this tile's scores were begun)
+            // (the products into O so far have completed: the issuer waited for them before this tile's scores, or see above)
+            tcgen05_fence_after_sync();
 #pragma unroll 1
             for (int c = 0; c < D; c += 8) {
               uint32_t o[8];
@@ -305,20 +249,32 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
         const float ref = m == -INFINITY ? 0.f : m;
         const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e), nref2 = pack_f32x2(-ref, -ref);
         uint64_t sum2[2] = {0, 0};
+        auto exponentials = [&](auto with_poly) {
 #pragma unroll
-        for (int c = 0; c < 4; c += 2) {
-          uint32_t pk[32];
+          for (int c = 0; c < 4; c += 2) {
+            uint32_t pk[32];
 #pragma unroll
-          for (int j = 0; j < 64; j += 2) {
-            const uint32_t(&v)[32] = x[c + (j >> 5)];
-            float a0, a1;
-            unpack_f32x2(fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2, nref2), a0, a1);
-            const float e0 = ex2(a0), e1 = ex2(a1);
-            sum2[(j >> 1) & 1] = add_f32x2(sum2[(j >> 1) & 1], pack_f32x2(e0, e1));
-            pk[j / 2] = pack_bf16(e0, e1);
+            for (int j = 0; j < 64; j += 2) {
+              const uint32_t(&v)[32] = x[c + (j >> 5)];
+              const uint64_t a2 = fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2, nref2);
+              float e0, e1;
+              if (decltype(with_poly)::value && ((kPolyPairMask >> ((j / 2) & 15)) & 1u)) {
+                exp2_poly(a2, e0, e1);
+              } else {
+                float a0, a1;
+                unpack_f32x2(a2, a0, a1);
+                e0 = ex2(a0);
+                e1 = ex2(a1);
+              }
+              sum2[(j >> 1) & 1] = add_f32x2(sum2[(j >> 1) & 1], pack_f32x2(e0, e1));
+              pk[j / 2] = pack_bf16(e0, e1);
+            }
+            tmem_st_32x32b_x32(t_p + 16 * c, pk);
           }
-          tmem_st_32x32b_x32(t_s + 16 * c, pk);
-        }
+        };
+        // (masked scores are -inf, which the polynomial would turn into something above 0)
+        if (whole) exponentials(std::true_type{});
+        else exponentials(std::false_type{});
         float s0, s1;
         unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
         l += s0 + s1;
@@ -364,6 +320,140 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
           }
         }
         if (valid && p.splits > 1) p.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
+      }
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+      if (warp == kProducer) {
+        // ------------------------------------------------------------------ producer
+        const int box = min(p.page_size, kTile);
+        const int per_tile = kTile / box, per_batch = 32 / per_tile;
+        int page = 0, n = 0;  // n: ring slots requested so far
+        bool ok = true;
+        for (int i = begin; i < end && ok; ++i) {
+          const int in_batch = (i - begin) % per_batch;
+          if (in_batch == 0) {
+            const int ti = i + lane / per_tile;
+            page = ti < end ? page_of(p, b, kt.tile_index(ti) * kTile + (lane % per_tile) * box) : 0;
+          }
+          const int slot = (kt.tile_index(i) * kTile) & (p.page_size - 1);
+          for (int kv = 0; kv < 2; ++kv, ++n) {
+            const int stage = n % kStages;
+            if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer)) { ok = false; break; }
+            if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensor);
+            __syncwarp();
+            for (int j = 0; j < per_tile; ++j) {
+              const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + j);
+              if (elect_one()) {
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h)
+                  tma_load_4d(ring + stage * C::kTensor + h * kHalf + j * box * 128, kv == 0 ? &tmap_k : &tmap_v, full(stage),
+                              h * 64, slot, kvh, pg);
+              }
+              __syncwarp();
+            }
+          }
+        }
+        if (!ok) {
+          // leave no copy in flight: give the last request of every stage a short time to land
+          volatile int never = 0;
+          for (int back = 1; back <= kStages && back <= n; ++back)
+            mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
+        }
+      } else if (warp == kIssuer) {
+        // ---------------------------------------------------------------- MMA issuer
+        const SlotView view[kSlots] = {slot_view(0), slot_view(1)};
+        constexpr uint32_t idesc_s = make_idesc_bf16(kTile, kTile, false, false);
+        constexpr uint32_t idesc_o = make_idesc_bf16(kTile, D, false, true);  // V is MN-major
+        uint32_t n_s[kSlots] = {0, 0}, n_o[kSlots] = {0, 0};  // products issued so far
+        bool ok = true;
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+          ok = ok && mbar_wait_warp(bar, parity & 1u, abort_flag, p.status, kTimeoutChunkMma);
+          return ok;
+        };
+        // S of slot s for the K tile in ring slot n
+        auto issue_scores = [&](int s, int n) {
+          if (C::kOwnP) {
+            if (n_s[s] > 0 && !wait(s_empty(s), n_s[s] - 1)) return;
+          } else if (n_o[s] > 0 && !wait(o_full(s), n_o[s] - 1)) {  // P lies in the columns that S is about to overwrite
+            return;
+          }
+          if (n_s[s] == 0 && !wait(q_full(s), 0)) return;
+          tcgen05_fence_after_sync();
+          const uint64_t q_desc = make_smem_desc(sQ + s * C::kTensor, 0, 1024);
+          const uint64_t k_desc = make_smem_desc(ring + (n % kStages) * C::kTensor, 0, 1024);
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint64_t step = (uint64_t)((ks >> 2) * (kHalf >> 4) + (ks & 3) * 2);
+              mma_bf16_ss(tmem + s * kTile, q_desc + step, k_desc + step, idesc_s, ks != 0 ? 1u : 0u);
+            }
+            mma_commit(s_full(s));
+          }
+          __syncwarp();
+          ++n_s[s];
+        };
+        // O of slot s += P V for the V tile in ring slot n
+        auto issue_output = [&](int s, int n) {
+          if (!wait(p_full(s), n_o[s])) return;
+          tcgen05_fence_after_sync();
+          const uint64_t v_desc = make_smem_desc(ring + (n % kStages) * C::kTensor, kHalf, 1024);
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = 0; ks < kTile / 16; ++ks)
+              mma_bf16_ts(tmem + C::kColO + s * D, tmem + C::col_p(s) + 8 * ks, v_desc + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o,
+                          (n_o[s] == 0 && ks == 0) ? 0u : 1u);
+            mma_commit(o_full(s));
+          }
+          __syncwarp();
+          ++n_o[s];
+        };
+        auto release = [&](int n) {  // of a ring slot, once every product issued so far has completed
+          if (elect_one()) mma_commit(empty(n % kStages));
+          __syncwarp();
+        };
+        if (begin < end && wait(full(0), 0)) {
+          const int key0 = kt.tile_index(begin) * kTile;
+#pragma unroll
+          for (int s = 0; s < kSlots; ++s)
+            if (ok && view[s].needs(key0)) issue_scores(s, 0);
+          release(0);
+        }
+        for (int i = begin; i < end && ok; ++i) {
+          const int key0 = kt.tile_index(i) * kTile, n = 2 * (i - begin);  // ring slots: K n, V n + 1, next K n + 2
+          const bool more = i + 1 < end;
+          const int next0 = more ? kt.tile_index(i + 1) * kTile : 0;
+          if (!wait(full((n + 1) % kStages), (n + 1) / kStages)) break;
+          if (key0 + kTile > kt.hi || (key0 < kt.lo && key0 + kTile > kt.sink_hi)) {
+            // values of keys in nobody's view: zeros
+            const uint32_t v_tile = ring + ((n + 1) % kStages) * C::kTensor;
+            for (int k = lane; k < kTile; k += 32) {
+              const int key = key0 + k;
+              if (!((key < kt.hi && key >= kt.lo) || key < kt.sink_hi)) {
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c)
+                  st_shared_v4(v_tile + (c >> 3) * kHalf + k * 128 + (c & 7) * 16, make_uint4(0, 0, 0, 0));
+              }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          if (more && !wait(full((n + 2) % kStages), (n + 2) / kStages)) break;
+#pragma unroll
+          for (int s = 0; s < kSlots; ++s) {
+            if (C::kOwnP && ok && more && view[s].needs(next0)) issue_scores(s, n + 2);
+            if (ok && view[s].needs(key0)) issue_output(s, n + 1);
+            if (!C::kOwnP && ok && more && view[s].needs(next0)) issue_scores(s, n + 2);
+          }
+          release(n + 1);
+          if (more) release(n + 2);
+        }
+        if (!ok) {
+          // products in flight still read shared and tensor memory: give them a short time to end
+          if (elect_one()) mma_commit(drained);
+          __syncwarp();
+          volatile int never = 0;
+          mbar_wait(drained, 0, &never, nullptr, 0, 20000000ull);
+        }
       }
     }
   }
