@@ -7,25 +7,25 @@
 // tiles, which halves what comes from L2.  While one slot's scores are being exponentiated the other slot's products
 // run.
 //
-//   warps 0-3, 4-7 : softmax of slot 0 / 1, one thread per row.  Read the row's 128 scores from tensor memory once, mask
-//                    them in tiles that are not in view as a whole, and form p = 2^(s * scale * log2 e - m).  m is a
-//                    reference that is raised only when a score exceeds it by more than 2^8 (then the output accumulator
-//                    and the row sum are rescaled through tensor memory); sums stay fp32, p is rounded to bf16 and goes
-//                    to tensor memory, where the second product reads it as its A operand.  At the end the same warps
-//                    divide by the sum and write the rows.
-//   warp 8         : MMA issuer (the warp walks the loop, one elected lane issues): S = Q K^T (128 x 128 x D) and
-//                    O += P V (128 x D x 128) of the slots in turn.  One issuer with a fixed turn keeps the slots half a
-//                    period apart, so that one's exponentials have the special-function unit to themselves while the
-//                    other's products run; with an issuer per slot they fell into step (2000 clk of exponentials and 2000
-//                    of waiting per tile where either takes 1000 alone).
-//   warp 9         : producer: looks the pages up and copies K and V tiles by TMA, one box per page, into a ring of four
+//   warps 0-3, 4-7 : softmax of slot 0 / 1, one thread per row.  For each block of 64 keys: read the row's scores from tensor
+//                    memory once, mask them in blocks that are not in view as a whole, and form
+//                    p = 2^(s * scale * log2 e - m).  m is a reference that is raised only when a score exceeds it by more
+//                    than 2^8 (then the output accumulator and the row sum are rescaled through tensor memory); sums stay
+//                    fp32, p is rounded to bf16 and goes back over the scores' columns, where the second product reads it
+//                    as its A operand.  At the end the same warps divide by the sum and write the rows.
+//   warps 8, 10    : score issuers of slot 0 / 1 (the warp walks the loop, one elected lane issues): S = Q K^T (128 x 64 x D).
+//   warps 9, 11    : output issuers: O += P V (128 x D x 64).
+//                    (One warp for all four streams spent more time on its waits, 800 clk per block and slot, than the
+//                    products take.)
+//   warp 12        : producer: looks the pages up and copies K and V tiles by TMA, one box per page, into a ring of four
 //                    32 KiB (head_dim 128) stages, K and V in turn.
-// Tensor memory, head_dim 128: two score buffers of 128 columns and two outputs of 128 fill it; P overwrites its own
-// scores, and the next S waits until the product that reads P has completed.  head_dim 64 leaves room for P of its own: the
-// next S is issued as soon as the scores have been read.
+// Tensor memory: per slot two score buffers of 64 columns and an output of D; with head_dim 128 that is all of it.  Two
+// buffers let the scores of the next block be formed while the current ones are exponentiated: the buffer they take was
+// last read by the product of the block before.  (With one buffer of 128 columns the softmax warps of a slot waited half
+// their time for two products in a row.)
 //
 // Values of keys in nobody's view may be anything (stale slots of a page, NaN) and would poison the product with
-// probability 0 * NaN: in the tiles that hold such keys the issuer overwrites them with zeros first.
+// probability 0 * NaN: in the tiles that hold such keys the issuers overwrite them with zeros first.
 // With `splits` > 1 the key tiles are shared out over that many CTAs, whose partial outputs paged_attention_join joins.
 #include <type_traits>
 
@@ -36,13 +36,11 @@ namespace paged {
 namespace {
 
 constexpr int kTile = 128;             // keys per tile, and rows per slot
+constexpr int kBlock = 64;             // keys per score buffer
 constexpr int kSlots = 2;
 constexpr int kSoftmaxWarps = 4;       // per slot
-constexpr int kIssuer = kSlots * kSoftmaxWarps, kProducer = kIssuer + 1;
-constexpr int kThreads = 384;          // (warps 10 and 11 only complete the third warpgroup, see kRegs*)
-// Registers: 168 a thread at launch (384 x 168 = 64512); the softmax warpgroups, which hold a row of scores, take what the
-// third gives up: 256 x 208 + 128 x 88 = 64512.
-constexpr int kRegsSoftmax = 208, kRegsRest = 88;
+constexpr int kIssuer0 = kSlots * kSoftmaxWarps, kProducer = kIssuer0 + 2 * kSlots;
+constexpr int kThreads = 32 * (kProducer + 1);
 constexpr int kStages = 4;
 constexpr int kHalf = kTile * 128;     // 64 columns of a tile: 128 lines of 128 bytes
 constexpr float kRaise = 8.f;          // powers of two by which a score may exceed the row's reference
@@ -80,11 +78,9 @@ template <int D>
 struct ChunkConfig {
   static constexpr int kTensor = kTile * D * 2;  // a Q, K or V tile
   static constexpr int kSmem = kSlots * kTensor + kStages * kTensor + 1024 /*barriers*/ + 1024 /*alignment*/;
-  // tensor-memory columns: scores of slot s at 128 s, output of slot s at 256 + D s; probabilities (two keys to a column)
-  // over the scores, or, where there is room, at 384 + 64 s
-  static constexpr bool kOwnP = D == 64;
+  // tensor-memory columns: score buffer b of slot s at 128 s + 64 b (its probabilities over it, two keys to a column), output
+  // of slot s at 256 + D s
   static constexpr uint32_t kColO = 256, kCols = 512;
-  static constexpr __host__ __device__ uint32_t col_p(int s) { return kOwnP ? 384 + 64 * s : 128 * s; }
 };
 
 // The view of one slot: keys [lo, hi) and sinks [0, sink_hi) are seen by some of its rows.
@@ -93,7 +89,7 @@ struct SlotView {
   int first_pos, last_pos;
   bool active;
   __device__ __forceinline__ bool needs(int key0) const {
-    return active && ((key0 < hi && key0 + kTile > lo) || key0 < sink_hi);
+    return active && ((key0 < hi && key0 + kBlock > lo) || key0 < sink_hi);
   }
 };
 
@@ -108,23 +104,22 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 32u + 8u * s; };
   auto q_full = [&](int s) { return bars + 64u + 8u * s; };
-  auto s_full = [&](int s) { return bars + 80u + 8u * s; };
-  auto p_full = [&](int s) { return bars + 96u + 8u * s; };
-  auto o_full = [&](int s) { return bars + 112u + 8u * s; };   // every product of the tile's output has completed
-  auto s_empty = [&](int s) { return bars + 128u + 8u * s; };  // the scores have been read (own P only)
-  const uint32_t drained = bars + 144u;
+  auto s_full = [&](int s, int b) { return bars + 80u + 16u * s + 8u * b; };
+  auto p_full = [&](int s, int b) { return bars + 112u + 16u * s + 8u * b; };
+  auto o_full = [&](int s, int b) { return bars + 144u + 16u * s + 8u * b; };  // the product that read buffer b has completed
+  auto drained = [&](int w) { return bars + 176u + 8u * w; };  // of the four issuers
   uint8_t* ctrl = smem_raw + (bars - smem_u32(smem_raw)) + 512;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kSlots); }
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(q_full(s), kSoftmaxWarps); mbar_init(s_full(s), 1); mbar_init(p_full(s), kSoftmaxWarps);
-      mbar_init(o_full(s), 1); mbar_init(s_empty(s), kSoftmaxWarps);
+      mbar_init(q_full(s), kSoftmaxWarps);
+      for (int b = 0; b < 2; ++b) { mbar_init(o_full(s, b), 1); mbar_init(s_full(s, b), 1); mbar_init(p_full(s, b), kSoftmaxWarps); }
     }
-    mbar_init(drained, 1);
+    for (int w = 0; w < 2 * kSlots; ++w) mbar_init(drained(w), 1);
     *abort_flag = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
@@ -152,6 +147,8 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
     const KeyTiles kt = key_tiles(p, seq.pos0 + row0 / p.group, seq.pos0 + last_row / p.group, seq.length, kTile);
     int begin, end;
     split_range(p, kt.n, split, begin, end);
+    const int blocks = 2 * (end - begin);
+    auto block_key = [&](int b) { return kt.tile_index(begin + (b >> 1)) * kTile + (b & 1) * kBlock; };
     auto slot_view = [&](int s) {
       SlotView v;
       const int r0 = row0 + s * kTile;
@@ -163,9 +160,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
       return v;
     };
 
-    // (each role's code is compiled for the registers that its branch sets)
-    if (warp < kIssuer) {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    if (warp < kIssuer0) {
       // ------------------------------------------------------------------- softmax
       const int s = warp >> 2, quarter = warp & 3;
       const int r = quarter * 32 + lane, row = row0 + s * kTile + r;
@@ -184,56 +179,54 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
         if (lane == 0) mbar_arrive(q_full(s));
       }
       const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16);
-      const uint32_t t_s = t_lane + s * kTile, t_p = t_lane + C::col_p(s), t_o = t_lane + C::kColO + s * D;
+      const uint32_t t_o = t_lane + C::kColO + s * D;
+      const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e);
       float m = -INFINITY, l = 0.f;
-      uint32_t done = 0;
+      uint32_t done = 0;  // blocks of this slot
       bool ok = true;
-      for (int i = begin; i < end; ++i) {
-        const int key0 = kt.tile_index(i) * kTile;
+      for (int b = 0; b < blocks; ++b) {
+        const int key0 = block_key(b);
         if (!view.needs(key0)) continue;
-        if (!mbar_wait_warp(s_full(s), done & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) { ok = false; break; }
+        const int buf = done & 1;
+        const uint32_t t_s = t_lane + s * kTile + buf * kBlock;
+        if (!mbar_wait_warp(s_full(s, buf), (done >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) { ok = false; break; }
         tcgen05_fence_after_sync();
-        uint32_t x[4][32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(t_s + 32 * c, x[c]);
+        uint32_t x[2][32];
+        tmem_ld_32x32b_x32(t_s, x[0]);
+        tmem_ld_32x32b_x32(t_s + 32, x[1]);
         tmem_ld_wait();
-        if (C::kOwnP) {
-          tcgen05_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(s_empty(s));
-        }
-        const bool whole = key0 + kTile - 1 <= view.first_pos && key0 + kTile <= seq.length &&
-                           (p.window == 0 || key0 > view.last_pos - p.window || key0 + kTile <= p.sinks);
+        const bool whole = key0 + kBlock - 1 <= view.first_pos && key0 + kBlock <= seq.length &&
+                           (p.window == 0 || key0 > view.last_pos - p.window || key0 + kBlock <= p.sinks);
         if (!whole) {
-          // columns [low, high) and [0, sink) of the tile are in this row's view
+          // columns [low, high) and [0, sink) of the block are in this row's view
           const int high = min(pos + 1, seq.length) - key0;
           const int low = p.window > 0 ? pos - p.window + 1 - key0 : 0;
           const int sink = p.window > 0 ? p.sinks - key0 : 0;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             const uint32_t seen = below(high - 32 * c) & (~below(low - 32 * c) | below(sink - 32 * c));
+            if (__any_sync(0xffffffffu, seen != 0xffffffffu)) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!((seen >> j) & 1u)) x[c][j] = 0xff800000u;  // -inf
+              for (int j = 0; j < 32; ++j)
+                if (!((seen >> j) & 1u)) x[c][j] = 0xff800000u;  // -inf
+            }
           }
         }
         float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < 32; j += 2)
+        for (int j = 0; j < 32; j += 4)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) mx4[c] = max3(mx4[c], __uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1]));
-        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2e;
-        if (C::kOwnP && done > 0 && !mbar_wait_warp(o_full(s), (done - 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) {
-          ok = false;  // (P and O: the previous product has to be through with them)
-          break;
-        }
+          for (int c = 0; c < 4; ++c)
+            mx4[c] = max3(mx4[c], __uint_as_float(x[c >> 1][j + 2 * (c & 1)]), __uint_as_float(x[c >> 1][j + 2 * (c & 1) + 1]));
+        const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * p.scale_log2e;
         const bool raise = mx > m + kRaise;  // also the first finite score of a row (m = -inf)
         if (__any_sync(0xffffffffu, raise)) {
           const float alpha = raise ? ex2(m - mx) : 1.f;
           if (raise) m = mx;
           l *= alpha;
           if (done > 0) {
-            // (the products into O so far have completed: the issuer waited for them before this tile's scores, or see above)
+            // every product into O so far has to be through with it; the one before last is, or these scores would not be here
+            if (!mbar_wait_warp(o_full(s, buf ^ 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) { ok = false; break; }
             tcgen05_fence_after_sync();
 #pragma unroll 1
             for (int c = 0; c < D; c += 8) {
@@ -247,45 +240,42 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
           }
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e), nref2 = pack_f32x2(-ref, -ref);
+        const uint64_t nref2 = pack_f32x2(-ref, -ref);
         uint64_t sum2[2] = {0, 0};
+        uint32_t pk[32];
         auto exponentials = [&](auto with_poly) {
 #pragma unroll
-          for (int c = 0; c < 4; c += 2) {
-            uint32_t pk[32];
-#pragma unroll
-            for (int j = 0; j < 64; j += 2) {
-              const uint32_t(&v)[32] = x[c + (j >> 5)];
-              const uint64_t a2 = fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2, nref2);
-              float e0, e1;
-              if (decltype(with_poly)::value && ((kPolyPairMask >> ((j / 2) & 15)) & 1u)) {
-                exp2_poly(a2, e0, e1);
-              } else {
-                float a0, a1;
-                unpack_f32x2(a2, a0, a1);
-                e0 = ex2(a0);
-                e1 = ex2(a1);
-              }
-              sum2[(j >> 1) & 1] = add_f32x2(sum2[(j >> 1) & 1], pack_f32x2(e0, e1));
-              pk[j / 2] = pack_bf16(e0, e1);
+          for (int j = 0; j < 64; j += 2) {
+            const uint32_t(&v)[32] = x[j >> 5];
+            const uint64_t a2 = fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2, nref2);
+            float e0, e1;
+            if (decltype(with_poly)::value && ((kPolyPairMask >> ((j / 2) & 15)) & 1u)) {
+              exp2_poly(a2, e0, e1);
+            } else {
+              float a0, a1;
+              unpack_f32x2(a2, a0, a1);
+              e0 = ex2(a0);
+              e1 = ex2(a1);
             }
-            tmem_st_32x32b_x32(t_p + 16 * c, pk);
+            sum2[(j >> 1) & 1] = add_f32x2(sum2[(j >> 1) & 1], pack_f32x2(e0, e1));
+            pk[j / 2] = pack_bf16(e0, e1);
           }
         };
         // (masked scores are -inf, which the polynomial would turn into something above 0)
         if (whole) exponentials(std::true_type{});
         else exponentials(std::false_type{});
+        tmem_st_32x32b_x32(t_s, pk);
         float s0, s1;
         unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
         l += s0 + s1;
         tmem_st_wait();
         tcgen05_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(s));
+        if (lane == 0) mbar_arrive(p_full(s, buf));
         ++done;
       }
       // ---- the row's output
-      if (ok && done > 0) ok = mbar_wait_warp(o_full(s), (done - 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax);
+      if (ok && done > 0) ok = mbar_wait_warp(o_full(s, (done - 1) & 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax);
       if (ok && view.active && *abort_flag == 0) {
         tcgen05_fence_after_sync();
         const float inv = l > 0.f ? 1.f / l : 0.f;  // nothing seen: zeros
@@ -321,139 +311,131 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
         }
         if (valid && p.splits > 1) p.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
       }
-    } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
-      if (warp == kProducer) {
-        // ------------------------------------------------------------------ producer
-        const int box = min(p.page_size, kTile);
-        const int per_tile = kTile / box, per_batch = 32 / per_tile;
-        int page = 0, n = 0;  // n: ring slots requested so far
-        bool ok = true;
-        for (int i = begin; i < end && ok; ++i) {
-          const int in_batch = (i - begin) % per_batch;
-          if (in_batch == 0) {
-            const int ti = i + lane / per_tile;
-            page = ti < end ? page_of(p, b, kt.tile_index(ti) * kTile + (lane % per_tile) * box) : 0;
-          }
-          const int slot = (kt.tile_index(i) * kTile) & (p.page_size - 1);
-          for (int kv = 0; kv < 2; ++kv, ++n) {
-            const int stage = n % kStages;
-            if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer)) { ok = false; break; }
-            if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensor);
-            __syncwarp();
-            for (int j = 0; j < per_tile; ++j) {
-              const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + j);
-              if (elect_one()) {
+    } else if (warp == kProducer) {
+      // ------------------------------------------------------------------ producer
+      const int box = min(p.page_size, kTile);
+      const int per_tile = kTile / box, per_batch = 32 / per_tile;
+      int page = 0, n = 0;  // n: ring slots requested so far
+      bool ok = true;
+      for (int i = begin; i < end && ok; ++i) {
+        const int in_batch = (i - begin) % per_batch;
+        if (in_batch == 0) {
+          const int ti = i + lane / per_tile;
+          page = ti < end ? page_of(p, b, kt.tile_index(ti) * kTile + (lane % per_tile) * box) : 0;
+        }
+        const int slot = (kt.tile_index(i) * kTile) & (p.page_size - 1);
+        for (int kv = 0; kv < 2; ++kv, ++n) {
+          const int stage = n % kStages;
+          if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer)) { ok = false; break; }
+          if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensor);
+          __syncwarp();
+          for (int j = 0; j < per_tile; ++j) {
+            const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + j);
+            if (elect_one()) {
 #pragma unroll
-                for (int h = 0; h < D / 64; ++h)
-                  tma_load_4d(ring + stage * C::kTensor + h * kHalf + j * box * 128, kv == 0 ? &tmap_k : &tmap_v, full(stage),
-                              h * 64, slot, kvh, pg);
+              for (int h = 0; h < D / 64; ++h)
+                tma_load_4d(ring + stage * C::kTensor + h * kHalf + j * box * 128, kv == 0 ? &tmap_k : &tmap_v, full(stage),
+                            h * 64, slot, kvh, pg);
+            }
+            __syncwarp();
+          }
+        }
+      }
+      if (!ok) {
+        // leave no copy in flight: give the last request of every stage a short time to land
+        volatile int never = 0;
+        for (int back = 1; back <= kStages && back <= n; ++back)
+          mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
+      }
+    } else {
+      // --------------------------------------------------------------- MMA issuers
+      const int s = (warp - kIssuer0) >> 1;
+      const SlotView view = slot_view(s);
+      uint32_t k = 0;  // products issued so far
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        ok = ok && mbar_wait_warp(bar, parity & 1u, abort_flag, p.status, kTimeoutChunkMma);
+        return ok;
+      };
+      constexpr uint64_t kBlockStep = (kBlock * 128) >> 4;  // descriptor step from a tile's first block to its second
+      if (((warp - kIssuer0) & 1) == 0) {
+        // ---- scores; K tile t is in ring slot 2 t
+        constexpr uint32_t idesc = make_idesc_bf16(kTile, kBlock, false, false);
+        const uint64_t q_desc = make_smem_desc(sQ + s * C::kTensor, 0, 1024);
+        if (view.active) wait(q_full(s), 0);
+        for (int b = 0; b < blocks && ok; ++b) {
+          const int n = b & ~1, stage = n % kStages;
+          if ((b & 1) == 0 && !wait(full(stage), n / kStages)) break;
+          if (view.needs(block_key(b))) {
+            const uint32_t buf = k & 1u;
+            // the buffer holds the probabilities of the block before last: the product that reads them must have completed
+            if (k >= 2 && !wait(o_full(s, buf), (k >> 1) - 1)) break;
+            tcgen05_fence_after_sync();
+            const uint64_t k_desc = make_smem_desc(ring + stage * C::kTensor, 0, 1024) + (b & 1) * kBlockStep;
+            if (elect_one()) {
+#pragma unroll
+              for (int ks = 0; ks < D / 16; ++ks) {
+                const uint64_t step = (uint64_t)((ks >> 2) * (kHalf >> 4) + (ks & 3) * 2);
+                mma_bf16_ss(tmem + s * kTile + buf * kBlock, q_desc + step, k_desc + step, idesc, ks != 0 ? 1u : 0u);
               }
+              mma_commit(s_full(s, buf));
+            }
+            __syncwarp();
+            ++k;
+          }
+          if ((b & 1) && elect_one()) mma_commit(empty(stage));  // both slots' issuers arrive, in need of the tile or not
+          __syncwarp();
+        }
+      } else {
+        // ---- output; V tile t is in ring slot 2 t + 1
+        constexpr uint32_t idesc = make_idesc_bf16(kTile, D, false, true);  // V is MN-major
+        for (int b = 0; b < blocks && ok; ++b) {
+          const int n = b | 1, stage = n % kStages;
+          const int key0 = block_key(b);
+          if ((b & 1) == 0) {
+            if (!wait(full(stage), n / kStages)) break;
+            if ((view.needs(key0) || view.needs(key0 + kBlock)) &&
+                (key0 + kTile > kt.hi || (key0 < kt.lo && key0 + kTile > kt.sink_hi))) {
+              // values of keys in nobody's view: zeros (both slots' issuers write the same; neither's product reads the
+              // tile before its own are in)
+              const uint32_t v_tile = ring + stage * C::kTensor;
+              for (int r = lane; r < kTile; r += 32) {
+                const int key = key0 + r;
+                if (!((key < kt.hi && key >= kt.lo) || key < kt.sink_hi)) {
+#pragma unroll
+                  for (int c = 0; c < D / 8; ++c)
+                    st_shared_v4(v_tile + (c >> 3) * kHalf + r * 128 + (c & 7) * 16, make_uint4(0, 0, 0, 0));
+                }
+              }
+              fence_proxy_async_smem();
               __syncwarp();
             }
           }
-        }
-        if (!ok) {
-          // leave no copy in flight: give the last request of every stage a short time to land
-          volatile int never = 0;
-          for (int back = 1; back <= kStages && back <= n; ++back)
-            mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
-        }
-      } else if (warp == kIssuer) {
-        // ---------------------------------------------------------------- MMA issuer
-        const SlotView view[kSlots] = {slot_view(0), slot_view(1)};
-        constexpr uint32_t idesc_s = make_idesc_bf16(kTile, kTile, false, false);
-        constexpr uint32_t idesc_o = make_idesc_bf16(kTile, D, false, true);  // V is MN-major
-        uint32_t n_s[kSlots] = {0, 0}, n_o[kSlots] = {0, 0};  // products issued so far
-        bool ok = true;
-        auto wait = [&](uint32_t bar, uint32_t parity) {
-          ok = ok && mbar_wait_warp(bar, parity & 1u, abort_flag, p.status, kTimeoutChunkMma);
-          return ok;
-        };
-        // S of slot s for the K tile in ring slot n
-        auto issue_scores = [&](int s, int n) {
-          if (C::kOwnP) {
-            if (n_s[s] > 0 && !wait(s_empty(s), n_s[s] - 1)) return;
-          } else if (n_o[s] > 0 && !wait(o_full(s), n_o[s] - 1)) {  // P lies in the columns that S is about to overwrite
-            return;
-          }
-          if (n_s[s] == 0 && !wait(q_full(s), 0)) return;
-          tcgen05_fence_after_sync();
-          const uint64_t q_desc = make_smem_desc(sQ + s * C::kTensor, 0, 1024);
-          const uint64_t k_desc = make_smem_desc(ring + (n % kStages) * C::kTensor, 0, 1024);
-          if (elect_one()) {
+          if (view.needs(key0)) {
+            const uint32_t buf = k & 1u;
+            if (!wait(p_full(s, buf), k >> 1)) break;
+            tcgen05_fence_after_sync();
+            const uint64_t v_desc = make_smem_desc(ring + stage * C::kTensor, kHalf, 1024) + (b & 1) * kBlockStep;
+            if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-              const uint64_t step = (uint64_t)((ks >> 2) * (kHalf >> 4) + (ks & 3) * 2);
-              mma_bf16_ss(tmem + s * kTile, q_desc + step, k_desc + step, idesc_s, ks != 0 ? 1u : 0u);
+              for (int ks = 0; ks < kBlock / 16; ++ks)
+                mma_bf16_ts(tmem + C::kColO + s * D, tmem + s * kTile + buf * kBlock + 8 * ks,
+                            v_desc + (uint64_t)(ks * ((16 * 128) >> 4)), idesc, (k == 0 && ks == 0) ? 0u : 1u);
+              mma_commit(o_full(s, buf));
             }
-            mma_commit(s_full(s));
-          }
-          __syncwarp();
-          ++n_s[s];
-        };
-        // O of slot s += P V for the V tile in ring slot n
-        auto issue_output = [&](int s, int n) {
-          if (!wait(p_full(s), n_o[s])) return;
-          tcgen05_fence_after_sync();
-          const uint64_t v_desc = make_smem_desc(ring + (n % kStages) * C::kTensor, kHalf, 1024);
-          if (elect_one()) {
-#pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-              mma_bf16_ts(tmem + C::kColO + s * D, tmem + C::col_p(s) + 8 * ks, v_desc + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o,
-                          (n_o[s] == 0 && ks == 0) ? 0u : 1u);
-            mma_commit(o_full(s));
-          }
-          __syncwarp();
-          ++n_o[s];
-        };
-        auto release = [&](int n) {  // of a ring slot, once every product issued so far has completed
-          if (elect_one()) mma_commit(empty(n % kStages));
-          __syncwarp();
-        };
-        if (begin < end && wait(full(0), 0)) {
-          const int key0 = kt.tile_index(begin) * kTile;
-#pragma unroll
-          for (int s = 0; s < kSlots; ++s)
-            if (ok && view[s].needs(key0)) issue_scores(s, 0);
-          release(0);
-        }
-        for (int i = begin; i < end && ok; ++i) {
-          const int key0 = kt.tile_index(i) * kTile, n = 2 * (i - begin);  // ring slots: K n, V n + 1, next K n + 2
-          const bool more = i + 1 < end;
-          const int next0 = more ? kt.tile_index(i + 1) * kTile : 0;
-          if (!wait(full((n + 1) % kStages), (n + 1) / kStages)) break;
-          if (key0 + kTile > kt.hi || (key0 < kt.lo && key0 + kTile > kt.sink_hi)) {
-            // values of keys in nobody's view: zeros
-            const uint32_t v_tile = ring + ((n + 1) % kStages) * C::kTensor;
-            for (int k = lane; k < kTile; k += 32) {
-              const int key = key0 + k;
-              if (!((key < kt.hi && key >= kt.lo) || key < kt.sink_hi)) {
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c)
-                  st_shared_v4(v_tile + (c >> 3) * kHalf + k * 128 + (c & 7) * 16, make_uint4(0, 0, 0, 0));
-              }
-            }
-            fence_proxy_async_smem();
             __syncwarp();
+            ++k;
           }
-          if (more && !wait(full((n + 2) % kStages), (n + 2) / kStages)) break;
-#pragma unroll
-          for (int s = 0; s < kSlots; ++s) {
-            if (C::kOwnP && ok && more && view[s].needs(next0)) issue_scores(s, n + 2);
-            if (ok && view[s].needs(key0)) issue_output(s, n + 1);
-            if (!C::kOwnP && ok && more && view[s].needs(next0)) issue_scores(s, n + 2);
-          }
-          release(n + 1);
-          if (more) release(n + 2);
-        }
-        if (!ok) {
-          // products in flight still read shared and tensor memory: give them a short time to end
-          if (elect_one()) mma_commit(drained);
+          if ((b & 1) && elect_one()) mma_commit(empty(stage));
           __syncwarp();
-          volatile int never = 0;
-          mbar_wait(drained, 0, &never, nullptr, 0, 20000000ull);
         }
+      }
+      if (!ok) {
+        // products in flight still read shared and tensor memory: give them a short time to end
+        if (elect_one()) mma_commit(drained(warp - kIssuer0));
+        __syncwarp();
+        volatile int never = 0;
+        mbar_wait(drained(warp - kIssuer0), 0, &never, nullptr, 0, 20000000ull);
       }
     }
   }
