@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(128) paged_attention_join(const Params p) {
 }
 
 struct Plan {
-  int rows_per_tile;            // 16, 32, 64: row kernel; 256: chunk kernel
+  int rows_per_tile;            // 16, 32, 64: row kernel; 128 (head_dim 64), 256: chunk kernel
   int splits, min_split_tiles;  // in key tiles of the kernel (64, 128)
 };
 
@@ -69,8 +69,8 @@ Plan plan(const pd_paged_attention_desc& d) {
   constexpr int kSms = 148;
   Plan pl{};
   const int64_t group = d.heads_q / d.heads_kv, rows = std::min(d.max_q_len, d.tokens) * group;
-  pl.rows_per_tile = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
-  const bool chunk = pl.rows_per_tile == 256;
+  pl.rows_per_tile = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : d.head_dim == 64 ? 128 : 256;
+  const bool chunk = pl.rows_per_tile > 64;
   const int64_t row_tiles = (rows + pl.rows_per_tile - 1) / pl.rows_per_tile;
   const int64_t items = row_tiles * d.heads_kv * d.batch;  // CTAs without splitting
   int64_t keys = d.max_kv_len;
@@ -81,7 +81,7 @@ Plan plan(const pd_paged_attention_desc& d) {
   int64_t want;
   if (chunk) {
     pl.min_split_tiles = 4;
-    want = items > 0 ? kSms / items : 1;
+    want = items > 0 ? kSms * (d.head_dim == 64 ? 2 : 1) / items : 1;
   } else {
     pl.min_split_tiles = items <= kSms ? 2 : 4;
     want = items > 0 ? (kSms * 2 * 6 + items - 1) / items : 1;
@@ -155,7 +155,7 @@ extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc,
   }
   logf("paged attention batch %d tokens %d (max %d) heads %d/%d x %d: tiles of %d rows, %d key splits", d.batch, d.tokens,
        d.max_q_len, d.heads_q, d.heads_kv, d.head_dim, pl.rows_per_tile, pl.splits);
-  const pd_status launched = pl.rows_per_tile == 256 ? paged::launch_chunk(d, p, k_cache, v_cache, stream)
+  const pd_status launched = pl.rows_per_tile > 64 ? paged::launch_chunk(d, p, k_cache, v_cache, stream)
                                                      : paged::launch_rows(d, p, k_cache, v_cache, pl.rows_per_tile, stream);
   if (launched != PD_OK) return launched;
   if (pl.splits > 1) {

@@ -37,35 +37,17 @@ namespace {
 
 constexpr int kTile = 128;             // keys per tile, and rows per slot
 constexpr int kBlock = 64;             // keys per score buffer
-constexpr int kSlots = 2;
 constexpr int kSoftmaxWarps = 4;       // per slot
-constexpr int kIssuer0 = kSlots * kSoftmaxWarps, kProducer = kIssuer0 + 2 * kSlots;
-constexpr int kThreads = 32 * (kProducer + 1);
 constexpr int kStages = 4;
 constexpr int kHalf = kTile * 128;     // 64 columns of a tile: 128 lines of 128 bytes
 constexpr float kRaise = 8.f;          // powers of two by which a score may exceed the row's reference
 
-// 2^a for two exponents of at most kRaise on the FMA pipe: 2^round(a) * P(a - round(a)), P the degree-3 fit printed by
-// fit_exp2_poly.py (relative error 7.5e-5, far below the rounding to bf16).
-constexpr uint32_t kPolyPairMask = 0xA888u;  // bit k: pair k of every sixteen (five sixteenths)
-__device__ __forceinline__ void exp2_poly(uint64_t a2, float& e0, float& e1) {
-  constexpr float c0 = 9.999280572e-01f, c1 = 6.932609677e-01f, c2 = 2.426111251e-01f, c3 = 5.517166853e-02f;
-  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it leaves round(a) in the low mantissa bits
-  float a0, a1;
-  unpack_f32x2(a2, a0, a1);
-  a2 = pack_f32x2(fmaxf(a0, -125.0f), fmaxf(a1, -125.0f));  // (below, the exponent field would wrap)
-  const uint64_t t2 = add_f32x2(a2, pack_f32x2(kMagic, kMagic));
-  const uint64_t f2 = fma_f32x2(add_f32x2(t2, pack_f32x2(-kMagic, -kMagic)), pack_f32x2(-1.0f, -1.0f), a2);
-  uint64_t p2 = fma_f32x2(pack_f32x2(c3, c3), f2, pack_f32x2(c2, c2));
-  p2 = fma_f32x2(p2, f2, pack_f32x2(c1, c1));
-  p2 = fma_f32x2(p2, f2, pack_f32x2(c0, c0));
-  uint32_t t0, t1, p0, p1;
-  unpack_b32x2(t2, t0, t1);
-  unpack_b32x2(p2, p0, p1);
-  e0 = __uint_as_float(p0 + (t0 << 23));
-  e1 = __uint_as_float(p1 + (t1 << 23));
+// A special-function instruction that keeps its place among the others.
+__device__ __forceinline__ float ex2_in_order(float x) {
+  float y;
+  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
-
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -76,11 +58,18 @@ __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu 
 
 template <int D>
 struct ChunkConfig {
+  // head_dim 128: two slots per CTA, one CTA per SM.  head_dim 64: half the tensor memory and a third of the shared memory do
+  // for one slot, and two CTAs per SM cover each other's start and end, which weigh more where a window keeps the walk short.
+  static constexpr int kSlots = D == 64 ? 1 : 2;
+  static constexpr int kCtasPerSm = D == 64 ? 2 : 1;
+  static constexpr int kIssuer0 = kSlots * kSoftmaxWarps, kProducer = kIssuer0 + 2 * kSlots;
+  static constexpr int kThreads = 32 * (kProducer + 1);
+  static constexpr int kRows = kSlots * kTile;
   static constexpr int kTensor = kTile * D * 2;  // a Q, K or V tile
   static constexpr int kSmem = kSlots * kTensor + kStages * kTensor + 1024 /*barriers*/ + 1024 /*alignment*/;
   // tensor-memory columns: score buffer b of slot s at 128 s + 64 b (its probabilities over it, two keys to a column), output
-  // of slot s at 256 + D s
-  static constexpr uint32_t kColO = 256, kCols = 512;
+  // of slot s behind them
+  static constexpr uint32_t kColO = kSlots * kTile, kCols = kSlots * 256;
 };
 
 // The view of one slot: keys [lo, hi) and sinks [0, sink_hi) are seen by some of its rows.
@@ -94,10 +83,11 @@ struct SlotView {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(ChunkConfig<D>::kThreads, ChunkConfig<D>::kCtasPerSm)
 paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                              const Params p) {
   using C = ChunkConfig<D>;
+  constexpr int kSlots = C::kSlots, kIssuer0 = C::kIssuer0, kProducer = C::kProducer;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t sQ = base, ring = sQ + kSlots * C::kTensor, bars = ring + kStages * C::kTensor;
@@ -137,13 +127,13 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
   griddep_launch_dependents();
 
   const int split = blockIdx.x % p.splits;
-  const int pairs = gridDim.x / p.splits;
-  const int pair = pairs - 1 - blockIdx.x / p.splits;  // the last rows see the most keys: they go first
+  const int tiles = gridDim.x / p.splits;
+  const int tile = tiles - 1 - blockIdx.x / p.splits;  // the last rows see the most keys: they go first
   const int kvh = blockIdx.y, b = blockIdx.z;
   const Sequence seq = load_sequence(p, b);
-  const int all_rows = seq.n * p.group, row0 = pair * kSlots * kTile;
+  const int all_rows = seq.n * p.group, row0 = tile * C::kRows;
   if (row0 < all_rows) {
-    const int last_row = min(row0 + kSlots * kTile, all_rows) - 1;
+    const int last_row = min(row0 + C::kRows, all_rows) - 1;
     const KeyTiles kt = key_tiles(p, seq.pos0 + row0 / p.group, seq.pos0 + last_row / p.group, seq.length, kTile);
     int begin, end;
     split_range(p, kt.n, split, begin, end);
@@ -243,27 +233,38 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
         const uint64_t nref2 = pack_f32x2(-ref, -ref);
         uint64_t sum2[2] = {0, 0};
         uint32_t pk[32];
-        auto exponentials = [&](auto with_poly) {
+        // Groups of sixteen, each group's sums and packing behind the next one's exponentials, in this order: left to the
+        // compiler, the special-function unit stood idle between them (894 against 867 us for 4 x 2048 tokens; 790 with no
+        // exponentials at all).
+        auto scale_group = [&](int g) {
 #pragma unroll
-          for (int j = 0; j < 64; j += 2) {
-            const uint32_t(&v)[32] = x[j >> 5];
-            const uint64_t a2 = fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2, nref2);
-            float e0, e1;
-            if (decltype(with_poly)::value && ((kPolyPairMask >> ((j / 2) & 15)) & 1u)) {
-              exp2_poly(a2, e0, e1);
-            } else {
-              float a0, a1;
-              unpack_f32x2(a2, a0, a1);
-              e0 = ex2(a0);
-              e1 = ex2(a1);
-            }
-            sum2[(j >> 1) & 1] = add_f32x2(sum2[(j >> 1) & 1], pack_f32x2(e0, e1));
-            pk[j / 2] = pack_bf16(e0, e1);
+          for (int j = 16 * g; j < 16 * g + 16; j += 2) {
+            uint32_t(&v)[32] = x[j >> 5];
+            float a0, a1;
+            unpack_f32x2(fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2, nref2), a0, a1);
+            v[j & 31] = __float_as_uint(a0);
+            v[(j & 31) + 1] = __float_as_uint(a1);
+          }
+#pragma unroll
+          for (int j = 16 * g; j < 16 * g + 16; ++j)
+            x[j >> 5][j & 31] = __float_as_uint(ex2_in_order(__uint_as_float(x[j >> 5][j & 31])));
+        };
+        auto pack_group = [&](int g) {
+#pragma unroll
+          for (int j = 16 * g; j < 16 * g + 16; j += 2) {
+            uint32_t(&v)[32] = x[j >> 5];
+            sum2[(j >> 1) & 1] = add_f32x2(sum2[(j >> 1) & 1], pack_b32x2(v[j & 31], v[(j & 31) + 1]));
+            pk[j / 2] = pack_bf16(__uint_as_float(v[j & 31]), __uint_as_float(v[(j & 31) + 1]));
           }
         };
-        // (masked scores are -inf, which the polynomial would turn into something above 0)
-        if (whole) exponentials(std::true_type{});
-        else exponentials(std::false_type{});
+        scale_group(0);
+        scale_group(1);
+        pack_group(0);
+        scale_group(2);
+        pack_group(1);
+        scale_group(3);
+        pack_group(2);
+        pack_group(3);
         tmem_st_32x32b_x32(t_s, pk);
         float s0, s1;
         unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
@@ -279,34 +280,54 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
       if (ok && view.active && *abort_flag == 0) {
         tcgen05_fence_after_sync();
         const float inv = l > 0.f ? 1.f / l : 0.f;  // nothing seen: zeros
-        const int64_t tok = seq.q0 + t;
-        const int64_t at = ((int64_t)split * p.tokens + tok) * p.heads_q + head;
+        const int64_t at = ((int64_t)split * p.tokens + seq.q0 + t) * p.heads_q + head;
+        if (p.splits == 1) {
+          // through shared memory (this warp's rows of the slot's Q tile, which every product has read), so that a store
+          // instruction writes whole rows
+          const uint32_t stage = sQ + s * C::kTensor + (uint32_t)(quarter * 32) * 128u;
 #pragma unroll
-        for (int c = 0; c < D; c += 32) {
-          uint32_t o[32];
-          if (done > 0) {
-            tmem_ld_32x32b_x32(t_o + c, o);
-            tmem_ld_wait();
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = 0;
-          }
-          if (valid && p.splits == 1) {
-            uint4* dst = reinterpret_cast<uint4*>(p.out + tok * p.ld_out + (int64_t)head * D + c);
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            if (done > 0) {
+              tmem_ld_32x32b_x32(t_o + c, o);
+              tmem_ld_wait();
+            }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
               uint32_t w[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j)
-                w[j] = pack_bf16(__uint_as_float(o[8 * u + 2 * j]) * inv, __uint_as_float(o[8 * u + 2 * j + 1]) * inv);
-              dst[u] = make_uint4(w[0], w[1], w[2], w[3]);
+                w[j] = done > 0 ? pack_bf16(__uint_as_float(o[8 * u + 2 * j]) * inv, __uint_as_float(o[8 * u + 2 * j + 1]) * inv) : 0u;
+              const int chunk = c / 8 + u;
+              st_shared_v4(stage + (chunk >> 3) * kHalf + (uint32_t)lane * 128u + (uint32_t)(((chunk & 7) ^ (lane & 7)) << 4),
+                           make_uint4(w[0], w[1], w[2], w[3]));
             }
-          } else if (valid && l > 0.f) {
-            float4* dst = reinterpret_cast<float4*>(p.part_o + at * D + c);
+          }
+          __syncwarp();
+          const int64_t out_at = valid ? (int64_t)(seq.q0 + t) * p.ld_out + (int64_t)head * D : -1;  // of this lane's row
+          constexpr int kLanes = D / 8;  // 16 bytes each: a row
+#pragma unroll 4
+          for (int r0 = 0; r0 < 32; r0 += 32 / kLanes) {
+            const int r2 = r0 + lane / kLanes, chunk = lane % kLanes;
+            const int64_t to = __shfl_sync(0xffffffffu, out_at, r2);
+            if (to >= 0) {
+              const float4 v = ld_shared_v4_f32(stage + (chunk >> 3) * kHalf + (uint32_t)r2 * 128u + (uint32_t)(((chunk & 7) ^ (r2 & 7)) << 4));
+              *reinterpret_cast<float4*>(p.out + to + chunk * 8) = v;
+            }
+          }
+        } else if (done > 0) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-              dst[u] = make_float4(__uint_as_float(o[4 * u]) * inv, __uint_as_float(o[4 * u + 1]) * inv,
-                                   __uint_as_float(o[4 * u + 2]) * inv, __uint_as_float(o[4 * u + 3]) * inv);
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld_32x32b_x32(t_o + c, o);
+            tmem_ld_wait();
+            if (valid && l > 0.f) {
+              float4* dst = reinterpret_cast<float4*>(p.part_o + at * D + c);
+#pragma unroll
+              for (int u = 0; u < 8; ++u)
+                dst[u] = make_float4(__uint_as_float(o[4 * u]) * inv, __uint_as_float(o[4 * u + 1]) * inv,
+                                     __uint_as_float(o[4 * u + 2]) * inv, __uint_as_float(o[4 * u + 3]) * inv);
+            }
           }
         }
         if (valid && p.splits > 1) p.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
@@ -455,9 +476,9 @@ pd_status launch(const pd_paged_attention_desc& d, const Params& p, const CUtens
   using C = ChunkConfig<D>;
   static PerDeviceFlag smem_allowed;
   if (pd_status st = allow_dynamic_smem(paged_attention_chunk_kernel<D>, C::kSmem, smem_allowed); st != PD_OK) return st;
-  const int64_t pairs = ((int64_t)p.max_q_len * p.group + kSlots * kTile - 1) / (kSlots * kTile);
-  if (pairs * p.splits > 0x7fffffff) return PD_ERR_BAD_SHAPE;
-  launch_pdl(paged_attention_chunk_kernel<D>, dim3((unsigned)(pairs * p.splits), d.heads_kv, d.batch), dim3(kThreads),
+  const int64_t tiles = ((int64_t)p.max_q_len * p.group + C::kRows - 1) / C::kRows;
+  if (tiles * p.splits > 0x7fffffff) return PD_ERR_BAD_SHAPE;
+  launch_pdl(paged_attention_chunk_kernel<D>, dim3((unsigned)(tiles * p.splits), d.heads_kv, d.batch), dim3(C::kThreads),
              C::kSmem, s, tk, tv, p);
   return check_launch();
 }
