@@ -133,8 +133,11 @@ __device__ __forceinline__ void norm_row(float (&v)[UNITS][8], int t, int units,
   }
 }
 
+// 1024 threads per SM at 64 registers: left alone, the compiler takes 80 to 98 and two or three rows of 4096 columns are in
+// flight per SM instead of four (16384 x 4096: 171 against 151 us; at 48 registers it spills, 177).  Rows beyond 8192
+// columns, 32 elements to a thread, need the registers more.
 template <typename TX, typename TY, int UNITS, int THREADS_PER_ROW, int THREADS_PER_CTA>
-__global__ void __launch_bounds__(THREADS_PER_CTA)
+__global__ void __launch_bounds__(THREADS_PER_CTA, UNITS > 2 ? 1 : 1024 / THREADS_PER_CTA)
 norm_gate_residual_rows_in_registers(const NormParams p) {
   constexpr int ROWS = THREADS_PER_CTA / THREADS_PER_ROW;
   __shared__ float2 scratch[2][THREADS_PER_ROW / 32];
