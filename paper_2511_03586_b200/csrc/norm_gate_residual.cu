@@ -10,10 +10,15 @@
 // warp shuffle tree and, for rows that several warps share, one barrier.  Only h and n are rounded, and n is computed
 // from the unrounded h.
 //
-// A thread holds UNITS groups of 8 elements.  Rows of up to 512 columns take a warp, longer ones a CTA.
+// A thread holds UNITS groups of 8 elements.  Rows of up to 512 columns take a warp, longer ones a CTA.  What holds long
+// runs of rows back is the latency of a row's reductions at 32 warps per SM (IPC 1.4), and the parameter vectors, which
+// come through an L1 that the rows flush (16384 x 4096, fp32 stream, RMSNorm and LayerNorm: 151 us, 129 of them without the
+// vectors, 127 without the norms).  For bf16 streams with many rows, persistent CTAs of several row groups have each
+// group's next row copied to shared memory in bulk while the current one is worked on, and keep the vectors there.
 #include <cmath>
 
 #include "pd_common.cuh"
+#include "sm100_ptx.cuh"
 
 namespace pd {
 namespace {
@@ -193,6 +198,200 @@ norm_gate_residual_rows_in_registers(const NormParams p) {
   }
 }
 
+// ---- many rows: persistent CTAs, rows prefetched -------------------------------------------
+constexpr int kTimeoutNorm = 321;  // left in the device status word when a row does not arrive
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+// Barrier of one row group (up to sixteen: group 0 takes the barrier of __syncthreads, which is not called any more then);
+// true if every thread of the group says so.
+template <int THREADS>
+__device__ __forceinline__ bool group_all(int group, bool yes) {
+  uint32_t r;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.u32 q, %1, 0;\n"
+      "bar.red.and.pred p, %2, %3, q;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(r)
+      : "r"(yes ? 1u : 0u), "r"(group), "n"(THREADS)
+      : "memory");
+  return r != 0;
+}
+template <int THREADS>
+__device__ __forceinline__ float2 group_sum2(int group, float a, float b, float2* scratch) {
+  a = warp_sum(a);
+  b = warp_sum(b);
+  if ((threadIdx.x & 31) == 0) scratch[(threadIdx.x % THREADS) >> 5] = make_float2(a, b);
+  asm volatile("bar.sync %0, %1;" ::"r"(group), "n"(THREADS) : "memory");
+  float2 r = scratch[0];
+#pragma unroll
+  for (int w = 1; w < THREADS / 32; ++w) { r.x += scratch[w].x; r.y += scratch[w].y; }
+  return r;
+}
+// 8 elements of a parameter vector kept as two planes of float4 (unit c: plane 0 entry c, plane 1 entry c), which reads
+// without bank conflicts.
+__device__ __forceinline__ void planes8(const float4* planes, int units, int c, float (&v)[8]) {
+  const float4 a = planes[c], b = planes[units + c];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+
+constexpr int kPrefetchThreads = 1024, kPrefetchUnits = 2;
+
+// T threads per row, 1024 / T row groups per CTA, one CTA per SM.
+template <typename TX, typename TY, int T>
+__global__ void __launch_bounds__(kPrefetchThreads, 1) norm_gate_residual_rows_prefetched(const NormParams p, int* status) {
+  constexpr int kGroups = kPrefetchThreads / T, UNITS = kPrefetchUnits;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ float2 scratch[kGroups][4][T / 32];  // two sums of either norm: a group's warps may be one sum apart
+  __shared__ __align__(8) uint64_t bars[kGroups];
+  __shared__ int abort_flag;
+  const int group = threadIdx.x / T, t = threadIdx.x % T;
+  const int units = p.cols >> 3;
+  const float inv_cols = 1.0f / (float)p.cols;
+  const uint32_t y_bytes = (uint32_t)p.cols * sizeof(TY), x_bytes = (uint32_t)p.cols * sizeof(TX);
+  uint8_t* ys = smem + (size_t)group * (y_bytes + x_bytes);
+  uint8_t* xs = ys + y_bytes;
+  float4* planes = reinterpret_cast<float4*>(smem + (size_t)kGroups * (y_bytes + x_bytes));
+  const uint32_t bar = sm100::smem_u32(&bars[group]);
+  if (threadIdx.x == 0) {
+    for (int g = 0; g < kGroups; ++g) sm100::mbar_init(sm100::smem_u32(&bars[g]), 1);
+    abort_flag = 0;
+    sm100::fence_barrier_init();
+    sm100::fence_proxy_async_smem();
+  }
+  griddep_wait();
+  griddep_launch_dependents();
+  // the parameter vectors that the norms use, in this order
+  const float4* vec[4] = {nullptr, nullptr, nullptr, nullptr};
+  {
+    const float* src[4] = {p.post_norm != PD_NORM_NONE ? p.post_gamma : nullptr, p.post_norm == PD_NORM_LAYER ? p.post_beta : nullptr,
+                           p.pre_norm != PD_NORM_NONE && p.n ? p.pre_gamma : nullptr,
+                           p.pre_norm == PD_NORM_LAYER && p.n ? p.pre_beta : nullptr};
+    float4* at = planes;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (src[k]) {
+        vec[k] = at;
+        for (int c = threadIdx.x; c < 2 * units; c += kPrefetchThreads)
+          at[(c & 1) * units + (c >> 1)] = __ldg(reinterpret_cast<const float4*>(src[k]) + c);
+        at += 2 * units;
+      }
+  }
+  __syncthreads();
+
+  const int64_t step = (int64_t)gridDim.x * kGroups;
+  int64_t row = (int64_t)blockIdx.x * kGroups + group;
+  auto fetch = [&](int64_t r) {  // by the group's first thread
+    sm100::mbar_arrive_expect_tx(bar, y_bytes + x_bytes);
+    bulk_load(sm100::smem_u32(ys), static_cast<const TY*>(p.y) + r * p.cols, y_bytes, bar);
+    bulk_load(sm100::smem_u32(xs), static_cast<const TX*>(p.x) + r * p.cols, x_bytes, bar);
+  };
+  if (t == 0 && row < p.rows) fetch(row);
+  uint32_t parity = 0;
+  // v <- norm(v)
+  auto norm = [&](float (&v)[UNITS][8], int kind, const float4* gamma, const float4* beta, float2 (*sums)[T / 32]) {
+    if (kind == PD_NORM_NONE) return;
+    float shift = 0.f;
+    if (kind == PD_NORM_LAYER) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i)
+        if (t + i * T < units)
+          sum += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
+      shift = group_sum2<T>(group, sum, 0.f, sums[0]).x * inv_cols;
+    }
+    float sum = 0.f, q = 0.f;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)
+      if (t + i * T < units)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float d = v[i][j] - shift;
+          v[i][j] = d;
+          sum += d;
+          q = fmaf(d, d, q);
+        }
+    const float2 m = group_sum2<T>(group, sum, q, sums[1]);
+    const float rest = kind == PD_NORM_LAYER ? m.x * inv_cols : 0.f;
+    const float rstd = rsqrtf(fmaxf(m.y * inv_cols - rest * rest, 0.f) + p.eps);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int c = t + i * T;
+      if (c < units) {
+        float w[8];
+        if (gamma) {
+          planes8(gamma, units, c, w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - rest) * (rstd * w[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - rest) * rstd;
+        }
+        if (beta) {
+          planes8(beta, units, c, w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] += w[j];
+        }
+      }
+    }
+  };
+  for (; row < p.rows; row += step, parity ^= 1u) {
+    const bool here = sm100::mbar_wait(bar, parity, &abort_flag, status, kTimeoutNorm);
+    decltype(load_raw8(static_cast<const TX*>(nullptr))) rx[UNITS];
+    float v[UNITS][8];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int c = t + i * T;
+      if (c < units) {
+        widen8(*(reinterpret_cast<const decltype(load_raw8(static_cast<const TY*>(nullptr)))*>(ys) + c), v[i]);
+        rx[i] = *(reinterpret_cast<const decltype(load_raw8(static_cast<const TX*>(nullptr)))*>(xs) + c);
+      }
+    }
+    // every thread has its part in registers (or one has waited in vain): the buffer is free for the next row
+    if (!group_all<T>(group, here)) {
+      // leave no copy in flight: give it a short time to land
+      volatile int never = 0;
+      sm100::mbar_wait(bar, parity, &never, nullptr, 0, 20000000ull);
+      break;
+    }
+    if (t == 0 && row + step < p.rows) fetch(row + step);
+    norm(v, p.post_norm, vec[0], vec[1], scratch[group]);
+    const TY* gate = p.gate ? static_cast<const TY*>(p.gate) + (row / p.gate_rows) * p.cols : nullptr;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int c = t + i * T;
+      if (c < units) {
+        float xv[8];
+        widen8(rx[i], xv);
+        if (gate) {
+          float gv[8];
+          widen8(load_gate8(gate + 8 * c), gv);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = fmaf(v[i][j], gv[j], p.alpha * xv[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = fmaf(p.alpha, xv[j], v[i][j]);
+        }
+        if (p.h) store8(static_cast<TX*>(p.h) + row * p.cols + 8 * c, v[i]);
+      }
+    }
+    if (p.n) {
+      norm(v, p.pre_norm, vec[2], vec[3], scratch[group] + 2);
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int c = t + i * T;
+        if (c < units) store8(static_cast<TY*>(p.n) + row * p.cols + 8 * c, v[i]);
+      }
+    }
+  }
+}
+
 __device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float widen(float v) { return v; }
 
@@ -260,11 +459,43 @@ void launch_rows(const NormParams& p, cudaStream_t s) {
   launch_pdl(norm_gate_residual_rows_in_registers<TX, TY, UNITS, THREADS, CTA>, dim3(grid), dim3(CTA), 0, s, p);
 }
 
+// Shared memory of the prefetching kernel: a row of x and y (bf16) for every group of t threads, and the vectors in use.
+int prefetch_smem(const NormParams& p, int t) {
+  int vectors = 0;
+  if (p.post_norm != PD_NORM_NONE) vectors += (p.post_gamma != nullptr) + (p.post_norm == PD_NORM_LAYER && p.post_beta != nullptr);
+  if (p.pre_norm != PD_NORM_NONE) vectors += (p.pre_gamma != nullptr) + (p.pre_norm == PD_NORM_LAYER && p.pre_beta != nullptr);
+  return kPrefetchThreads / t * p.cols * 4 + vectors * p.cols * 4;
+}
+constexpr int kPrefetchMaxSmem = 222 * 1024;
+constexpr int kPrefetchMinRows = 3;  // rows of every group
+
+template <typename TX, typename TY, int T>
+pd_status launch_prefetched(const NormParams& p, cudaStream_t s) {
+  static PerDeviceFlag smem_allowed;
+  if (pd_status st = allow_dynamic_smem(norm_gate_residual_rows_prefetched<TX, TY, T>, kPrefetchMaxSmem, smem_allowed); st != PD_OK) return st;
+  int* status = device_status_ptr();
+  if (!status) return PD_ERR_CUDA;
+  logf("norm gate residual norm %lld x %d: %d rows in flight per SM, the next ones prefetched", (long long)p.rows, p.cols, kPrefetchThreads / T);
+  launch_pdl(norm_gate_residual_rows_prefetched<TX, TY, T>, dim3(sm_count()), dim3(kPrefetchThreads),
+             prefetch_smem(p, T), s, p, status);
+  return check_launch();
+}
+
 template <typename TX, typename TY>
 pd_status launch(const NormParams& p, cudaStream_t s) {
   const bool vec_ok = p.cols % 8 == 0 && p.cols <= 32768 && aligned16(p.y) && aligned16(p.x) && aligned16(p.gate) &&
                       aligned16(p.h) && aligned16(p.n) && aligned16(p.post_gamma) && aligned16(p.post_beta) &&
                       aligned16(p.pre_gamma) && aligned16(p.pre_beta);
+  // Measured (16384 rows, RMSNorm twice, us prefetched / not): bf16 streams, 4096 columns 98 / 108, 8192 columns 209 / 241,
+  // 1024 columns 27 / 28; with an fp32 stream 157 / 153, so not there.  1184 rows of 4096 columns: 11.9 / 12.2.
+  if constexpr (sizeof(TX) + sizeof(TY) == 4) {
+    if (vec_ok && p.cols > 1024 && p.cols <= 8192) {
+      const int t = p.cols <= 2048 ? 128 : p.cols <= 4096 ? 256 : 512;
+      if (p.rows >= kPrefetchMinRows * (int64_t)(kPrefetchThreads / t) * sm_count() && prefetch_smem(p, t) <= kPrefetchMaxSmem)
+        return t == 128 ? launch_prefetched<TX, TY, 128>(p, s) : t == 256 ? launch_prefetched<TX, TY, 256>(p, s)
+                                                                         : launch_prefetched<TX, TY, 512>(p, s);
+    }
+  }
   logf("norm gate residual norm %lld x %d: %s", (long long)p.rows, p.cols,
        !vec_ok ? "scalar path (unaligned, ragged or very long rows)" : p.cols <= 512 ? "one warp per row, row in registers"
        : "one CTA per row, row in registers");

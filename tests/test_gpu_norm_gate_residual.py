@@ -153,3 +153,24 @@ def test_binding_refusals():
         api.pd_norm_gate_residual_norm(y.t(), x.t())
     with pytest.raises(api.PdError):
         api.pd_norm_gate_residual_norm(y, x, eps=-1.0)
+
+
+@pytest.mark.parametrize("cols", [1032, 2048, 4096, 4104, 8192])
+@pytest.mark.parametrize("norms", [("rms", "rms"), ("layer", "layer"), ("none", "layer"), ("rms", "none"), ("none", "none")], ids=str)
+def test_prefetched_rows(cols, norms):
+    """bf16 streams of many rows: more rows than the persistent groups take in three turns, and not a multiple of them."""
+    run(3 * 8 * 148 + 5 if cols <= 2048 else 3 * 4 * 148 + 7, cols, BF16, BF16, *norms, groups=1)
+    run(2000, cols, BF16, BF16, *norms, groups=7, drop=("post_beta", "pre_gamma"))
+
+
+def test_prefetched_rows_in_place():
+    from paper_2511_03586_b200 import api
+    x, y, gate, vec = make(4000, 4096, BF16, BF16, 4000)
+    h, n = api.pd_norm_gate_residual_norm(y, x, gate=gate, post_norm="layer", **vec)
+    x2, y2 = x.clone(), y.clone()
+    api.pd_norm_gate_residual_norm(y2, x2, gate=gate, post_norm="layer", h=x2, n=y2, **vec)
+    assert torch.equal(x2, h) and torch.equal(y2, n)
+    for _ in range(3):
+        again = api.pd_norm_gate_residual_norm(y, x, gate=gate, post_norm="layer", **vec)
+        assert torch.equal(again[0], h) and torch.equal(again[1], n)
+    assert api.pd_get_device_status() == 0
