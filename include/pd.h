@@ -436,8 +436,9 @@ pd_status pd_kv_cache_append(const pd_paged_attention_desc* desc, const void* k_
  * A query that sees nothing (position in front of 0) gets zeros.  q, out: bf16,
  * strides in desc; out must not overlap an input.  head_dim 64 or 128,
  * heads_q / heads_kv at most 64, page_size a power of two from 8 to 4096,
- * max_pages * page_size and tokens * heads_q / heads_kv at most 2^30, batch and
- * heads_kv at most 65535 (else PD_ERR_UNSUPPORTED).  kv_len beyond max_pages pages:
+ * max_pages * page_size, tokens * heads_q / heads_kv and the blocks of 64 keys of
+ * all sequences and cache heads together, batch * heads_kv * max_pages * page_size
+ * / 64, at most 2^30, batch and heads_kv at most 65535 (else PD_ERR_UNSUPPORTED).  kv_len beyond max_pages pages:
  * keys end with the table.  Base pointers 16-byte aligned, strides multiples of 8
  * elements (else PD_ERR_ALIGNMENT).  Scores, softmax statistics and sums are
  * fp32; the exponentials are rounded to bf16 for the second product, which

@@ -48,6 +48,7 @@ __global__ void __launch_bounds__(128) paged_attention_join(const Params p) {
 struct Plan {
   int rows_per_tile;            // 16, 32, 64: row kernel; 128 (head_dim 64), 256: chunk kernel
   int splits, min_split_tiles;  // in key tiles of the kernel (64, 128)
+  bool whole_items;
 };
 
 constexpr int kMaxPositions = 1 << 30;  // of a sequence's table, and rows of a cache head: sums of two stay in 32 bits
@@ -61,7 +62,8 @@ bool supported(const pd_paged_attention_desc& d) {
   return (d.head_dim == 64 || d.head_dim == 128) && d.heads_q / d.heads_kv <= 64 && d.page_size >= 8 &&
          d.page_size <= 4096 && (d.page_size & (d.page_size - 1)) == 0 &&
          (int64_t)d.max_pages * d.page_size <= kMaxPositions && (int64_t)d.tokens * (d.heads_q / d.heads_kv) <= kMaxPositions &&
-         d.batch <= 65535 && d.heads_kv <= 65535;
+         (int64_t)d.batch * d.heads_kv * (((int64_t)d.max_pages * d.page_size + 63) / 64) <= kMaxPositions && d.batch <= 65535 &&
+         d.heads_kv <= 65535;
 }
 
 // Depends on the desc alone (the workspace size follows from it).
@@ -76,26 +78,33 @@ Plan plan(const pd_paged_attention_desc& d) {
   int64_t keys = d.max_kv_len;
   if (d.window > 0) keys = std::min<int64_t>(keys, (int64_t)d.window + d.sinks + d.max_q_len);
   const int64_t tile = chunk ? 128 : 64, tiles = (keys + tile - 1) / tile;
-  // Row kernel: two CTAs fit on an SM; about six waves of them even out ragged lengths.  Chunk kernel: one CTA per SM, and
-  // splits only to fill the SMs.  No share below min_split_tiles.
-  int64_t want;
-  if (chunk) {
-    pl.min_split_tiles = 4;
-    want = items > 0 ? kSms * (d.head_dim == 64 ? 2 : 1) / items : 1;
-  } else {
-    pl.min_split_tiles = items <= kSms ? 2 : 4;
-    want = items > 0 ? (kSms * 2 * 6 + items - 1) / items : 1;
+  if (!chunk) {
+    // two CTAs per SM share all key tiles evenly; fewer when there are not enough tiles for that
+    pl.min_split_tiles = 1;
+    pl.whole_items = tiles <= 2;
+    const int64_t all = std::max<int64_t>(tiles, 1) * d.heads_kv * d.batch;
+    pl.splits = (int)std::min<int64_t>(2 * kSms, std::max<int64_t>(all / pl.min_split_tiles, 1));
+    return pl;
   }
+  // One or two CTAs per SM, and splits only to fill the SMs, none below min_split_tiles.
+  pl.min_split_tiles = 4;
+  int64_t want = items > 0 ? kSms * (d.head_dim == 64 ? 2 : 1) / items : 1;
   want = std::min<int64_t>(want, (tiles + pl.min_split_tiles - 1) / pl.min_split_tiles);
   pl.splits = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 256);
   return pl;
 }
 
+// Rows of partial results in the workspace, and entries of the piece table behind them.
+size_t partial_rows(const pd_paged_attention_desc& d, const Plan& pl) {
+  if (pl.rows_per_tile > 64) return pl.splits > 1 ? (size_t)pl.splits * d.tokens * d.heads_q : 0;
+  return (size_t)2 * pl.splits * pl.rows_per_tile;
+}
+size_t table_entries(const pd_paged_attention_desc& d, const Plan& pl) {
+  return pl.rows_per_tile > 64 ? 0 : (size_t)d.batch * d.heads_kv;
+}
 size_t workspace_bytes(const pd_paged_attention_desc& d) {
   const Plan pl = plan(d);
-  if (pl.splits <= 1) return 0;
-  const size_t rows = (size_t)d.tokens * d.heads_q;
-  return pl.splits * rows * ((size_t)d.head_dim + 1) * sizeof(float);
+  return partial_rows(d, pl) * ((size_t)d.head_dim + 1) * sizeof(float) + table_entries(d, pl) * sizeof(int2);
 }
 
 }  // namespace
@@ -147,18 +156,20 @@ extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc,
   p.num_pages = d.num_pages; p.page_size = d.page_size; p.max_pages = d.max_pages;
   while ((1 << p.page_shift) < d.page_size) ++p.page_shift;
   p.max_q_len = std::min(d.max_q_len, d.tokens); p.window = std::min(d.window, paged::kMaxPositions); p.sinks = d.sinks;
-  p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles;
+  p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles; p.whole_items = pl.whole_items;
   p.scale_log2e = (float)((double)d.scale * 1.4426950408889634);
-  if (pl.splits > 1) {
+  if (need > 0) {
+    const size_t rows = paged::partial_rows(d, pl);  // (an even number in the row kernel: the table is aligned)
     p.part_o = static_cast<float*>(workspace);
-    p.part_lse = p.part_o + (size_t)pl.splits * d.tokens * d.heads_q * d.head_dim;
+    p.part_lse = p.part_o + rows * d.head_dim;
+    p.pieces = reinterpret_cast<int2*>(p.part_lse + rows);
   }
-  logf("paged attention batch %d tokens %d (max %d) heads %d/%d x %d: tiles of %d rows, %d key splits", d.batch, d.tokens,
-       d.max_q_len, d.heads_q, d.heads_kv, d.head_dim, pl.rows_per_tile, pl.splits);
+  logf("paged attention batch %d tokens %d (max %d) heads %d/%d x %d: tiles of %d rows, %s %d", d.batch, d.tokens,
+       d.max_q_len, d.heads_q, d.heads_kv, d.head_dim, pl.rows_per_tile, pl.rows_per_tile > 64 ? "key splits" : "CTAs", pl.splits);
   const pd_status launched = pl.rows_per_tile > 64 ? paged::launch_chunk(d, p, k_cache, v_cache, stream)
                                                      : paged::launch_rows(d, p, k_cache, v_cache, pl.rows_per_tile, stream);
   if (launched != PD_OK) return launched;
-  if (pl.splits > 1) {
+  if (pl.rows_per_tile > 64 && pl.splits > 1) {
     const int64_t rows = (int64_t)d.tokens * d.heads_q;
     const unsigned grid = (unsigned)((rows + 3) / 4);
     if (d.head_dim == 64) launch_pdl(paged::paged_attention_join<64>, dim3(grid), dim3(128), 0, stream, p);

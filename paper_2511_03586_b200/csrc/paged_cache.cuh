@@ -17,14 +17,18 @@ struct Params {
   const __nv_bfloat16* q;
   __nv_bfloat16* out;
   const int32_t *block_table, *cu_q, *kv_len;
-  float* part_o;    // split keys only: [splits][tokens * heads_q][head_dim] partial outputs (normalised), then
-  float* part_lse;  // [splits][tokens * heads_q] logarithms (base 2) of their sums of exponentials
+  // Partial outputs (normalised) and the logarithms (base 2) of their sums of exponentials: [splits][tokens * heads_q]
+  // (chunk kernel), or [2 CTAs][rows per tile] with the places of an item's pieces (row kernel).
+  float *part_o, *part_lse;
+  int2* pieces;
   int* status;
   int64_t ld_q, ld_out;
   int batch, tokens, heads_q, heads_kv, group;
   int num_pages, page_size, page_shift, max_pages;
   int max_q_len, window, sinks;
-  int splits, min_split_tiles;
+  int splits;           // of the keys of every row tile (chunk kernel), CTAs in all (row kernel)
+  int min_split_tiles;  // the smallest share of key tiles
+  int whole_items;      // row kernel: no item is shared out (short contexts: nothing to join)
   float scale_log2e;
 };
 
