@@ -5,11 +5,12 @@
 //   the running kept weight exceeds u times its total.
 //
 // The row is never sorted as a whole.  A cut is "the first rank at which a running sum reaches a target", and a histogram
-// over value (bins of 1/32 in (max - logit) / T) says which bin holds it; the logits of that bin, a few hundred of a
-// hundred thousand, are gathered in one CTA, where the same search goes on over (value, index) until it is down to one.
-//   top-k            : histogram of counts; everything down to the bin of rank k is gathered, and the rest (top-p, min-p,
-//                      the draw) happens on that short list.
-//   top-p, no top-k  : the histogram is of weights; the logits of the bin that holds the cut are gathered.
+// of counts over value (bins of 1/64 in (max - logit) / T) says which bin holds it; the logits of that bin, a few hundred of
+// a hundred thousand, are gathered in one CTA, where the search goes on over (value, index) until it is down to one.
+//   top-k            : everything down to the bin of rank k is gathered, and the rest (top-p, min-p) happens on that list.
+//   top-p, no top-k  : weights within a bin differ by 1.6 %, so the counts bound the weight before and behind every bin, and
+//                      with these the bins, one to three of them, that can hold the cut; the exact weight of all, and of
+//                      what lies above these bins, is then summed in one pass.
 //   neither          : sums alone.
 // The token is then found by prefix sums over warps' shares, and by a scan of one warp's share.
 // Rows whose candidates do not fit the list (thousands of equal logits, a very large k) take histograms of exact weights
@@ -36,8 +37,9 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 1024;           // bins of 1/32 in z = (max - logit) / T, up to z = 32 (weight 2^-46: zero units)
-constexpr float kBinsPerUnit = 32.f;
+constexpr int kBins = 2048;           // bins of 1/64 in z = (max - logit) / T, up to z = 32 (weight 2^-46: zero units)
+constexpr float kBinsPerUnit = 64.f;
+constexpr int kSlowBins = 1024;       // bins of a step of the search without a list
 constexpr int kList = 2048;           // candidates that one CTA takes
 constexpr int kTable = 512;
 constexpr int kFixed = 44;            // weights in units of 2^-44
@@ -121,14 +123,14 @@ static_assert(kTable == 512 && kTable == kThreads, "weight() shifts by 9, and ev
 
 struct SlowSearch {
   // own histogram (weights in two halves), then the cluster's sums of the bins this CTA owns (first level, later levels)
-  uint32_t count[kBins], lo[kBins], hi[kBins];
-  uint32_t sum_count[2][kBins];
-  u64 sum_weight[2][kBins];
+  uint32_t count[kSlowBins], lo[kSlowBins], hi[kSlowBins];
+  uint32_t sum_count[2][kSlowBins];
+  u64 sum_weight[2][kSlowBins];
 };
 struct FastSearch {
-  uint32_t hist[2 * kBins];  // own histogram: counts, or the lower and the upper halves of weights
-  u64 sum[kBins];            // the cluster's
-  u64 list[kList];           // candidates as (key, index), in CTA 0
+  uint32_t hist[kBins];  // own counts
+  uint32_t sum[kBins];   // the cluster's
+  u64 list[kList];       // candidates as (key, index), in CTA 0
 };
 
 struct Shared {
@@ -137,9 +139,10 @@ struct Shared {
     SlowSearch slow;
     FastSearch fast;
   };
-  // filled by the cluster's CTAs, entry r by CTA r (the first two in every CTA, share_weight in CTA 0 alone)
+  // filled by the cluster's CTAs, entry r by CTA r (the peer_ ones in every CTA, share_weight in CTA 0 alone)
   float peer_max[kMaxCluster];
   uint32_t peer_candidates[kMaxCluster];
+  u64 peer_total[kMaxCluster], peer_above[kMaxCluster];
   u64 share_weight[kMaxCluster * kWarps];  // kept weight of every warp's share, candidates not included at first
   uint32_t candidates, own_candidates;
   uint32_t first_max;
@@ -152,9 +155,10 @@ struct Shared {
   u64 warp_weight[kWarps];
   uint32_t warp_count[kWarps];
   u64 warp_high[kWarps];
+  double warp_low_sum[kWarps], warp_high_sum[kWarps];
   float warp_max[kWarps];
   // result of a search step
-  int found_bin;
+  int found_bin, found_bin2;
   u64 found_weight_before, found_weight;
   uint32_t found_count_before, found_count;
   uint32_t range[2];
@@ -196,11 +200,11 @@ __device__ __forceinline__ void add_to_bin(Shared& sh, int b, u64 w) {
   if (hi) atomicAdd(&sh.slow.hi[b], hi);
 }
 
-// Sums the cluster's histograms: CTA r gets the bins [r, r + 1) * kBins / n, and every CTA the sums over these slices of
+// Sums the cluster's histograms: CTA r gets the bins [r, r + 1) * kSlowBins / n, and every CTA the sums over these slices of
 // bins.  `level` 0 keeps the sums of the first histogram for a second search.
 __device__ void sum_bins(cg::cluster_group& cluster, Shared& sh, int level, int n, int rank) {
   cluster.sync();  // every histogram is complete
-  const int own = kBins / n;
+  const int own = kSlowBins / n;
   u64 tw = 0;
   uint32_t tc = 0;
   for (int i = threadIdx.x; i < own; i += kThreads) {
@@ -232,7 +236,7 @@ __device__ void sum_bins(cg::cluster_group& cluster, Shared& sh, int level, int 
 // Finds the first bin at which the running count (by_count) or weight reaches `target`, and leaves it in sh.found_*; the
 // last non-empty bin when the total stays below.  Collective over the CTA; every CTA of the cluster finds the same.
 __device__ void find_bin(cg::cluster_group& cluster, Shared& sh, int level, int n, bool by_count, u64 target) {
-  const int own = kBins / n;
+  const int own = kSlowBins / n;
   __syncthreads();  // the previous search's result and scratch have been read
   u64 before_w = 0;
   uint32_t before_c = 0;
@@ -255,10 +259,10 @@ __device__ void find_bin(cg::cluster_group& cluster, Shared& sh, int level, int 
   const Shared* peer = cluster.map_shared_rank(&sh, owner < 0 ? 0 : owner);
   // thread i takes `per` consecutive bins of the owner's slice
   const int per = (own + kThreads - 1) / kThreads;
-  u64 w[kBins / kThreads], tw = 0;
-  uint32_t c[kBins / kThreads], tc = 0;
+  u64 w[kSlowBins / kThreads], tw = 0;
+  uint32_t c[kSlowBins / kThreads], tc = 0;
 #pragma unroll
-  for (int j = 0; j < kBins / kThreads; ++j) {
+  for (int j = 0; j < kSlowBins / kThreads; ++j) {
     const int i = threadIdx.x * per + j;
     const bool in = j < per && i < own;
     w[j] = in ? peer->slow.sum_weight[level][i] : 0;
@@ -277,7 +281,7 @@ __device__ void find_bin(cg::cluster_group& cluster, Shared& sh, int level, int 
   uint32_t rc = c0 + sc - tc;
   // candidate bins: every non-empty bin whose predecessor sum is below the target; the last of them is the answer
 #pragma unroll
-  for (int j = 0; j < kBins / kThreads; ++j) {
+  for (int j = 0; j < kSlowBins / kThreads; ++j) {
     if (c[j] > 0 && (by_count ? (u64)rc : rw) < target) atomicMax(&sh.found_bin, (int)threadIdx.x * per + j);
     rw += w[j];
     rc += c[j];
@@ -286,7 +290,7 @@ __device__ void find_bin(cg::cluster_group& cluster, Shared& sh, int level, int 
   rw = w0 + sw - tw;
   rc = c0 + sc - tc;
 #pragma unroll
-  for (int j = 0; j < kBins / kThreads; ++j) {
+  for (int j = 0; j < kSlowBins / kThreads; ++j) {
     if (j < per && sh.found_bin == (int)threadIdx.x * per + j) {
       sh.found_weight_before = rw;
       sh.found_count_before = rc;
@@ -323,7 +327,7 @@ __device__ SlowCut search(cg::cluster_group& cluster, Shared& sh, const Row& row
     uint32_t lo = key_of(row.max), hi = key_of(-INFINITY);
     while (lo < hi) {
       const uint32_t mid = lo + (hi - lo) / 2;
-      if (row.bin(value_of(mid)) >= b) hi = mid; else lo = mid + 1;
+      if (row.bin(value_of(mid)) / 2 >= b) hi = mid; else lo = mid + 1;
     }
     sh.range[threadIdx.x] = lo;
   }
@@ -332,8 +336,8 @@ __device__ SlowCut search(cg::cluster_group& cluster, Shared& sh, const Row& row
   for (;;) {
     const uint32_t width = hi - lo;
     int shift = 0;
-    while ((width - 1) >> shift >= (uint32_t)kBins) ++shift;
-    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.slow.count[i] = sh.slow.lo[i] = sh.slow.hi[i] = 0;
+    while ((width - 1) >> shift >= (uint32_t)kSlowBins) ++shift;
+    for (int i = threadIdx.x; i < kSlowBins; i += kThreads) sh.slow.count[i] = sh.slow.lo[i] = sh.slow.hi[i] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < len; i += kThreads) {
       const uint32_t k = key_of(vals[i]);
@@ -466,19 +470,14 @@ __device__ __forceinline__ u64 draw_target(const SampleParams& p, int64_t row, u
 }
 
 // Sums the cluster's histograms into every CTA's fast.sum: CTA r adds up bins [r, r + 1) * kBins / n and hands them out.
-template <bool WEIGHTS>
 __device__ void sum_histograms(cg::cluster_group& cluster, Shared& sh, int n, int rank) {
   cluster.sync();  // every histogram is complete
   const int own = kBins / n;
   for (int i = threadIdx.x; i < own; i += kThreads) {
     const int b = rank * own + i;
-    u64 part[kMaxCluster], sum = 0;
+    uint32_t part[kMaxCluster], sum = 0;
 #pragma unroll
-    for (int r = 0; r < kMaxCluster; ++r) {
-      const uint32_t* hist = r < n ? cluster.map_shared_rank(&sh, r)->fast.hist : nullptr;
-      part[r] = r < n ? hist[b] : 0;
-      if (WEIGHTS) part[r] += r < n ? (u64)hist[kBins + b] << 32 : 0;
-    }
+    for (int r = 0; r < kMaxCluster; ++r) part[r] = r < n ? cluster.map_shared_rank(&sh, r)->fast.hist[b] : 0;
 #pragma unroll
     for (int r = 0; r < kMaxCluster; ++r) sum += part[r];
 #pragma unroll
@@ -488,34 +487,81 @@ __device__ void sum_histograms(cg::cluster_group& cluster, Shared& sh, int n, in
   cluster.sync();  // the sums are in, and nobody reads a histogram any more
 }
 
-// The first bin at which the running sum reaches target(total): sh.found_bin, the sum before and through it
-// (found_weight_before, found_weight); the last bin if the total stays below.
-template <typename F>
-__device__ void locate(Shared& sh, F&& target_of) {
-  constexpr int kEach = kBins / kThreads;
-  u64 c[kEach], sum = 0;
+// The first bin through which there are `rank` logits or more (the last bin if there are fewer in all): sh.found_bin, and
+// their number, sh.found_count.
+constexpr int kEach = kBins / kThreads;
+__device__ void locate_rank(Shared& sh, uint32_t rank) {
+  uint32_t c[kEach], sum = 0;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) { c[j] = sh.fast.sum[threadIdx.x * kEach + j]; sum += c[j]; }
-  const u64 upto = block_scan_u64(sh, sum);
+  const uint32_t upto = (uint32_t)block_scan_u64(sh, sum);
   if (threadIdx.x == kThreads - 1) {
-    sh.total = upto;
     sh.found_bin = kBins - 1;
-    sh.found_weight_before = upto - c[kEach - 1];
-    sh.found_weight = upto;
+    sh.found_count = upto;
   }
   __syncthreads();
-  const u64 target = target_of(sh.total);
-  u64 run = upto - sum;
+  uint32_t run = upto - sum;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
-    const u64 before = run;
+    const uint32_t before = run;
     run += c[j];
-    if (before < target && run >= target) {
+    if (before < rank && run >= rank) {
       sh.found_bin = threadIdx.x * kEach + j;
-      sh.found_weight_before = before;
-      sh.found_weight = run;
+      sh.found_count = run;
     }
   }
+  __syncthreads();
+}
+
+// The bins that can hold the cut at the share `top_p` of all weight: the first bin b at which prefix(b) >= top_p (prefix(b) +
+// suffix(b)), where prefix is the weight of the bins up to b and suffix that of the bins behind it, that is
+//   (1 - top_p) prefix(b) >= top_p suffix(b).
+// The logits of bin b lie within half a bin (and the rounding of bin()) of z = b / 64, so counts bound both sums from below
+// and above: sh.found_bin is the first bin where the condition may hold, sh.found_bin2 the first where it must.
+__device__ void locate_weight(Shared& sh, float top_p, int vocab) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  double lo[kEach], hi[kEach], lo_sum = 0.0, hi_sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int b = threadIdx.x * kEach + j;
+    const double c = (double)sh.fast.sum[b];
+    const float mid = __expf(-(float)b / kBinsPerUnit);  // (relative error below 1e-5: within the margin)
+    lo[j] = c * (mid * (1.f - 0.51f / kBinsPerUnit));                   // e^-x >= 1 - x
+    hi[j] = c * (mid * (1.f + 0.52f / kBinsPerUnit));                   // e^x <= 1 + x + x^2, x = 0.51 / 64
+    lo_sum += lo[j];
+    hi_sum += hi[j];
+  }
+  double lo_upto = lo_sum, hi_upto = hi_sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double u = __shfl_up_sync(0xffffffffu, lo_upto, o), v = __shfl_up_sync(0xffffffffu, hi_upto, o);
+    if (lane >= o) { lo_upto += u; hi_upto += v; }
+  }
+  if (lane == 31) { sh.warp_low_sum[warp] = lo_upto; sh.warp_high_sum[warp] = hi_upto; }
+  if (threadIdx.x == 0) sh.found_bin = sh.found_bin2 = kBins - 1;
+  __syncthreads();
+  double lo_all = 0.0, hi_all = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w == warp) { lo_upto += lo_all; hi_upto += hi_all; }
+    lo_all += sh.warp_low_sum[w];
+    hi_all += sh.warp_high_sum[w];
+  }
+  // Weights are rounded to units: half a unit each, and the sums here to 1e-16 of themselves.
+  const double slack = vocab * (1.0 / (double)(1ull << kFixed)) + 1e-13 * hi_all;
+  const double p = fmax((double)top_p, 0.0);
+  double lo_run = lo_upto - lo_sum, hi_run = hi_upto - hi_sum;
+  int first_may = kBins, first_must = kBins;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    lo_run += lo[j];
+    hi_run += hi[j];
+    const int b = threadIdx.x * kEach + j;
+    if (first_may == kBins && (1.0 - p) * (hi_run + slack) + slack >= p * (lo_all - lo_run - slack)) first_may = b;
+    if (first_must == kBins && (1.0 - p) * (lo_run - slack) - slack >= p * (hi_all - hi_run + slack)) first_must = b;
+  }
+  if (first_may < kBins) atomicMin(&sh.found_bin, first_may);
+  if (first_must < kBins) atomicMin(&sh.found_bin2, first_must);
   __syncthreads();
 }
 
@@ -525,7 +571,7 @@ __device__ __forceinline__ float candidate_value(u64 c) { return value_of((uint3
 // Candidates are collected in the CTA first (over the histograms, which have served by then): one trip to CTA 0 per
 // candidate would stall its warp for a microsecond each.
 __device__ __forceinline__ u64* own_list(Shared& sh) { return reinterpret_cast<u64*>(sh.fast.hist); }
-static_assert(2 * kBins * sizeof(uint32_t) + kBins * sizeof(u64) >= kList * sizeof(u64), "a whole list fits over the histograms");
+static_assert(2 * kBins * sizeof(uint32_t) >= kList * sizeof(u64), "a whole list fits over the histograms");
 // Walks this warp's share as for_share does; the logits for which f(v) is true become candidates.  They are noted as bits
 // and appended once for every 16 groups, since an append costs an atomic's round trip.
 template <typename F>
@@ -684,12 +730,12 @@ __device__ void slow_path(cg::cluster_group& cluster, const SampleParams& p, Sha
   cut.key = 0xffffffffu;  // nothing cut off
   cut.ties = 0;
   cluster.sync();  // the list's memory is free
-  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.slow.count[i] = sh.slow.lo[i] = sh.slow.hi[i] = 0;
+  for (int i = threadIdx.x; i < kSlowBins; i += kThreads) sh.slow.count[i] = sh.slow.lo[i] = sh.slow.hi[i] = 0;
   __syncthreads();
   for (int i = threadIdx.x; i < len; i += kThreads) {
     const float v = vals[i];
-    const int b = row.bin(v);
-    if (b < kBins) add_to_bin(sh, b, row.weight(v));
+    const int b = row.bin(v) / 2;
+    if (b < kSlowBins) add_to_bin(sh, b, row.weight(v));
   }
   sum_bins(cluster, sh, 0, n, rank);
   u64 kept_total = 0;
@@ -807,7 +853,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t i_row = blockIdx.x / n;
   sh.table[threadIdx.x] = exp2(kFixed + threadIdx.x / (double)kTable);
-  for (int i = threadIdx.x; i < 2 * kBins; i += kThreads) sh.fast.hist[i] = 0;
+  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.fast.hist[i] = 0;
   if (threadIdx.x == 0) { sh.candidates = sh.own_candidates = 0; sh.first_max = 0xffffffffu; }
   griddep_wait();
   griddep_launch_dependents();
@@ -864,15 +910,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   }
   const int share = ((p.slice + kWarps - 1) / kWarps + 31) / 32 * 32;  // of a warp, contiguous
   const int w_begin = min(warp * share, len), w_end = min(w_begin + share, len);
-  if (top_k > 1 && top_k < p.vocab) {
+  const bool by_rank = top_k > 1 && top_k < p.vocab;
+  if (by_rank || top_p < 1.f) {
     for_share(vals, w_begin, w_end, [&](float v, int) {
       const int b = row.bin(v);
       if (b < kBins) atomicAdd(&sh.fast.hist[b], 1u);
     });
-    sum_histograms<false>(cluster, sh, n, rank);
-    locate(sh, [&](u64) { return (u64)top_k; });
+    sum_histograms(cluster, sh, n, rank);
+  }
+  if (by_rank) {
+    locate_rank(sh, (uint32_t)top_k);
     const int bin = sh.found_bin;
-    const uint32_t count = (uint32_t)sh.found_weight;
+    const uint32_t count = sh.found_count;
     if (count > (uint32_t)kList) {
       slow_path<T>(cluster, p, sh, row, vals, i_row, start, len, n, rank, top_k, top_p, min_weight);
       return;
@@ -907,41 +956,51 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
     return;
   }
   if (top_p < 1.f) {
-    for_share(vals, w_begin, w_end, [&](float v, int) {
-      const int b = row.bin(v);
-      const double w = row.biased_weight(v);
-      if (b < kBins) {
-        const uint32_t lo = (uint32_t)__double2loint(w), old = atomicAdd(&sh.fast.hist[b], lo);
-        const uint32_t hi = (uint32_t)(__double2hiint(w) - Row::kBiasHigh) + (old + lo < old ? 1u : 0u);
-        if (hi) atomicAdd(&sh.fast.hist[kBins + b], hi);
-      }
-    });
-    sum_histograms<true>(cluster, sh, n, rank);
-    u64 need = 0;
-    locate(sh, [&](u64 total) { return need = max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)total), 1ull); });
-    const int bin = sh.found_bin;
-    const u64 before = sh.found_weight_before;
-    double kept = 0.0;
+    locate_weight(sh, top_p, p.vocab);
+    const int low = sh.found_bin, high = sh.found_bin2;
+    double all = 0.0, above = 0.0, kept = 0.0;
     if (min_weight <= 1)
       collect_share(sh, vals, start, w_begin, w_end, [&](float v) {
         const int b = row.bin(v);
-        kept += row.weight_d(b < bin ? v : row.floor);
-        return b == bin;
+        const double w = row.weight_d(v);
+        all += w;
+        above += b < low ? w : 0.0;
+        return b >= low && b <= high;
       });
     else
       collect_share(sh, vals, start, w_begin, w_end, [&](float v) {
         const int b = row.bin(v);
-        const double w = row.weight_d(b < bin ? v : row.floor);
-        kept += w >= (double)min_weight ? w : 0.0;
-        return b == bin;
+        const double w = row.weight_d(v);
+        all += w;
+        above += b < low ? w : 0.0;
+        kept += b < low && w >= (double)min_weight ? w : 0.0;
+        return b >= low && b <= high;
       });
+    if (min_weight <= 1) kept = above;
     push_candidates(sh, first);
     const u64 kept_sum = warp_sum_u64((u64)kept);
     if (lane == 0) first->share_weight[rank * kWarps + warp] = kept_sum;
-    if (threadIdx.x < n) cluster.map_shared_rank(&sh, threadIdx.x)->peer_candidates[rank] = sh.own_candidates;
+    const u64 all_sum = warp_sum_u64((u64)all), above_sum = warp_sum_u64((u64)above);
+    if (lane == 0) { sh.warp_weight[warp] = all_sum; sh.warp_high[warp] = above_sum; }
+    __syncthreads();
+    if (threadIdx.x < n) {
+      u64 cta_all = 0, cta_above = 0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) { cta_all += sh.warp_weight[w]; cta_above += sh.warp_high[w]; }
+      Shared* peer = cluster.map_shared_rank(&sh, threadIdx.x);
+      peer->peer_total[rank] = cta_all;
+      peer->peer_above[rank] = cta_above;
+      peer->peer_candidates[rank] = sh.own_candidates;
+    }
     cluster.sync();
     uint32_t count = 0;
-    for (int r = 0; r < n; ++r) count += sh.peer_candidates[r];
+    u64 total = 0, before = 0;
+    for (int r = 0; r < n; ++r) {
+      count += sh.peer_candidates[r];
+      total += sh.peer_total[r];
+      before += sh.peer_above[r];
+    }
+    const u64 need = max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)total), 1ull);
     if (count > (uint32_t)kList) {
       slow_path<T>(cluster, p, sh, row, vals, i_row, start, len, n, rank, top_k, top_p, min_weight);
       return;
