@@ -495,6 +495,15 @@ def _call(fn, device: int, stream, *args) -> None:
         raise PdError(status, fn.__name__)
 
 
+def _lend(stream, *tensors) -> None:
+    """Tensors that were allocated here, on the current stream, for a call on ``stream``: their memory is not handed out
+    again before that stream is through with it."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def _token_stride(t: torch.Tensor, name: str) -> int:
     """Elements from token to token of [tokens, heads, head_dim] whose heads lie side by side."""
     if t.dim() != 3:
@@ -567,6 +576,7 @@ def pd_attention_paged_fwd(q, k_cache, v_cache, block_table, cu_q, kv_len, *, ma
     if out is None:
         out = q.new_empty((tokens, heads_q, head_dim))
         op, ld_out = out.data_ptr(), heads_q * head_dim
+        _lend(stream, out)
     else:
         op, ld_out = _on(device, out, torch.bfloat16, "out", False), _token_stride(out, "out")
         if out.shape != q.shape:
@@ -577,6 +587,7 @@ def pd_attention_paged_fwd(q, k_cache, v_cache, block_table, cu_q, kv_len, *, ma
         ws_bytes = _lib.pd_attention_paged_workspace_bytes(desc)
         workspace = q.new_empty((ws_bytes,), dtype=torch.uint8) if ws_bytes else None
         ws = workspace.data_ptr() if ws_bytes else None
+        _lend(stream, workspace)
     else:
         ws, ws_bytes = _on(device, workspace, torch.uint8, "workspace"), workspace.numel()
     _call(_lib.pd_attention_paged_fwd, device, stream, desc, qp, kc, vc, table, cu, lens, op, ws, ws_bytes)
@@ -632,10 +643,12 @@ def pd_norm_gate_residual_norm(y, x, *, gate=None, gate_rows: int | None = None,
             raise ValueError("gate has too few rows")
     if h is None:
         h = torch.empty_like(x)
+        _lend(stream, h)
     elif h.shape != x.shape:
         raise ValueError("h must be [rows, cols]")
     if n is None:
         n = torch.empty_like(y)
+        _lend(stream, n)
     elif n.shape != y.shape:
         raise ValueError("n must be [rows, cols]")
     hp, np_ = _on(device, h, x.dtype, "h"), _on(device, n, y.dtype, "n")
@@ -657,8 +670,10 @@ def pd_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None
         raise TypeError("u must be a tensor")
     if tokens is None:
         tokens = logits.new_empty((rows,), dtype=torch.int32)
+        _lend(stream, tokens)
     if probs is None:
         probs = logits.new_empty((rows,), dtype=torch.float32)
+        _lend(stream, probs)
     ptrs = []
     for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
                            ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("u", u, torch.float32),

@@ -324,3 +324,29 @@ def test_binding_refusals():
 def test_no_wait_ran_out():
     from paper_2511_03586_b200 import api
     assert api.pd_get_device_status() == 0
+
+
+def test_stream_argument_keeps_memory():
+    """Calls on a stream that is behind: the tensors made for them, and dropped at once, are not handed out meanwhile."""
+    p = Paged([(1, 3000), (1, 2000)], 8, 2, 128, 16, seed=11)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)          # some ten milliseconds
+    outs = [p.attend(stream=s) for _ in range(4)]
+    scribble = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(64)]
+    s.synchronize()
+    del scribble
+    for o in outs:
+        p.check(o)
+
+
+@pytest.mark.parametrize("batch", [33, 200])
+def test_large_batches(batch):
+    """More sequences than a warp has lanes, and than a block has threads, with empty and absent ones among them."""
+    lens = [(0 if i % 7 == 3 else 1, (i * 37) % 300 + 1) for i in range(batch)]
+    lens = [(n, kv if n else 0) for n, kv in lens]
+    p = Paged(lens, 4, 2, 64, 16, seed=batch)
+    p.check(p.attend())
+    p = Paged([(2 if n else 0, max(kv, 2) if n else 0) for n, kv in lens], 8, 1, 64, 16, seed=batch, window=40, sinks=3)
+    p.check(p.attend())
