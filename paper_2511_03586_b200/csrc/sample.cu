@@ -24,7 +24,9 @@
 //
 // HBM-bound in principle: the logits are read once, 4 (or 2) bytes each, and held in the shared memory of a cluster of
 // 1 to 8 CTAs (distributed by contiguous slices, so that index order is slice order).  In fact the passes over shared
-// memory, the double-precision exponentials (ten operations each) and the cluster's barriers weigh more.
+// memory, the double-precision exponentials (eight operations each) and the cluster's barriers weigh more: 256 x 128000
+// fp32 logits with top-p take 184 us, 20 of which the bytes need; stopped after the maximum, 43; after the histogram, 76;
+// after locating the cut's bins, 85; after the exact sums, 151.  CTAs of 256 threads and 128 registers take 202 us.
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -68,6 +70,20 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float((a & 0x80000000u) ? a ^ 0x80000000u : ~a);
 }
 
+// 2^(44 + i / 512), by the Taylor series of exp (22 terms: ln 2 to the 23rd over 23! is 1e-26).
+struct PowerTable {
+  double v[kTable];
+  constexpr PowerTable() : v() {
+    for (int i = 0; i < kTable; ++i) {
+      const double x = 0.69314718055994530942 * i / kTable;
+      double e = 1.0;
+      for (int k = 22; k > 0; --k) e = 1.0 + e * x / k;
+      v[i] = e * (double)(1ull << kFixed);
+    }
+  }
+};
+__device__ constexpr PowerTable kPowers{};
+
 struct Row {
   float max;
   float floor;       // logits at or below it weigh nothing (half a unit is at z = -31.2): they are raised to it
@@ -90,20 +106,21 @@ struct Row {
   }
   // 2^52 plus the weight of logit v in units of 2^-44: a whole number whose low bits are the weight.
   // Without branches, and with what the conversion, the double-precision and the integer pipe can each bear (integer
-  // operations were the limit when the float was widened by its bits and the exceptions were selected at the end).
+  // operations were the limit when the float was widened by its bits and the exceptions were selected at the end; now
+  // the double-precision pipe, at half the rate of single precision, is: eight operations, each a step of the formula).
   __device__ __forceinline__ double biased_weight(float v) const {
     constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits hold the rounded integer
-    const double y = ((double)fmaxf(v, floor) - max_d) * per_step;
-    const double r = y + kMagic;
+    const double d = (double)fmaxf(v, floor) - max_d;
+    const double r = fma(d, per_step, kMagic);
     const int n = __double2loint(r);
     constexpr double c = 0.69314718055994530942 / kTable;
-    const double f = y - (r - kMagic);
+    const double f = fma(d, per_step, kMagic - r);
     double q = fma(c * c * c / 6.0, f, c * c / 2.0);
     q = fma(q, f, c);
     q = fma(q, f, 1.0);
-    q *= table[n & (kTable - 1)];
-    q = __hiloint2double(__double2hiint(q) + ((n << 11) & 0xfff00000), __double2loint(q));  // times 2^(n >> 9)
-    return q + kBias;  // rounds to an integer
+    const double t = table[n & (kTable - 1)];
+    const double t2 = __hiloint2double(__double2hiint(t) + ((n << 11) & 0xfff00000), __double2loint(t));  // times 2^(n >> 9)
+    return fma(t2, q, kBias);  // rounds to an integer
   }
   static constexpr double kBias = 4503599627370496.0;  // 2^52
   static constexpr int kBiasHigh = 0x43300000;         // its upper word
@@ -113,10 +130,12 @@ struct Row {
     return (u64)(uint32_t)(__double2hiint(w) - kBiasHigh) << 32 | (uint32_t)__double2loint(w);
   }
   __device__ __forceinline__ double weight_d(float v) const { return biased_weight(v) - kBias; }
-  // bin: a monotone function of v (each rounding is monotone); at least kBins for weights of zero
+  // 2^23 plus the bin of v: a monotone function of v (each rounding is monotone), compared as a float, NaN (0 * inf) and
+  // kBinEnd or more for weights of zero
+  __device__ __forceinline__ float biased_bin(float v) const { return fmaf(max - v, bin_scale, kBinBias); }
+  static constexpr float kBinBias = 8388608.f, kBinEnd = kBinBias + kBins;
   __device__ __forceinline__ int bin(float v) const {
-    const float t = fminf((max - v) * bin_scale, (float)kBins);  // (NaN, from 0 * inf: kBins)
-    return __float_as_int(t + 8388608.f) & 0xffff;               // 2^23: rounds to an integer
+    return __float_as_int(fminf(biased_bin(v), kBinEnd)) & 0xffff;  // (NaN: kBins)
   }
 };
 static_assert(kTable == 512 && kTable == kThreads, "weight() shifts by 9, and every thread fills an entry");
@@ -155,7 +174,7 @@ struct Shared {
   u64 warp_weight[kWarps];
   uint32_t warp_count[kWarps];
   u64 warp_high[kWarps];
-  double warp_low_sum[kWarps], warp_high_sum[kWarps];
+  float2 warp_bounds[kWarps];
   float warp_max[kWarps];
   // result of a search step
   int found_bin, found_bin2;
@@ -373,7 +392,7 @@ template <>
 __device__ __forceinline__ float widen<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
 
 // NaN counts as -inf, -0 as +0.
-__device__ __forceinline__ float clean(float v) { return v != v ? -INFINITY : v + 0.0f; }
+__device__ __forceinline__ float clean(float v) { return fmaxf(v, -INFINITY) + 0.0f; }
 // Two kinds of rows are mapped to ordinary ones, in shared memory, once their maximum is known.  With logits of +inf, these
 // become 0 and all others -inf.  Where 33 T below the maximum is out of range, every finite logit is near -2^128:
 // logits and T are scaled by a power of two.
@@ -518,47 +537,52 @@ __device__ void locate_rank(Shared& sh, uint32_t rank) {
 //   (1 - top_p) prefix(b) >= top_p suffix(b).
 // The logits of bin b lie within half a bin (and the rounding of bin()) of z = b / 64, so counts bound both sums from below
 // and above: sh.found_bin is the first bin where the condition may hold, sh.found_bin2 the first where it must.
+//
+// Single precision will do: the sums are off by 2^-18 of themselves at most (40 additions and products of positive terms,
+// expf to 1e-6 besides), which the factors' margins hold.  Sums run from the far end, so that a small suffix, which a
+// top_p near 1 is decided by, is not a difference of large numbers.
 __device__ void locate_weight(Shared& sh, float top_p, int vocab) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  double lo[kEach], hi[kEach], lo_sum = 0.0, hi_sum = 0.0;
+  float lo[kEach], hi[kEach], lo_sum = 0.f, hi_sum = 0.f;
+  const int last = kBins - 1 - (int)threadIdx.x * kEach;  // this thread's bins: last, last - 1, ..
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
-    const int b = threadIdx.x * kEach + j;
-    const double c = (double)sh.fast.sum[b];
-    const float mid = __expf(-(float)b / kBinsPerUnit);  // (relative error below 1e-5: within the margin)
-    lo[j] = c * (mid * (1.f - 0.51f / kBinsPerUnit));                   // e^-x >= 1 - x
-    hi[j] = c * (mid * (1.f + 0.52f / kBinsPerUnit));                   // e^x <= 1 + x + x^2, x = 0.51 / 64
+    const float c = (float)sh.fast.sum[last - j];                       // (below 2^24)
+    const float mid = __expf(-(float)(last - j) / kBinsPerUnit);
+    lo[j] = c * (mid * (1.f - 0.515f / kBinsPerUnit));                  // e^-x >= 1 - x, x = 0.51 / 64
+    hi[j] = c * (mid * (1.f + 0.525f / kBinsPerUnit));                  // e^x <= 1 + x + x^2
     lo_sum += lo[j];
     hi_sum += hi[j];
   }
-  double lo_upto = lo_sum, hi_upto = hi_sum;
+  float lo_upto = lo_sum, hi_upto = hi_sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const double u = __shfl_up_sync(0xffffffffu, lo_upto, o), v = __shfl_up_sync(0xffffffffu, hi_upto, o);
+    const float u = __shfl_up_sync(0xffffffffu, lo_upto, o), v = __shfl_up_sync(0xffffffffu, hi_upto, o);
     if (lane >= o) { lo_upto += u; hi_upto += v; }
   }
-  if (lane == 31) { sh.warp_low_sum[warp] = lo_upto; sh.warp_high_sum[warp] = hi_upto; }
+  float lo_run = __shfl_up_sync(0xffffffffu, lo_upto, 1), hi_run = __shfl_up_sync(0xffffffffu, hi_upto, 1);
+  if (lane == 0) lo_run = hi_run = 0.f;
+  if (lane == 31) sh.warp_bounds[warp] = make_float2(lo_upto, hi_upto);
   if (threadIdx.x == 0) sh.found_bin = sh.found_bin2 = kBins - 1;
   __syncthreads();
-  double lo_all = 0.0, hi_all = 0.0;
+  float lo_all = 0.f, hi_all = 0.f;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w == warp) { lo_upto += lo_all; hi_upto += hi_all; }
-    lo_all += sh.warp_low_sum[w];
-    hi_all += sh.warp_high_sum[w];
+    const float2 b = sh.warp_bounds[w];
+    if (w == warp) { lo_run += lo_all; hi_run += hi_all; }  // now the weight behind this thread's bins
+    lo_all += b.x;
+    hi_all += b.y;
   }
-  // Weights are rounded to units: half a unit each, and the sums here to 1e-16 of themselves.
-  const double slack = vocab * (1.0 / (double)(1ull << kFixed)) + 1e-13 * hi_all;
-  const double p = fmax((double)top_p, 0.0);
-  double lo_run = lo_upto - lo_sum, hi_run = hi_upto - hi_sum;
+  // Weights are rounded to units, half a unit each; the differences below are off by 2^-18 of the sum of all.
+  const float units = vocab * (1.f / (float)(1ull << kFixed)), off = hi_all * 0x1p-18f;
+  const float p = fmaxf(top_p, 0.f), rest = 1.f - p;
   int first_may = kBins, first_must = kBins;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
+    if (rest * (hi_all - hi_run + off) + units >= p * lo_run) first_may = last - j;
+    if (rest * (lo_all - lo_run - off) - units >= p * hi_run) first_must = last - j;
     lo_run += lo[j];
     hi_run += hi[j];
-    const int b = threadIdx.x * kEach + j;
-    if (first_may == kBins && (1.0 - p) * (hi_run + slack) + slack >= p * (lo_all - lo_run - slack)) first_may = b;
-    if (first_must == kBins && (1.0 - p) * (lo_run - slack) - slack >= p * (hi_all - hi_run + slack)) first_must = b;
   }
   if (first_may < kBins) atomicMin(&sh.found_bin, first_may);
   if (first_must < kBins) atomicMin(&sh.found_bin2, first_must);
@@ -573,29 +597,34 @@ __device__ __forceinline__ float candidate_value(u64 c) { return value_of((uint3
 __device__ __forceinline__ u64* own_list(Shared& sh) { return reinterpret_cast<u64*>(sh.fast.hist); }
 static_assert(2 * kBins * sizeof(uint32_t) >= kList * sizeof(u64), "a whole list fits over the histograms");
 // Walks this warp's share as for_share does; the logits for which f(v) is true become candidates.  They are noted as bits
-// and appended once for every 16 groups, since an append costs an atomic's round trip.
+// and appended once for every 8 groups, since an append costs an atomic's round trip.
 template <typename F>
 __device__ __forceinline__ void collect_share(Shared& sh, const float* vals, int start, int begin, int end, F&& f) {
   const int lane = threadIdx.x & 31;
-  for (int base = begin; base < end; base += 16 * 128) {
-    u64 bits = 0;
+  for (int base = begin; base < end; base += 8 * 128) {
+    uint32_t bits = 0;
 #pragma unroll 2
-    for (int g = 0; g < 16; ++g) {
+    for (int g = 0; g < 8; ++g) {
       const int i = base + g * 128 + 4 * lane;
       if (base + g * 128 >= end) break;
       if (i < end) {
         const float4 v = *reinterpret_cast<const float4*>(vals + i);
-        const uint32_t four = (f(v.x) ? 1u : 0u) | (f(v.y) ? 2u : 0u) | (f(v.z) ? 4u : 0u) | (f(v.w) ? 8u : 0u);
-        bits |= (u64)four << (4 * g);
+        uint32_t four = 0;
+        if (f(v.x)) four |= 1u;
+        if (f(v.y)) four |= 2u;
+        if (f(v.z)) four |= 4u;
+        if (f(v.w)) four |= 8u;
+        bits |= four << (4 * g);
       }
     }
-    const uint32_t mine = __popcll(bits);
+    if (!__any_sync(0xffffffffu, bits != 0)) continue;
+    const uint32_t mine = __popc(bits);
     const uint32_t upto = warp_scan_u32(mine);
     uint32_t at = 0;
-    if (lane == 31 && upto > 0) at = atomicAdd(&sh.own_candidates, upto);
+    if (lane == 31) at = atomicAdd(&sh.own_candidates, upto);
     at = __shfl_sync(0xffffffffu, at, 31) + upto - mine;
     for (; bits != 0; bits &= bits - 1, ++at) {
-      const int b = __ffsll((long long)bits) - 1, i = base + (b >> 2) * 128 + 4 * lane + (b & 3);
+      const int b = __ffs((int)bits) - 1, i = base + (b >> 2) * 128 + 4 * lane + (b & 3);
       if (at < (uint32_t)kList) own_list(sh)[at] = candidate(vals[i], start + i);
     }
   }
@@ -895,7 +924,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   const int n = (int)cluster_size(), rank = (int)cluster_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t i_row = blockIdx.x / n;
-  sh.table[threadIdx.x] = exp2(kFixed + threadIdx.x / (double)kTable);
+  sh.table[threadIdx.x] = kPowers.v[threadIdx.x];
   for (int i = threadIdx.x; i < kBins; i += kThreads) sh.fast.hist[i] = 0;
   if (threadIdx.x == 0) { sh.candidates = sh.own_candidates = 0; sh.first_max = 0xffffffffu; }
   griddep_wait();
@@ -956,8 +985,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   const bool by_rank = top_k > 1 && top_k < p.vocab;
   if (by_rank || top_p < 1.f) {
     for_share(vals, w_begin, w_end, [&](float v, int) {
-      const int b = row.bin(v);
-      if (b < kBins) atomicAdd(&sh.fast.hist[b], 1u);
+      const float b = row.biased_bin(v);
+      if (b < Row::kBinEnd) atomicAdd(&sh.fast.hist[__float_as_int(b) & 0xffff], 1u);
     });
     sum_histograms(cluster, sh, n, rank);
   }
@@ -969,7 +998,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
       slow_path<T>(cluster, p, sh, row, vals, i_row, start, len, n, rank, top_k, top_p, min_weight);
       return;
     }
-    collect_share(sh, vals, start, w_begin, w_end, [&](float v) { return row.bin(v) <= bin; });
+    const float last_bin = Row::kBinBias + bin;
+    collect_share(sh, vals, start, w_begin, w_end, [&](float v) { return row.biased_bin(v) <= last_bin; });
     push_candidates(sh, first);
     cluster.sync();
     if (rank != 0) return;
@@ -1005,23 +1035,26 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   if (top_p < 1.f) {
     locate_weight(sh, top_p, p.vocab);
     const int low = sh.found_bin, high = sh.found_bin2;
+    const float low_bin = Row::kBinBias + low, high_bin = Row::kBinBias + high;
     double all = 0.0, above = 0.0, kept = 0.0;
     if (min_weight <= 1)
       collect_share(sh, vals, start, w_begin, w_end, [&](float v) {
-        const int b = row.bin(v);
+        const float b = row.biased_bin(v);
         const double w = row.weight_d(v);
         all += w;
-        above += b < low ? w : 0.0;
-        return b >= low && b <= high;
+        if (b < low_bin) above += w;
+        return b >= low_bin && b <= high_bin;
       });
     else
       collect_share(sh, vals, start, w_begin, w_end, [&](float v) {
-        const int b = row.bin(v);
+        const float b = row.biased_bin(v);
         const double w = row.weight_d(v);
         all += w;
-        above += b < low ? w : 0.0;
-        kept += b < low && w >= (double)min_weight ? w : 0.0;
-        return b >= low && b <= high;
+        if (b < low_bin) {
+          above += w;
+          if (w >= (double)min_weight) kept += w;
+        }
+        return b >= low_bin && b <= high_bin;
       });
     if (min_weight <= 1) kept = above;
     push_candidates(sh, first);

@@ -127,6 +127,16 @@ def test_wide_and_narrow_rows():
         check(x.contiguous(), [0.37], **s)
 
 
+@pytest.mark.parametrize("spread", [0.01, 1.0, 6.0])
+def test_top_p_towards_its_ends(spread):
+    """The bins that may hold the cut are bounded in single precision: shares close to 0 and to 1, flat and peaked rows."""
+    x, u = logits_of(6, 60000, seed=77)
+    x = (x - x.mean()) * (spread / x.std())
+    for top_p in (1e-30, 1e-6, 1e-3, 0.3, 0.5, 0.75, 0.999, 0.99999, 1.0 - 2.0 ** -24):
+        check(x, u, top_p=top_p)
+        check(x, u, top_p=top_p, min_p=1e-4)
+
+
 @pytest.mark.parametrize("ld", [1003, 1024, 1500])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
 def test_strided_rows(ld, dtype):
