@@ -19,8 +19,10 @@
  *    launch that failed, with earlier kernels already on the stream: after
  *    PD_ERR_CUDA from them, y and the workspace hold unspecified values.
  *  - PD_OK means "enqueued".  The tensor-core entry points (pd_gemm_*,
- *    pd_swiglu_gemm, pd_attention_fwd, the layer and stack calls) bound every
- *    wait inside their kernels; a kernel whose wait ran out returns early and
+ *    pd_swiglu_gemm, pd_attention_fwd, pd_attention_paged_fwd, the layer and
+ *    stack calls) and pd_norm_gate_residual_norm (which prefetches long runs of
+ *    rows) bound every wait inside their kernels; a kernel whose wait ran out
+ *    returns early and
  *    leaves a code in the device status word, so their results are valid only
  *    if pd_get_device_status reports 0 after the stream has been synchronised.
  *    The word is shared by all streams of the device.
@@ -398,7 +400,8 @@ pd_status pd_encoder_layer_fwd_profiled(const pd_encoder_layer_desc* desc,
  *    have any entry (an evicted page, -1), and slots behind kv_len, or in front
  *    of the window, may hold anything, NaN included.  An entry outside
  *    [0, num_pages) is never followed: keys and values there count as zeros.
- *  - What is visible to any query of a sequence has to be finite.
+ *  - What is visible to any query of a sequence has to be finite, and so have the
+ *    scaled scores in fp32.
  *  - The sequences' pages may be shared for reading (a common prefix). */
 typedef struct {
   int32_t batch, tokens;               /* sequences; rows of the token tensors */
@@ -419,7 +422,8 @@ typedef struct {
  * k_new, v_new: bf16 [tokens, heads_kv, head_dim] with ld_new elements from token to
  * token (a column block of a packed projection); desc: batch, tokens, heads_kv,
  * head_dim (a multiple of 8, at most 1024), num_pages, page_size (any), max_pages
- * and the cache strides are used, the rest is ignored.  All pointers 16-byte
+ * and the cache strides are used, the rest is ignored; at most 2^30 tokens and
+ * sequences, 65536 heads (else PD_ERR_UNSUPPORTED).  All pointers 16-byte
  * aligned (the int32 arrays 4-byte), ld_new a multiple of 8, else
  * PD_ERR_ALIGNMENT.  A token whose position lies in front of 0, beyond max_pages
  * pages or on a page outside [0, num_pages) is dropped; tokens of different
@@ -438,15 +442,17 @@ pd_status pd_kv_cache_append(const pd_paged_attention_desc* desc, const void* k_
  * heads_q / heads_kv at most 64, page_size a power of two from 8 to 4096,
  * max_pages * page_size, tokens * heads_q / heads_kv and the blocks of 64 keys of
  * all sequences and cache heads together, batch * heads_kv * max_pages * page_size
- * / 64, at most 2^30, batch and heads_kv at most 65535 (else PD_ERR_UNSUPPORTED).  kv_len beyond max_pages pages:
- * keys end with the table.  Base pointers 16-byte aligned, strides multiples of 8
+ * / 64, at most 2^30, tokens * heads_q below 2^31, batch and heads_kv at most 65535
+ * (else PD_ERR_UNSUPPORTED).  kv_len beyond max_pages pages: keys end with the
+ * table.  Base pointers 16-byte aligned, strides multiples of 8
  * elements (else PD_ERR_ALIGNMENT).  Scores, softmax statistics and sums are
  * fp32; the exponentials are rounded to bf16 for the second product, which
  * accumulates in fp32.
  * workspace: 256-byte aligned, pd_attention_paged_workspace_bytes(desc) bytes (it
- * depends on the desc alone and may be 0, as it is for an invalid desc), else PD_ERR_WORKSPACE_TOO_SMALL; when few rows meet long caches the keys
- * are split over CTAs, whose partial sums a second kernel joins.  Two calls that
- * may run at the same time need a workspace each. */
+ * depends on the desc alone, is 0 for an empty or invalid desc and may be 0 for
+ * chunks of many rows), else PD_ERR_WORKSPACE_TOO_SMALL; where rows are few the
+ * keys are split over CTAs, whose partial sums a second kernel joins.  Two calls
+ * that may run at the same time need a workspace each. */
 size_t pd_attention_paged_workspace_bytes(const pd_paged_attention_desc* desc);
 pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc, const void* q, const void* k_cache,
                                  const void* v_cache, const int32_t* block_table, const int32_t* cu_q,
@@ -465,7 +471,8 @@ pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc, const void
  * x, h: [rows, cols] of x_dtype; y, n: [rows, cols] of y_dtype; gate: [ceil(rows /
  * gate_rows), cols] of y_dtype, or NULL for ones; all contiguous.  gate_rows >= 1:
  * rows that share a gate (1: a gate for every row; rows: one for all).  All sums
- * are fp32, n is computed from h before h is rounded.  h may alias x, n may
+ * are fp32 (so are the squares, which have to stay in its range), n is computed
+ * from h before h is rounded.  h may alias x, n may
  * alias y; nothing else may overlap.  h or n may be NULL when it is not wanted
  * (not both); n is not computed for PD_NORM_NONE as Pre unless it is asked for.
  * Pointers aligned to their elements (else PD_ERR_ALIGNMENT); 16-byte alignment

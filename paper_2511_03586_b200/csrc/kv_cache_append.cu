@@ -23,6 +23,7 @@ struct AppendParams {
 };
 
 constexpr int kWarps = 4;
+constexpr int kMaxIndex = 1 << 30;  // of tokens and sequences: sums with a search's steps stay in 32 bits
 
 __global__ void __launch_bounds__(32 * kWarps) kv_cache_append_kernel(const AppendParams p) {
   const int lane = threadIdx.x & 31;
@@ -81,7 +82,8 @@ extern "C" pd_status pd_kv_cache_append(const pd_paged_attention_desc* desc, con
   const pd_paged_attention_desc& d = *desc;
   if (d.batch < 0 || d.tokens < 0) return PD_ERR_BAD_SHAPE;
   if (d.heads_kv <= 0 || d.head_dim <= 0 || d.num_pages <= 0 || d.page_size <= 0 || d.max_pages <= 0) return PD_ERR_BAD_SHAPE;
-  if (d.head_dim % 8 != 0 || d.head_dim > 1024 || d.heads_kv > 65536) return PD_ERR_UNSUPPORTED;
+  if (d.head_dim % 8 != 0 || d.head_dim > 1024 || d.heads_kv > 65536 || d.batch > pd::kMaxIndex || d.tokens > pd::kMaxIndex)
+    return PD_ERR_UNSUPPORTED;
   if (ld_new < (int64_t)d.heads_kv * d.head_dim) return PD_ERR_BAD_SHAPE;
   if (d.page_stride <= 0 || d.slot_stride <= 0 || d.head_stride <= 0) return PD_ERR_BAD_SHAPE;
   if (d.batch == 0 || d.tokens == 0) return PD_OK;

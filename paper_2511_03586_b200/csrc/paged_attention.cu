@@ -60,6 +60,7 @@ bool valid(const pd_paged_attention_desc& d) {
 }
 bool supported(const pd_paged_attention_desc& d) {
   return (d.head_dim == 64 || d.head_dim == 128) && d.heads_q / d.heads_kv <= 64 && d.page_size >= 8 &&
+         (int64_t)d.tokens * d.heads_q <= 0x7fffffff &&
          d.page_size <= 4096 && (d.page_size & (d.page_size - 1)) == 0 &&
          (int64_t)d.max_pages * d.page_size <= kMaxPositions && (int64_t)d.tokens * (d.heads_q / d.heads_kv) <= kMaxPositions &&
          (int64_t)d.batch * d.heads_kv * (((int64_t)d.max_pages * d.page_size + 63) / 64) <= kMaxPositions && d.batch <= 65535 &&

@@ -453,6 +453,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) paged_attention_join_rows(con
   const int rows = seq.n * p.group;
   if (rows <= (int)blockIdx.z * kJoinWarps || pieces.x < 0) return;  // (no CTA had this item and wrote its entry; or one CTA had all of it)
   const int first_cta = pieces.x >> 1, n = pieces.y - first_cta + 1;
+  // (a CTA whose wait for a key tile ran out has left the entry as it was in the workspace)
+  if (first_cta >= p.splits || pieces.y >= p.splits || pieces.y < first_cta) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int per_row = 1;
   while (2 * per_row * rows <= kJoinWarps) per_row *= 2;

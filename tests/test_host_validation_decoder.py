@@ -138,3 +138,11 @@ def test_binding_wants_cuda_tensors():
         api.pd_norm_gate_residual_norm(t[0], t[0])
     with pytest.raises(TypeError):
         api.pd_sample(t[0], t[0])
+
+
+def test_extents_beyond_the_kernels_index_types():
+    many = dict(batch=1, tokens=(1 << 24), heads_kv=128, heads_q=128, head_dim=64, ld_q=1 << 20, ld_out=1 << 20)
+    assert attend(**many) == UNSUP                       # tokens * heads_q = 2^31: the joining kernel's grid
+    assert lib.pd_attention_paged_workspace_bytes(ctypes.byref(paged(**many))) == 0
+    assert append(tokens=(1 << 30) + 1) == UNSUP
+    assert append(batch=(1 << 30) + 1) == UNSUP
