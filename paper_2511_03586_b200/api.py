@@ -495,13 +495,22 @@ def _call(fn, device: int, stream, *args) -> None:
         raise PdError(status, fn.__name__)
 
 
-def _lend(stream, *tensors) -> None:
-    """Tensors that were allocated here, on the current stream, for a call on ``stream``: their memory is not handed out
-    again before that stream is through with it."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+def _new(like, shape, dtype, stream) -> torch.Tensor:
+    """A tensor for a call on ``stream``, from that stream's memory: what the current stream has freed it may still be
+    writing.  The caller may use it on the current stream, which is recorded, so that the memory is not handed out again
+    before both are through with it."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(torch.cuda.current_stream(like.device))
+    return t
+
+
+def _int32(what: str, *values) -> None:
+    """The desc's fields are 32 bits wide and would drop the rest."""
+    if max(values) > 0x7fffffff or min(values) < -0x80000000:
+        raise ValueError(f"{what} must fit 32 bits")
 
 
 def _token_stride(t: torch.Tensor, name: str) -> int:
@@ -533,6 +542,7 @@ def _paged_cache(device: int, k_cache, v_cache, block_table, cu_q, kv_len):
     batch, max_pages = block_table.shape
     if kv_len.shape[0] != batch or cu_q.shape[0] != batch + 1:
         raise ValueError("block_table must be [batch, max_pages], cu_q [batch + 1], kv_len [batch]")
+    _int32("the caches' and the table's extents", num_pages, page_size, heads, head_dim, batch, max_pages)
     # strides of extents of one are never used; the library still asks for legal ones
     strides = (strides[0] if num_pages > 1 else page_size * heads * head_dim,
                strides[1] if page_size > 1 else heads * head_dim, strides[2] if heads > 1 else head_dim)
@@ -552,6 +562,7 @@ def pd_kv_cache_append(k_new, v_new, k_cache, v_cache, block_table, cu_q, kv_len
         raise ValueError("k_new and v_new must be [tokens, heads_kv, head_dim]")
     if ld != _token_stride(v_new, "v_new"):
         raise ValueError("k_new and v_new must have the same token stride")
+    _int32("tokens", k_new.shape[0], 0)
     d = PagedAttentionDesc(batch, k_new.shape[0], 0, heads, head_dim, *pages, 0, 0, 0, 0, 0.0, 0, 0, *strides)
     _call(_lib.pd_kv_cache_append, device, stream, d, k, v, ld, kc, vc, table, cu, lens)
 
@@ -574,20 +585,19 @@ def pd_attention_paged_fwd(q, k_cache, v_cache, block_table, cu_q, kv_len, *, ma
     if d != head_dim:
         raise ValueError("q and the caches must have the same head_dim")
     if out is None:
-        out = q.new_empty((tokens, heads_q, head_dim))
+        out = _new(q, (tokens, heads_q, head_dim), torch.bfloat16, stream)
         op, ld_out = out.data_ptr(), heads_q * head_dim
-        _lend(stream, out)
     else:
         op, ld_out = _on(device, out, torch.bfloat16, "out", False), _token_stride(out, "out")
         if out.shape != q.shape:
             raise ValueError("out must have the shape of q")
+    _int32("tokens, max_q_len, max_kv_len, window and sinks", tokens, max_q_len, max_kv_len, window, sinks)
     desc = PagedAttentionDesc(batch, tokens, heads_q, heads_kv, head_dim, *pages, max_q_len, max_kv_len, window, sinks,
                               head_dim ** -0.5 if scale is None else scale, ld_q, ld_out, *strides)
     if workspace is None:
         ws_bytes = _lib.pd_attention_paged_workspace_bytes(desc)
-        workspace = q.new_empty((ws_bytes,), dtype=torch.uint8) if ws_bytes else None
+        workspace = _new(q, (ws_bytes,), torch.uint8, stream) if ws_bytes else None
         ws = workspace.data_ptr() if ws_bytes else None
-        _lend(stream, workspace)
     else:
         ws, ws_bytes = _on(device, workspace, torch.uint8, "workspace"), workspace.numel()
     _call(_lib.pd_attention_paged_fwd, device, stream, desc, qp, kc, vc, table, cu, lens, op, ws, ws_bytes)
@@ -642,13 +652,11 @@ def pd_norm_gate_residual_norm(y, x, *, gate=None, gate_rows: int | None = None,
         if gate_rows < 1 or -(-rows // gate_rows) > groups:
             raise ValueError("gate has too few rows")
     if h is None:
-        h = torch.empty_like(x)
-        _lend(stream, h)
+        h = _new(x, x.shape, x.dtype, stream)
     elif h.shape != x.shape:
         raise ValueError("h must be [rows, cols]")
     if n is None:
-        n = torch.empty_like(y)
-        _lend(stream, n)
+        n = _new(y, y.shape, y.dtype, stream)
     elif n.shape != y.shape:
         raise ValueError("n must be [rows, cols]")
     hp, np_ = _on(device, h, x.dtype, "h"), _on(device, n, y.dtype, "n")
@@ -669,11 +677,9 @@ def pd_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None
     if u is None:
         raise TypeError("u must be a tensor")
     if tokens is None:
-        tokens = logits.new_empty((rows,), dtype=torch.int32)
-        _lend(stream, tokens)
+        tokens = _new(logits, (rows,), torch.int32, stream)
     if probs is None:
-        probs = logits.new_empty((rows,), dtype=torch.float32)
-        _lend(stream, probs)
+        probs = _new(logits, (rows,), torch.float32, stream)
     ptrs = []
     for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
                            ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("u", u, torch.float32),

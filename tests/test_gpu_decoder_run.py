@@ -179,3 +179,30 @@ def test_two_streams_at_once():
         check(outs[i][0], run[5])
         for o in outs[i][1:]:
             assert torch.equal(o, outs[i][0])
+
+
+def test_explicit_stream_takes_no_memory_that_the_current_one_still_writes():
+    """What is allocated for a call on another stream must not be what the current stream has freed but not finished with."""
+    from paper_2511_03586_b200 import api
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    y, x, logits, u = rand(64, 512), rand(64, 512), rand(8, 4000), torch.rand(8, generator=g, device="cuda")
+    q, cache = rand(2, 8, 64), rand(40, 16, 2, 64)
+    table, cu, lens = torch.arange(40, dtype=torch.int32, device="cuda").view(2, 20), ints([0, 1, 2]), ints([300, 40])
+    calls = (lambda s: api.pd_norm_gate_residual_norm(y, x, stream=s),
+             lambda s: api.pd_sample(logits, u, stream=s),
+             lambda s: (api.pd_attention_paged_fwd(q, cache, cache, table, cu, lens, max_q_len=1, max_kv_len=320, stream=s),))
+    side = torch.cuda.Stream()
+    for call in calls:
+        want = [t.clone() for t in call(None)]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(100_000_000)                 # the fills below happen after the call on the other stream
+        held = [[torch.empty_like(t) for t in want] for _ in range(4)]
+        for t in (t for ts in held for t in ts):
+            t.fill_(1)
+        del held, t
+        got = call(side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)

@@ -350,3 +350,16 @@ def test_large_batches(batch):
     p.check(p.attend())
     p = Paged([(2 if n else 0, max(kv, 2) if n else 0) for n, kv in lens], 8, 1, 64, 16, seed=batch, window=40, sinks=3)
     p.check(p.attend())
+
+
+def test_values_beyond_32_bits_are_refused():
+    """The descriptor's fields would drop the upper half: a window of 2^32 + 5 keys must not become one of 5."""
+    from paper_2511_03586_b200 import api
+    case = dict(max_q_len=1, max_kv_len=64)
+    q, cache = torch.zeros(1, 2, 64, device="cuda", dtype=torch.bfloat16), torch.zeros(4, 16, 2, 64, device="cuda", dtype=torch.bfloat16)
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(1, 4)
+    cu, lens = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([0, 1], [64]))
+    for name in ("max_q_len", "max_kv_len", "window", "sinks"):
+        for v in (2 ** 31, 2 ** 32 + 5, -2 ** 31 - 1):
+            with pytest.raises(ValueError):
+                api.pd_attention_paged_fwd(q, cache, cache, table, cu, lens, **{**case, name: v})
