@@ -78,7 +78,7 @@ Plan plan(const pd_paged_attention_desc& d) {
   const int64_t items = row_tiles * d.heads_kv * d.batch;  // CTAs without splitting
   int64_t keys = d.max_kv_len;
   if (d.window > 0) keys = std::min<int64_t>(keys, (int64_t)d.window + d.sinks + d.max_q_len);
-  const int64_t tile = chunk ? 128 : 64, tiles = (keys + tile - 1) / tile;
+  const int64_t tile = !chunk ? 64 : d.head_dim == 64 ? 64 : 128, tiles = (keys + tile - 1) / tile;
   if (!chunk) {
     // two CTAs per SM share all key tiles evenly; fewer when there are not enough tiles for that
     pl.min_split_tiles = 1;
@@ -87,9 +87,9 @@ Plan plan(const pd_paged_attention_desc& d) {
     pl.splits = (int)std::min<int64_t>(2 * kSms, std::max<int64_t>(all / pl.min_split_tiles, 1));
     return pl;
   }
-  // One or two CTAs per SM, and splits only to fill the SMs, none below min_split_tiles.
-  pl.min_split_tiles = 4;
-  int64_t want = items > 0 ? kSms * (d.head_dim == 64 ? 2 : 1) / items : 1;
+  // One or four CTAs per SM, and splits only to fill the SMs, none below min_split_tiles.
+  pl.min_split_tiles = d.head_dim == 64 ? 8 : 4;
+  int64_t want = items > 0 ? kSms * (d.head_dim == 64 ? 4 : 1) / items : 1;
   want = std::min<int64_t>(want, (tiles + pl.min_split_tiles - 1) / pl.min_split_tiles);
   pl.splits = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 256);
   return pl;
