@@ -363,3 +363,31 @@ def test_values_beyond_32_bits_are_refused():
         for v in (2 ** 31, 2 ** 32 + 5, -2 ** 31 - 1):
             with pytest.raises(ValueError):
                 api.pd_attention_paged_fwd(q, cache, cache, table, cu, lens, **{**case, name: v})
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[(60, 700), (300, 300)], [(40, 4000)]], ids=["whole", "split"])
+def test_growing_scores_of_chunks(lens, d):
+    """As test_growing_scores, for either kernel of chunks: rescaling while products are in flight, in pages of 8."""
+    p = Paged(lens, 4, 2, d, 8, seed=5)
+    for k, (_, kv) in zip(p.k_seq, lens):
+        k.copy_((torch.arange(kv, device="cuda")[:, None, None] * (21.0 / kv) - 10).expand_as(k))
+    for b, (k, (_, kv)) in enumerate(zip(p.k_seq, lens)):
+        for i in range(-(-kv // 8)):
+            m = min(kv, 8 * i + 8) - 8 * i
+            p.k_cache[int(p.table[b, i]), :m] = k[8 * i:8 * i + m]
+    p.q.copy_(torch.ones_like(p.q))
+    p.check(p.attend())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 5), (9000, 0)])
+def test_chunks_over_long_caches(d, window, sinks):
+    """Few rows of the chunk kernels over many keys: shares of the keys, joined; more sequences than fill the SMs, not shared."""
+    p = Paged([(40, 20011), (17, 300), (0, 64), (33, 9000)], 8, 2, d, 32, seed=d, window=window, sinks=sinks)
+    out = p.attend()
+    p.check(out)
+    assert torch.equal(p.attend(), out)
+    p.check(p.attend(max_kv_len=1))            # not shared out: one walk per row tile
+    many = Paged([(33, 100 + 13 * i) for i in range(40)], 8, 2, d, 16, seed=1, window=window, sinks=sinks)
+    many.check(many.attend())
