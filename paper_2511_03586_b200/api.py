@@ -469,13 +469,16 @@ def _on(device: int, t, dtype, name: str, dense: bool = True) -> int | None:
     """Address of ``t`` (None for None) after checking its device, type and, unless told otherwise, density."""
     if t is None:
         return None
+    try:
+        if t.get_device() == device and t.dtype is dtype and (not dense or t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor) or t.get_device() != device:
         raise TypeError(f"{name} must be a tensor on cuda:{device}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if dense and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _call(fn, device: int, stream, *args) -> None:
@@ -486,7 +489,7 @@ def _call(fn, device: int, stream, *args) -> None:
         raise ValueError(f"stream must belong to cuda:{device}")
     else:
         handle = stream.cuda_stream
-    if torch.cuda.current_device() == device:
+    if torch._C._cuda_getDevice() == device:
         status = fn(*args, handle)
     else:
         with torch.cuda.device(device):
@@ -509,6 +512,7 @@ def _new(like, stream, n: int | None = None, dtype=None) -> torch.Tensor:
 
 
 _DENSE = torch.contiguous_format
+_MAX = 0x7fffffff  # of the descs' 32-bit fields
 
 
 def _token_stride(t: torch.Tensor, name: str) -> int:
@@ -540,7 +544,7 @@ def _paged_cache(device: int, k_cache, v_cache, block_table, cu_q, kv_len):
     batch, max_pages = block_table.shape
     if kv_len.shape[0] != batch or cu_q.shape[0] != batch + 1:
         raise ValueError("block_table must be [batch, max_pages], cu_q [batch + 1], kv_len [batch]")
-    if num_pages > 0x7fffffff or page_size > 0x7fffffff or max_pages > 0x7fffffff or batch > 0x7fffffff:
+    if num_pages > _MAX or page_size > _MAX or max_pages > _MAX or batch > _MAX:
         raise ValueError("the caches' and the table's extents must fit 32 bits")
     # strides of extents of one are never used; the library still asks for legal ones
     strides = (strides[0] if num_pages > 1 else page_size * heads * head_dim,
@@ -562,7 +566,7 @@ def pd_kv_cache_append(k_new, v_new, k_cache, v_cache, block_table, cu_q, kv_len
         raise ValueError("k_new and v_new must be [tokens, heads_kv, head_dim]")
     if v_new.stride() != k_new.stride() and ld != _token_stride(v_new, "v_new"):
         raise ValueError("k_new and v_new must have the same token stride")
-    if tokens > 0x7fffffff:
+    if tokens > _MAX:
         raise ValueError("tokens must fit 32 bits")
     desc = PagedAttentionDesc(batch, tokens, 0, heads, head_dim, *pages, 0, 0, 0, 0, 0.0, 0, 0, *strides)
     _call(_lib.pd_kv_cache_append, device, stream, desc, k, v, ld, kc, vc, table, cu, lens)
@@ -593,7 +597,8 @@ def pd_attention_paged_fwd(q, k_cache, v_cache, block_table, cu_q, kv_len, *, ma
         if out.shape != q.shape:
             raise ValueError("out must have the shape of q")
     # the desc's fields are 32 bits wide and would drop the rest
-    if max(tokens, max_q_len, max_kv_len, window, sinks) > 0x7fffffff or min(max_q_len, max_kv_len, window, sinks) < -0x80000000:
+    if not (tokens <= _MAX and -_MAX <= max_q_len <= _MAX and -_MAX <= max_kv_len <= _MAX and -_MAX <= window <= _MAX and
+            -_MAX <= sinks <= _MAX):
         raise ValueError("tokens, max_q_len, max_kv_len, window and sinks must fit 32 bits")
     desc = PagedAttentionDesc(batch, tokens, heads_q, heads_kv, head_dim, *pages, max_q_len, max_kv_len, window, sinks,
                               head_dim ** -0.5 if scale is None else scale, ld_q, ld_out, *strides)
@@ -612,8 +617,10 @@ _PD_DTYPES = {torch.bfloat16: PD_BF16, torch.float32: PD_F32}
 
 
 def _vector(device: int, t, cols: int, name: str) -> int | None:
+    if t is None:
+        return None
     ptr = _on(device, t, torch.float32, name)
-    if t is not None and t.numel() != cols:
+    if t.numel() != cols:
         raise ValueError(f"{name} must have {cols} elements")
     return ptr
 
