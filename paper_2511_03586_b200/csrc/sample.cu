@@ -680,13 +680,13 @@ __device__ u64 select_candidate(Shared& sh, const u64 (&c)[kPer], const u64 (&am
     __syncthreads();
     const u64 mine = ((u64)hi_sum[threadIdx.x] << 32) + lo_sum[threadIdx.x];
     const u64 upto = before + block_scan_u64(sh, mine);
-    if (upto - mine < target && target <= upto) {
+    if (upto - mine < target && (target <= upto || threadIdx.x == kThreads - 1)) {  // (or: the search ends whatever the sums are)
       sh.found_bin = threadIdx.x;
       sh.found_weight_before = upto - mine;
       sh.found_count = count[threadIdx.x];
     }
     __syncthreads();
-    const u64 first = lo + ((u64)sh.found_bin << shift);
+    const u64 first = min(lo + ((u64)sh.found_bin << shift), hi);
     if (shift == 0) return first;
     hi = min(hi, first + ((1ull << shift) - 1));
     lo = first;
