@@ -25,7 +25,7 @@
 // HBM-bound in principle: the logits are read once, 4 (or 2) bytes each, and held in the shared memory of a cluster of
 // 1 to 8 CTAs (distributed by contiguous slices, so that index order is slice order).  In fact the passes over shared
 // memory, the double-precision exponentials (eight operations each) and the cluster's barriers weigh more: 256 x 128000
-// fp32 logits with top-p take 184 us, 20 of which the bytes need; stopped after the maximum, 43; after the histogram, 76;
+// fp32 logits with top-p take 182 us, 20 of which the bytes need; stopped after the maximum, 43; after the histogram, 76;
 // after locating the cut's bins, 85; after the exact sums, 151.  CTAs of 256 threads and 128 registers take 202 us.
 #include <cooperative_groups.h>
 
@@ -649,20 +649,19 @@ __device__ u64 select_candidate(Shared& sh, const u64 (&c)[kPer], const u64 (&am
   uint32_t* hi_sum = sh.fast.hist + kThreads;
   uint32_t* count = sh.fast.hist + 2 * kThreads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  u64 lo = ~0ull, hi = 0;
+  // the range of the values (the indexes take all of theirs)
+  uint32_t lo_key = ~0u, hi_key = 0;
 #pragma unroll
   for (int j = 0; j < kPer; ++j)
-    if (amount[j] > 0) { lo = min(lo, c[j]); hi = max(hi, c[j]); }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
+    if (amount[j] > 0) { lo_key = min(lo_key, (uint32_t)(c[j] >> 32)); hi_key = max(hi_key, (uint32_t)(c[j] >> 32)); }
+  lo_key = __reduce_min_sync(0xffffffffu, lo_key);
+  hi_key = __reduce_max_sync(0xffffffffu, hi_key);
   __syncthreads();
-  if (lane == 0) { sh.warp_weight[warp] = lo; sh.warp_high[warp] = hi; }
+  if (lane == 0) { sh.warp_count[warp] = lo_key; sh.warp_high[warp] = hi_key; }
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) { lo = min(lo, sh.warp_weight[w]); hi = max(hi, sh.warp_high[w]); }
+  lo_key = __reduce_min_sync(0xffffffffu, sh.warp_count[lane % kWarps]);
+  hi_key = __reduce_max_sync(0xffffffffu, (uint32_t)sh.warp_high[lane % kWarps]);
+  u64 lo = (u64)lo_key << 32, hi = (u64)hi_key << 32 | 0xffffffffu;
   u64 before = 0;
   for (;;) {
     const u64 span = hi - lo;
@@ -751,7 +750,9 @@ __device__ __forceinline__ void add_to_shares(Shared& sh, const SampleParams& p,
   for (int j = 0; j < kPer; ++j)
     if (c[j] <= last && w[j] >= min_weight) {
       const int index = (int)(uint32_t)c[j], cta = index / p.slice;
-      atomicAdd(&sh.share_weight[cta * kWarps + (index - cta * p.slice) / share], w[j]);
+      uint32_t* half = reinterpret_cast<uint32_t*>(&sh.share_weight[cta * kWarps + (index - cta * p.slice) / share]);
+      const uint32_t add = (uint32_t)w[j], old = atomicAdd(half, add);  // (no native 64-bit addition in shared memory)
+      atomicAdd(half + 1, (uint32_t)(w[j] >> 32) + (old + add < old ? 1u : 0u));
     }
 }
 
@@ -778,19 +779,27 @@ __device__ void finish_shares(const SampleParams& p, Shared& sh, const Row& row,
   const int end = min(min(start + share, (cta + 1) * p.slice), p.vocab);
   u64 before = sh.found_weight_before;
   const T* src = static_cast<const T*>(p.logits) + i_row * p.ld;
-  for (int base = start; base < end; base += kThreads) {  // (one step for shares of up to 512)
-    const int i = base + threadIdx.x;
-    u64 w = 0;
-    if (i < end) {
-      const float v = remapped(clean(widen<T>(src[i])), remap);
-      if (candidate(v, i) <= last) w = row.weight(v);
-      if (w < min_weight) w = 0;
+  for (int base = start; base < end; base += 2 * kThreads) {  // (one step for shares of up to 1024)
+    const int i = base + 2 * threadIdx.x;
+    u64 w[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      w[j] = 0;
+      if (i + j < end) {
+        const float v = remapped(clean(widen<T>(src[i + j])), remap);
+        if (candidate(v, i + j) <= last) w[j] = row.weight(v);
+        if (w[j] < min_weight) w[j] = 0;
+      }
     }
-    const u64 to = before + block_scan_u64(sh, w);
-    if (to - w <= target && target < to) write_token(p, i_row, i, w, total);
+    const u64 to = before + block_scan_u64(sh, w[0] + w[1]), from = to - w[0] - w[1];
+    if (from <= target && target < to) {
+      const int j = target < from + w[0] ? 0 : 1;
+      write_token(p, i_row, i + j, w[j], total);
+    }
     if (threadIdx.x == kThreads - 1) sh.token_weight = to;
     __syncthreads();
     before = sh.token_weight;
+    if (target < before) break;
   }
 }
 
