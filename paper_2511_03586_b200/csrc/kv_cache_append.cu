@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(32 * kWarps) kv_cache_append_kernel(const Appe
   }
   const int b = paged::find_sequence(p.cu_q, p.batch, t);
   if (b >= p.batch || t < __ldg(p.cu_q + b)) return;  // padding behind the last sequence
-  const int pos = __ldg(p.kv_len + b) - (__ldg(p.cu_q + b + 1) - t);
+  const int pos = max(__ldg(p.kv_len + b), 0) - (__ldg(p.cu_q + b + 1) - t);
   if (pos < 0) return;
   const int index = pos / p.page_size, slot = pos - index * p.page_size;
   if (index >= p.max_pages) return;

@@ -174,3 +174,17 @@ def test_prefetched_rows_in_place():
         again = api.pd_norm_gate_residual_norm(y, x, gate=gate, post_norm="layer", **vec)
         assert torch.equal(again[0], h) and torch.equal(again[1], n)
     assert api.pd_get_device_status() == 0
+
+
+@pytest.mark.parametrize("cols", [2048, 4096, 8192])
+def test_in_place_with_rows_prefetched(cols):
+    """Rows are copied to shared memory while the one before is written over its own inputs: none may come out twice normed."""
+    from paper_2511_03586_b200 import api
+    rows = 4000
+    x, y, gate, vec = make(rows, cols, BF16, BF16, rows)
+    h, n = api.pd_norm_gate_residual_norm(y, x, gate=gate, **vec)
+    for _ in range(3):
+        x2, y2 = x.clone(), y.clone()
+        api.pd_norm_gate_residual_norm(y2, x2, gate=gate, h=x2, n=y2, **vec)
+        assert torch.equal(x2, h) and torch.equal(y2, n)
+    assert api.pd_get_device_status() == 0

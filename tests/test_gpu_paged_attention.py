@@ -391,3 +391,16 @@ def test_chunks_over_long_caches(d, window, sinks):
     p.check(p.attend(max_kv_len=1))            # not shared out: one walk per row tile
     many = Paged([(33, 100 + 13 * i) for i in range(40)], 8, 2, d, 16, seed=1, window=window, sinks=sinks)
     many.check(many.attend())
+
+
+@pytest.mark.parametrize("lens", ["single", "chunk"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_extreme_window_sinks_and_lengths(lens, d):
+    """The largest window and sinks see everything; lengths in front of 0 leave nothing to see."""
+    p = Paged(LENS[lens], 8, 2, d, 16, seed=13)
+    for window, sinks in ((2 ** 31 - 1, 0), (1, 2 ** 31 - 1), (2 ** 31 - 1, 2 ** 31 - 1)):
+        p.check(p.attend(window=window, sinks=sinks))
+    for kv in (0, -1, -2 ** 31):
+        p.kv.fill_(kv)
+        out = p.attend()
+        assert (out[:int(p.cu[-1])] == 0).all()
