@@ -25,8 +25,8 @@
 // HBM-bound in principle: the logits are read once, 4 (or 2) bytes each, and held in the shared memory of a cluster of
 // 1 to 8 CTAs (distributed by contiguous slices, so that index order is slice order).  In fact the passes over shared
 // memory, the double-precision exponentials (eight operations each) and the cluster's barriers weigh more: 256 x 128000
-// fp32 logits with top-p take 182 us, 20 of which the bytes need; stopped after the maximum, 43; after the histogram, 76;
-// after locating the cut's bins, 85; after the exact sums, 151.  CTAs of 256 threads and 128 registers take 202 us.
+// fp32 logits with top-p take 177 us, 20 of which the bytes need; stopped after the maximum, 43; after the cut's bins are
+// known, about 80; after the exact sums, 156.  CTAs of 256 threads and 128 registers take 202 us (against 184 then).
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -147,10 +147,14 @@ struct SlowSearch {
   u64 sum_weight[2][kSlowBins];
 };
 struct FastSearch {
-  uint32_t hist[kBins];  // own counts
-  uint32_t sum[kBins];   // the cluster's
-  u64 list[kList];       // candidates as (key, index), in CTA 0
+  uint32_t hist[kBins / 2];  // own counts, two to a word (a slice has fewer than 2^16 logits)
+  union {
+    uint32_t sum[kBins];     // the cluster's
+    u64 own[kList];          // then the CTA's candidates, then scratch of the search among all
+  };
+  u64 list[kList];           // candidates as (key, index), in CTA 0
 };
+static_assert(kMaxVocab / kMaxCluster < 65536);
 
 struct Shared {
   double table[kTable];
@@ -488,27 +492,29 @@ __device__ __forceinline__ u64 draw_target(const SampleParams& p, int64_t row, u
   return __umul64hi(total, (u64)((double)u * 18446744073709551616.0));            // floor(u * total) < total
 }
 
-// Sums the cluster's histograms into every CTA's fast.sum: CTA r adds up bins [r, r + 1) * kBins / n and hands them out.
-__device__ void sum_histograms(cg::cluster_group& cluster, Shared& sh, int n, int rank) {
+// Sums the cluster's histograms into every CTA's fast.sum.  The histograms stay as they are until the next cluster barrier.
+constexpr int kEach = kBins / kThreads;
+__device__ void sum_histograms(cg::cluster_group& cluster, Shared& sh, int n) {
+  static_assert(kEach == 4, "a thread's bins are two words");
   cluster.sync();  // every histogram is complete
-  const int own = kBins / n;
-  for (int i = threadIdx.x; i < own; i += kThreads) {
-    const int b = rank * own + i;
-    uint32_t part[kMaxCluster], sum = 0;
+  uint2 part[kMaxCluster];
 #pragma unroll
-    for (int r = 0; r < kMaxCluster; ++r) part[r] = r < n ? cluster.map_shared_rank(&sh, r)->fast.hist[b] : 0;
+  for (int r = 0; r < kMaxCluster; ++r)
+    part[r] = r < n ? reinterpret_cast<const uint2*>(cluster.map_shared_rank(&sh, r)->fast.hist)[threadIdx.x] : make_uint2(0, 0);
+  uint4 sum = make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int r = 0; r < kMaxCluster; ++r) sum += part[r];
-#pragma unroll
-    for (int r = 0; r < kMaxCluster; ++r)
-      if (r < n) cluster.map_shared_rank(&sh, r)->fast.sum[b] = sum;
+  for (int r = 0; r < kMaxCluster; ++r) {
+    sum.x += part[r].x & 0xffffu;
+    sum.y += part[r].x >> 16;
+    sum.z += part[r].y & 0xffffu;
+    sum.w += part[r].y >> 16;
   }
-  cluster.sync();  // the sums are in, and nobody reads a histogram any more
+  reinterpret_cast<uint4*>(sh.fast.sum)[threadIdx.x] = sum;
+  __syncthreads();
 }
 
 // The first bin through which there are `rank` logits or more (the last bin if there are fewer in all): sh.found_bin, and
 // their number, sh.found_count.
-constexpr int kEach = kBins / kThreads;
 __device__ void locate_rank(Shared& sh, uint32_t rank) {
   uint32_t c[kEach], sum = 0;
 #pragma unroll
@@ -592,10 +598,9 @@ __device__ void locate_weight(Shared& sh, float top_p, int vocab) {
 __device__ __forceinline__ u64 candidate(float v, int index) { return (u64)key_of(v) << 32 | (uint32_t)index; }
 __device__ __forceinline__ float candidate_value(u64 c) { return value_of((uint32_t)(c >> 32)); }
 
-// Candidates are collected in the CTA first (over the histograms, which have served by then): one trip to CTA 0 per
+// Candidates are collected in the CTA first (over the cluster's counts, which have served by then): one trip to CTA 0 per
 // candidate would stall its warp for a microsecond each.
-__device__ __forceinline__ u64* own_list(Shared& sh) { return reinterpret_cast<u64*>(sh.fast.hist); }
-static_assert(2 * kBins * sizeof(uint32_t) >= kList * sizeof(u64), "a whole list fits over the histograms");
+__device__ __forceinline__ u64* own_list(Shared& sh) { return sh.fast.own; }
 // Walks this warp's share as for_share does; the logits for which f(v) is true become candidates.  They are noted as bits
 // and appended once for every 8 groups, since an append costs an atomic's round trip.
 template <typename F>
@@ -645,9 +650,9 @@ __device__ void push_candidates(Shared& sh, Shared* first) {
 // time; candidates differ (by index, if not by value), so the last range holds one.
 constexpr int kPer = kList / kThreads;
 __device__ u64 select_candidate(Shared& sh, const u64 (&c)[kPer], const u64 (&amount)[kPer], u64 target) {
-  uint32_t* lo_sum = sh.fast.hist;  // (the histograms and the CTA's own list have served)
-  uint32_t* hi_sum = sh.fast.hist + kThreads;
-  uint32_t* count = sh.fast.hist + 2 * kThreads;
+  uint32_t* lo_sum = sh.fast.sum;  // (the counts and the CTA's own list have served)
+  uint32_t* hi_sum = sh.fast.sum + kThreads;
+  uint32_t* count = sh.fast.sum + 2 * kThreads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // the range of the values (the indexes take all of theirs)
   uint32_t lo_key = ~0u, hi_key = 0;
@@ -934,7 +939,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t i_row = blockIdx.x / n;
   sh.table[threadIdx.x] = kPowers.v[threadIdx.x];
-  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.fast.hist[i] = 0;
+  for (int i = threadIdx.x; i < kBins / 2; i += kThreads) sh.fast.hist[i] = 0;
   if (threadIdx.x == 0) { sh.candidates = sh.own_candidates = 0; sh.first_max = 0xffffffffu; }
   griddep_wait();
   griddep_launch_dependents();
@@ -995,9 +1000,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   if (by_rank || top_p < 1.f) {
     for_share(vals, w_begin, w_end, [&](float v, int) {
       const float b = row.biased_bin(v);
-      if (b < Row::kBinEnd) atomicAdd(&sh.fast.hist[__float_as_int(b) & 0xffff], 1u);
+      if (b < Row::kBinEnd) atomicAdd(&sh.fast.hist[(__float_as_int(b) & 0xffff) >> 1], __float_as_int(b) & 1 ? 0x10000u : 1u);
     });
-    sum_histograms(cluster, sh, n, rank);
+    sum_histograms(cluster, sh, n);
   }
   if (by_rank) {
     locate_rank(sh, (uint32_t)top_k);
