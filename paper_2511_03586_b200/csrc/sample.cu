@@ -941,6 +941,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   sh.table[threadIdx.x] = kPowers.v[threadIdx.x];
   for (int i = threadIdx.x; i < kBins / 2; i += kThreads) sh.fast.hist[i] = 0;
   if (threadIdx.x == 0) { sh.candidates = sh.own_candidates = 0; sh.first_max = 0xffffffffu; }
+  __syncwarp();
+  cluster_started_arrive();
   griddep_wait();
   griddep_launch_dependents();
 
@@ -958,6 +960,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   mx = warp_max(mx);
   if (lane == 0) sh.warp_max[warp] = mx;
   __syncthreads();
+  cluster_started_wait();  // the row's loads lie between
   if (threadIdx.x < n) {
     for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, sh.warp_max[w]);
     cluster.map_shared_rank(&sh, threadIdx.x)->peer_max[rank] = mx;
