@@ -101,6 +101,7 @@ layernorm_rows_cluster(const float* __restrict__ x, const float* __restrict__ ga
   const int chunk4 = (cols4 + (int)cluster_size() - 1) / (int)cluster_size();  // float4 per CTA, at most VPT * THREADS
   const int base = (int)cluster_rank() * chunk4;
   const int end = min(base + chunk4, cols4);
+  cluster_started_arrive();
   griddep_wait();
   griddep_launch_dependents();
   const float4* xr = reinterpret_cast<const float4*>(x + row * cols);
@@ -113,6 +114,7 @@ layernorm_rows_cluster(const float* __restrict__ x, const float* __restrict__ ga
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) s += (v[i].x + v[i].y) + (v[i].z + v[i].w);
+  cluster_started_wait();
   const float mu0 = cluster_allreduce<false>(block_reduce<NWARPS, false>(s, scratch, 0), xchg) * inv_cols;
   // centre on the first estimate and refine it with the mean of the residuals, as in the single-CTA kernel
   float d1 = 0.f, d2 = 0.f;

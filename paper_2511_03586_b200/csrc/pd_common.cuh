@@ -152,6 +152,7 @@ __device__ __forceinline__ void cluster_started_wait() { asm volatile("barrier.c
 // All-reduce over the cluster of one value per CTA (`v`, identical in all threads of the CTA): thread k writes it
 // into slot [own rank] of CTA k's exchange array, a cluster barrier (release / acquire) publishes the writes,
 // and everyone combines the slots in rank order.  `xchg`: 8 floats of shared memory used by no other reduction.
+// The caller has completed cluster_started_wait().
 template <bool IS_MAX>
 __device__ __forceinline__ float cluster_allreduce(float v, float* xchg) {
   const unsigned n = cluster_size(), rank = cluster_rank();

@@ -67,6 +67,7 @@ rmsnorm_rows_cluster(const float* __restrict__ x, const float* __restrict__ gamm
   const int chunk4 = (cols4 + (int)cluster_size() - 1) / (int)cluster_size();  // float4 per CTA, at most VPT * THREADS
   const int base = (int)cluster_rank() * chunk4;
   const int end = min(base + chunk4, cols4);
+  cluster_started_arrive();
   griddep_wait();
   griddep_launch_dependents();
   const float4* xr = reinterpret_cast<const float4*>(x + row * cols);
@@ -79,6 +80,7 @@ rmsnorm_rows_cluster(const float* __restrict__ x, const float* __restrict__ gamm
   float q = 0.f;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) q += (v[i].x * v[i].x + v[i].y * v[i].y) + (v[i].z * v[i].z + v[i].w * v[i].w);
+  cluster_started_wait();
   q = cluster_allreduce<false>(block_reduce<NWARPS, false>(q, scratch, 0), xchg);
   const float rstd = rsqrtf(q / (float)cols + eps);
 #pragma unroll

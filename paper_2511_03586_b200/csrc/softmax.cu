@@ -84,6 +84,7 @@ softmax_rows_cluster(const float* __restrict__ x, OutT* __restrict__ y, int64_t 
   const int chunk4 = (cols4 + (int)cluster_size() - 1) / (int)cluster_size();  // float4 per CTA, at most VPT * THREADS
   const int base = (int)cluster_rank() * chunk4;
   const int end = min(base + chunk4, cols4);
+  cluster_started_arrive();
   griddep_wait();
   griddep_launch_dependents();
   const float4* xr = reinterpret_cast<const float4*>(x + row * cols);
@@ -96,6 +97,7 @@ softmax_rows_cluster(const float* __restrict__ x, OutT* __restrict__ y, int64_t 
   float m = kNegInf;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) m = fmaxf(m, fmaxf(fmaxf(v[i].x, v[i].y), fmaxf(v[i].z, v[i].w)));
+  cluster_started_wait();
   m = cluster_allreduce<true>(block_reduce<NWARPS, true>(m, scratch, 0), xchg[0]);
   float s = 0.f;
 #pragma unroll

@@ -28,7 +28,10 @@ def kernel_body(file, name):
     raise AssertionError(f"{file}: {name} does not end")
 
 
-@pytest.mark.parametrize("file,name", [("sample.cu", "sample_rows_cluster")])
+@pytest.mark.parametrize("file,name", [
+    ("sample.cu", "sample_rows_cluster"), ("softmax.cu", "softmax_rows_cluster"), ("layernorm.cu", "layernorm_rows_cluster"),
+    ("rmsnorm.cu", "rmsnorm_rows_cluster"), ("gemm_tcgen05_2cta.cu", "gemm_bf16_tcgen05_pair_kernel"),
+    ("gemm_tcgen05_ln.cu", "gemm_bias_residual_layernorm_kernel"), ("gemm_tcgen05_splitk.cu", "gemm_bf16_splitk_cluster_kernel")])
 def test_cluster_barrier_before_the_first_remote_access(file, name):
     body = kernel_body(file, name)
     remote, barrier = REMOTE.search(body), BARRIER.search(body)
