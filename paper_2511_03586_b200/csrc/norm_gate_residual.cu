@@ -520,19 +520,20 @@ extern "C" pd_status pd_norm_gate_residual_norm(const pd_norm_gate_residual_desc
                                                 const void* gate, const float* post_gamma, const float* post_beta,
                                                 const float* pre_gamma, const float* pre_beta, void* h, void* n,
                                                 cudaStream_t stream) {
-  if (!desc || !y || !x || (!h && !n)) return PD_ERR_NULL_POINTER;
+  if (!desc) return PD_ERR_NULL_POINTER;
   const pd_norm_gate_residual_desc& d = *desc;
   if (d.rows < 0 || d.cols <= 0 || d.cols > 0x7fffffff || !(d.eps >= 0.f) || !std::isfinite(d.alpha)) return PD_ERR_BAD_SHAPE;
   if (gate && d.gate_rows < 1) return PD_ERR_BAD_SHAPE;
   auto is_dtype = [](int t) { return t == PD_BF16 || t == PD_F32; };
   auto is_norm = [](int k) { return k >= PD_NORM_NONE && k <= PD_NORM_LAYER; };
   if (!is_dtype(d.x_dtype) || !is_dtype(d.y_dtype) || !is_norm(d.post_norm) || !is_norm(d.pre_norm)) return PD_ERR_BAD_SHAPE;
+  if (d.rows == 0) return PD_OK;  // (an empty tensor's pointers may be null)
+  if (!y || !x || (!h && !n)) return PD_ERR_NULL_POINTER;
   auto bits = [](const void* q) { return reinterpret_cast<uintptr_t>(q); };
   const uintptr_t xb = bits(x) | bits(h), yb = bits(y) | bits(n) | bits(gate);
   if ((xb & (d.x_dtype == PD_F32 ? 3u : 1u)) || (yb & (d.y_dtype == PD_F32 ? 3u : 1u)) ||
       ((bits(post_gamma) | bits(post_beta) | bits(pre_gamma) | bits(pre_beta)) & 3u))
     return PD_ERR_ALIGNMENT;
-  if (d.rows == 0) return PD_OK;
   if (pd_status st = pd::require_sm100(); st != PD_OK) return st;
   pd::NormParams p{y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta, h, n, d.rows, gate ? d.gate_rows : 1,
                    (int)d.cols, d.post_norm, d.pre_norm, d.alpha, d.eps};

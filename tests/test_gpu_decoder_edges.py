@@ -1,0 +1,26 @@
+"""Edges of the decoder operators, through the binding: empty batches, very long rows, padded batches, layouts and page sizes
+beyond the ordinary ones."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def test_empty_batches():
+    from paper_2511_03586_b200 import api
+    e = lambda *s, t=BF16: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
+    x = e(0, 64)
+    h, n = api.pd_norm_gate_residual_norm(x, x, gate=e(0, 64), post_gamma=torch.ones(64, device="cuda"))
+    assert h.shape == n.shape == (0, 64)
+    api.pd_norm_gate_residual_norm(x, x, h=x, n=x)
+    tokens, probs = api.pd_sample(e(0, 100, t=F32), e(0, t=F32), top_k=e(0, t=I32))
+    assert tokens.shape == probs.shape == (0,)
+    cache = torch.full((4, 16, 2, 64), 7.0, dtype=BF16, device="cuda")
+    for batch in (0, 2):                                  # no sequences; sequences without new tokens
+        table, lens = torch.zeros(batch, 3, dtype=I32, device="cuda"), torch.full((batch,), 5, dtype=I32, device="cuda")
+        cu = torch.zeros(batch + 1, dtype=I32, device="cuda")
+        api.pd_kv_cache_append(e(0, 2, 64), e(0, 2, 64), cache, cache, table, cu, lens)
+        out = api.pd_attention_paged_fwd(e(0, 4, 64), cache, cache, table, cu, lens, max_q_len=0, max_kv_len=48)
+        assert out.shape == (0, 4, 64)
+    assert bool((cache == 7.0).all())
