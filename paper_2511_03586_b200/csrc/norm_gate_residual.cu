@@ -396,6 +396,7 @@ __device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162floa
 __device__ __forceinline__ float widen(float v) { return v; }
 
 // Any length and alignment: a CTA per row that reads the row again for every statistic (from L2).
+// Columns are counted in 64 bits: a thread's step behind the end of a row of 2^31 - 1 does not fit 32.
 template <typename TX, typename TY>
 __global__ void __launch_bounds__(256) norm_gate_residual_generic(const NormParams p) {
   __shared__ float2 scratch[2][8];
@@ -414,12 +415,12 @@ __global__ void __launch_bounds__(256) norm_gate_residual_generic(const NormPara
       float shift = 0.f;
       if (kind == PD_NORM_LAYER) {
         float s = 0.f;
-        for (int j = threadIdx.x; j < p.cols; j += 256) s += value(j);
+        for (int64_t j = threadIdx.x; j < p.cols; j += 256) s += value(j);
         shift = block_sum2<8>(s, 0.f, scratch, slot).x * inv_cols;
         slot ^= 1;
       }
       float s = 0.f, q = 0.f;
-      for (int j = threadIdx.x; j < p.cols; j += 256) {
+      for (int64_t j = threadIdx.x; j < p.cols; j += 256) {
         const float d = value(j) - shift;
         s += d;
         q = fmaf(d, d, q);
@@ -430,19 +431,19 @@ __global__ void __launch_bounds__(256) norm_gate_residual_generic(const NormPara
       mean = shift + rest;
       rstd = rsqrtf(fmaxf(m.y * inv_cols - rest * rest, 0.f) + p.eps);
     };
-    auto affine = [&](int kind, float v, float mean, float rstd, const float* gamma, const float* beta, int j) {
+    auto affine = [&](int kind, float v, float mean, float rstd, const float* gamma, const float* beta, int64_t j) {
       if (kind == PD_NORM_NONE) return v;
       v = (v - mean) * (rstd * (gamma ? gamma[j] : 1.f));
       return kind == PD_NORM_LAYER && beta ? v + beta[j] : v;
     };
     float post_mean, post_rstd, pre_mean = 0.f, pre_rstd = 1.f;
-    stats(p.post_norm, [&](int j) { return widen(y[j]); }, post_mean, post_rstd);
-    auto h = [&](int j) {
+    stats(p.post_norm, [&](int64_t j) { return widen(y[j]); }, post_mean, post_rstd);
+    auto h = [&](int64_t j) {
       const float v = affine(p.post_norm, widen(y[j]), post_mean, post_rstd, p.post_gamma, p.post_beta, j);
       return fmaf(v, gate ? widen(gate[j]) : 1.f, p.alpha * widen(x[j]));
     };
     if (p.n) stats(p.pre_norm, h, pre_mean, pre_rstd);
-    for (int j = threadIdx.x; j < p.cols; j += 256) {
+    for (int64_t j = threadIdx.x; j < p.cols; j += 256) {
       const float v = h(j);
       const float n = affine(p.pre_norm, v, pre_mean, pre_rstd, p.pre_gamma, p.pre_beta, j);
       if (p.h) store_out1(static_cast<TX*>(p.h), row * p.cols + j, v);

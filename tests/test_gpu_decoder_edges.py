@@ -1,5 +1,7 @@
 """Edges of the decoder operators, through the binding: empty batches, very long rows, padded batches, layouts and page sizes
 beyond the ordinary ones."""
+import ctypes
+
 import pytest
 import torch
 
@@ -24,3 +26,19 @@ def test_empty_batches():
         out = api.pd_attention_paged_fwd(e(0, 4, 64), cache, cache, table, cu, lens, max_q_len=0, max_kv_len=48)
         assert out.shape == (0, 4, 64)
     assert bool((cache == 7.0).all())
+
+
+def test_norms_of_the_longest_row():
+    """2^31 - 1 columns: the last step of a thread that walks them lies beyond 32 bits."""
+    from paper_2511_03586_b200 import api
+    cols = 2 ** 31 - 1
+    ramp = (torch.arange(1 << 20, device="cuda") % 241 - 120).to(BF16)
+    x = ramp.repeat(2048)[:cols].view(1, cols)
+    y = torch.full((1, cols), 0.5, dtype=BF16, device="cuda")
+    h = torch.zeros_like(x)
+    d = api.NormGateResidualDesc(1, cols, 1, api.PD_BF16, api.PD_BF16, 0, 0, 1.0, 1e-5)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert api._lib.pd_norm_gate_residual_norm(ctypes.byref(d), y.data_ptr(), x.data_ptr(), *(None,) * 5, h.data_ptr(), None, stream) == 0
+    h.sub_(0.5)                                            # (exact: |x| <= 120, halves)
+    step = 1 << 28
+    assert all(torch.equal(h[:, i:i + step], x[:, i:i + step]) for i in range(0, cols, step))
