@@ -5,6 +5,8 @@ import ctypes
 import pytest
 import torch
 
+import decoder_reference as ref
+
 pytestmark = pytest.mark.gpu
 BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
 
@@ -42,3 +44,20 @@ def test_norms_of_the_longest_row():
     h.sub_(0.5)                                            # (exact: |x| <= 120, halves)
     step = 1 << 28
     assert all(torch.equal(h[:, i:i + step], x[:, i:i + step]) for i in range(0, cols, step))
+
+
+@pytest.mark.parametrize("norms", [("rms", "rms"), ("layer", "rms")], ids=str)
+@pytest.mark.parametrize("cols", [(1 << 18) + 8, (1 << 22) + 1])
+def test_norms_of_long_rows(cols, norms):
+    """Sums of millions of terms, of one size and sign (where roundings do not cancel) or two: 1e-5 of the value, or of the
+    row's RMS where that is larger, as for rows of any length."""
+    from paper_2511_03586_b200 import api
+    y = torch.full((2, cols), 1.1, device="cuda")
+    if norms[0] == "layer":
+        y[:, ::2] = -0.3
+    x = torch.full((2, cols), 0.7, device="cuda")
+    got = api.pd_norm_gate_residual_norm(y, x, post_norm=norms[0], pre_norm=norms[1])
+    want = ref.norm_gate_residual_norm(y, x, None, 1, 1.0, 1e-5, norms[0], None, None, norms[1], None, None)
+    for g, w in zip(got, want):
+        bound = 1e-5 * torch.maximum(w.abs(), w.pow(2).mean(-1, keepdim=True).sqrt())
+        assert ((g.double() - w).abs() <= bound).all()
