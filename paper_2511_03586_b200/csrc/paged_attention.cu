@@ -16,13 +16,22 @@ __global__ void __launch_bounds__(128) paged_attention_join(const Params p) {
   const int lane = threadIdx.x & 31;
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t rows = (int64_t)p.tokens * p.heads_q;
+  const int64_t rows = (int64_t)p.part_tokens * p.heads_q;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (row >= rows) return;
-  const int t = (int)(row / p.heads_q), h = (int)(row % p.heads_q);
-  // padding tokens, and tokens beyond max_q_len, have no partial results
-  const int b = find_sequence(p.cu_q, p.batch, t);
-  if (b >= p.batch || (unsigned)(t - __ldg(p.cu_q + b)) >= (unsigned)p.max_q_len) return;
+  const int h = (int)(row % p.heads_q);
+  int t = (int)(row / p.heads_q);  // the place of a token's partial results
+  // padding tokens, tokens beyond max_q_len, and places that a sequence does not fill have none
+  if (p.part_by_sequence) {
+    const int b = t / p.max_q_len;
+    const Sequence seq = load_sequence(p, b);
+    t -= b * p.max_q_len;
+    if (t >= seq.n) return;
+    t += seq.q0;
+  } else {
+    const int b = find_sequence(p.cu_q, p.batch, t);
+    if (b >= p.batch || (unsigned)(t - __ldg(p.cu_q + b)) >= (unsigned)p.max_q_len) return;
+  }
   const int per = D / 32;
   float lse_max = -INFINITY;
   for (int z = lane; z < p.splits; z += 32) lse_max = fmaxf(lse_max, p.part_lse[z * rows + row]);
@@ -95,9 +104,13 @@ Plan plan(const pd_paged_attention_desc& d) {
   return pl;
 }
 
+// Tokens that can have partial results in the chunk kernel (a token tensor may be padded to any length), at most d.tokens.
+int64_t partial_tokens(const pd_paged_attention_desc& d) {
+  return std::min<int64_t>(d.tokens, (int64_t)d.batch * std::min(d.max_q_len, d.tokens));
+}
 // Rows of partial results in the workspace, and entries of the piece table behind them.
 size_t partial_rows(const pd_paged_attention_desc& d, const Plan& pl) {
-  if (pl.rows_per_tile > 64) return pl.splits > 1 ? (size_t)pl.splits * d.tokens * d.heads_q : 0;
+  if (pl.rows_per_tile > 64) return pl.splits > 1 ? (size_t)pl.splits * partial_tokens(d) * d.heads_q : 0;
   return (size_t)2 * pl.splits * pl.rows_per_tile;
 }
 size_t table_entries(const pd_paged_attention_desc& d, const Plan& pl) {
@@ -157,6 +170,7 @@ extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc,
   p.num_pages = d.num_pages; p.page_size = d.page_size; p.max_pages = d.max_pages;
   while ((1 << p.page_shift) < d.page_size) ++p.page_shift;
   p.max_q_len = std::min(d.max_q_len, d.tokens); p.window = std::min(d.window, paged::kMaxPositions); p.sinks = d.sinks;
+  p.part_tokens = (int)paged::partial_tokens(d); p.part_by_sequence = p.part_tokens < d.tokens;
   p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles; p.whole_items = pl.whole_items;
   p.scale_log2e = (float)((double)d.scale * 1.4426950408889634);
   if (need > 0) {
@@ -171,7 +185,7 @@ extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc,
                                                      : paged::launch_rows(d, p, k_cache, v_cache, pl.rows_per_tile, stream);
   if (launched != PD_OK) return launched;
   if (pl.rows_per_tile > 64 && pl.splits > 1) {
-    const int64_t rows = (int64_t)d.tokens * d.heads_q;
+    const int64_t rows = (int64_t)p.part_tokens * d.heads_q;
     const unsigned grid = (unsigned)((rows + 3) / 4);
     if (d.head_dim == 64) launch_pdl(paged::paged_attention_join<64>, dim3(grid), dim3(128), 0, stream, p);
     else launch_pdl(paged::paged_attention_join<128>, dim3(grid), dim3(128), 0, stream, p);

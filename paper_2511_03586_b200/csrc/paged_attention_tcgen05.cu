@@ -88,7 +88,7 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
   const int lane = threadIdx.x & 31;
   tcgen05_fence_after_sync();
   const float inv = l > 0.f ? 1.f / l : 0.f;  // nothing seen: zeros
-  const int64_t at = ((int64_t)split * p.tokens + seq.q0 + t) * p.heads_q + head;
+  const int64_t at = ((int64_t)split * p.part_tokens + seq.part0 + t) * p.heads_q + head;
   if (p.splits == 1) {
     // through shared memory, so that a store instruction writes whole rows
 #pragma unroll

@@ -17,7 +17,7 @@ struct Params {
   const __nv_bfloat16* q;
   __nv_bfloat16* out;
   const int32_t *block_table, *cu_q, *kv_len;
-  // Partial outputs (normalised) and the logarithms (base 2) of their sums of exponentials: [splits][tokens * heads_q]
+  // Partial outputs (normalised) and the logarithms (base 2) of their sums of exponentials: [splits][part_tokens * heads_q]
   // (chunk kernel), or [2 CTAs][rows per tile] with the places of an item's pieces (row kernel).
   float *part_o, *part_lse;
   int2* pieces;
@@ -26,6 +26,9 @@ struct Params {
   int batch, tokens, heads_q, heads_kv, group;
   int num_pages, page_size, page_shift, max_pages;
   int max_q_len, window, sinks;
+  // Tokens that can have partial results in the chunk kernel: all rows of the token tensors, or, where these are padded to
+  // more than max_q_len for each sequence, that many places a sequence.
+  int part_tokens, part_by_sequence;
   int splits;           // of the keys of every row tile (chunk kernel), CTAs in all (row kernel)
   int min_split_tiles;  // the smallest share of key tiles
   int whole_items;      // row kernel: no item is shared out (short contexts: nothing to join)
@@ -57,6 +60,7 @@ struct Sequence {
   int q0, n;     // first token row, new tokens (as many as are computed)
   int pos0;      // position of the first new token (negative when kv_len is short of n)
   int length;    // keys that the block table can name
+  int part0;     // place of the first token's partial results
 };
 
 __device__ __forceinline__ Sequence load_sequence(const Params& p, int b) {
@@ -69,6 +73,7 @@ __device__ __forceinline__ Sequence load_sequence(const Params& p, int b) {
   s.n = min(e - a, p.max_q_len);
   s.pos0 = len - (e - a);
   s.length = (int)(len < cap ? len : cap);
+  s.part0 = p.part_by_sequence ? b * p.max_q_len : a;
   return s;
 }
 

@@ -61,3 +61,28 @@ def test_norms_of_long_rows(cols, norms):
     for g, w in zip(got, want):
         bound = 1e-5 * torch.maximum(w.abs(), w.pow(2).mean(-1, keepdim=True).sqrt())
         assert ((g.double() - w).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[(130, 3000)], [(40, 2500), (0, 10), (33, 33), (1, 1900), (0, 0)]], ids=["one", "some"])
+@pytest.mark.parametrize("pad", [0, 2, 3000])
+def test_padded_batches_with_split_keys(lens, pad, d):
+    """Few rows over many keys, which the chunk kernels share out, in token tensors of a fixed size."""
+    from test_gpu_paged_attention import Paged
+    p = Paged(lens, 8, 2, d, 16, seed=pad + d, pad=pad)
+    out = torch.full_like(p.q, 3.0)
+    for _ in range(2):
+        p.attend(out=out)
+        p.check(out)
+        assert bool((out[sum(n for n, _ in lens):] == 3.0).all())
+    cut = max(n for n, _ in lens) - 5                      # new tokens beyond max_q_len are not computed
+    short = torch.full_like(p.q, 3.0)
+    p.attend(out=short, max_q_len=cut)
+    start = 0
+    for b, (n, kv) in enumerate(lens):
+        m = min(n, cut)
+        want, mag = ref.attention(p.q[start:start + m], p.k_seq[b], p.v_seq[b], kv - n)
+        bound = (2 ** -8 + 2 ** -10) * mag + 2 ** -8 * want.abs() + 1e-30   # as in test_gpu_paged_attention
+        assert ((short[start:start + m].double() - want).abs() <= bound).all()
+        assert bool((short[start + m:start + n] == 3.0).all())
+        start += n

@@ -23,3 +23,24 @@ def test_empty_norms_have_null_pointers():
         assert lib.pd_norm_gate_residual_norm(ctypes.byref(NormGateResidualDesc(**{**d, **bad})), *nulls, None) == SHAPE
     d["rows"] = 1
     assert lib.pd_norm_gate_residual_norm(ctypes.byref(NormGateResidualDesc(**d)), *nulls, None) == NULLP
+
+
+def paged(**kw):
+    d = dict(batch=1, tokens=128, heads_q=32, heads_kv=8, head_dim=128, num_pages=8192, page_size=16, max_pages=8192,
+             max_q_len=128, max_kv_len=131072, window=0, sinks=0, scale=0.125, ld_q=4096, ld_out=4096, page_stride=16384,
+             slot_stride=1024, head_stride=128)
+    d.update(kw)
+    return PagedAttentionDesc(**d)
+
+
+def test_workspace_does_not_grow_with_padding():
+    """Partial results belong to tokens: at most max_q_len for each sequence, however long the token tensors are."""
+    def need(**kw):
+        return lib.pd_attention_paged_workspace_bytes(ctypes.byref(paged(**kw)))
+    full = need()
+    assert 0 < full < 32 << 20                              # (about 148 tiles of 256 rows, 129 floats each, at most)
+    for tokens in (129, 65536, 1 << 20):
+        assert need(tokens=tokens) == full
+    for d in (64, 128):
+        assert need(batch=3, max_q_len=40, tokens=65536, head_dim=d) == need(batch=3, max_q_len=40, tokens=120, head_dim=d)
+    assert need(batch=3, max_q_len=128, tokens=200) <= need(batch=3, max_q_len=128, tokens=384)
