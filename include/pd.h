@@ -401,7 +401,7 @@ pd_status pd_encoder_layer_fwd_profiled(const pd_encoder_layer_desc* desc,
  *    of the window, may hold anything, NaN included.  An entry outside
  *    [0, num_pages) is never followed: keys and values there count as zeros.
  *  - What is visible to any query of a sequence has to be finite, and so have the
- *    scaled scores in fp32.
+ *    scores q . k in fp32; scaled, they stay below 2^127 in size.
  *  - The sequences' pages may be shared for reading (a common prefix). */
 typedef struct {
   int32_t batch, tokens;               /* sequences; rows of the token tensors */
@@ -411,7 +411,7 @@ typedef struct {
   int32_t max_kv_len;  /* launch: new tokens beyond max_q_len are not computed; longer caches only take longer */
   int32_t window;      /* keys a query sees, its own position included; 0: all before it */
   int32_t sinks;       /* first tokens of the sequence that stay visible whatever the window */
-  float scale;         /* of the scores, before the softmax; above 0 */
+  float scale;         /* of the scores, before the softmax; above 0, at most 2^127 */
   int64_t ld_q, ld_out;                           /* elements from token to token; head h at column h * head_dim */
   int64_t page_stride, slot_stride, head_stride;  /* of both caches, in elements */
 } pd_paged_attention_desc;

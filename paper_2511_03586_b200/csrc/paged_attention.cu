@@ -60,12 +60,15 @@ struct Plan {
   bool whole_items;
 };
 
+// The scale of scores as powers of two, which the kernels compute with.
+float base2_scale(float scale) { return (float)((double)scale * 1.4426950408889634); }
+
 constexpr int kMaxPositions = 1 << 30;  // of a sequence's table, and rows of a cache head: sums of two stay in 32 bits
 
 bool valid(const pd_paged_attention_desc& d) {
   return d.batch >= 0 && d.tokens >= 0 && d.heads_q > 0 && d.heads_kv > 0 && d.head_dim > 0 &&
          d.heads_q % d.heads_kv == 0 && d.num_pages > 0 && d.page_size > 0 && d.max_pages > 0 && d.max_q_len >= 0 &&
-         d.max_kv_len >= 0 && d.window >= 0 && d.sinks >= 0 && std::isfinite(d.scale) && d.scale > 0.f;
+         d.max_kv_len >= 0 && d.window >= 0 && d.sinks >= 0 && std::isfinite(base2_scale(d.scale)) && d.scale > 0.f;
 }
 bool supported(const pd_paged_attention_desc& d) {
   return (d.head_dim == 64 || d.head_dim == 128) && d.heads_q / d.heads_kv <= 64 && d.page_size >= 8 &&
@@ -172,7 +175,7 @@ extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc,
   p.max_q_len = std::min(d.max_q_len, d.tokens); p.window = std::min(d.window, paged::kMaxPositions); p.sinks = d.sinks;
   p.part_tokens = (int)paged::partial_tokens(d); p.part_by_sequence = p.part_tokens < d.tokens;
   p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles; p.whole_items = pl.whole_items;
-  p.scale_log2e = (float)((double)d.scale * 1.4426950408889634);
+  p.scale_log2e = paged::base2_scale(d.scale);
   if (need > 0) {
     const size_t rows = paged::partial_rows(d, pl);  // (an even number in the row kernel: the table is aligned)
     p.part_o = static_cast<float*>(workspace);

@@ -44,3 +44,13 @@ def test_workspace_does_not_grow_with_padding():
     for d in (64, 128):
         assert need(batch=3, max_q_len=40, tokens=65536, head_dim=d) == need(batch=3, max_q_len=40, tokens=120, head_dim=d)
     assert need(batch=3, max_q_len=128, tokens=200) <= need(batch=3, max_q_len=128, tokens=384)
+
+
+def test_scale_is_finite_in_powers_of_two_as_well():
+    """The kernels compute with scale * log2 e: infinite, it would make NaN of a score of zero."""
+    def need(scale):
+        return lib.pd_attention_paged_workspace_bytes(ctypes.byref(paged(scale=scale)))
+    assert need(2.0 ** 127) == need(0.125) > 0
+    d = paged(scale=3e38)
+    assert need(3e38) == 0
+    assert lib.pd_attention_paged_fwd(ctypes.byref(d), *(None,) * 8, 0, None) == SHAPE   # (no pointer, so it cannot run either way)
