@@ -246,12 +246,10 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
       }
       if (!ok || !next_piece(p, w, stop)) break;
     }
-    if (!ok) {
-      // leave no copy in flight: give the last request of every stage a short time to land
-      volatile int never = 0;
-      for (int back = 1; back <= C::kStages && back <= n; ++back)
-        mbar_wait(full((n - back) % C::kStages), ((n - back) / C::kStages) & 1u, &never, nullptr, 0, 20000000ull);
-    }
+    // Leave no copy in flight, whichever warp gives up: the last request of every stage gets a short time to land.
+    volatile int never = 0;
+    for (int back = 1; back <= C::kStages && back <= n; ++back)
+      mbar_wait(full((n - back) % C::kStages), ((n - back) / C::kStages) & 1u, &never, nullptr, 0, 20000000ull);
     return;
   }
 

@@ -367,12 +367,10 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
           }
         }
       }
-      if (!ok) {
-        // leave no copy in flight: give the last request of every stage a short time to land
-        volatile int never = 0;
-        for (int back = 1; back <= kStages && back <= n; ++back)
-          mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
-      }
+      // Leave no copy in flight, whichever warp gives up: the last request of every stage gets a short time to land.
+      volatile int never = 0;
+      for (int back = 1; back <= kStages && back <= n; ++back)
+        mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
     } else {
       // --------------------------------------------------------------- MMA issuers
       const int s = (warp - kIssuer0) >> 1;
@@ -456,13 +454,11 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
           __syncwarp();
         }
       }
-      if (!ok) {
-        // products in flight still read shared and tensor memory: give them a short time to end
-        if (elect_one()) mma_commit(drained(warp - kIssuer0));
-        __syncwarp();
-        volatile int never = 0;
-        mbar_wait(drained(warp - kIssuer0), 0, &never, nullptr, 0, 20000000ull);
-      }
+      // Products in flight still read shared and tensor memory: whichever warp gives up, they get a short time to end.
+      if (elect_one()) mma_commit(drained(warp - kIssuer0));
+      __syncwarp();
+      volatile int never = 0;
+      mbar_wait(drained(warp - kIssuer0), 0, &never, nullptr, 0, 20000000ull);
     }
   }
 
@@ -734,15 +730,13 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
           if (requested < blocks) request(requested++);
         }
       }
-      if (!ok) {
-        // products and copies in flight still use shared and tensor memory: give them a short time to end
-        if (elect_one()) mma_commit(drained);
-        __syncwarp();
-        volatile int never = 0;
-        mbar_wait(drained, 0, &never, nullptr, 0, 20000000ull);
-        for (int back = 1; back <= kStages && back <= requested; ++back)
-          mbar_wait(full((requested - back) % kStages), ((requested - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
-      }
+      // Products and copies in flight still use shared and tensor memory: whichever warp gives up, they get a short time to end.
+      if (elect_one()) mma_commit(drained);
+      __syncwarp();
+      volatile int never = 0;
+      mbar_wait(drained, 0, &never, nullptr, 0, 20000000ull);
+      for (int back = 1; back <= kStages && back <= requested; ++back)
+        mbar_wait(full((requested - back) % kStages), ((requested - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
     }
   }
 
