@@ -445,12 +445,12 @@ def pd_clear_device_status() -> None:
 
 
 def pd_debug_set_wait_limit_ns(limit_ns: int) -> None:
-    """Time after which a wait inside the single-CTA contraction kernel gives up (default 2 s)."""
+    """Time after which a wait inside the contraction, paged attention and row-prefetching norm kernels gives up (default 2 s)."""
     _check(_lib.pd_debug_set_wait_limit_ns(int(limit_ns)), "pd_debug_set_wait_limit_ns")
 
 
 def pd_debug_withhold_loads(on: bool) -> None:
-    """Test switch: the single-CTA contraction kernel's producer issues no load, so a bounded wait runs out."""
+    """Test switch: the producers of the same kernels issue no load, so a bounded wait runs out."""
     _check(_lib.pd_debug_withhold_loads(int(bool(on))), "pd_debug_withhold_loads")
 
 

@@ -30,6 +30,8 @@ struct NormParams {
   int64_t rows, gate_rows;
   int cols, post_norm, pre_norm;
   float alpha, eps;
+  unsigned long long wait_limit_ns;  // (of the kernel that prefetches rows, as is the next one)
+  int withhold_loads;                // test switch: rows are not requested, and the first wait for one runs out
 };
 
 struct Raw8f { float4 a, b; };
@@ -288,6 +290,7 @@ __global__ void __launch_bounds__(kPrefetchThreads, 1) norm_gate_residual_rows_p
   const int64_t step = (int64_t)gridDim.x * kGroups;
   int64_t row = (int64_t)blockIdx.x * kGroups + group;
   auto fetch = [&](int64_t r) {  // by the group's first thread
+    if (p.withhold_loads) return;
     sm100::mbar_arrive_expect_tx(bar, y_bytes + x_bytes);
     bulk_load(sm100::smem_u32(ys), static_cast<const TY*>(p.y) + r * p.cols, y_bytes, bar);
     bulk_load(sm100::smem_u32(xs), static_cast<const TX*>(p.x) + r * p.cols, x_bytes, bar);
@@ -342,7 +345,7 @@ __global__ void __launch_bounds__(kPrefetchThreads, 1) norm_gate_residual_rows_p
     }
   };
   for (; row < p.rows; row += step, parity ^= 1u) {
-    const bool here = sm100::mbar_wait(bar, parity, &abort_flag, status, kTimeoutNorm);
+    const bool here = sm100::mbar_wait(bar, parity, &abort_flag, status, kTimeoutNorm, p.wait_limit_ns);
     decltype(load_raw8(static_cast<const TX*>(nullptr))) rx[UNITS];
     float v[UNITS][8];
 #pragma unroll
@@ -551,7 +554,7 @@ extern "C" pd_status pd_norm_gate_residual_norm(const pd_norm_gate_residual_desc
     return PD_ERR_ALIGNMENT;
   if (pd_status st = pd::require_sm100(); st != PD_OK) return st;
   pd::NormParams p{y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta, h, n, d.rows, gate ? d.gate_rows : 1,
-                   (int)d.cols, d.post_norm, d.pre_norm, d.alpha, d.eps};
+                   (int)d.cols, d.post_norm, d.pre_norm, d.alpha, d.eps, pd::debug_wait_limit_ns(), pd::debug_withhold_loads()};
   if (d.x_dtype == PD_BF16)
     return d.y_dtype == PD_BF16 ? pd::launch<__nv_bfloat16, __nv_bfloat16>(p, stream) : pd::launch<__nv_bfloat16, float>(p, stream);
   return d.y_dtype == PD_BF16 ? pd::launch<float, __nv_bfloat16>(p, stream) : pd::launch<float, float>(p, stream);

@@ -168,6 +168,7 @@ extern "C" pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc,
   p.block_table = block_table; p.cu_q = cu_q; p.kv_len = kv_len;
   p.status = device_status_ptr();
   if (!p.status) return PD_ERR_CUDA;
+  p.wait_limit_ns = debug_wait_limit_ns(); p.withhold_loads = debug_withhold_loads();
   p.ld_q = d.ld_q; p.ld_out = d.ld_out;
   p.batch = d.batch; p.tokens = d.tokens; p.heads_q = d.heads_q; p.heads_kv = d.heads_kv; p.group = d.heads_q / d.heads_kv;
   p.num_pages = d.num_pages; p.page_size = d.page_size; p.max_pages = d.max_pages;

@@ -215,7 +215,7 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
     const int box = min(p.page_size, kTile);
     const int per_tile = kTile / box;
     const int per_batch = 32 / per_tile;
-    bool ok = true;
+    bool ok = !p.withhold_loads;
     int n = 0;  // stages requested so far
     while (ok) {
       const int end = min(w.end, w.tiles.n);
@@ -229,7 +229,7 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
         const int slot = (w.tiles.tile_index(i) * kTile) & (p.page_size - 1);  // 0 unless a page holds several tiles
         for (int kv = 0; kv < 2; ++kv, ++n) {
           const int stage = n % C::kStages;
-          if (!mbar_wait_warp(empty(stage), ((n / C::kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutRowsProducer)) { ok = false; break; }
+          if (!mbar_wait_warp(empty(stage), ((n / C::kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutRowsProducer, p.wait_limit_ns)) { ok = false; break; }
           if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensorBytes);
           __syncwarp();
           for (int j = 0; j < per_tile; ++j) {
@@ -294,7 +294,7 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
       const int v_stage = n % C::kStages, v_phase = (n / C::kStages) & 1;
       ++n;
       // (a warp that gives up goes on to the barrier below, which tells the others)
-      if (!mbar_wait_warp(full(k_stage), k_phase, abort_flag, p.status, kTimeoutRowsConsumer)) { failed = true; break; }
+      if (!mbar_wait_warp(full(k_stage), k_phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
       const uint32_t sk = ring + k_stage * C::kTensorBytes, sv = ring + v_stage * C::kTensorBytes;
       const int key0 = kt.tile_index(i) * kTile + wk * kKeys;
       float s[NT][4];
@@ -355,7 +355,7 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
         pf[n >> 1][(n & 1) * 2] = pack_bf16(e0, e1);
         pf[n >> 1][(n & 1) * 2 + 1] = pack_bf16(e2, e3);
       }
-      if (!mbar_wait_warp(full(v_stage), v_phase, abort_flag, p.status, kTimeoutRowsConsumer)) { failed = true; break; }
+      if (!mbar_wait_warp(full(v_stage), v_phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
 #pragma unroll
       for (int k = 0; k < kKeys / 16; ++k) {
         const int row = wk * kKeys + k * 16 + v_row;

@@ -236,7 +236,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
         if (!view.needs(key0)) continue;
         const int buf = done & 1;
         const uint32_t t_s = t_lane + s * kTile + buf * kBlock;
-        if (!mbar_wait_warp(s_full(s, buf), (done >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) { ok = false; break; }
+        if (!mbar_wait_warp(s_full(s, buf), (done >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns)) { ok = false; break; }
         tcgen05_fence_after_sync();
         uint32_t x[2][32];
         tmem_ld_32x32b_x32(t_s, x[0]);
@@ -273,7 +273,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
           l *= alpha;
           if (done > 0) {
             // every product into O so far has to be through with it; the one before last is, or these scores would not be here
-            if (!mbar_wait_warp(o_full(s, buf ^ 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) { ok = false; break; }
+            if (!mbar_wait_warp(o_full(s, buf ^ 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns)) { ok = false; break; }
             tcgen05_fence_after_sync();
 #pragma unroll 1
             for (int c = 0; c < D; c += 8) {
@@ -333,7 +333,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
         ++done;
       }
       // ---- the row's output
-      if (ok && done > 0) ok = mbar_wait_warp(o_full(s, (done - 1) & 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax);
+      if (ok && done > 0) ok = mbar_wait_warp(o_full(s, (done - 1) & 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns);
       if (ok && view.active && *abort_flag == 0) {
         write_rows<D>(p, seq, split, t, head, valid, done > 0, m, l, t_o, sQ + s * C::kTensor + (uint32_t)(quarter * 32) * 128u);
       }
@@ -342,7 +342,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
       const int box = min(p.page_size, kTile);
       const int per_tile = kTile / box, per_batch = 32 / per_tile;
       int page = 0, n = 0;  // n: ring slots requested so far
-      bool ok = true;
+      bool ok = !p.withhold_loads;
       for (int i = begin; i < end && ok; ++i) {
         const int in_batch = (i - begin) % per_batch;
         if (in_batch == 0) {
@@ -352,7 +352,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
         const int slot = (kt.tile_index(i) * kTile) & (p.page_size - 1);
         for (int kv = 0; kv < 2; ++kv, ++n) {
           const int stage = n % kStages;
-          if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer)) { ok = false; break; }
+          if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer, p.wait_limit_ns)) { ok = false; break; }
           if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensor);
           __syncwarp();
           for (int j = 0; j < per_tile; ++j) {
@@ -378,7 +378,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
       uint32_t k = 0;  // products issued so far
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        ok = ok && mbar_wait_warp(bar, parity & 1u, abort_flag, p.status, kTimeoutChunkMma);
+        ok = ok && mbar_wait_warp(bar, parity & 1u, abort_flag, p.status, kTimeoutChunkMma, p.wait_limit_ns);
         return ok;
       };
       constexpr uint64_t kBlockStep = (kBlock * 128) >> 4;  // descriptor step from a tile's first block to its second
@@ -563,7 +563,7 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
       bool ok = true;
       for (int i = 0; i < blocks; ++i) {
         const int key0 = kt.tile_index(begin + i) * kBlock;
-        if (!mbar_wait_warp(s_full, i & 1u, abort_flag, p.status, kTimeoutChunkSoftmax)) { ok = false; break; }
+        if (!mbar_wait_warp(s_full, i & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns)) { ok = false; break; }
         tcgen05_fence_after_sync();
         uint32_t x[32], x1[32];
         tmem_ld_32x32b_x32(t_lane, x);
@@ -644,7 +644,7 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
         if (lane == 0) mbar_arrive(p_full);
       }
       if (ok && blocks > 0)
-        ok = mbar_wait_warp(o_full, (blocks - 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax);
+        ok = mbar_wait_warp(o_full, (blocks - 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns);
       if (ok && *abort_flag == 0)
         write_rows<D>(p, seq, split, t, head, valid, blocks > 0, m, l, t_o, sQ + (uint32_t)(warp * 32) * 128u);
     } else {
@@ -675,7 +675,7 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
       };
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        ok = ok && mbar_wait_warp(bar, parity & 1u, abort_flag, p.status, kTimeoutChunkMma);
+        ok = ok && mbar_wait_warp(bar, parity & 1u, abort_flag, p.status, kTimeoutChunkMma, p.wait_limit_ns);
         return ok;
       };
       constexpr uint32_t s_idesc = make_idesc_bf16(kTile, kBlock, false, false);
@@ -695,7 +695,7 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
         __syncwarp();
       };
       int requested = 0;
-      for (; requested < min(blocks, kStages); ++requested) request(requested);
+      for (; requested < min(blocks, kStages) && !p.withhold_loads; ++requested) request(requested);
       if (blocks > 0 && wait(q_full, 0)) scores(0);
       for (int i = 0; i < blocks && ok; ++i) {
         const int key0 = kt.tile_index(begin + i) * kBlock;

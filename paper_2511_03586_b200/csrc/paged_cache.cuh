@@ -22,6 +22,8 @@ struct Params {
   float *part_o, *part_lse;
   int2* pieces;
   int* status;
+  unsigned long long wait_limit_ns;  // of every bounded wait
+  int withhold_loads;                // test switch: key tiles are not requested, and the first wait for one runs out
   int64_t ld_q, ld_out;
   int batch, tokens, heads_q, heads_kv, group;
   int num_pages, page_size, page_shift, max_pages;

@@ -25,8 +25,8 @@ int sm_count();
 // Device address of the status word the bounded waits report to (nullptr on failure).
 int* device_status_ptr();
 // Test aids behind pd_debug_set_wait_limit_ns / pd_debug_withhold_loads: the time after which a wait inside the
-// single-CTA contraction kernel gives up (default 2 s), and whether that kernel's producer skips its loads, so
-// that the wait for them runs out.
+// contraction, paged attention and row-prefetching norm kernels gives up (default 2 s), and whether these kernels'
+// producers skip their loads, so that the wait for them runs out.
 uint64_t debug_wait_limit_ns();
 int debug_withhold_loads();
 // Variant-selection log: with PD_LOG=1 in the environment every launcher writes one line to stderr naming the
