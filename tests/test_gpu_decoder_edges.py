@@ -86,3 +86,47 @@ def test_padded_batches_with_split_keys(lens, pad, d):
         assert ((short[start:start + m].double() - want).abs() <= bound).all()
         assert bool((short[start + m:start + n] == 3.0).all())
         start += n
+
+
+@pytest.mark.parametrize("page", [512, 1024, 4096])
+@pytest.mark.parametrize("layout", ["slots", "heads"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_over_large_pages(page, layout, d):
+    from test_gpu_paged_attention import Paged
+    lens = [(1, 3), (1, page - 1), (1, page), (1, page + 1), (3, 2 * page + 130)]
+    for window, sinks in ((0, 0), (70, 5)):
+        p = Paged(lens, 8, 2, d, page, layout=layout, seed=page, window=window, sinks=sinks)
+        p.check(p.attend())
+        p = Paged([(100, page + 40), (30, 30)], 8, 2, d, page, layout=layout, seed=page + 1, window=window, sinks=sinks)
+        p.check(p.attend())
+
+
+@pytest.mark.parametrize("page", [1, 16, 48, 512, 4096])
+@pytest.mark.parametrize("heads,d", [(2, 64), (8, 128), (1, 128), (3, 8)], ids=str)
+def test_append_to_caches_whose_heads_lie_outside_their_slots(heads, d, page):
+    """[pages, heads, slots, d], a block of a larger cache: page, slot and head strides that are not those of dense rows."""
+    from paper_2511_03586_b200 import api
+    lens = [(5, 5), (1, page), (7, 2 * page + 3), (0, 4)]
+    need = [-(-kv // page) for _, kv in lens]
+    whole = torch.full((2, sum(need) + 2, heads + 1, page, d), 7.0, dtype=BF16, device="cuda")
+    k_cache, v_cache = whole[0, :, 1:].transpose(1, 2), whole[1, :, 1:].transpose(1, 2)
+    tokens = sum(n for n, _ in lens)
+    packed = torch.randn(tokens + 2, (4 + 2 * heads) * d, device="cuda").bfloat16()
+    k = packed[:, 4 * d:(4 + heads) * d].unflatten(1, (heads, d))
+    v = packed[:, (4 + heads) * d:].unflatten(1, (heads, d))
+    table = torch.full((len(lens), max(need)), -1, dtype=I32)
+    pages = torch.randperm(sum(need) + 2, generator=torch.Generator().manual_seed(page)).tolist()
+    cu, want, at = [0], whole.clone(), 0
+    for b, (n, kv) in enumerate(lens):
+        table[b, :need[b]] = torch.tensor(pages[at:at + need[b]], dtype=I32)
+        at += need[b]
+        for i in range(n):
+            pos = kv - n + i
+            if pos < 0:
+                continue                                   # a new token in front of the sequence is dropped
+            want[0, table[b, pos // page], 1:, pos % page] = k[cu[-1] + i]
+            want[1, table[b, pos // page], 1:, pos % page] = v[cu[-1] + i]
+        cu.append(cu[-1] + n)
+    api.pd_kv_cache_append(k, v, k_cache, v_cache, table.cuda(), torch.tensor(cu, dtype=I32, device="cuda"),
+                           torch.tensor([kv for _, kv in lens], dtype=I32, device="cuda"))
+    assert torch.equal(whole, want)
