@@ -400,6 +400,8 @@ __device__ __forceinline__ float widen(float v) { return v; }
 
 // Any length and alignment: a CTA per row that reads the row again for every statistic (from L2).
 // Columns are counted in 64 bits: a thread's step behind the end of a row of 2^31 - 1 does not fit 32.
+// h is computed once for every pass over the row, with its roundings written out, so that the passes agree on it: contracted
+// differently they were a step apart, which LayerNorm of a row of one value multiplies by 1 / sqrt(eps).
 // A thread adds runs of 64 terms in single precision (off by 2^-18 at most) and the runs in double: one running sum is off by
 // 7e-5 over the 16384 terms of 4 million equal columns.
 template <typename TX, typename TY>
@@ -450,14 +452,14 @@ __global__ void __launch_bounds__(256) norm_gate_residual_generic(const NormPara
     };
     auto affine = [&](int kind, float v, float mean, float rstd, const float* gamma, const float* beta, int64_t j) {
       if (kind == PD_NORM_NONE) return v;
-      v = (v - mean) * (rstd * (gamma ? gamma[j] : 1.f));
-      return kind == PD_NORM_LAYER && beta ? v + beta[j] : v;
+      v = __fmul_rn(v - mean, __fmul_rn(rstd, gamma ? gamma[j] : 1.f));
+      return kind == PD_NORM_LAYER && beta ? __fadd_rn(v, beta[j]) : v;
     };
     float post_mean, post_rstd, pre_mean = 0.f, pre_rstd = 1.f;
     stats(p.post_norm, [&](int64_t j) { return widen(y[j]); }, post_mean, post_rstd);
     auto h = [&](int64_t j) {
       const float v = affine(p.post_norm, widen(y[j]), post_mean, post_rstd, p.post_gamma, p.post_beta, j);
-      return fmaf(v, gate ? widen(gate[j]) : 1.f, p.alpha * widen(x[j]));
+      return gate ? __fmaf_rn(v, widen(gate[j]), __fmul_rn(p.alpha, widen(x[j]))) : __fmaf_rn(p.alpha, widen(x[j]), v);
     };
     if (p.n) stats(p.pre_norm, h, pre_mean, pre_rstd);
     for (int64_t j = threadIdx.x; j < p.cols; j += 256) {

@@ -130,3 +130,18 @@ def test_append_to_caches_whose_heads_lie_outside_their_slots(heads, d, page):
     api.pd_kv_cache_append(k, v, k_cache, v_cache, table.cuda(), torch.tensor(cu, dtype=I32, device="cuda"),
                            torch.tensor([kv for _, kv in lens], dtype=I32, device="cuda"))
     assert torch.equal(whole, want)
+
+
+@pytest.mark.parametrize("cols", [1, 64, 65, 1000, 1001, 4096, 4097, 32768, 40001])
+@pytest.mark.parametrize("post", ["none", "rms", "layer"])
+@pytest.mark.parametrize("gate", [None, 0.7])
+def test_layernorm_of_rows_of_one_value(cols, post, gate):
+    """h does not vary within a row, whatever its rounding, so that LayerNorm leaves beta: a mean that is off by 5e-6 of the value
+    is put right by the mean of the deviations, to 3e-11 of it, of which 1 / sqrt(eps) makes 1e-8.  1e-5, as for other rows."""
+    from paper_2511_03586_b200 import api
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    y, x = ((torch.randn(50, 1, generator=g, device="cuda") * 3).expand(50, cols).contiguous() for _ in range(2))
+    beta = torch.randn(cols, generator=g, device="cuda").abs() + 0.5
+    gates = None if gate is None else torch.full((1, cols), gate, device="cuda")
+    _, n = api.pd_norm_gate_residual_norm(y, x, gate=gates, alpha=1.3, post_norm=post, pre_norm="layer", pre_beta=beta)
+    assert ((n - beta).abs() <= 1e-5 * beta).all()
