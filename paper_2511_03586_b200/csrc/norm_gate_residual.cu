@@ -506,8 +506,9 @@ pd_status launch(const NormParams& p, cudaStream_t s) {
   const bool vec_ok = p.cols % 8 == 0 && p.cols <= 32768 && aligned16(p.y) && aligned16(p.x) && aligned16(p.gate) &&
                       aligned16(p.h) && aligned16(p.n) && aligned16(p.post_gamma) && aligned16(p.post_beta) &&
                       aligned16(p.pre_gamma) && aligned16(p.pre_beta);
-  // Measured (16384 rows, RMSNorm twice, us prefetched / not): bf16 streams, 4096 columns 98 / 108, 8192 columns 209 / 241,
-  // 1024 columns 27 / 28; with an fp32 stream 157 / 153, so not there.  1184 rows of 4096 columns: 11.9 / 12.2.
+  // Measured (16384 rows, RMSNorm twice, single calls, us prefetched / not): bf16 streams, 4096 columns 96 / 109, 8192 columns
+  // 209 / 234, 1024 columns 27 / 28; with a gate for every row 141 / 141 (4096) and 293 / 305 (8192).  An fp32 stream, with gates
+  // and a LayerNorm, took 157 / 153 (160 in long runs), so not there.  1184 rows of 4096 columns: 11.9 / 12.2.
   if constexpr (sizeof(TX) + sizeof(TY) == 4) {
     if (vec_ok && p.cols > 1024 && p.cols <= 8192) {
       const int t = p.cols <= 2048 ? 128 : p.cols <= 4096 ? 256 : 512;

@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(128) paged_attention_join(const Params p) {
 
 struct Plan {
   int rows_per_tile;            // 16, 32, 64: row kernel; 128 (head_dim 64), 256: chunk kernel
-  int splits, min_split_tiles;  // in key tiles of the kernel (64, 128)
+  int splits, min_split_tiles;  // in key tiles of the kernel (64, 128); the latter of the chunk kernels alone
   bool whole_items;
 };
 
@@ -81,7 +81,7 @@ bool supported(const pd_paged_attention_desc& d) {
 
 // Depends on the desc alone (the workspace size follows from it).
 Plan plan(const pd_paged_attention_desc& d) {
-  constexpr int kSms = 148;
+  constexpr int kSms = 148;  // (not asked of the device: the workspace follows from the desc alone)
   Plan pl{};
   const int64_t group = d.heads_q / d.heads_kv, rows = std::min(d.max_q_len, d.tokens) * group;
   pl.rows_per_tile = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : d.head_dim == 64 ? 128 : 256;
@@ -93,10 +93,9 @@ Plan plan(const pd_paged_attention_desc& d) {
   const int64_t tile = !chunk ? 64 : d.head_dim == 64 ? 64 : 128, tiles = (keys + tile - 1) / tile;
   if (!chunk) {
     // two CTAs per SM share all key tiles evenly; fewer when there are not enough tiles for that
-    pl.min_split_tiles = 1;
     pl.whole_items = tiles <= 2;
-    const int64_t all = std::max<int64_t>(tiles, 1) * d.heads_kv * d.batch;
-    pl.splits = (int)std::min<int64_t>(2 * kSms, std::max<int64_t>(all / pl.min_split_tiles, 1));
+    const int64_t all = std::max<int64_t>(tiles, 1) * d.heads_kv * d.batch;  // (not 0: an empty batch launches nothing)
+    pl.splits = (int)std::min<int64_t>(2 * kSms, all);
     return pl;
   }
   // One or four CTAs per SM, and splits only to fill the SMs, none below min_split_tiles.

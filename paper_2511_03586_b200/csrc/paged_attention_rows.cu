@@ -62,7 +62,7 @@ __device__ __forceinline__ bool first_piece(const Params& p, int cta, Piece& w, 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int found_b, found_base, total;
   auto deal = [&]() {
-    share = max((total + (int)gridDim.x - 1) / (int)gridDim.x, p.min_split_tiles);
+    share = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 1);
     const int64_t at = (int64_t)cta * share;
     start = (int)min(at, (int64_t)total);
     stop = (int)min(at + share, (int64_t)total);

@@ -32,7 +32,7 @@ struct Params {
   // more than max_q_len for each sequence, that many places a sequence.
   int part_tokens, part_by_sequence;
   int splits;           // of the keys of every row tile (chunk kernel), CTAs in all (row kernel)
-  int min_split_tiles;  // the smallest share of key tiles
+  int min_split_tiles;  // the smallest share of key tiles (chunk kernel)
   int whole_items;      // row kernel: no item is shared out (short contexts: nothing to join)
   float scale_log2e;
 };

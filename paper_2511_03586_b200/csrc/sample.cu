@@ -25,8 +25,9 @@
 // HBM-bound in principle: the logits are read once, 4 (or 2) bytes each, and held in the shared memory of a cluster of
 // 1 to 8 CTAs (distributed by contiguous slices, so that index order is slice order).  In fact the passes over shared
 // memory, the double-precision exponentials (eight operations each) and the cluster's barriers weigh more: 256 x 128000
-// fp32 logits with top-p take 177 us, 20 of which the bytes need; stopped after the maximum, 43; after the cut's bins are
-// known, about 80; after the exact sums, 156.  CTAs of 256 threads and 128 registers take 202 us (against 184 then).
+// fp32 logits with top-p take 180 us, 20 of which the bytes need; stopped after the maximum, 43; after the cut's bins are
+// known, about 80; after the exact sums, 156 (the last three of a launch of 177).  CTAs of 256 threads and 128 registers take
+// 202 us (against 184 then).  Two CTAs fit an SM up to vocabularies of about 145800; 151936 logits take 274 us.
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -544,9 +545,10 @@ __device__ void locate_rank(Shared& sh, uint32_t rank) {
 // The logits of bin b lie within half a bin (and the rounding of bin()) of z = b / 64, so counts bound both sums from below
 // and above: sh.found_bin is the first bin where the condition may hold, sh.found_bin2 the first where it must.
 //
-// Single precision will do: the sums are off by 2^-18 of themselves at most (40 additions and products of positive terms,
-// expf to 1e-6 besides), which the factors' margins hold.  Sums run from the far end, so that a small suffix, which a
-// top_p near 1 is decided by, is not a difference of large numbers.
+// Single precision will do: the sums are off by 2^-18 of themselves at most (40 additions and products of positive terms),
+// and a term by what __expf is, 2 + 1.173 x steps at most, 39 or 5e-6 of itself at x = 32.  The terms' factors leave room for
+// both: they are 8e-5 (lower) and 1.7e-4 (upper) away from the bounds they stand for.  Sums run from the far end, so that a
+// small suffix, which a top_p near 1 is decided by, is not a difference of large numbers.
 __device__ void locate_weight(Shared& sh, float top_p, int vocab) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   float lo[kEach], hi[kEach], lo_sum = 0.f, hi_sum = 0.f;
@@ -889,9 +891,7 @@ __device__ void slow_path(cg::cluster_group& cluster, const SampleParams& p, Sha
     }
     return;
   }
-  float u = __ldg(p.u + i_row);
-  u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;  // NaN: 0
-  const u64 target = __umul64hi(total, (u64)((double)u * 18446744073709551616.0));  // floor(u * total) < total
+  const u64 target = draw_target(p, i_row, total);
   for (int w = 0; w < warp; ++w) {
     const uint32_t kept = equal_before >= cut.ties ? 0 : min(sh.warp_count[w], cut.ties - equal_before);
     before += sh.warp_weight[w] + kept * each;
