@@ -147,8 +147,14 @@ __device__ __forceinline__ unsigned cluster_size() {
 // A CTA's shared memory may be accessed from another only once it is known to run: every thread of the cluster arrives
 // first thing in the kernel, and waits in front of the first remote access (what lies between hides the barrier).
 // Orders what the CTAs wrote to their own shared memory before the arrival, too.
-__device__ __forceinline__ void cluster_started_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_started_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_started_arrive() {
+  __syncwarp();  // (the aligned forms want whole warps)
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_started_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // All-reduce over the cluster of one value per CTA (`v`, identical in all threads of the CTA): thread k writes it
 // into slot [own rank] of CTA k's exchange array, a cluster barrier (release / acquire) publishes the writes,
 // and everyone combines the slots in rank order.  `xchg`: 8 floats of shared memory used by no other reduction.

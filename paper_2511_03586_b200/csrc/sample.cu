@@ -941,7 +941,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows_cluster(const SampleP
   sh.table[threadIdx.x] = kPowers.v[threadIdx.x];
   for (int i = threadIdx.x; i < kBins / 2; i += kThreads) sh.fast.hist[i] = 0;
   if (threadIdx.x == 0) { sh.candidates = sh.own_candidates = 0; sh.first_max = 0xffffffffu; }
-  __syncwarp();
   cluster_started_arrive();
   griddep_wait();
   griddep_launch_dependents();
