@@ -19,8 +19,8 @@
  *    launch that failed, with earlier kernels already on the stream: after
  *    PD_ERR_CUDA from them, y and the workspace hold unspecified values.
  *  - PD_OK means "enqueued".  The tensor-core entry points (pd_gemm_*,
- *    pd_swiglu_gemm, pd_attention_fwd, pd_attention_paged_fwd, the layer and
- *    stack calls) and pd_norm_gate_residual_norm (which prefetches long runs of
+ *    pd_swiglu_gemm, pd_attention_fwd, pd_attention_paged_fwd,
+ *    pd_attention_paged_q8_fwd, the layer and stack calls) and pd_norm_gate_residual_norm (which prefetches long runs of
  *    rows) bound every wait inside their kernels; a kernel whose wait ran out
  *    returns early and
  *    leaves a code in the device status word, so their results are valid only
@@ -61,7 +61,9 @@ typedef enum {
   PD_ERR_DEVICE_TIMEOUT = 7
 } pd_status;
 
-typedef enum { PD_BF16 = 0, PD_F32 = 1 } pd_dtype;
+/* PD_I8 and PD_E4M3 (8-bit floats of 4 exponent and 3 mantissa bits) are types of paged caches; every other
+ * argument of type pd_dtype is PD_BF16 or PD_F32. */
+typedef enum { PD_BF16 = 0, PD_F32 = 1, PD_I8 = 2, PD_E4M3 = 3 } pd_dtype;
 
 /* Human-readable name of a status; static storage, never null. */
 const char* pd_status_string(pd_status status);
@@ -84,7 +86,7 @@ pd_status pd_clear_device_status(void);
  * reported, it does not take the system down).
  * pd_debug_set_wait_limit_ns: the time after which a wait inside the single-CTA
  * and the CTA-pair contraction kernels (pd_set_gemm_tile_mode(1) / (2)), the
- * kernels of pd_attention_paged_fwd and the one of pd_norm_gate_residual_norm
+ * kernels of pd_attention_paged_fwd and pd_attention_paged_q8_fwd and the one of pd_norm_gate_residual_norm
  * that prefetches rows gives up, 1 us to 10 s (else PD_ERR_BAD_SHAPE); default 2 s.
  * pd_debug_withhold_loads(1): those kernels' producers issue no load, so the
  * warp that feeds the tensor core waits for its first operand stage in vain,
@@ -461,6 +463,72 @@ pd_status pd_attention_paged_fwd(const pd_paged_attention_desc* desc, const void
                                  const int32_t* kv_len, void* out, void* workspace, size_t workspace_bytes,
                                  cudaStream_t stream);
 
+/* ---- the same cache in 8 bits, and the rotation of what goes into it ----
+ * An 8-bit cache has the layout of the bf16 one, in elements of one byte (its strides
+ * are then multiples of 16), and a scale for every block of `block` tokens of a head:
+ * element (page, slot, head, d) stands for
+ *   cache[page, slot, head, d] * scale[page, head, slot / block].
+ * block: a power of two that divides page_size.  k_scale, v_scale: fp32 [num_pages,
+ * heads_kv, page_size / block], dense.  Scales are not negative. */
+typedef struct {
+  pd_dtype dtype; /* of both caches: PD_I8 or PD_E4M3 */
+  int32_t block;
+  float *k_scale, *v_scale; /* written by the append, read by the attention */
+} pd_cache_scales;
+
+/* Rotation of a head's first rotary_dim elements by the token's position p in its
+ * sequence: with theta_i = p * inv_freq[i], i < rotary_dim / 2, pair i = (a, b) becomes
+ *   amplitude * (a cos theta_i - b sin theta_i, a sin theta_i + b cos theta_i).
+ * Angles are formed in 64 bits, so far positions are as exact as near ones. */
+typedef struct {
+  int32_t rotary_dim;    /* a multiple of 8, at most head_dim; 0: nothing is rotated */
+  int32_t interleaved;   /* pair i: elements 2i and 2i + 1 (1), or i and i + rotary_dim / 2 (0) */
+  float amplitude;       /* usually 1 */
+  const float* inv_freq; /* device, fp32 [rotary_dim / 2] */
+} pd_rope_desc;
+
+/* pd_kv_cache_append with the rotation on the way, into a bf16 or an 8-bit cache:
+ *   q_out[t, h, :] = R_p q[t, h, :],  K[p] = R_p k_new[t],  V[p] = v_new[t]
+ * for position p of token t (as in pd_kv_cache_append).  desc: batch, tokens, heads_q,
+ * heads_kv, head_dim (a multiple of 8, at most 256), num_pages, page_size, max_pages,
+ * ld_q (of q), ld_out (of q_out) and the cache strides are used, the rest is ignored.
+ * q, q_out: bf16 [tokens, heads_q, head_dim], q_out may be q (with ld_out == ld_q);
+ * both NULL: keys and values only.  k_new, v_new, ld_new: as in pd_kv_cache_append.
+ *  - scales == NULL: bf16 caches; results are rounded once.
+ *  - else 8-bit caches.  For every block and head that gets new tokens, with m the
+ *    largest magnitude of these tokens' (rotated) elements and Q = 127 (PD_I8) or 448
+ *    (PD_E4M3): scale = m / Q, or the scale that is there if that is larger and the
+ *    block holds tokens in front of the new ones already.  Where it grew, the older
+ *    tokens' elements e become round(e * old / new); the new ones' are round(x / scale),
+ *    both to nearest, ties to even.  So a block that is filled token by token has lost at
+ *    most half a step of its last scale for every time that it grew, and one that is
+ *    written at once half a step.  A block whose older tokens several sequences share
+ *    (a common prefix) has to be copied first.  m / Q below 2^-126 counts as 2^-126.
+ *  - Rows behind the last sequence, and tokens whose position lies in front of 0, are left
+ *    as they were in q_out and the caches; tokens without a place in the cache (beyond
+ *    max_pages, or on a page outside [0, num_pages)) in the caches only, and they do
+ *    not count for a scale.  New elements have to be finite, rotated too.
+ * At most 2^30 tokens, 65535 sequences, 65536 heads (else PD_ERR_UNSUPPORTED); pointers
+ * 16-byte aligned (inv_freq, scales and the int32 arrays 4-byte), strides multiples of 8
+ * elements (of an 8-bit cache: 16), else PD_ERR_ALIGNMENT.  tokens = 0 or batch = 0 is a no-op. */
+pd_status pd_rope_kv_cache_append(const pd_paged_attention_desc* desc, const pd_rope_desc* rope,
+                                  const pd_cache_scales* scales, const void* q, void* q_out, const void* k_new,
+                                  const void* v_new, int64_t ld_new, void* k_cache, void* v_cache,
+                                  const int32_t* block_table, const int32_t* cu_q, const int32_t* kv_len,
+                                  cudaStream_t stream);
+
+/* pd_attention_paged_fwd over an 8-bit cache:
+ *   out[t, h] = sum_j softmax_j(scale * ks_j * (q[t, h] . k[j])) * vs_j * v[j]
+ * with k[j], v[j] the stored elements and ks_j, vs_j the scales of their blocks.  Arguments,
+ * limits, errors, workspace and what may lie in slots and entries out of view as there;
+ * scales out of view may be anything, too.  The dequantised keys and values that a query
+ * sees have to be finite. */
+size_t pd_attention_paged_q8_workspace_bytes(const pd_paged_attention_desc* desc);
+pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* desc, const pd_cache_scales* scales, const void* q,
+                                    const void* k_cache, const void* v_cache, const int32_t* block_table,
+                                    const int32_t* cu_q, const int32_t* kv_len, void* out, void* workspace,
+                                    size_t workspace_bytes, cudaStream_t stream);
+
 /* What stands between two blocks of a layer, in one pass over memory (operators
  * "rmsnorm", "layernorm", "add"): the norm after the block that produced y, its
  * gate, the scaled residual sum, and the norm before the next block:
@@ -516,6 +584,41 @@ pd_status pd_norm_gate_residual_norm(const pd_norm_gate_residual_desc* desc, con
 pd_status pd_sample(const void* logits, pd_dtype dtype, int64_t rows, int64_t vocab, int64_t ld,
                     const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                     const float* u, int32_t* tokens, float* probs, cudaStream_t stream);
+
+/* What is done to logits before a token is drawn from them, in one pass: for row i and
+ * token j, with n the number of times that j occurs in row i's history behind its prompt,
+ *   z = logits[i,j]
+ *   z = z > 0 ? z / repetition[i] : z * repetition[i]   if j occurs in the history at all
+ *   z = z - frequency[i] * n - presence[i]              if n > 0
+ *   z = z + bias                                        if row i's bias list names j
+ *   out[i,j] = z, or -inf where row i's mask forbids j.
+ *  - history: int32 [rows, history_cols] with ld_history elements from row to row, or NULL:
+ *    the first history_len[i] entries of row i (taken into [0, history_cols]; NULL: all),
+ *    of which the first prompt_len[i] are the prompt (NULL: none).  Entries outside
+ *    [0, vocab) do not count.
+ *  - repetition, frequency, presence: fp32 [rows], or NULL for none.  A repetition that is
+ *    not positive and finite counts as 1.
+ *  - bias_tokens (int32), bias_values (fp32): [rows, bias_cols], dense.  Entries whose token
+ *    lies outside [0, vocab) do not count; of several for one token the last does.  -inf is
+ *    a value like any other.  bias_cols = 0: none.
+ *  - mask: bits, 32 tokens to a word from the lowest bit on, [mask_rows, ld_mask words]; a
+ *    set bit allows the token.  NULL: all are allowed.  mask_row: int32 [rows], the row of
+ *    the mask that holds for row i; outside [0, mask_rows): all tokens are allowed.
+ *    NULL: row i (mask_rows at least rows, else PD_ERR_BAD_SHAPE).
+ * logits: [rows, vocab] of dtype, out: of out_dtype, aligned to their elements; out may
+ * be logits (same type and stride).  Arithmetic is fp32, out is rounded once.
+ * vocab at most 2^24, history_cols below 2^20, bias_cols at most 2047 (else
+ * PD_ERR_UNSUPPORTED).  rows = 0 is a no-op. */
+typedef struct {
+  int64_t rows, vocab, ld_logits, ld_out;
+  pd_dtype dtype, out_dtype;
+  int64_t history_cols, ld_history, bias_cols, mask_rows, ld_mask;
+} pd_penalize_desc;
+pd_status pd_penalize_logits(const pd_penalize_desc* desc, const void* logits, void* out, const int32_t* history,
+                             const int32_t* history_len, const int32_t* prompt_len, const float* repetition,
+                             const float* frequency, const float* presence, const int32_t* bias_tokens,
+                             const float* bias_values, const uint32_t* mask, const int32_t* mask_row,
+                             cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libpd.so")
 
 PD_OK = 0
-PD_BF16, PD_F32 = 0, 1
+PD_BF16, PD_F32, PD_I8, PD_E4M3 = 0, 1, 2, 3
 
 EXPORTS = (
     "pd_status_string", "pd_last_cuda_error", "pd_get_device_status", "pd_clear_device_status",
@@ -27,7 +27,8 @@ EXPORTS = (
     "pd_encoder_layer_workspace_bytes", "pd_encoder_layer_workspace_layout", "pd_encoder_layer_fwd", "pd_encoder_layer_stage_count",
     "pd_encoder_layer_stage_name", "pd_encoder_layer_fwd_profiled", "pd_encoder_layer_static_scratch_bytes",
     "pd_encoder_layer_fwd_static", "pd_kv_cache_append", "pd_attention_paged_workspace_bytes",
-    "pd_attention_paged_fwd", "pd_norm_gate_residual_norm", "pd_sample",
+    "pd_attention_paged_fwd", "pd_norm_gate_residual_norm", "pd_sample", "pd_rope_kv_cache_append",
+    "pd_attention_paged_q8_workspace_bytes", "pd_attention_paged_q8_fwd", "pd_penalize_logits",
 )
 
 
@@ -61,6 +62,21 @@ class NormGateResidualDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("rows", "cols", "gate_rows")] + [
         (n, ctypes.c_int32) for n in ("x_dtype", "y_dtype", "post_norm", "pre_norm")] + [
             (n, ctypes.c_float) for n in ("alpha", "eps")]
+
+
+class CacheScales(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("block", ctypes.c_int32), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float),
+                ("inv_freq", ctypes.c_void_p)]
+
+
+class PenalizeDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "vocab", "ld_logits", "ld_out")] + [
+        (n, ctypes.c_int32) for n in ("dtype", "out_dtype")] + [
+            (n, ctypes.c_int64) for n in ("history_cols", "ld_history", "bias_cols", "mask_rows", "ld_mask")]
 
 
 def _load() -> ctypes.CDLL:
@@ -126,6 +142,14 @@ def _load() -> ctypes.CDLL:
     lib.pd_norm_gate_residual_norm.restype = st
     lib.pd_sample.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.pd_sample.restype = st
+    lib.pd_rope_kv_cache_append.argtypes = [vp] * 7 + [i64] + [vp] * 6
+    lib.pd_rope_kv_cache_append.restype = st
+    lib.pd_attention_paged_q8_workspace_bytes.argtypes = [vp]
+    lib.pd_attention_paged_q8_workspace_bytes.restype = ctypes.c_size_t
+    lib.pd_attention_paged_q8_fwd.argtypes = [vp] * 10 + [ctypes.c_size_t, vp]
+    lib.pd_attention_paged_q8_fwd.restype = st
+    lib.pd_penalize_logits.argtypes = [vp] * 14
+    lib.pd_penalize_logits.restype = st
     return lib
 
 
@@ -518,7 +542,10 @@ _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 # The descs' fields, packed as C lays them out (half the time of filling a structure, and values beyond a field's 32 bits
 # raise instead of losing their upper half).
 _PAGED_DESC, _NORM_DESC = struct.Struct("@12if5q"), struct.Struct("@3q4i2f")
+_SCALES_DESC, _ROPE_DESC, _PENALIZE_DESC = struct.Struct("@2i2P"), struct.Struct("@2ifP"), struct.Struct("@4q2i5q")
 assert _PAGED_DESC.size == ctypes.sizeof(PagedAttentionDesc) and _NORM_DESC.size == ctypes.sizeof(NormGateResidualDesc)
+assert (_SCALES_DESC.size == ctypes.sizeof(CacheScales) and _ROPE_DESC.size == ctypes.sizeof(RopeDesc)
+        and _PENALIZE_DESC.size == ctypes.sizeof(PenalizeDesc))
 
 
 def _pack(layout: struct.Struct, *values) -> bytes:
@@ -539,9 +566,9 @@ def _token_stride(t: torch.Tensor, name: str) -> int:
     return token_stride if tokens > 1 else heads * d
 
 
-def _paged_cache(device: int, k_cache, v_cache, block_table, cu_q, kv_len):
+def _paged_cache(device: int, k_cache, v_cache, block_table, cu_q, kv_len, dtype=_BF16):
     """The cache's extents (as the desc has them), its strides, and the addresses of the five tensors."""
-    kc, vc = _on(device, k_cache, _BF16, "k_cache", False), _on(device, v_cache, _BF16, "v_cache", False)
+    kc, vc = _on(device, k_cache, dtype, "k_cache", False), _on(device, v_cache, dtype, "v_cache", False)
     table, cu, lens = _on(device, block_table, _I32, "block_table"), _on(device, cu_q, _I32, "cu_q"), _on(device, kv_len, _I32, "kv_len")
     shape, strides, other = k_cache.shape, k_cache.stride(), v_cache.stride()
     if len(shape) != 4 or v_cache.shape != shape:
@@ -708,3 +735,166 @@ def pd_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None
             raise ValueError(f"{name} must have one value per row")
     _call(_lib.pd_sample, device, stream, lp, code, rows, vocab, logits.stride(0) if rows > 1 else vocab, *ptrs)
     return tokens, probs
+
+
+_Q8_DTYPES = {torch.int8: PD_I8, torch.float8_e4m3fn: PD_E4M3}
+
+
+def _q8_type(k_cache) -> int:
+    code = _Q8_DTYPES.get(getattr(k_cache, "dtype", None))
+    if code is None:
+        raise TypeError("k_cache must be torch.int8 or torch.float8_e4m3fn")
+    return code
+
+
+def _cache_scales(device: int, code: int, k_scale, v_scale, num_pages: int, page_size: int, heads: int) -> bytes:
+    """The scales' desc; the block of tokens follows from the shape."""
+    kp, vp = _on(device, k_scale, _F32, "k_scale"), _on(device, v_scale, _F32, "v_scale")
+    if kp is None or vp is None:
+        raise TypeError("an 8-bit cache needs k_scale and v_scale")
+    shape = k_scale.shape
+    if len(shape) != 3 or shape[0] != num_pages or shape[1] != heads or shape[2] < 1 or page_size % shape[2] or v_scale.shape != shape:
+        raise ValueError("k_scale and v_scale must be [pages, heads_kv, page_size / block]")
+    return _pack(_SCALES_DESC, code, page_size // shape[2], kp, vp)
+
+
+def pd_rope_kv_cache_append(k_new, v_new, k_cache, v_cache, block_table, cu_q, kv_len, *, q=None, q_out=None, inv_freq=None,
+                            interleaved: bool = False, amplitude: float = 1.0, k_scale=None, v_scale=None, stream=None):
+    """Rotates the new tokens' queries and keys by their positions (``inv_freq``: fp32, one for each pair of the leading
+    elements of a head; None: no rotation) and appends keys and values to the caches, as pd_kv_cache_append does.  Caches of
+    torch.int8 or torch.float8_e4m3fn take ``k_scale`` and ``v_scale`` (fp32 [pages, heads_kv, page_size / block]), which are
+    brought up to date.  ``q`` (bf16 [tokens, heads_q, head_dim]) goes to ``q_out``, which may be q; returns q_out, None
+    without q."""
+    device = _device(k_new, "k_new")
+    quantised = k_scale is not None or v_scale is not None
+    code = _q8_type(k_cache) if quantised else 0
+    (batch, heads, head_dim, num_pages, page_size, max_pages), strides, (kc, vc, table, cu, lens) = _paged_cache(
+        device, k_cache, v_cache, block_table, cu_q, kv_len, k_cache.dtype if quantised else _BF16)
+    scales = _cache_scales(device, code, k_scale, v_scale, num_pages, page_size, heads) if quantised else None
+    k, v = _on(device, k_new, _BF16, "k_new", False), _on(device, v_new, _BF16, "v_new", False)
+    ld = _token_stride(k_new, "k_new")
+    tokens, new_heads, d = k_new.shape
+    if new_heads != heads or d != head_dim or v_new.shape != k_new.shape:
+        raise ValueError("k_new and v_new must be [tokens, heads_kv, head_dim]")
+    if v_new.stride() != k_new.stride() and ld != _token_stride(v_new, "v_new"):
+        raise ValueError("k_new and v_new must have the same token stride")
+    qp = op = None
+    heads_q = ld_q = ld_out = 0
+    if q is not None:
+        qp, ld_q = _on(device, q, _BF16, "q", False), _token_stride(q, "q")
+        q_tokens, heads_q, d = q.shape
+        if q_tokens != tokens or d != head_dim:
+            raise ValueError("q must be [tokens, heads_q, head_dim]")
+        if q_out is None:
+            q_out = _new(q, stream)
+            op, ld_out = q_out.data_ptr(), heads_q * head_dim
+        else:
+            op, ld_out = _on(device, q_out, _BF16, "q_out", False), _token_stride(q_out, "q_out")
+            if q_out.shape != q.shape:
+                raise ValueError("q_out must have the shape of q")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    freq = _on(device, inv_freq, _F32, "inv_freq")
+    rope = _pack(_ROPE_DESC, 0 if inv_freq is None else 2 * inv_freq.numel(), bool(interleaved), amplitude, freq or 0)
+    desc = _pack(_PAGED_DESC, batch, tokens, heads_q, heads, head_dim, num_pages, page_size, max_pages, 0, 0, 0, 0, 0.0,
+                 ld_q, ld_out, *strides)
+    _call(_lib.pd_rope_kv_cache_append, device, stream, desc, rope, scales, qp, op, k, v, ld, kc, vc, table, cu, lens)
+    return q_out
+
+
+def pd_attention_paged_q8_workspace_bytes(desc: PagedAttentionDesc) -> int:
+    return int(_lib.pd_attention_paged_q8_workspace_bytes(ctypes.byref(desc)))
+
+
+def pd_attention_paged_q8_fwd(q, k_cache, v_cache, k_scale, v_scale, block_table, cu_q, kv_len, *, max_q_len: int,
+                              max_kv_len: int, window: int = 0, sinks: int = 0, scale: float | None = None, out=None,
+                              workspace=None, stream=None) -> torch.Tensor:
+    """pd_attention_paged_fwd over caches of torch.int8 or torch.float8_e4m3fn, whose elements stand for themselves times
+    ``k_scale`` and ``v_scale`` (fp32 [pages, heads_kv, page_size / block])."""
+    device = _device(q, "q")
+    code = _q8_type(k_cache)
+    (batch, heads_kv, head_dim, num_pages, page_size, max_pages), strides, (kc, vc, table, cu, lens) = _paged_cache(
+        device, k_cache, v_cache, block_table, cu_q, kv_len, k_cache.dtype)
+    scales = _cache_scales(device, code, k_scale, v_scale, num_pages, page_size, heads_kv)
+    qp, ld_q = _on(device, q, _BF16, "q", False), _token_stride(q, "q")
+    tokens, heads_q, d = q.shape
+    if d != head_dim:
+        raise ValueError("q and the caches must have the same head_dim")
+    if out is None:
+        out = _new(q, stream)
+        op, ld_out = out.data_ptr(), heads_q * head_dim
+    else:
+        op, ld_out = _on(device, out, _BF16, "out", False), _token_stride(out, "out")
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    desc = _pack(_PAGED_DESC, batch, tokens, heads_q, heads_kv, head_dim, num_pages, page_size, max_pages, max_q_len, max_kv_len,
+                 window, sinks, head_dim ** -0.5 if scale is None else scale, ld_q, ld_out, *strides)
+    if workspace is None:
+        ws_bytes = _lib.pd_attention_paged_q8_workspace_bytes(desc)
+        workspace = _new(q, stream, ws_bytes, torch.uint8) if ws_bytes else None
+        ws = workspace.data_ptr() if ws_bytes else None
+    else:
+        ws, ws_bytes = _on(device, workspace, torch.uint8, "workspace"), workspace.numel()
+    _call(_lib.pd_attention_paged_q8_fwd, device, stream, desc, scales, qp, kc, vc, table, cu, lens, op, ws, ws_bytes)
+    return out
+
+
+def _row_stride(t, name: str) -> int:
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be two-dimensional with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def pd_penalize_logits(logits, *, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None,
+                       presence=None, bias_tokens=None, bias_values=None, mask=None, mask_row=None, out=None, stream=None):
+    """Penalties for repeated tokens, biases and masks on logits (bf16 or fp32 [rows, vocab], rows of any stride), which
+    pd_sample draws from; returns ``out`` (by default a new tensor like logits; it may be logits, or of the other type).
+
+    history: int32 [rows, columns], the tokens of the prompt (the first ``prompt_len`` of a row) and of the answer so far, of
+    which ``history_len`` are there; repetition, frequency, presence: fp32 [rows]; bias_tokens int32, bias_values fp32: [rows,
+    entries]; mask: int32 [mask rows, ceil(vocab / 32) or more], set bits are allowed, ``mask_row`` (int32 [rows]) names a row's
+    mask, -1 for none.  None switches any of them off."""
+    device = _device(logits, "logits")
+    code, lp, ld = _float_type(logits, "logits"), logits.data_ptr(), _row_stride(logits, "logits")
+    rows, vocab = logits.shape
+    if out is None:
+        out = _new(logits, stream)
+        out_code, op, ld_out = code, out.data_ptr(), vocab
+    else:
+        out_code, op, ld_out = _float_type(out, "out"), _on(device, out, out.dtype, "out", False), _row_stride(out, "out")
+        if out.shape != logits.shape:
+            raise ValueError("out must have the shape of logits")
+    history_cols = ld_history = 0
+    hp = _on(device, history, _I32, "history", False)
+    if history is not None:
+        ld_history = _row_stride(history, "history")
+        if history.shape[0] != rows:
+            raise ValueError("history must have a row for each row of logits")
+        history_cols = history.shape[1]
+    elif history_len is not None or prompt_len is not None:
+        raise ValueError("history_len and prompt_len need a history")
+    ptrs = []
+    for name, t, dtype in (("history_len", history_len, _I32), ("prompt_len", prompt_len, _I32), ("repetition", repetition, _F32),
+                           ("frequency", frequency, _F32), ("presence", presence, _F32)):
+        ptrs.append(_on(device, t, dtype, name))
+        if t is not None and t.numel() != rows:
+            raise ValueError(f"{name} must have one value per row")
+    bt, bv = _on(device, bias_tokens, _I32, "bias_tokens"), _on(device, bias_values, _F32, "bias_values")
+    bias_cols = 0
+    if bias_tokens is not None or bias_values is not None:
+        if bias_tokens is None or bias_values is None or bias_tokens.dim() != 2 or bias_tokens.shape[0] != rows or bias_values.shape != bias_tokens.shape:
+            raise ValueError("bias_tokens and bias_values must be [rows, entries]")
+        bias_cols = bias_tokens.shape[1]
+    mp, mr = _on(device, mask, _I32, "mask", False), _on(device, mask_row, _I32, "mask_row")
+    mask_rows = ld_mask = 0
+    if mask is not None:
+        ld_mask, mask_rows = _row_stride(mask, "mask"), mask.shape[0]
+        if mask.shape[1] * 32 < vocab:
+            raise ValueError("mask must have a bit for every token")
+        if mask_row is None and mask_rows < rows:
+            raise ValueError("mask must have a row for each row of logits")
+    if mask_row is not None and (mask is None or mask_row.numel() != rows):
+        raise ValueError("mask_row needs a mask, and one value per row")
+    desc = _pack(_PENALIZE_DESC, rows, vocab, ld, ld_out, code, out_code, history_cols, ld_history, bias_cols, mask_rows, ld_mask)
+    _call(_lib.pd_penalize_logits, device, stream, desc, lp, op, hp, *ptrs, bt, bv, mp, mr)
+    return out

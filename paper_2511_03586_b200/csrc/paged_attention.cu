@@ -60,25 +60,6 @@ struct Plan {
   bool whole_items;
 };
 
-// The scale of scores as powers of two, which the kernels compute with.
-float base2_scale(float scale) { return (float)((double)scale * 1.4426950408889634); }
-
-constexpr int kMaxPositions = 1 << 30;  // of a sequence's table, and rows of a cache head: sums of two stay in 32 bits
-
-bool valid(const pd_paged_attention_desc& d) {
-  return d.batch >= 0 && d.tokens >= 0 && d.heads_q > 0 && d.heads_kv > 0 && d.head_dim > 0 &&
-         d.heads_q % d.heads_kv == 0 && d.num_pages > 0 && d.page_size > 0 && d.max_pages > 0 && d.max_q_len >= 0 &&
-         d.max_kv_len >= 0 && d.window >= 0 && d.sinks >= 0 && std::isfinite(base2_scale(d.scale)) && d.scale > 0.f;
-}
-bool supported(const pd_paged_attention_desc& d) {
-  return (d.head_dim == 64 || d.head_dim == 128) && d.heads_q / d.heads_kv <= 64 && d.page_size >= 8 &&
-         (int64_t)d.tokens * d.heads_q <= 0x7fffffff &&
-         d.page_size <= 4096 && (d.page_size & (d.page_size - 1)) == 0 &&
-         (int64_t)d.max_pages * d.page_size <= kMaxPositions && (int64_t)d.tokens * (d.heads_q / d.heads_kv) <= kMaxPositions &&
-         (int64_t)d.batch * d.heads_kv * (((int64_t)d.max_pages * d.page_size + 63) / 64) <= kMaxPositions && d.batch <= 65535 &&
-         d.heads_kv <= 65535;
-}
-
 // Depends on the desc alone (the workspace size follows from it).
 Plan plan(const pd_paged_attention_desc& d) {
   constexpr int kSms = 148;  // (not asked of the device: the workspace follows from the desc alone)

@@ -3,6 +3,8 @@
 // Internal to the library.
 #pragma once
 
+#include <cmath>
+
 #include "gemm_common.cuh"
 
 namespace pd {
@@ -143,6 +145,26 @@ inline bool make_cache_map(CUtensorMap* map, const void* cache, const pd_paged_a
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(cache), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// ---- argument checks of the attention over the cache
+// The scale of scores as powers of two, which the kernels compute with.
+inline float base2_scale(float scale) { return (float)((double)scale * 1.4426950408889634); }
+
+constexpr int kMaxPositions = 1 << 30;  // of a sequence's table, and rows of a cache head: sums of two stay in 32 bits
+
+inline bool valid(const pd_paged_attention_desc& d) {
+  return d.batch >= 0 && d.tokens >= 0 && d.heads_q > 0 && d.heads_kv > 0 && d.head_dim > 0 &&
+         d.heads_q % d.heads_kv == 0 && d.num_pages > 0 && d.page_size > 0 && d.max_pages > 0 && d.max_q_len >= 0 &&
+         d.max_kv_len >= 0 && d.window >= 0 && d.sinks >= 0 && std::isfinite(base2_scale(d.scale)) && d.scale > 0.f;
+}
+inline bool supported(const pd_paged_attention_desc& d) {
+  return (d.head_dim == 64 || d.head_dim == 128) && d.heads_q / d.heads_kv <= 64 && d.page_size >= 8 &&
+         (int64_t)d.tokens * d.heads_q <= 0x7fffffff &&
+         d.page_size <= 4096 && (d.page_size & (d.page_size - 1)) == 0 &&
+         (int64_t)d.max_pages * d.page_size <= kMaxPositions && (int64_t)d.tokens * (d.heads_q / d.heads_kv) <= kMaxPositions &&
+         (int64_t)d.batch * d.heads_kv * (((int64_t)d.max_pages * d.page_size + 63) / 64) <= kMaxPositions && d.batch <= 65535 &&
+         d.heads_kv <= 65535;
 }
 
 // Launchers (each in its own file).  `rows_per_tile` of the row kernel: 16, 32 or 64.

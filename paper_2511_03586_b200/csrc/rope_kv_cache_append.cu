@@ -1,0 +1,431 @@
+// Rotates the new tokens' queries and keys by their positions and appends keys and values to the paged cache, as bf16 or
+// in 8 bits with a scale for each block of tokens and head:
+//
+//   theta_i = p * inv_freq[i],   (a, b) -> amplitude * (a cos theta_i - b sin theta_i, a sin theta_i + b cos theta_i)
+//
+// for the pairs (a, b) = (x[i], x[i + R/2]) or, interleaved, (x[2i], x[2i + 1]) of a head's first R elements.
+//
+// Angles: far positions make p * inv_freq as large as 10^6 radians, where fp32 keeps two digits of the angle.  The number of
+// turns p * inv_freq / 2 pi is formed in 64 bits (p has 31 bits, inv_freq 24: off by 2^-52 of itself), its whole part dropped,
+// and the rest, at most half a turn, goes through sincospif.  A warp does that once per token for all its heads.
+//
+// Bound: HBM for prompts.  Every element of q, k and v is read once and written once (the rotation is 6 operations on 4 bytes);
+// a decode batch is one launch and a chain of four dependent loads.
+//
+// The 8-bit cache: a block's scale is its largest magnitude over the top of the type, so all of its new tokens have to be seen
+// before the first is rounded.  A CTA takes one block of one sequence, a warp one head of K or V of it: the warp's share is held
+// in registers between the two passes as long as it has at most 512 units of 8 elements (32 tokens of 128), and read again, from
+// the L2 cache, beyond that.  Values are rounded once, from the rotated fp32 ones.  A block that held older tokens keeps its scale
+// unless a new token exceeds it; then the older values are rounded again, to the larger step.
+#include "cache_q8.cuh"
+
+namespace pd {
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kUnit = 8;         // elements that one lane handles at a time: four pairs, or eight elements that are not rotated
+constexpr int kHeld = 16;        // units a lane holds between the passes of the 8-bit form
+constexpr int kGroup = 32 * kHeld;
+constexpr int kMaxDim = 256;
+constexpr int kMaxPairs = kMaxDim / 2;
+constexpr int kMaxIndex = 1 << 30;
+
+struct RopeParams {
+  const __nv_bfloat16 *q, *k_new, *v_new;
+  __nv_bfloat16* q_out;
+  uint8_t *k_cache, *v_cache;
+  float *k_scale, *v_scale;
+  const float* inv_freq;
+  const int32_t *block_table, *cu_q, *kv_len;
+  int64_t ld_q, ld_q_out, ld_new, page_stride, slot_stride, head_stride;  // in elements
+  paged::Scales scales;
+  float amplitude;
+  int rotary, interleaved;
+  int batch, tokens, heads_q, heads_kv, head_dim;
+  int num_pages, page_size, max_pages;
+  int parts;           // warps that share a token
+  int rounds;          // 8-bit form: CTAs that share a block, each up to kWarps heads of K or of V
+  int64_t block_ctas;  // 8-bit form: CTAs in front of the ones that rotate queries
+};
+
+// cos and sin of position `pos` times inv_freq[i], times the amplitude.
+__device__ __forceinline__ float2 turn_of(const RopeParams& p, int pos, int i) {
+  const double turns = (double)pos * (double)__ldg(p.inv_freq + i) * 0.15915494309189533577;  // 1 / 2 pi
+  float s, c;
+  sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+  return make_float2(c * p.amplitude, s * p.amplitude);
+}
+
+// Unit u of a head: its eight elements lie at `first` and, for split pairs, four at each of `first` and `second`.
+struct Place {
+  int first, second;
+  bool rotated, split;
+};
+__device__ __forceinline__ Place place_of(const RopeParams& p, int u) {
+  Place at;
+  at.rotated = u * kUnit < p.rotary;
+  at.split = at.rotated && !p.interleaved;
+  at.first = at.split ? 4 * u : kUnit * u;
+  at.second = at.first + (at.split ? p.rotary / 2 : 4);
+  return at;
+}
+__device__ __forceinline__ uint4 load_unit(const __nv_bfloat16* head, const Place& at) {
+  if (!at.split) return __ldcs(reinterpret_cast<const uint4*>(head + at.first));
+  const uint2 a = __ldcs(reinterpret_cast<const uint2*>(head + at.first)), b = __ldcs(reinterpret_cast<const uint2*>(head + at.second));
+  return make_uint4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ float2 bf16_pair(uint32_t v) {
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+// The unit's elements in fp32, rotated by the four turns behind `turns` (of this unit).
+__device__ __forceinline__ void rotate_unit(uint4 raw, const Place& at, const float2* turns, float (&x)[8]) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = bf16_pair(w[i]);
+    x[2 * i] = v.x;
+    x[2 * i + 1] = v.y;
+  }
+  if (!at.rotated) return;
+  auto turn = [](float& a, float& b, float2 t) {
+    const float a0 = a, b0 = b;
+    a = fmaf(a0, t.x, -(b0 * t.y));
+    b = fmaf(a0, t.y, b0 * t.x);
+  };
+  if (at.split) {  // (two loops, so that the elements stay in registers)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) turn(x[i], x[i + 4], turns[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) turn(x[2 * i], x[2 * i + 1], turns[i]);
+  }
+}
+__device__ __forceinline__ void store_unit(__nv_bfloat16* head, const Place& at, const float (&x)[8]) {
+  const uint4 v = make_uint4(paged::pack_bf16(x[0], x[1]), paged::pack_bf16(x[2], x[3]), paged::pack_bf16(x[4], x[5]), paged::pack_bf16(x[6], x[7]));
+  if (!at.split) {
+    *reinterpret_cast<uint4*>(head + at.first) = v;
+  } else {
+    *reinterpret_cast<uint2*>(head + at.first) = make_uint2(v.x, v.y);
+    *reinterpret_cast<uint2*>(head + at.second) = make_uint2(v.z, v.w);
+  }
+}
+
+// A sequence's new tokens: rows [q0, q0 + n), the first at position pos0 (negative where kv_len is short of n).
+struct NewTokens {
+  int q0, n, pos0;
+};
+__device__ __forceinline__ NewTokens new_tokens(const RopeParams& p, int b) {
+  NewTokens s;
+  s.q0 = min(max(__ldg(p.cu_q + b), 0), p.tokens);
+  s.n = min(max(__ldg(p.cu_q + b + 1), s.q0), p.tokens) - s.q0;
+  s.pos0 = max(__ldg(p.kv_len + b), 0) - s.n;
+  return s;
+}
+__device__ __forceinline__ int page_at(const RopeParams& p, int b, int pos) {
+  const int i = pos / p.page_size;
+  if (i >= p.max_pages) return -1;
+  const int page = __ldg(p.block_table + (int64_t)b * p.max_pages + i);
+  return (unsigned)page < (unsigned)p.num_pages ? page : -1;
+}
+
+// `part` of the heads of token t: queries to q_out and, for a bf16 cache (CACHE), keys and values to their slot.  A warp.
+template <bool CACHE>
+__device__ __forceinline__ void rotate_token(const RopeParams& p, int t, int part, float2* turns) {
+  const int lane = threadIdx.x & 31;
+  const int b = paged::find_sequence(p.cu_q, p.batch, t);
+  if (b >= p.batch || t < __ldg(p.cu_q + b)) return;  // padding behind the last sequence
+  const NewTokens s = new_tokens(p, b);
+  const int pos = s.pos0 + (t - s.q0);
+  if (pos < 0) return;
+  const int page = CACHE ? page_at(p, b, pos) : -1;
+  const int heads = p.heads_q + (page >= 0 ? 2 * p.heads_kv : 0);
+  const int units = p.head_dim / kUnit;
+  // the heads of this part, in whole warps' worths of units
+  const int all = heads * units;
+  const int per = ((all + p.parts - 1) / p.parts + 31) & ~31;
+  const int begin = part * per, end = min(begin + per, all);
+  if (begin >= end) return;
+  for (int i = lane; i < p.rotary / 2; i += 32) turns[i] = turn_of(p, pos, i);
+  __syncwarp();
+  const int64_t slot = page < 0 ? 0 : (int64_t)page * p.page_stride + (int64_t)(pos % p.page_size) * p.slot_stride;
+  constexpr int kAhead = 4;
+  for (int i0 = begin + lane; i0 < end; i0 += 32 * kAhead) {
+    uint4 raw[kAhead];
+    Place at[kAhead];
+    int head[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + 32 * j;
+      head[j] = i / units;
+      at[j] = place_of(p, i - head[j] * units);
+      if (i < end) {
+        const int h = head[j] - p.heads_q;
+        const __nv_bfloat16* src = h < 0 ? p.q + (int64_t)t * p.ld_q + (int64_t)head[j] * p.head_dim
+                                   : h < p.heads_kv ? p.k_new + (int64_t)t * p.ld_new + (int64_t)h * p.head_dim
+                                                    : p.v_new + (int64_t)t * p.ld_new + (int64_t)(h - p.heads_kv) * p.head_dim;
+        if (h >= p.heads_kv) { at[j].rotated = at[j].split = false; at[j].first = (i - head[j] * units) * kUnit; }
+        raw[j] = load_unit(src, at[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + 32 * j;
+      if (i < end) {
+        const int h = head[j] - p.heads_q;
+        float x[8];
+        rotate_unit(raw[j], at[j], turns + 4 * (i - head[j] * units), x);
+        __nv_bfloat16* dst = h < 0 ? p.q_out + (int64_t)t * p.ld_q_out + (int64_t)head[j] * p.head_dim
+                                   : reinterpret_cast<__nv_bfloat16*>(h < p.heads_kv ? p.k_cache : p.v_cache) + slot +
+                                         (int64_t)(h < p.heads_kv ? h : h - p.heads_kv) * p.head_stride;
+        store_unit(dst, at[j], x);
+      }
+    }
+  }
+}
+
+// Where the blocks of sequence b begin in the count of places for blocks: as many as its new tokens can touch, and no more
+// than one and two halves of them, so that a place's sequence is found from cu_q alone.
+__device__ __forceinline__ int64_t first_block_place(const RopeParams& p, int b) {
+  return (int64_t)(min(max(__ldg(p.cu_q + b), 0), p.tokens) >> p.scales.shift) + 2 * (int64_t)b;
+}
+
+// One block of one sequence, and up to kWarps heads of K or of V of it.  A CTA.
+template <pd_dtype T>
+__device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t place, int round, float2* turns) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // the last sequence whose places begin at or in front of `place`: a 32-way search by every warp for itself
+  int lo = 0, hi = p.batch - 1;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32;
+    const int i = lo + 1 + lane * step;
+    const unsigned le = __ballot_sync(0xffffffffu, i <= hi && first_block_place(p, i) <= place);
+    const int k = __popc(le);
+    if (k == 0) { hi = lo; break; }
+    const int next = lo + 1 + (k - 1) * step;
+    hi = min(lo + k * step, hi);
+    lo = next;
+  }
+  const int b = lo;
+  const NewTokens s = new_tokens(p, b);
+  const int shift = p.scales.shift;
+  const int from = max(s.pos0, 0), to = s.pos0 + s.n;  // positions of the new tokens that have one
+  if (from >= to) return;
+  const int64_t index = (from >> shift) + (place - first_block_place(p, b));
+  if (index > ((to - 1) >> shift)) return;
+  const int start = (int)index << shift;
+  const int page = page_at(p, b, start);
+  if (page < 0) return;
+  const int first = max(start, from), last = (int)min((long long)start + (1ll << shift), (long long)to);
+  const int old = first - start;  // older tokens of the block
+  const int slot0 = start % p.page_size;
+
+  const int rounds_k = (p.heads_kv + kWarps - 1) / kWarps;
+  const bool keys = round < rounds_k;
+  const int head = (keys ? round : round - rounds_k) * kWarps + warp;
+  const bool mine = head < p.heads_kv;
+  const int units = p.head_dim / kUnit;
+  const __nv_bfloat16* src = (keys ? p.k_new : p.v_new) + (int64_t)(s.q0 + first - s.pos0) * p.ld_new + (int64_t)head * p.head_dim;
+  uint8_t* dst = (keys ? p.k_cache : p.v_cache) + (int64_t)page * p.page_stride + (int64_t)slot0 * p.slot_stride + (int64_t)head * p.head_stride;
+  float* scale_at = (keys ? p.k_scale : p.v_scale) + p.scales.at(page, head, slot0);
+  const float before = mine && old > 0 ? *scale_at : 0.f;
+
+  const int per_group = kGroup / units;  // tokens
+  const int tokens = last - first, groups = (tokens + per_group - 1) / per_group;
+  const int pairs = p.rotary / 2;
+  auto place_in = [&](int u) {
+    Place at = place_of(p, u);
+    if (!keys) { at.rotated = at.split = false; at.first = u * kUnit; at.second = at.first + 4; }
+    return at;
+  };
+  uint4 held[kHeld];
+  auto load_group = [&](int g) {
+    const int n = min(per_group, tokens - g * per_group) * units;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      const int i = lane + 32 * j;
+      if (mine && i < n) {
+        const int t = i / units;
+        held[j] = load_unit(src + (int64_t)(g * per_group + t) * p.ld_new, place_in(i - t * units));
+      }
+    }
+  };
+  auto turn_group = [&](int g) {  // cos and sin of the group's tokens; collective over the CTA
+    if (!keys || pairs == 0) return;
+    __syncthreads();
+    const int n = min(per_group, tokens - g * per_group) * pairs;
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const int t = i / pairs;
+      turns[i] = turn_of(p, first + g * per_group + t, i - t * pairs);
+    }
+    __syncthreads();
+  };
+  float most = 0.f;
+  for (int g = 0; g < groups; ++g) {
+    load_group(g);
+    turn_group(g);
+    const int n = mine ? min(per_group, tokens - g * per_group) * units : 0;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      const int i = lane + 32 * j;
+      if (i < n) {
+        const int t = i / units, u = i - t * units;
+        float x[8];
+        rotate_unit(held[j], place_in(u), turns + t * pairs + 4 * u, x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[k]));
+      }
+    }
+  }
+  most = warp_max(most);
+  // (a scale below the normal range would have no reciprocal)
+  const float need = most > 0.f ? fmaxf(most / paged::q8_top<T>(), 1.17549435e-38f) : 0.f;
+  const float scale = fmaxf(before, need), inv = scale > 0.f ? 1.f / scale : 0.f;
+  for (int g = 0; g < groups; ++g) {
+    if (groups > 1) {
+      load_group(g);
+      turn_group(g);
+    }
+    const int n = mine ? min(per_group, tokens - g * per_group) * units : 0;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      const int i = lane + 32 * j;
+      if (i < n) {
+        const int t = i / units, u = i - t * units;
+        const Place at = place_in(u);
+        float x[8];
+        rotate_unit(held[j], at, turns + t * pairs + 4 * u, x);
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          w[k] = paged::q8_pair_from_float<T>(x[4 * k] * inv, x[4 * k + 1] * inv) |
+                 paged::q8_pair_from_float<T>(x[4 * k + 2] * inv, x[4 * k + 3] * inv) << 16;
+        uint8_t* row = dst + (int64_t)(old + g * per_group + t) * p.slot_stride;
+        if (at.split) {
+          *reinterpret_cast<uint32_t*>(row + at.first) = w[0];
+          *reinterpret_cast<uint32_t*>(row + at.second) = w[1];
+        } else {
+          *reinterpret_cast<uint2*>(row + at.first) = make_uint2(w[0], w[1]);
+        }
+      }
+    }
+  }
+  if (!mine) return;
+  if (old > 0 && scale > before) {
+    const float ratio = before / scale;
+    for (int i = lane; i < old * units; i += 32) {
+      const int t = i / units;
+      uint2* at = reinterpret_cast<uint2*>(dst + (int64_t)t * p.slot_stride + (i - t * units) * kUnit);
+      const uint2 v = *at;
+      uint32_t w[2] = {v.x, v.y};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float2 a = paged::q8_pair_to_float<T>(w[k]), c = paged::q8_pair_to_float<T>(w[k] >> 16);
+        w[k] = paged::q8_pair_from_float<T>(a.x * ratio, a.y * ratio) | paged::q8_pair_from_float<T>(c.x * ratio, c.y * ratio) << 16;
+      }
+      *at = make_uint2(w[0], w[1]);
+    }
+  }
+  if (lane == 0) *scale_at = scale;
+}
+
+// bf16 cache: a warp for every part of a token.
+__global__ void __launch_bounds__(kThreads) rope_kv_cache_append_kernel(const RopeParams p) {
+  __shared__ float2 turns[kWarps][kMaxPairs];
+  griddep_wait();
+  griddep_launch_dependents();
+  const int warp = threadIdx.x >> 5;
+  const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
+  const int64_t t = w / p.parts;
+  if (t < p.tokens) rotate_token<true>(p, (int)t, (int)(w - t * p.parts), turns[warp]);
+}
+
+// 8-bit cache: the first CTAs take blocks of keys and values, the others parts of tokens' queries.
+template <pd_dtype T>
+__global__ void __launch_bounds__(kThreads, 2) rope_kv_cache_append_q8_kernel(const RopeParams p) {
+  __shared__ float2 turns[kGroup * 4];  // of a group's tokens: 512 units, at most four pairs each
+  static_assert(kWarps * kMaxPairs <= kGroup * 4);
+  griddep_wait();
+  griddep_launch_dependents();
+  if ((int64_t)blockIdx.x < p.block_ctas) {
+    quantise_block<T>(p, blockIdx.x / p.rounds, blockIdx.x % p.rounds, turns);
+    return;
+  }
+  const int warp = threadIdx.x >> 5;
+  const int64_t w = ((int64_t)blockIdx.x - p.block_ctas) * kWarps + warp;
+  const int64_t t = w / p.parts;
+  if (t < p.tokens) rotate_token<false>(p, (int)t, (int)(w - t * p.parts), turns + warp * kMaxPairs);
+}
+
+}  // namespace
+}  // namespace pd
+
+extern "C" pd_status pd_rope_kv_cache_append(const pd_paged_attention_desc* desc, const pd_rope_desc* rope,
+                                             const pd_cache_scales* scales, const void* q, void* q_out, const void* k_new,
+                                             const void* v_new, int64_t ld_new, void* k_cache, void* v_cache,
+                                             const int32_t* block_table, const int32_t* cu_q, const int32_t* kv_len,
+                                             cudaStream_t stream) {
+  using namespace pd;
+  if (!desc || !rope) return PD_ERR_NULL_POINTER;
+  const pd_paged_attention_desc& d = *desc;
+  const bool queries = q != nullptr || q_out != nullptr;
+  if (d.batch < 0 || d.tokens < 0 || d.heads_kv <= 0 || d.head_dim <= 0 || d.num_pages <= 0 || d.page_size <= 0 || d.max_pages <= 0 ||
+      (queries && d.heads_q <= 0))
+    return PD_ERR_BAD_SHAPE;
+  if (rope->rotary_dim < 0 || rope->rotary_dim > d.head_dim || (rope->interleaved != 0 && rope->interleaved != 1) ||
+      !(fabsf(rope->amplitude) <= 3.402823466e38f))
+    return PD_ERR_BAD_SHAPE;
+  if (scales && (!paged::q8_dtype(scales->dtype) || !paged::q8_block_valid(scales->block, d.page_size))) return PD_ERR_BAD_SHAPE;
+  if (d.head_dim % kUnit != 0 || d.head_dim > kMaxDim || rope->rotary_dim % 8 != 0 || d.heads_kv > 65536 || d.batch > 65535 ||
+      d.tokens > kMaxIndex || (queries && d.heads_q > 65536))
+    return PD_ERR_UNSUPPORTED;
+  if (ld_new < (int64_t)d.heads_kv * d.head_dim || d.page_stride <= 0 || d.slot_stride <= 0 || d.head_stride <= 0) return PD_ERR_BAD_SHAPE;
+  if (queries && (d.ld_q < (int64_t)d.heads_q * d.head_dim || d.ld_out < (int64_t)d.heads_q * d.head_dim)) return PD_ERR_BAD_SHAPE;
+  if (d.batch == 0 || d.tokens == 0) return PD_OK;
+  if (!k_new || !v_new || !k_cache || !v_cache || !block_table || !cu_q || !kv_len || (queries && (!q || !q_out)) ||
+      (rope->rotary_dim > 0 && !rope->inv_freq) || (scales && (!scales->k_scale || !scales->v_scale)))
+    return PD_ERR_NULL_POINTER;
+  auto bits = [](const void* v) { return reinterpret_cast<uintptr_t>(v); };
+  const int64_t cache_strides = d.page_stride | d.slot_stride | d.head_stride;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q) || !aligned16(q_out) ||
+      (ld_new & 7) != 0 || (queries && ((d.ld_q | d.ld_out) & 7) != 0) || (cache_strides & (scales ? 15 : 7)) != 0 ||
+      ((bits(block_table) | bits(cu_q) | bits(kv_len) | bits(rope->inv_freq)) & 3u) != 0 ||
+      (scales && ((bits(scales->k_scale) | bits(scales->v_scale)) & 3u) != 0))
+    return PD_ERR_ALIGNMENT;
+
+  RopeParams p{};
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.q_out = static_cast<__nv_bfloat16*>(q_out);
+  p.k_new = static_cast<const __nv_bfloat16*>(k_new);
+  p.v_new = static_cast<const __nv_bfloat16*>(v_new);
+  p.k_cache = static_cast<uint8_t*>(k_cache);
+  p.v_cache = static_cast<uint8_t*>(v_cache);
+  p.inv_freq = rope->inv_freq;
+  p.block_table = block_table; p.cu_q = cu_q; p.kv_len = kv_len;
+  p.ld_q = d.ld_q; p.ld_q_out = d.ld_out; p.ld_new = ld_new;
+  p.page_stride = d.page_stride; p.slot_stride = d.slot_stride; p.head_stride = d.head_stride;
+  p.amplitude = rope->amplitude; p.rotary = rope->rotary_dim; p.interleaved = rope->interleaved;
+  p.batch = d.batch; p.tokens = d.tokens; p.heads_q = queries ? d.heads_q : 0; p.heads_kv = d.heads_kv; p.head_dim = d.head_dim;
+  p.num_pages = d.num_pages; p.page_size = d.page_size; p.max_pages = d.max_pages;
+  // A warp per token while tokens fill the SMs (eight warps each), several for fewer tokens, none with less than 64 units.
+  const int64_t units = ((int64_t)p.heads_q + (scales ? 0 : 2 * (int64_t)d.heads_kv)) * (d.head_dim / kUnit);
+  int64_t parts = (148 * kWarps + d.tokens - 1) / d.tokens;
+  if (parts > (units + 63) / 64) parts = (units + 63) / 64;
+  p.parts = (int)(parts < 1 ? 1 : parts);
+  const int64_t token_ctas = units == 0 ? 0 : ((int64_t)d.tokens * p.parts + kWarps - 1) / kWarps;
+  if (scales) {
+    p.scales = paged::make_scales(*scales, d.heads_kv, d.page_size);
+    p.k_scale = scales->k_scale; p.v_scale = scales->v_scale;
+    p.rounds = 2 * ((d.heads_kv + kWarps - 1) / kWarps);
+    p.block_ctas = (((int64_t)d.tokens >> p.scales.shift) + 2 * (int64_t)d.batch) * p.rounds;
+  }
+  const int64_t ctas = p.block_ctas + token_ctas;
+  if (ctas > 0x7fffffff) return PD_ERR_UNSUPPORTED;
+  if (pd_status st = require_sm100(); st != PD_OK) return st;
+  logf("rope kv cache append: %d tokens of %d sequences, %s cache, %lld + %lld CTAs", d.tokens, d.batch,
+       !scales ? "bf16" : scales->dtype == PD_I8 ? "int8" : "e4m3", (long long)p.block_ctas, (long long)token_ctas);
+  auto kernel = !scales ? rope_kv_cache_append_kernel
+                        : scales->dtype == PD_I8 ? rope_kv_cache_append_q8_kernel<PD_I8> : rope_kv_cache_append_q8_kernel<PD_E4M3>;
+  launch_pdl(kernel, dim3((unsigned)ctas), dim3(kThreads), 0, stream, p);
+  return check_launch();
+}
