@@ -47,6 +47,31 @@ __device__ __forceinline__ uint32_t q8_pair_from_float(float a, float b) {
   }
 }
 
+// The four values of a word as fp16, exactly: bytes 0 and 2 in `even`, 1 and 3 in `odd` (ADJACENT: 0 and 1, 2 and 3).
+// int8: 1024 + (x ^ 0x80) has x + 128 in fp16's lowest mantissa bits, so that an and, an xor (one instruction together) and a
+// subtraction of 1152 make two values.
+template <pd_dtype T, bool ADJACENT>
+__device__ __forceinline__ void q8_word_to_half(uint32_t w, uint32_t& even, uint32_t& odd) {
+  if constexpr (T == PD_I8) {
+    static_assert(!ADJACENT);
+    const uint32_t bias = 0x64806480u;  // 1152, twice
+    asm("lop3.b32 %0, %2, 0x00ff00ff, %3, 0x6a;\n\t"  // (a & b) ^ c
+        "lop3.b32 %1, %4, 0x00ff00ff, %3, 0x6a;"
+        : "=r"(even), "=r"(odd) : "r"(w), "r"(bias), "r"(w >> 8));
+    asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(even) : "r"(bias));
+    asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(odd) : "r"(bias));
+  } else {
+    if constexpr (!ADJACENT) w = __byte_perm(w, 0, 0x3120);
+    asm("{\n\t"
+        ".reg .b16 lo, hi;\n\t"
+        "mov.b32 {lo, hi}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, lo;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, hi;\n\t"
+        "}"
+        : "=r"(even), "=r"(odd) : "r"(w));
+  }
+}
+
 // ---- host side -----------------------------------------------------------------------
 inline bool q8_dtype(pd_dtype t) { return t == PD_I8 || t == PD_E4M3; }
 // A power of two that divides the page.
@@ -59,6 +84,23 @@ inline Scales make_scales(const pd_cache_scales& s, int heads_kv, int page_size)
   r.page_stride = (int64_t)heads_kv * r.blocks_per_page;
   return r;
 }
+
+// Tensor map of one cache: {head_dim, page_size, heads_kv, num_pages} bytes, boxes of a head's elements x `box_rows` slots.
+inline bool make_cache_map_q8(CUtensorMap* map, const void* cache, const pd_paged_attention_desc& d, int box_rows) {
+  gemm::EncodeTiledFn fn = gemm::encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)d.head_dim, (cuuint64_t)d.page_size, (cuuint64_t)d.heads_kv, (cuuint64_t)d.num_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)d.slot_stride, (cuuint64_t)d.head_stride, (cuuint64_t)d.page_stride};
+  const cuuint32_t box[4] = {(cuuint32_t)d.head_dim, (cuuint32_t)box_rows, 1, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(cache), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            d.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Launcher (in its own file).  `rows_per_tile`: 8, 16, 32 or 64.
+pd_status launch_rows_q8(const pd_paged_attention_desc& d, Params& p, pd_dtype type, const Scales& scales, const void* k_cache,
+                         const void* v_cache, int rows_per_tile, cudaStream_t s);
 
 }  // namespace paged
 }  // namespace pd

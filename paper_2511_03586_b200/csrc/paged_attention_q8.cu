@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(128) paged_attention_q8_kernel(const Params p,
   for (int j = 0; j < kPer; ++j) p.out[(int64_t)t * p.ld_out + (int64_t)h * D + lane * kPer + j] = __float2bfloat16_rn(o[j] * inv);
 }
 
-size_t workspace_bytes(const pd_paged_attention_desc&) { return 0; }
+inline Plan plan_q8(const pd_paged_attention_desc& d) { return plan(d, 8); }
 
 }  // namespace
 }  // namespace paged
@@ -63,7 +63,7 @@ size_t workspace_bytes(const pd_paged_attention_desc&) { return 0; }
 extern "C" size_t pd_attention_paged_q8_workspace_bytes(const pd_paged_attention_desc* desc) {
   if (!desc || !pd::paged::valid(*desc) || !pd::paged::supported(*desc)) return 0;
   if (desc->batch == 0 || desc->tokens == 0 || desc->max_q_len == 0) return 0;
-  return pd::paged::workspace_bytes(*desc);
+  return pd::paged::workspace_bytes(*desc, pd::paged::plan_q8(*desc));
 }
 
 extern "C" pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* desc, const pd_cache_scales* scales, const void* q,
@@ -84,28 +84,22 @@ extern "C" pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* de
       ((d.page_stride | d.slot_stride | d.head_stride) & 15) != 0 ||
       ((bits(block_table) | bits(cu_q) | bits(kv_len) | bits(scales->k_scale) | bits(scales->v_scale)) & 3u) != 0)
     return PD_ERR_ALIGNMENT;
-  const size_t need = paged::workspace_bytes(d);
+  const paged::Plan pl = paged::plan_q8(d);
+  const size_t need = paged::workspace_bytes(d, pl);
   if (need > 0) {
     if (!workspace) return PD_ERR_NULL_POINTER;
     if (workspace_bytes < need) return PD_ERR_WORKSPACE_TOO_SMALL;
     if ((bits(workspace) & 255u) != 0) return PD_ERR_ALIGNMENT;
   }
   if (pd_status st = require_sm100(); st != PD_OK) return st;
-  paged::Params p{};
-  p.q = static_cast<const __nv_bfloat16*>(q);
-  p.out = static_cast<__nv_bfloat16*>(out);
-  p.block_table = block_table; p.cu_q = cu_q; p.kv_len = kv_len;
-  p.ld_q = d.ld_q; p.ld_out = d.ld_out;
-  p.batch = d.batch; p.tokens = d.tokens; p.heads_q = d.heads_q; p.heads_kv = d.heads_kv; p.group = d.heads_q / d.heads_kv;
-  p.num_pages = d.num_pages; p.page_size = d.page_size; p.max_pages = d.max_pages;
-  while ((1 << p.page_shift) < d.page_size) ++p.page_shift;
-  p.max_q_len = d.max_q_len < d.tokens ? d.max_q_len : d.tokens;
-  p.window = d.window < paged::kMaxPositions ? d.window : paged::kMaxPositions; p.sinks = d.sinks;
-  p.scale_log2e = paged::base2_scale(d.scale);
+  paged::Params p = paged::make_params(d, pl, q, block_table, cu_q, kv_len, out, workspace);
+  if (!p.status) return PD_ERR_CUDA;
+  const paged::Scales sc = paged::make_scales(*scales, d.heads_kv, d.page_size);
+  if (pl.rows_per_tile <= 64) return paged::launch_rows_q8(d, p, scales->dtype, sc, k_cache, v_cache, pl.rows_per_tile, stream);
   const bool i8 = scales->dtype == PD_I8;
   auto kernel = d.head_dim == 64 ? (i8 ? paged::paged_attention_q8_kernel<PD_I8, 64> : paged::paged_attention_q8_kernel<PD_E4M3, 64>)
                                  : (i8 ? paged::paged_attention_q8_kernel<PD_I8, 128> : paged::paged_attention_q8_kernel<PD_E4M3, 128>);
   launch_pdl(kernel, dim3((unsigned)(((int64_t)d.tokens * d.heads_q + 3) / 4)), dim3(128), 0, stream, p, static_cast<const uint8_t*>(k_cache),
-             static_cast<const uint8_t*>(v_cache), d.page_stride, d.slot_stride, d.head_stride, paged::make_scales(*scales, d.heads_kv, d.page_size));
+             static_cast<const uint8_t*>(v_cache), d.page_stride, d.slot_stride, d.head_stride, sc);
   return check_launch();
 }

@@ -3,6 +3,7 @@
 // Internal to the library.
 #pragma once
 
+#include <algorithm>
 #include <cmath>
 
 #include "gemm_common.cuh"
@@ -165,6 +166,81 @@ inline bool supported(const pd_paged_attention_desc& d) {
          (int64_t)d.max_pages * d.page_size <= kMaxPositions && (int64_t)d.tokens * (d.heads_q / d.heads_kv) <= kMaxPositions &&
          (int64_t)d.batch * d.heads_kv * (((int64_t)d.max_pages * d.page_size + 63) / 64) <= kMaxPositions && d.batch <= 65535 &&
          d.heads_kv <= 65535;
+}
+
+struct Plan {
+  int rows_per_tile;            // up to 64: row kernel; 128, 256: chunk kernel
+  int splits, min_split_tiles;  // in key tiles of the kernel (64, 128); the latter of the chunk kernels alone
+  bool whole_items;
+};
+
+// Depends on the desc alone (the workspace size follows from it).  `smallest`: rows of the smallest tile.
+inline Plan plan(const pd_paged_attention_desc& d, int smallest = 16) {
+  constexpr int kSms = 148;  // (not asked of the device: the workspace follows from the desc alone)
+  Plan pl{};
+  const int64_t group = d.heads_q / d.heads_kv, rows = std::min(d.max_q_len, d.tokens) * group;
+  pl.rows_per_tile = rows <= smallest ? smallest : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : d.head_dim == 64 ? 128 : 256;
+  const bool chunk = pl.rows_per_tile > 64;
+  const int64_t row_tiles = (rows + pl.rows_per_tile - 1) / pl.rows_per_tile;
+  const int64_t items = row_tiles * d.heads_kv * d.batch;  // CTAs without splitting
+  int64_t keys = d.max_kv_len;
+  if (d.window > 0) keys = std::min<int64_t>(keys, (int64_t)d.window + d.sinks + d.max_q_len);
+  const int64_t tile = !chunk ? 64 : d.head_dim == 64 ? 64 : 128, tiles = (keys + tile - 1) / tile;
+  if (!chunk) {
+    // two CTAs per SM share all key tiles evenly; fewer when there are not enough tiles for that
+    pl.whole_items = tiles <= 2;
+    const int64_t all = std::max<int64_t>(tiles, 1) * d.heads_kv * d.batch;  // (not 0: an empty batch launches nothing)
+    pl.splits = (int)std::min<int64_t>(2 * kSms, all);
+    return pl;
+  }
+  // One or four CTAs per SM, and splits only to fill the SMs, none below min_split_tiles.
+  pl.min_split_tiles = d.head_dim == 64 ? 8 : 4;
+  int64_t want = items > 0 ? kSms * (d.head_dim == 64 ? 4 : 1) / items : 1;
+  want = std::min<int64_t>(want, (tiles + pl.min_split_tiles - 1) / pl.min_split_tiles);
+  pl.splits = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 256);
+  return pl;
+}
+
+// Tokens that can have partial results in the chunk kernel (a token tensor may be padded to any length), at most d.tokens.
+inline int64_t partial_tokens(const pd_paged_attention_desc& d) {
+  return std::min<int64_t>(d.tokens, (int64_t)d.batch * std::min(d.max_q_len, d.tokens));
+}
+// Rows of partial results in the workspace, and entries of the piece table behind them.
+inline size_t partial_rows(const pd_paged_attention_desc& d, const Plan& pl) {
+  if (pl.rows_per_tile > 64) return pl.splits > 1 ? (size_t)pl.splits * partial_tokens(d) * d.heads_q : 0;
+  return (size_t)2 * pl.splits * pl.rows_per_tile;
+}
+inline size_t table_entries(const pd_paged_attention_desc& d, const Plan& pl) {
+  return pl.rows_per_tile > 64 ? 0 : (size_t)d.batch * d.heads_kv;
+}
+inline size_t workspace_bytes(const pd_paged_attention_desc& d, const Plan& pl) {
+  return partial_rows(d, pl) * ((size_t)d.head_dim + 1) * sizeof(float) + table_entries(d, pl) * sizeof(int2);
+}
+
+// The kernels' parameters for a call with this plan (p.status is null where the device has no status word).
+inline Params make_params(const pd_paged_attention_desc& d, const Plan& pl, const void* q, const int32_t* block_table, const int32_t* cu_q,
+                          const int32_t* kv_len, void* out, void* workspace) {
+  Params p{};
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.block_table = block_table; p.cu_q = cu_q; p.kv_len = kv_len;
+  p.status = device_status_ptr();
+  p.wait_limit_ns = debug_wait_limit_ns(); p.withhold_loads = debug_withhold_loads();
+  p.ld_q = d.ld_q; p.ld_out = d.ld_out;
+  p.batch = d.batch; p.tokens = d.tokens; p.heads_q = d.heads_q; p.heads_kv = d.heads_kv; p.group = d.heads_q / d.heads_kv;
+  p.num_pages = d.num_pages; p.page_size = d.page_size; p.max_pages = d.max_pages;
+  while ((1 << p.page_shift) < d.page_size) ++p.page_shift;
+  p.max_q_len = std::min(d.max_q_len, d.tokens); p.window = std::min(d.window, kMaxPositions); p.sinks = d.sinks;
+  p.part_tokens = (int)partial_tokens(d); p.part_by_sequence = p.part_tokens < d.tokens;
+  p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles; p.whole_items = pl.whole_items;
+  p.scale_log2e = base2_scale(d.scale);
+  if (workspace && workspace_bytes(d, pl) > 0) {
+    const size_t rows = partial_rows(d, pl);  // (an even number in the row kernel: the table is aligned)
+    p.part_o = static_cast<float*>(workspace);
+    p.part_lse = p.part_o + rows * d.head_dim;
+    p.pieces = reinterpret_cast<int2*>(p.part_lse + rows);
+  }
+  return p;
 }
 
 // Launchers (each in its own file).  `rows_per_tile` of the row kernel: 16, 32 or 64.

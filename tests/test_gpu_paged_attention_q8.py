@@ -5,7 +5,13 @@ rounding, 2^-10 of the former for the fp32 parts), plus what comes of keys and v
 their scale: a value is off by 2^-8 of itself at most, 2^-8 of sum_j p_j |v_j| again; a score by 2^-8 sum_i |q_i k_i| scale at the
 very worst, and, since D independent roundings do not conspire, by less than six times their root mean square 2^-8 / sqrt(3)
 sqrt(sum_i (q_i k_i)^2) scale.  The weights move by that much, relative, and so does the result: by at most
-sum_j p_j e_j |v_j - out| <= e_max (sum_j p_j |v_j| + |out|)."""
+sum_j p_j e_j |v_j - out| <= e_max (sum_j p_j |v_j| + |out|).
+
+The kernels for few rows take the exponentials times the scale of the values as fp16 instead, below 2^15 and in units of
+v_top / 2^11, with v_top less than twice the largest scale of a value in view.  That is 2^-11 of each, well within the 2^-8 above,
+down to fp16's smallest normal number, and half of its smallest number, 2^-25 units, below.  The sum of exponentials that it is
+divided by is at least 1, a stored value times the largest scale at most the largest value of the head, V (the largest value of a
+block takes up the type's range): another 2^-25 2^-11 2 V = 2^-35 V for every key."""
 import pytest
 import torch
 
@@ -105,7 +111,8 @@ class PagedQ8:
             # the largest root of sum_i (q_i k_i)^2 of a head's keys, bounded through the keys' elementwise maxima
             most = self.k_seq[b].abs().amax(0).repeat_interleave(group, 0) if kv else torch.zeros_like(q[0]).double()
             e = 6 * 2 ** -8 / 3 ** 0.5 * (q.double() * most).pow(2).sum(-1, keepdim=True).sqrt() * (scale or q.shape[2] ** -0.5)
-            bound = (2 * 2 ** -8 + 2 ** -10) * mag + 2 ** -8 * want.abs() + e * (mag + want.abs()) + 1e-30
+            v_most = self.v_seq[b].abs().amax((0, 2)).repeat_interleave(group)[:, None] if kv else 0.0
+            bound = (2 * 2 ** -8 + 2 ** -10) * mag + 2 ** -8 * want.abs() + e * (mag + want.abs()) + 2 ** -35 * kv * v_most + 1e-30
             worst = ((got - want).abs() / bound).max().item()
             assert worst <= 1.0, (b, n, kv, worst)
             start += n
