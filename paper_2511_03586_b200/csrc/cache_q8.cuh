@@ -2,6 +2,8 @@
 // Internal to the library.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "paged_cache.cuh"
 
 namespace pd {
@@ -98,7 +100,9 @@ inline bool make_cache_map_q8(CUtensorMap* map, const void* cache, const pd_page
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Launcher (in its own file).  `rows_per_tile`: 8, 16, 32 or 64.
+// Launchers (each in its own file).  `rows_per_tile` of the row kernel: 8, 16, 32 or 64.
+pd_status launch_chunk_q8(const pd_paged_attention_desc& d, const Params& p, pd_dtype type, const Scales& scales, const void* k_cache,
+                          const void* v_cache, cudaStream_t s);
 pd_status launch_rows_q8(const pd_paged_attention_desc& d, Params& p, pd_dtype type, const Scales& scales, const void* k_cache,
                          const void* v_cache, int rows_per_tile, cudaStream_t s);
 

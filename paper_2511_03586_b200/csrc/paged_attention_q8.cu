@@ -1,60 +1,12 @@
-// Attention over an 8-bit paged cache: a warp per token and query head walks the keys that the token sees.
+// Entry point of the attention over an 8-bit paged cache: argument checks and the choice of kernel.
 #include "cache_q8.cuh"
+#include "paged_join.cuh"
 
 namespace pd {
 namespace paged {
 namespace {
 
-template <pd_dtype T, int D>
-__global__ void __launch_bounds__(128) paged_attention_q8_kernel(const Params p, const uint8_t* k_cache, const uint8_t* v_cache,
-                                                                 int64_t page_stride, int64_t slot_stride, int64_t head_stride,
-                                                                 const Scales scales) {
-  griddep_wait();
-  griddep_launch_dependents();
-  constexpr int kPer = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= (int64_t)p.tokens * p.heads_q) return;
-  const int t = (int)(row / p.heads_q), h = (int)(row % p.heads_q), kvh = h / p.group;
-  const int b = find_sequence(p.cu_q, p.batch, t);
-  if (b >= p.batch) return;
-  const Sequence seq = load_sequence(p, b);
-  if (t < seq.q0 || t - seq.q0 >= seq.n) return;
-  const int pos = seq.pos0 + (t - seq.q0);
-  float q[kPer], o[kPer], m = -INFINITY, l = 0.f;
-  for (int j = 0; j < kPer; ++j) {
-    q[j] = __bfloat162float(p.q[(int64_t)t * p.ld_q + (int64_t)h * D + lane * kPer + j]);
-    o[j] = 0.f;
-  }
-  const int end = min(pos + 1, seq.length);
-  for (int key = 0; key < end; ++key) {
-    if (p.window > 0 && key <= pos - p.window && key >= p.sinks) continue;
-    const int page = page_of(p, b, key), slot = key & (p.page_size - 1);
-    float k[kPer], v[kPer], ks = 0.f, vs = 0.f;
-    for (int j = 0; j < kPer; ++j) k[j] = v[j] = 0.f;
-    if (page < p.num_pages) {
-      const int64_t at = page * page_stride + slot * slot_stride + kvh * head_stride + lane * kPer;
-      for (int j = 0; j < kPer; j += 2) {
-        const float2 a = q8_pair_to_float<T>(*reinterpret_cast<const uint16_t*>(k_cache + at + j));
-        const float2 c = q8_pair_to_float<T>(*reinterpret_cast<const uint16_t*>(v_cache + at + j));
-        k[j] = a.x; k[j + 1] = a.y; v[j] = c.x; v[j + 1] = c.y;
-      }
-      ks = scales.k[scales.at(page, kvh, slot)];
-      vs = scales.v[scales.at(page, kvh, slot)];
-    }
-    float s = 0.f;
-    for (int j = 0; j < kPer; ++j) s = fmaf(q[j], k[j], s);
-    s = warp_sum(s) * ks * p.scale_log2e;
-    const float top = fmaxf(m, s), alpha = exp2f(m - top), e = exp2f(s - top);
-    m = top;
-    l = l * alpha + e;
-    for (int j = 0; j < kPer; ++j) o[j] = fmaf(e * vs, v[j], o[j] * alpha);
-  }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  for (int j = 0; j < kPer; ++j) p.out[(int64_t)t * p.ld_out + (int64_t)h * D + lane * kPer + j] = __float2bfloat16_rn(o[j] * inv);
-}
-
-inline Plan plan_q8(const pd_paged_attention_desc& d) { return plan(d, 8); }
+Plan plan_q8(const pd_paged_attention_desc& d) { return plan(d, 8, true); }
 
 }  // namespace
 }  // namespace paged
@@ -95,11 +47,9 @@ extern "C" pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* de
   paged::Params p = paged::make_params(d, pl, q, block_table, cu_q, kv_len, out, workspace);
   if (!p.status) return PD_ERR_CUDA;
   const paged::Scales sc = paged::make_scales(*scales, d.heads_kv, d.page_size);
+  logf("paged attention (%s) batch %d tokens %d (max %d) heads %d/%d x %d: tiles of %d rows, %s %d", scales->dtype == PD_I8 ? "int8" : "e4m3",
+       d.batch, d.tokens, d.max_q_len, d.heads_q, d.heads_kv, d.head_dim, pl.rows_per_tile, pl.rows_per_tile > 64 ? "key splits" : "CTAs", pl.splits);
   if (pl.rows_per_tile <= 64) return paged::launch_rows_q8(d, p, scales->dtype, sc, k_cache, v_cache, pl.rows_per_tile, stream);
-  const bool i8 = scales->dtype == PD_I8;
-  auto kernel = d.head_dim == 64 ? (i8 ? paged::paged_attention_q8_kernel<PD_I8, 64> : paged::paged_attention_q8_kernel<PD_E4M3, 64>)
-                                 : (i8 ? paged::paged_attention_q8_kernel<PD_I8, 128> : paged::paged_attention_q8_kernel<PD_E4M3, 128>);
-  launch_pdl(kernel, dim3((unsigned)(((int64_t)d.tokens * d.heads_q + 3) / 4)), dim3(128), 0, stream, p, static_cast<const uint8_t*>(k_cache),
-             static_cast<const uint8_t*>(v_cache), d.page_stride, d.slot_stride, d.head_stride, sc);
-  return check_launch();
+  if (pd_status st = paged::launch_chunk_q8(d, p, scales->dtype, sc, k_cache, v_cache, stream); st != PD_OK) return st;
+  return pl.splits > 1 ? paged::launch_join(d, p, stream) : PD_OK;
 }

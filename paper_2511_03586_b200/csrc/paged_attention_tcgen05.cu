@@ -2,7 +2,8 @@
 //
 //   out[t, h] = sum_j softmax_j(scale * q[t, h] . k[j]) v[j],   j visible from token t's position
 //
-// Two kernels, one per head_dim; the one for 64 is described further down.  In the one for 128 a CTA takes two consecutive
+// Two kernels; the one for a bf16 cache with head_dim 64 is described further down.  In the one for head_dim 128, and for 8-bit
+// caches with either, a CTA takes two consecutive
 // tiles ("slots") of 128 rows of one cache head (a row is a token and one of the query heads that share the cache head) and
 // walks the key tiles of 128 keys that any of them sees; both slots read the same K and V tiles, which halves what comes
 // from L2.  While one slot's scores are being exponentiated the other slot's products run.
@@ -19,6 +20,7 @@
 //                    products take.)
 //   warp 12        : producer: looks the pages up and copies K and V tiles by TMA, one box per page, into a ring of four
 //                    32 KiB stages, K and V in turn.
+//   8-bit caches     : warps 12-15 in its place, which load, convert and write the same tiles (convert_tiles).
 // Tensor memory: per slot two score buffers of 64 columns and an output of 128; that is all of it.  Two
 // buffers let the scores of the next block be formed while the current ones are exponentiated: the buffer they take was
 // last read by the product of the block before.  (With one buffer of 128 columns the softmax warps of a slot waited half
@@ -29,7 +31,7 @@
 // With `splits` > 1 the key tiles are shared out over that many CTAs, whose partial outputs paged_attention_join joins.
 #include <type_traits>
 
-#include "paged_cache.cuh"
+#include "cache_q8.cuh"
 
 namespace pd {
 namespace paged {
@@ -56,17 +58,34 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // the lowest n bits, n clamped to [0, 32]
 __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; }
 
-// head_dim 128: two slots per CTA, one CTA per SM.
+// Where keys and values come from.  A bf16 cache: by TMA.
+struct TiledCache {
+  static constexpr bool kBytes = false;
+  CUtensorMap k, v;
+};
+// An 8-bit cache: by plain loads of four warps, which multiply by the scales and round to bf16.
+template <pd_dtype TYPE>
+struct ByteCache {
+  static constexpr bool kBytes = true;
+  static constexpr pd_dtype T = TYPE;
+  const uint8_t *k, *v;
+  int64_t page_stride, slot_stride, head_stride;
+  Scales scales;
+};
+
+// Two slots per CTA, one CTA per SM.
+template <int HEAD_DIM, typename Cache>
 struct WideConfig {
-  static constexpr int D = 128, kSlots = 2;
+  static constexpr int D = HEAD_DIM, kSlots = 2;
+  static constexpr int kProducers = Cache::kBytes ? 4 : 1;  // warps
   static constexpr int kIssuer0 = kSlots * kSoftmaxWarps, kProducer = kIssuer0 + 2 * kSlots;
-  static constexpr int kThreads = 32 * (kProducer + 1);
+  static constexpr int kThreads = 32 * (kProducer + kProducers);
   static constexpr int kRows = kSlots * kTile;
   static constexpr int kTensor = kTile * D * 2;  // a Q, K or V tile
   static constexpr int kSmem = kSlots * kTensor + kStages * kTensor + 1024 /*barriers*/ + 1024 /*alignment*/;
   // tensor-memory columns: score buffer b of slot s at 128 s + 64 b (its probabilities over it, two keys to a column), output
   // of slot s behind them
-  static constexpr uint32_t kColO = kSlots * kTile, kCols = kSlots * 256;
+  static constexpr uint32_t kColO = kSlots * kTile, kCols = 512;
 };
 
 // The view of one slot: keys [lo, hi) and sinks [0, sink_hi) are seen by some of its rows.
@@ -139,11 +158,77 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
   if (valid && p.splits > 1) p.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
 }
 
-__global__ void __launch_bounds__(WideConfig::kThreads, 1)
-paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
-                             const Params p) {
-  using C = WideConfig;
-  constexpr int D = C::D;
+// Keys and values of an 8-bit cache into the ring, as the bf16 numbers nearest to what they stand for: one of four warps, which
+// share every tile, 32 keys each.  A lane has 16 elements of a key at a time and loads a whole tile's worth of them ahead, while
+// the tile before is converted.  Keys in nobody's view, and ones without a page, become zeros.
+//   Conversion: a byte becomes fp16 (exact), fp32, times its scale, bf16: 3 to 4 instructions, as many for a tile of K or V as
+//   a sixth of what the softmax of the two slots takes.  Rounding keys and values to bf16 is off by 2^-9 of each in the mean; the scales
+//   kept apart from the products would cost the softmax, the busiest part, two multiplications a score instead.
+template <int D, typename Cache>
+__device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& p, const KeyTiles& kt, int kvh, int b, int begin, int end,
+                                              int warp, uint32_t ring, uint32_t bars, volatile int* abort_flag) {
+  constexpr int kLanes = D / 16, kRowsAtOnce = 32 / kLanes, kSteps = 32 / kRowsAtOnce, kTensor = kTile * D * 2;
+  const int lane = threadIdx.x & 31, chunk = lane % kLanes, in_step = lane / kLanes;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 32u + 8u * s; };
+  uint4 data[2][kSteps];
+  float scale[2][kSteps];
+  int page = 0;  // of step `lane % kSteps` (pages hold eight slots at least, a step's keys share one)
+  auto first_key = [&](int i) { return kt.tile_index(i) * kTile + warp * 32; };
+  auto load = [&](int i, int kv) {
+    const int key0 = first_key(i);
+    if (kv == 0) page = page_of(p, b, key0 + (lane % kSteps) * kRowsAtOnce);
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      const int pg = __shfl_sync(0xffffffffu, page, j);
+      const int key = key0 + j * kRowsAtOnce + in_step, slot = key & (p.page_size - 1);
+      const bool there = pg < p.num_pages && ((key < kt.hi && key >= kt.lo) || key < kt.sink_hi);
+      const uint8_t* src = (kv == 0 ? cache.k : cache.v) + (int64_t)pg * cache.page_stride + (int64_t)slot * cache.slot_stride + (int64_t)kvh * cache.head_stride;
+      data[kv][j] = there ? __ldg(reinterpret_cast<const uint4*>(src) + chunk) : make_uint4(0, 0, 0, 0);
+      scale[kv][j] = there ? __ldg((kv == 0 ? cache.scales.k : cache.scales.v) + cache.scales.at(pg, kvh, slot)) : 0.f;
+    }
+  };
+  if (p.withhold_loads || begin >= end) return;
+  load(begin, 0);
+  load(begin, 1);
+  int n = 0;
+  for (int i = begin; i < end; ++i) {
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv, ++n) {
+      const int stage = n % kStages;
+      if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer, p.wait_limit_ns)) return;
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        const uint32_t w[4] = {data[kv][j].x, data[kv][j].y, data[kv][j].z, data[kv][j].w};
+        uint32_t out[8];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          constexpr bool kAdjacent = Cache::T != PD_I8;
+          uint32_t even, odd;
+          q8_word_to_half<Cache::T, kAdjacent>(w[c], even, odd);
+          const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), o = __half22float2(*reinterpret_cast<__half2*>(&odd));
+          const float s = scale[kv][j];
+          out[2 * c] = kAdjacent ? pack_bf16(a.x * s, a.y * s) : pack_bf16(a.x * s, o.x * s);
+          out[2 * c + 1] = kAdjacent ? pack_bf16(o.x * s, o.y * s) : pack_bf16(a.y * s, o.y * s);
+        }
+        const int r = warp * 32 + j * kRowsAtOnce + in_step;
+        const uint32_t row = ring + stage * kTensor + (chunk >> 2) * kHalf + (uint32_t)r * 128u;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          st_shared_v4(row + (uint32_t)((((2 * chunk + c) & 7) ^ (r & 7)) << 4), make_uint4(out[4 * c], out[4 * c + 1], out[4 * c + 2], out[4 * c + 3]));
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full(stage));
+      if (i + 1 < end) load(i + 1, kv);
+    }
+  }
+}
+
+template <int D, typename Cache>
+__global__ void __launch_bounds__(WideConfig<D, Cache>::kThreads, 1)
+paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p) {
+  using C = WideConfig<D, Cache>;
   constexpr int kSlots = C::kSlots, kIssuer0 = C::kIssuer0, kProducer = C::kProducer;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -161,7 +246,7 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kSlots); }
+    for (int s = 0; s < kStages; ++s) { mbar_init(full(s), C::kProducers); mbar_init(empty(s), kSlots); }
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(q_full(s), kSoftmaxWarps);
       for (int b = 0; b < 2; ++b) { mbar_init(o_full(s, b), 1); mbar_init(s_full(s, b), 1); mbar_init(p_full(s, b), kSoftmaxWarps); }
@@ -174,7 +259,9 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
   if (warp == kProducer) {
     tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::kCols);
     tmem_relinquish_alloc_permit();
-    if (lane == 0) { prefetch_tensormap(&tmap_k); prefetch_tensormap(&tmap_v); }
+    if constexpr (!Cache::kBytes) {
+      if (lane == 0) { prefetch_tensormap(&cache.k); prefetch_tensormap(&cache.v); }
+    }
   }
   tcgen05_fence_before_sync();
   __syncthreads();
@@ -337,40 +424,45 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
       if (ok && view.active && *abort_flag == 0) {
         write_rows<D>(p, seq, split, t, head, valid, done > 0, m, l, t_o, sQ + s * C::kTensor + (uint32_t)(quarter * 32) * 128u);
       }
-    } else if (warp == kProducer) {
-      // ------------------------------------------------------------------ producer
-      const int box = min(p.page_size, kTile);
-      const int per_tile = kTile / box, per_batch = 32 / per_tile;
-      int page = 0, n = 0;  // n: ring slots requested so far
-      bool ok = !p.withhold_loads;
-      for (int i = begin; i < end && ok; ++i) {
-        const int in_batch = (i - begin) % per_batch;
-        if (in_batch == 0) {
-          const int ti = i + lane / per_tile;
-          page = ti < end ? page_of(p, b, kt.tile_index(ti) * kTile + (lane % per_tile) * box) : 0;
-        }
-        const int slot = (kt.tile_index(i) * kTile) & (p.page_size - 1);
-        for (int kv = 0; kv < 2; ++kv, ++n) {
-          const int stage = n % kStages;
-          if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer, p.wait_limit_ns)) { ok = false; break; }
-          if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensor);
-          __syncwarp();
-          for (int j = 0; j < per_tile; ++j) {
-            const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + j);
-            if (elect_one()) {
-#pragma unroll
-              for (int h = 0; h < D / 64; ++h)
-                tma_load_4d(ring + stage * C::kTensor + h * kHalf + j * box * 128, kv == 0 ? &tmap_k : &tmap_v, full(stage),
-                            h * 64, slot, kvh, pg);
-            }
+    } else if (warp >= kProducer) {
+      if constexpr (Cache::kBytes) {
+        // ---------------------------------------------------------------- converters
+        convert_tiles<D>(cache, p, kt, kvh, b, begin, end, warp - kProducer, ring, bars, abort_flag);
+      } else {
+        // ------------------------------------------------------------------ producer
+        const int box = min(p.page_size, kTile);
+        const int per_tile = kTile / box, per_batch = 32 / per_tile;
+        int page = 0, n = 0;  // n: ring slots requested so far
+        bool ok = !p.withhold_loads;
+        for (int i = begin; i < end && ok; ++i) {
+          const int in_batch = (i - begin) % per_batch;
+          if (in_batch == 0) {
+            const int ti = i + lane / per_tile;
+            page = ti < end ? page_of(p, b, kt.tile_index(ti) * kTile + (lane % per_tile) * box) : 0;
+          }
+          const int slot = (kt.tile_index(i) * kTile) & (p.page_size - 1);
+          for (int kv = 0; kv < 2; ++kv, ++n) {
+            const int stage = n % kStages;
+            if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer, p.wait_limit_ns)) { ok = false; break; }
+            if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kTensor);
             __syncwarp();
+            for (int j = 0; j < per_tile; ++j) {
+              const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + j);
+              if (elect_one()) {
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h)
+                  tma_load_4d(ring + stage * C::kTensor + h * kHalf + j * box * 128, kv == 0 ? &cache.k : &cache.v, full(stage),
+                              h * 64, slot, kvh, pg);
+              }
+              __syncwarp();
+            }
           }
         }
+        // Leave no copy in flight, whichever warp gives up: the last request of every stage gets a short time to land.
+        volatile int never = 0;
+        for (int back = 1; back <= kStages && back <= n; ++back)
+          mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
       }
-      // Leave no copy in flight, whichever warp gives up: the last request of every stage gets a short time to land.
-      volatile int never = 0;
-      for (int back = 1; back <= kStages && back <= n; ++back)
-        mbar_wait(full((n - back) % kStages), ((n - back) / kStages) & 1u, &never, nullptr, 0, 20000000ull);
     } else {
       // --------------------------------------------------------------- MMA issuers
       const int s = (warp - kIssuer0) >> 1;
@@ -418,10 +510,10 @@ paged_attention_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const _
           const int key0 = block_key(b);
           if ((b & 1) == 0) {
             if (!wait(full(stage), n / kStages)) break;
-            if ((view.needs(key0) || view.needs(key0 + kBlock)) &&
+            if (!Cache::kBytes && (view.needs(key0) || view.needs(key0 + kBlock)) &&
                 (key0 + kTile > kt.hi || (key0 < kt.lo && key0 + kTile > kt.sink_hi))) {
               // values of keys in nobody's view: zeros (both slots' issuers write the same; neither's product reads the
-              // tile before its own are in)
+              // tile before its own are in; the converters of an 8-bit cache have left zeros there)
               const uint32_t v_tile = ring + stage * C::kTensor;
               for (int r = lane; r < kTile; r += 32) {
                 const int key = key0 + r;
@@ -752,26 +844,44 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
   }
 }
 
-// Launches a kernel of `rows` rows per CTA and key blocks of `block` slots per TMA box.
-template <typename C>
-pd_status launch(void (*kernel)(CUtensorMap, CUtensorMap, Params), int rows, int block, const pd_paged_attention_desc& d, const Params& p,
-                 const void* k_cache, const void* v_cache, cudaStream_t s) {
-  CUtensorMap tk, tv;
-  const int box = d.page_size < block ? d.page_size : block;
-  if (!make_cache_map(&tk, k_cache, d, box) || !make_cache_map(&tv, v_cache, d, box)) return PD_ERR_UNSUPPORTED;
-  static PerDeviceFlag smem_allowed;
+// Launches a kernel of `rows` rows per CTA.
+template <typename C, typename... KArgs, typename... Args>
+pd_status launch(void (*kernel)(KArgs...), int rows, const pd_paged_attention_desc& d, const Params& p, PerDeviceFlag& smem_allowed,
+                 cudaStream_t s, const Args&... args) {
   if (pd_status st = allow_dynamic_smem(kernel, C::kSmem, smem_allowed); st != PD_OK) return st;
   const int64_t tiles = ((int64_t)p.max_q_len * p.group + rows - 1) / rows;
   if (tiles * p.splits > 0x7fffffff) return PD_ERR_BAD_SHAPE;
-  launch_pdl(kernel, dim3((unsigned)(tiles * p.splits), d.heads_kv, d.batch), dim3(C::kThreads), C::kSmem, s, tk, tv, p);
+  launch_pdl(kernel, dim3((unsigned)(tiles * p.splits), d.heads_kv, d.batch), dim3(C::kThreads), C::kSmem, s, args..., p);
   return check_launch();
+}
+
+template <int D, pd_dtype T>
+pd_status launch_bytes(const pd_paged_attention_desc& d, const Params& p, const Scales& scales, const void* k_cache, const void* v_cache,
+                       cudaStream_t s) {
+  using Cache = ByteCache<T>;
+  using C = WideConfig<D, Cache>;
+  const Cache cache{static_cast<const uint8_t*>(k_cache), static_cast<const uint8_t*>(v_cache), d.page_stride, d.slot_stride, d.head_stride, scales};
+  static PerDeviceFlag smem_allowed;
+  return launch<C>(paged_attention_chunk_kernel<D, Cache>, C::kRows, d, p, smem_allowed, s, cache);
 }
 
 }  // namespace
 
 pd_status launch_chunk(const pd_paged_attention_desc& d, const Params& p, const void* k_cache, const void* v_cache, cudaStream_t s) {
-  if (d.head_dim == 128) return launch<WideConfig>(paged_attention_chunk_kernel, WideConfig::kRows, kTile, d, p, k_cache, v_cache, s);
-  return launch<NarrowConfig>(paged_attention_chunk_narrow_kernel, kTile, kBlock, d, p, k_cache, v_cache, s);
+  TiledCache cache;
+  const int block = d.head_dim == 128 ? kTile : kBlock, box = d.page_size < block ? d.page_size : block;
+  if (!make_cache_map(&cache.k, k_cache, d, box) || !make_cache_map(&cache.v, v_cache, d, box)) return PD_ERR_UNSUPPORTED;
+  static PerDeviceFlag wide_allowed, narrow_allowed;
+  using Wide = WideConfig<128, TiledCache>;
+  if (d.head_dim == 128) return launch<Wide>(paged_attention_chunk_kernel<128, TiledCache>, Wide::kRows, d, p, wide_allowed, s, cache);
+  return launch<NarrowConfig>(paged_attention_chunk_narrow_kernel, kTile, d, p, narrow_allowed, s, cache.k, cache.v);
+}
+
+pd_status launch_chunk_q8(const pd_paged_attention_desc& d, const Params& p, pd_dtype type, const Scales& scales, const void* k_cache,
+                          const void* v_cache, cudaStream_t s) {
+  if (d.head_dim == 64)
+    return type == PD_I8 ? launch_bytes<64, PD_I8>(d, p, scales, k_cache, v_cache, s) : launch_bytes<64, PD_E4M3>(d, p, scales, k_cache, v_cache, s);
+  return type == PD_I8 ? launch_bytes<128, PD_I8>(d, p, scales, k_cache, v_cache, s) : launch_bytes<128, PD_E4M3>(d, p, scales, k_cache, v_cache, s);
 }
 
 }  // namespace paged

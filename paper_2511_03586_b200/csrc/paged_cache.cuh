@@ -174,18 +174,20 @@ struct Plan {
   bool whole_items;
 };
 
-// Depends on the desc alone (the workspace size follows from it).  `smallest`: rows of the smallest tile.
-inline Plan plan(const pd_paged_attention_desc& d, int smallest = 16) {
+// Depends on the desc alone (the workspace size follows from it).  `smallest`: rows of the smallest tile;
+// `wide`: chunks take 256 rows and key tiles of 128 whatever the head_dim.
+inline Plan plan(const pd_paged_attention_desc& d, int smallest = 16, bool wide = false) {
   constexpr int kSms = 148;  // (not asked of the device: the workspace follows from the desc alone)
   Plan pl{};
+  const bool narrow = d.head_dim == 64 && !wide;
   const int64_t group = d.heads_q / d.heads_kv, rows = std::min(d.max_q_len, d.tokens) * group;
-  pl.rows_per_tile = rows <= smallest ? smallest : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : d.head_dim == 64 ? 128 : 256;
+  pl.rows_per_tile = rows <= smallest ? smallest : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : narrow ? 128 : 256;
   const bool chunk = pl.rows_per_tile > 64;
   const int64_t row_tiles = (rows + pl.rows_per_tile - 1) / pl.rows_per_tile;
   const int64_t items = row_tiles * d.heads_kv * d.batch;  // CTAs without splitting
   int64_t keys = d.max_kv_len;
   if (d.window > 0) keys = std::min<int64_t>(keys, (int64_t)d.window + d.sinks + d.max_q_len);
-  const int64_t tile = !chunk ? 64 : d.head_dim == 64 ? 64 : 128, tiles = (keys + tile - 1) / tile;
+  const int64_t tile = !chunk || narrow ? 64 : 128, tiles = (keys + tile - 1) / tile;
   if (!chunk) {
     // two CTAs per SM share all key tiles evenly; fewer when there are not enough tiles for that
     pl.whole_items = tiles <= 2;
@@ -194,8 +196,8 @@ inline Plan plan(const pd_paged_attention_desc& d, int smallest = 16) {
     return pl;
   }
   // One or four CTAs per SM, and splits only to fill the SMs, none below min_split_tiles.
-  pl.min_split_tiles = d.head_dim == 64 ? 8 : 4;
-  int64_t want = items > 0 ? kSms * (d.head_dim == 64 ? 4 : 1) / items : 1;
+  pl.min_split_tiles = narrow ? 8 : 4;
+  int64_t want = items > 0 ? kSms * (narrow ? 4 : 1) / items : 1;
   want = std::min<int64_t>(want, (tiles + pl.min_split_tiles - 1) / pl.min_split_tiles);
   pl.splits = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 256);
   return pl;
