@@ -43,6 +43,7 @@ constexpr int kSoftmaxWarps = 4;       // per slot
 constexpr int kStages = 4;
 constexpr int kHalf = kTile * 128;     // 64 columns of a tile: 128 lines of 128 bytes
 constexpr float kRaise = 8.f;          // powers of two by which a score may exceed the row's reference
+constexpr float kOffset = 7.f;         // powers of two more in P, as fp16: 2^(kRaise + kOffset) is below its largest
 
 // A special-function instruction that keeps its place among the others.
 __device__ __forceinline__ float ex2_in_order(float x) {
@@ -63,7 +64,7 @@ struct TiledCache {
   static constexpr bool kBytes = false;
   CUtensorMap k, v;
 };
-// An 8-bit cache: by plain loads of four warps, which multiply by the scales and round to bf16.
+// An 8-bit cache: by plain loads of four warps, which make fp16 of it; Q and P are fp16 then, too.
 template <pd_dtype TYPE>
 struct ByteCache {
   static constexpr bool kBytes = true;
@@ -99,14 +100,14 @@ struct SlotView {
 };
 
 // The output of a warp's 32 rows, one per lane: row (token t of the sequence, head), its reference m, sum l and accumulator (at
-// t_o, once `any` product has gone into it).  `stage`: shared memory that the warp may use, 32 lines of 128 bytes for every
+// t_o, in units of `unit`, once `any` product has gone into it).  `stage`: shared memory that the warp may use, 32 lines of 128 bytes for every
 // 64 columns (its rows of the Q tile, which every product has read by then).
 template <int D>
 __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq, int split, int t, int head, bool valid, bool any,
-                                           float m, float l, uint32_t t_o, uint32_t stage) {
+                                           float m, float l, float unit, uint32_t t_o, uint32_t stage) {
   const int lane = threadIdx.x & 31;
   tcgen05_fence_after_sync();
-  const float inv = l > 0.f ? 1.f / l : 0.f;  // nothing seen: zeros
+  const float inv = l > 0.f ? unit / l : 0.f;  // nothing seen: zeros
   const int64_t at = ((int64_t)split * p.part_tokens + seq.part0 + t) * p.heads_q + head;
   if (p.splits == 1) {
     // through shared memory, so that a store instruction writes whole rows
@@ -158,69 +159,118 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
   if (valid && p.splits > 1) p.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
 }
 
-// Keys and values of an 8-bit cache into the ring, as the bf16 numbers nearest to what they stand for: one of four warps, which
-// share every tile, 32 keys each.  A lane has 16 elements of a key at a time and loads a whole tile's worth of them ahead, while
-// the tile before is converted.  Keys in nobody's view, and ones without a page, become zeros.
-//   Conversion: a byte becomes fp16 (exact), fp32, times its scale, bf16: 3 to 4 instructions, as many for a tile of K or V as
-//   a sixth of what the softmax of the two slots takes.  Rounding keys and values to bf16 is off by 2^-9 of each in the mean; the scales
-//   kept apart from the products would cost the softmax, the busiest part, two multiplications a score instead.
+// Keys and values of an 8-bit cache into the ring, as fp16: one of four warps, which share every tile, 32 keys each.  A lane has
+// 16 elements of a key at a time and loads a whole tile's worth of them ahead, while the tile before is converted.  Keys in
+// nobody's view, and ones without a page, become zeros.
+//
+// A stored byte is exact in fp16.  Where the warp's 32 keys share a scale (blocks of 32 tokens and more, usually) that is what goes
+// into the product, and the scale goes with the group of 32 keys: to the softmax, which multiplies the group's scores by it, and for
+// values adds its logarithm to the exponents and takes it out of the sums.  Where they have several, the elements are
+// multiplied by their scale over the power of two below the largest one (as a high and a low fp16, so that the product is
+// rounded once, 2^-12 of it at most), and the power of two goes with the group.
+//   Instructions per tile and warp: 600 or 1000, where the softmax of the two slots takes 3300 of a scheduler's.  (Elements times their
+//   scales in fp32, rounded to bf16, took 1800, and 4 x 2048 tokens over up to 16384 keys 2033 us.)
+// factors: of the last four tiles, each 4 scales of keys and 4 logarithms of scales of values, as floats.
+template <pd_dtype T>
+__device__ __forceinline__ void convert_16(uint4 v, uint32_t (&out)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    if constexpr (T == PD_I8) q8_word_to_half<T, false>(__byte_perm(w[c], 0, 0x3120), out[2 * c], out[2 * c + 1]);
+    else q8_word_to_half<T, true>(w[c], out[2 * c], out[2 * c + 1]);
+  }
+}
 template <int D, typename Cache>
 __device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& p, const KeyTiles& kt, int kvh, int b, int begin, int end,
-                                              int warp, uint32_t ring, uint32_t bars, volatile int* abort_flag) {
+                                              int warp, uint32_t ring, uint32_t bars, uint32_t factors, volatile int* abort_flag) {
   constexpr int kLanes = D / 16, kRowsAtOnce = 32 / kLanes, kSteps = 32 / kRowsAtOnce, kTensor = kTile * D * 2;
   const int lane = threadIdx.x & 31, chunk = lane % kLanes, in_step = lane / kLanes;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 32u + 8u * s; };
   uint4 data[2][kSteps];
-  float scale[2][kSteps];
-  int page = 0;  // of step `lane % kSteps` (pages hold eight slots at least, a step's keys share one)
-  auto first_key = [&](int i) { return kt.tile_index(i) * kTile + warp * 32; };
-  auto load = [&](int i, int kv) {
-    const int key0 = first_key(i);
-    if (kv == 0) page = page_of(p, b, key0 + (lane % kSteps) * kRowsAtOnce);
+  float scale[2];          // of this lane's key, 0 where there is none
+  int64_t row_at = -1;     // where this lane's key is in the caches
+  auto load_data = [&](int kv) {
+    const uint8_t* from = (kv == 0 ? cache.k : cache.v) + 16 * chunk;
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
-      const int pg = __shfl_sync(0xffffffffu, page, j);
-      const int key = key0 + j * kRowsAtOnce + in_step, slot = key & (p.page_size - 1);
-      const bool there = pg < p.num_pages && ((key < kt.hi && key >= kt.lo) || key < kt.sink_hi);
-      const uint8_t* src = (kv == 0 ? cache.k : cache.v) + (int64_t)pg * cache.page_stride + (int64_t)slot * cache.slot_stride + (int64_t)kvh * cache.head_stride;
-      data[kv][j] = there ? __ldg(reinterpret_cast<const uint4*>(src) + chunk) : make_uint4(0, 0, 0, 0);
-      scale[kv][j] = there ? __ldg((kv == 0 ? cache.scales.k : cache.scales.v) + cache.scales.at(pg, kvh, slot)) : 0.f;
+      const int64_t at = __shfl_sync(0xffffffffu, row_at, j * kRowsAtOnce + in_step);
+      data[kv][j] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(from + at)) : make_uint4(0, 0, 0, 0);
     }
   };
+  auto look_up = [&](int i) {  // the tile's rows and scales
+    const int key = kt.tile_index(i) * kTile + warp * 32 + lane, slot = key & (p.page_size - 1);
+    const int page = page_of(p, b, key);
+    const bool there = page < p.num_pages && ((key < kt.hi && key >= kt.lo) || key < kt.sink_hi);
+    row_at = there ? (int64_t)page * cache.page_stride + (int64_t)slot * cache.slot_stride + (int64_t)kvh * cache.head_stride : -1;
+    scale[0] = there ? __ldg(cache.scales.k + cache.scales.at(page, kvh, slot)) : 0.f;
+    scale[1] = there ? __ldg(cache.scales.v + cache.scales.at(page, kvh, slot)) : 0.f;
+  };
   if (p.withhold_loads || begin >= end) return;
-  load(begin, 0);
-  load(begin, 1);
+  look_up(begin);
+  load_data(0);
+  load_data(1);
   int n = 0;
   for (int i = begin; i < end; ++i) {
+    // ---- the group's factors, and what is left for its keys
+    uint32_t pair[2];     // this lane's key: its scale over the group's factor, high and low fp16
+    bool uniform[2];
+    float factor[2];
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(scale[kv]));
+      uniform[kv] = __all_sync(0xffffffffu, row_at < 0 || __float_as_uint(scale[kv]) == most);
+      const uint32_t exponent = min(max(most >> 23, 1u), 253u);
+      factor[kv] = uniform[kv] ? __uint_as_float(most) : __uint_as_float(exponent << 23);
+      const float rest = scale[kv] * __uint_as_float((254u - exponent) << 23);  // below 2
+      const __half high = __float2half_rn(rest), low = __float2half_rn(rest - __half2float(high));
+      pair[kv] = (uint32_t)__half_as_ushort(high) | (uint32_t)__half_as_ushort(low) << 16;
+    }
+    if (lane == 0) {
+      const uint32_t to = factors + 32u * ((i - begin) & 3) + 4u * warp;
+      st_shared_f32(to, factor[0]);
+      st_shared_f32(to + 16u, log2f(factor[1]));
+    }
+    const bool no_values = factor[1] == 0.f;  // a scale of zero: zeros, whatever is stored
+    if (i + 1 < end) look_up(i + 1);
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv, ++n) {
       const int stage = n % kStages;
       if (!mbar_wait_warp(empty(stage), ((n / kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutChunkProducer, p.wait_limit_ns)) return;
-#pragma unroll
-      for (int j = 0; j < kSteps; ++j) {
-        const uint32_t w[4] = {data[kv][j].x, data[kv][j].y, data[kv][j].z, data[kv][j].w};
-        uint32_t out[8];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          constexpr bool kAdjacent = Cache::T != PD_I8;
-          uint32_t even, odd;
-          q8_word_to_half<Cache::T, kAdjacent>(w[c], even, odd);
-          const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), o = __half22float2(*reinterpret_cast<__half2*>(&odd));
-          const float s = scale[kv][j];
-          out[2 * c] = kAdjacent ? pack_bf16(a.x * s, a.y * s) : pack_bf16(a.x * s, o.x * s);
-          out[2 * c + 1] = kAdjacent ? pack_bf16(o.x * s, o.y * s) : pack_bf16(a.y * s, o.y * s);
-        }
+      auto store = [&](int j, const uint32_t (&out)[8]) {
         const int r = warp * 32 + j * kRowsAtOnce + in_step;
         const uint32_t row = ring + stage * kTensor + (chunk >> 2) * kHalf + (uint32_t)r * 128u;
 #pragma unroll
         for (int c = 0; c < 2; ++c)
           st_shared_v4(row + (uint32_t)((((2 * chunk + c) & 7) ^ (r & 7)) << 4), make_uint4(out[4 * c], out[4 * c + 1], out[4 * c + 2], out[4 * c + 3]));
+      };
+      if (uniform[kv]) {
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+          uint32_t out[8];
+          convert_16<Cache::T>(kv == 1 && no_values ? make_uint4(0, 0, 0, 0) : data[kv][j], out);
+          store(j, out);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+          uint32_t out[8];
+          convert_16<Cache::T>(data[kv][j], out);
+          const uint32_t mine = __shfl_sync(0xffffffffu, pair[kv], j * kRowsAtOnce + in_step);
+          const uint32_t high = __byte_perm(mine, 0, 0x1010), low = __byte_perm(mine, 0, 0x3232);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            uint32_t t;
+            asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(t) : "r"(out[c]), "r"(low));
+            asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(out[c]) : "r"(out[c]), "r"(high), "r"(t));
+          }
+          store(j, out);
+        }
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(full(stage));
-      if (i + 1 < end) load(i + 1, kv);
+      if (i + 1 < end) load_data(kv);
     }
   }
 }
@@ -240,6 +290,7 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
   auto p_full = [&](int s, int b) { return bars + 112u + 16u * s + 8u * b; };
   auto o_full = [&](int s, int b) { return bars + 144u + 16u * s + 8u * b; };  // the product that read buffer b has completed
   auto drained = [&](int w) { return bars + 176u + 8u * w; };  // of the four issuers
+  const uint32_t factors = bars + 256u;                        // 8-bit caches: of four tiles
   uint8_t* ctrl = smem_raw + (bars - smem_u32(smem_raw)) + 512;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + 4);
@@ -302,20 +353,46 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
       const bool valid = row < all_rows;
       const int t = valid ? row / p.group : 0, head = kvh * p.group + (valid ? row % p.group : 0);
       const int pos = seq.pos0 + t;
+      float row_scale = p.scale_log2e;
       if (view.active) {
         const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)(seq.q0 + t) * p.ld_q + (int64_t)head * D);
         const uint32_t dst = sQ + s * C::kTensor + (uint32_t)r * 128u;
+        float up = 1.f;
+        if constexpr (Cache::kBytes) {
+          // fp16: the row's largest magnitude is taken to [2^14, 2^15) by a power of two, which the scores are divided by again
+          uint32_t most = 0;
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c)
-          st_shared_v4(dst + (c >> 3) * kHalf + (uint32_t)(((c & 7) ^ (r & 7)) << 4), valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0));
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 v = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+            most = max(most, max(max((v.x << 16) & 0x7fffffffu, v.x & 0x7fff0000u), max((v.y << 16) & 0x7fffffffu, v.y & 0x7fff0000u)));
+            most = max(most, max(max((v.z << 16) & 0x7fffffffu, v.z & 0x7fff0000u), max((v.w << 16) & 0x7fffffffu, v.w & 0x7fff0000u)));
+          }
+          const int shift = min(max(14 + 127 - (int)(most >> 23), -126), 126);
+          up = __uint_as_float((uint32_t)(127 + shift) << 23);
+          row_scale *= __uint_as_float((uint32_t)(127 - shift) << 23);
+        }
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          uint4 v = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+          if constexpr (Cache::kBytes) {
+            auto half = [&](uint32_t two) {
+              const __half2 h = __floats2half2_rn(__uint_as_float(two << 16) * up, __uint_as_float(two & 0xffff0000u) * up);
+              return *reinterpret_cast<const uint32_t*>(&h);
+            };
+            v = make_uint4(half(v.x), half(v.y), half(v.z), half(v.w));
+          }
+          st_shared_v4(dst + (c >> 3) * kHalf + (uint32_t)(((c & 7) ^ (r & 7)) << 4), v);
+        }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full(s));
       }
       const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16);
       const uint32_t t_o = t_lane + C::kColO + s * D;
-      const uint64_t scale2 = pack_f32x2(p.scale_log2e, p.scale_log2e);
       float m = -INFINITY, l = 0.f;
+      // 8-bit caches: O is in units of 2^unit, at least the largest scale of values so far; P carries kOffset powers of two more,
+      // so that what fp16 loses of small exponentials is below 2^-32 of the largest
+      float unit = -1e30f;
       uint32_t done = 0;  // blocks of this slot
       bool ok = true;
       for (int b = 0; b < blocks; ++b) {
@@ -352,12 +429,31 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
 #pragma unroll
           for (int c = 0; c < 4; ++c)
             mx4[c] = max3(mx4[c], __uint_as_float(x[c >> 1][j + 2 * (c & 1)]), __uint_as_float(x[c >> 1][j + 2 * (c & 1) + 1]));
-        const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * p.scale_log2e;
+        // of either half of the block: the scale of its scores, and what its exponents get beside them
+        float scale[2] = {p.scale_log2e, p.scale_log2e}, shift[2] = {0.f, 0.f}, mx;
+        bool grown = false;
+        if constexpr (Cache::kBytes) {
+          const uint32_t at = factors + 32u * ((b >> 1) & 3) + 8u * (b & 1);
+          const float2 k = ld_shared_v2_f32(at), v = ld_shared_v2_f32(at + 16u);
+          scale[0] = fmaxf(k.x * row_scale, 1.17549435e-38f);  // (-inf times it stays -inf)
+          scale[1] = fmaxf(k.y * row_scale, 1.17549435e-38f);
+          mx = fmaxf(fmaxf(mx4[0], mx4[1]) * scale[0], fmaxf(mx4[2], mx4[3]) * scale[1]);
+          shift[0] = v.x;
+          shift[1] = v.y;
+          grown = fmaxf(v.x, v.y) > unit;
+        } else {
+          mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * p.scale_log2e;
+        }
         const bool raise = mx > m + kRaise;  // also the first finite score of a row (m = -inf)
-        if (__any_sync(0xffffffffu, raise)) {
-          const float alpha = raise ? ex2(m - mx) : 1.f;
+        if (__any_sync(0xffffffffu, raise || grown)) {
+          float alpha = raise ? ex2(m - mx) : 1.f;
           if (raise) m = mx;
           l *= alpha;
+          if (grown) {  // (all rows alike)
+            const float larger = ceilf(fmaxf(shift[0], shift[1])) + 1.f;
+            alpha *= ex2(unit - larger);
+            unit = larger;
+          }
           if (done > 0) {
             // every product into O so far has to be through with it; the one before last is, or these scores would not be here
             if (!mbar_wait_warp(o_full(s, buf ^ 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns)) { ok = false; break; }
@@ -374,8 +470,15 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
           }
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        const uint64_t nref2 = pack_f32x2(-ref, -ref);
-        uint64_t sum2[2] = {0, 0};
+        uint64_t scale2[2], nref2[2], sum2[2][2] = {{0, 0}, {0, 0}};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          // (a half without values to speak of is kept 100 powers of two below the unit, where the exponentials are still there to be added up)
+          if constexpr (Cache::kBytes) shift[h] = fmaxf(shift[h] - unit, -100.f);
+          const float add = Cache::kBytes ? kOffset + shift[h] - ref : -ref;
+          scale2[h] = pack_f32x2(scale[h], scale[h]);
+          nref2[h] = pack_f32x2(add, add);
+        }
         uint32_t pk[32];
         // Groups of sixteen, each group's sums and packing behind the next one's exponentials, in this order: left to the
         // compiler, the special-function unit stood idle between them (894 against 867 us for 4 x 2048 tokens; 790 with no
@@ -385,7 +488,7 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
           for (int j = 16 * g; j < 16 * g + 16; j += 2) {
             uint32_t(&v)[32] = x[j >> 5];
             float a0, a1;
-            unpack_f32x2(fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2, nref2), a0, a1);
+            unpack_f32x2(fma_f32x2(pack_b32x2(v[j & 31], v[(j & 31) + 1]), scale2[j >> 5], nref2[j >> 5]), a0, a1);
             v[j & 31] = __float_as_uint(a0);
             v[(j & 31) + 1] = __float_as_uint(a1);
           }
@@ -397,8 +500,14 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
 #pragma unroll
           for (int j = 16 * g; j < 16 * g + 16; j += 2) {
             uint32_t(&v)[32] = x[j >> 5];
-            sum2[(j >> 1) & 1] = add_f32x2(sum2[(j >> 1) & 1], pack_b32x2(v[j & 31], v[(j & 31) + 1]));
-            pk[j / 2] = pack_bf16(__uint_as_float(v[j & 31]), __uint_as_float(v[(j & 31) + 1]));
+            uint64_t& sum = sum2[Cache::kBytes ? j >> 5 : 0][(j >> 1) & 1];
+            sum = add_f32x2(sum, pack_b32x2(v[j & 31], v[(j & 31) + 1]));
+            if constexpr (Cache::kBytes) {
+              const __half2 h = __floats2half2_rn(__uint_as_float(v[j & 31]), __uint_as_float(v[(j & 31) + 1]));
+              pk[j / 2] = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+              pk[j / 2] = pack_bf16(__uint_as_float(v[j & 31]), __uint_as_float(v[(j & 31) + 1]));
+            }
           }
         };
         scale_group(0);
@@ -411,8 +520,14 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
         pack_group(3);
         tmem_st_32x32b_x32(t_s, pk);
         float s0, s1;
-        unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
-        l += s0 + s1;
+        unpack_f32x2(add_f32x2(sum2[0][0], sum2[0][1]), s0, s1);
+        if constexpr (Cache::kBytes) {
+          float s2, s3;
+          unpack_f32x2(add_f32x2(sum2[1][0], sum2[1][1]), s2, s3);
+          l += (s0 + s1) * ex2(-shift[0]) + (s2 + s3) * ex2(-shift[1]);
+        } else {
+          l += s0 + s1;
+        }
         tmem_st_wait();
         tcgen05_fence_before_sync();
         __syncwarp();
@@ -422,12 +537,13 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
       // ---- the row's output
       if (ok && done > 0) ok = mbar_wait_warp(o_full(s, (done - 1) & 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns);
       if (ok && view.active && *abort_flag == 0) {
-        write_rows<D>(p, seq, split, t, head, valid, done > 0, m, l, t_o, sQ + s * C::kTensor + (uint32_t)(quarter * 32) * 128u);
+        write_rows<D>(p, seq, split, t, head, valid, done > 0, Cache::kBytes ? m - kOffset : m, l, Cache::kBytes ? ex2(unit) : 1.f, t_o,
+                      sQ + s * C::kTensor + (uint32_t)(quarter * 32) * 128u);
       }
     } else if (warp >= kProducer) {
       if constexpr (Cache::kBytes) {
         // ---------------------------------------------------------------- converters
-        convert_tiles<D>(cache, p, kt, kvh, b, begin, end, warp - kProducer, ring, bars, abort_flag);
+        convert_tiles<D>(cache, p, kt, kvh, b, begin, end, warp - kProducer, ring, bars, factors, abort_flag);
       } else {
         // ------------------------------------------------------------------ producer
         const int box = min(p.page_size, kTile);
@@ -476,7 +592,7 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
       constexpr uint64_t kBlockStep = (kBlock * 128) >> 4;  // descriptor step from a tile's first block to its second
       if (((warp - kIssuer0) & 1) == 0) {
         // ---- scores; K tile t is in ring slot 2 t
-        constexpr uint32_t idesc = make_idesc_bf16(kTile, kBlock, false, false);
+        constexpr uint32_t idesc = Cache::kBytes ? make_idesc_f16(kTile, kBlock, false, false) : make_idesc_bf16(kTile, kBlock, false, false);
         const uint64_t q_desc = make_smem_desc(sQ + s * C::kTensor, 0, 1024);
         if (view.active) wait(q_full(s), 0);
         for (int b = 0; b < blocks && ok; ++b) {
@@ -504,7 +620,7 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
         }
       } else {
         // ---- output; V tile t is in ring slot 2 t + 1
-        constexpr uint32_t idesc = make_idesc_bf16(kTile, D, false, true);  // V is MN-major
+        constexpr uint32_t idesc = Cache::kBytes ? make_idesc_f16(kTile, D, false, true) : make_idesc_bf16(kTile, D, false, true);  // V is MN-major
         for (int b = 0; b < blocks && ok; ++b) {
           const int n = b | 1, stage = n % kStages;
           const int key0 = block_key(b);
@@ -740,7 +856,7 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
       if (ok && blocks > 0)
         ok = mbar_wait_warp(o_full, (blocks - 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns);
       if (ok && *abort_flag == 0)
-        write_rows<D>(p, seq, split, t, head, valid, blocks > 0, m, l, t_o, sQ + (uint32_t)(warp * 32) * 128u);
+        write_rows<D>(p, seq, split, t, head, valid, blocks > 0, m, l, 1.f, t_o, sQ + (uint32_t)(warp * 32) * 128u);
     } else {
       // ------------------------------------------- producer and issuer of both products
       const int box = min(p.page_size, kBlock);

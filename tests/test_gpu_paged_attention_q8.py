@@ -1,17 +1,18 @@
 """Attention over an 8-bit paged cache, against the definition in 64 bits.
 
-Tolerance, element by element: as for the bf16 cache (2^-8 of sum_j p_j |v_j| for the exponentials, 2^-8 of the result for its
-rounding, 2^-10 of the former for the fp32 parts), plus what comes of keys and values that are rounded to bf16 once they carry
-their scale: a value is off by 2^-8 of itself at most, 2^-8 of sum_j p_j |v_j| again; a score by 2^-8 sum_i |q_i k_i| scale at the
-very worst, and, since D independent roundings do not conspire, by less than six times their root mean square 2^-8 / sqrt(3)
-sqrt(sum_i (q_i k_i)^2) scale.  The weights move by that much, relative, and so does the result: by at most
-sum_j p_j e_j |v_j - out| <= e_max (sum_j p_j |v_j| + |out|).
+Tolerance, element by element.  Exponentials times the scales of values are rounded to fp16 for the second product (half a step:
+2^-11 relative) while their sum stays fp32: 2^-11 sum_j p_j |v_j|; the result is rounded to bf16 once, 2^-8 of itself; the fp32
+parts are held by 2^-10 sum_j p_j |v_j| as in the test of the bf16 cache.  Stored values are exact in fp16, but where keys of several
+scales share a group they are multiplied by their scales and rounded to fp16: another 2^-11 sum_j p_j |v_j| for the values, and
+for a score 2^-11 sum_i |q_i k_i| scale at the very worst; D independent roundings do not conspire, and their sum is less than six
+times its root mean square 2^-11 / sqrt(3) sqrt(sum_i (q_i k_i)^2) scale.  The weights move by that much, relative, and the result by
+at most sum_j p_j e_j |v_j - out| <= e_max (sum_j p_j |v_j| + |out|).
 
-The kernels for few rows take the exponentials times the scale of the values as fp16 instead, below 2^15 and in units of
-v_top / 2^11, with v_top less than twice the largest scale of a value in view.  That is 2^-11 of each, well within the 2^-8 above,
-down to fp16's smallest normal number, and half of its smallest number, 2^-25 units, below.  The sum of exponentials that it is
-divided by is at least 1, a stored value times the largest scale at most the largest value of the head, V (the largest value of a
-block takes up the type's range): another 2^-25 2^-11 2 V = 2^-35 V for every key."""
+Below its smallest normal number fp16 is off by half of its smallest one, 2^-25.  Exponentials with scales are in units of at most
+4 F / 2^7 (F: the largest scale of a value in view; the kernel for few rows: 2 F / 2^11), the sum that they are divided by is at
+least 1, and a stored value times F is at most the largest value of the head, V, since the largest value of a block takes up the
+type's range: 2^-25 2^-7 4 V = 2^-30 V for every key.  Values that were multiplied by their scales are in units of F at most: 2^-25 F,
+less than 2^-30 V once more."""
 import pytest
 import torch
 
@@ -110,9 +111,9 @@ class PagedQ8:
             group = q.shape[1] // self.k_seq[b].shape[1]
             # the largest root of sum_i (q_i k_i)^2 of a head's keys, bounded through the keys' elementwise maxima
             most = self.k_seq[b].abs().amax(0).repeat_interleave(group, 0) if kv else torch.zeros_like(q[0]).double()
-            e = 6 * 2 ** -8 / 3 ** 0.5 * (q.double() * most).pow(2).sum(-1, keepdim=True).sqrt() * (scale or q.shape[2] ** -0.5)
+            e = 6 * 2 ** -11 / 3 ** 0.5 * (q.double() * most).pow(2).sum(-1, keepdim=True).sqrt() * (scale or q.shape[2] ** -0.5)
             v_most = self.v_seq[b].abs().amax((0, 2)).repeat_interleave(group)[:, None] if kv else 0.0
-            bound = (2 * 2 ** -8 + 2 ** -10) * mag + 2 ** -8 * want.abs() + e * (mag + want.abs()) + 2 ** -35 * kv * v_most + 1e-30
+            bound = (2 * 2 ** -11 + 2 ** -10) * mag + 2 ** -8 * want.abs() + e * (mag + want.abs()) + 2 ** -30 * (kv + 1) * v_most + 1e-30
             worst = ((got - want).abs() / bound).max().item()
             assert worst <= 1.0, (b, n, kv, worst)
             start += n
