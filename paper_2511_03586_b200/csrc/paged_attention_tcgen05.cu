@@ -171,6 +171,22 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
 //   Instructions per tile and warp: 600 or 1000, where the softmax of the two slots takes 3300 of a scheduler's.  (Elements times their
 //   scales in fp32, rounded to bf16, took 1800, and 4 x 2048 tokens over up to 16384 keys 2033 us.)
 // factors: of the last four tiles, each 4 scales of keys and 4 logarithms of scales of values, as floats.
+
+// 16 bytes, or zeros; a load that stays where it is written (the compiler moves a plain one to where its result is used).
+__device__ __forceinline__ uint4 load_if(const uint8_t* from, bool there) {
+  uint4 v;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.u32 p, %5, 0;\n"
+      "mov.b32 %0, 0; mov.b32 %1, 0; mov.b32 %2, 0; mov.b32 %3, 0;\n"
+      "@p ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];\n"
+      "}\n"
+      : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
+      : "l"(from), "r"((uint32_t)there)
+      : "memory");
+  return v;
+}
 template <pd_dtype T>
 __device__ __forceinline__ void convert_16(uint4 v, uint32_t (&out)[8]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -188,51 +204,68 @@ __device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& 
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 32u + 8u * s; };
   uint4 data[2][kSteps];
-  float scale[2];          // of this lane's key, 0 where there is none
-  int64_t row_at = -1;     // where this lane's key is in the caches
-  auto load_data = [&](int kv) {
-    const uint8_t* from = (kv == 0 ? cache.k : cache.v) + 16 * chunk;
+  // Of the next tile: the page of every step's keys (pages hold eight slots at least, a step's four or eight keys share one),
+  // which keys there are, and this lane's key's scales (0 where there is none); of the one behind it this lane's key's page.
+  int pages[kSteps], page;
+  uint32_t there;
+  float scale[2];
+  auto first_key = [&](int i) { return kt.tile_index(i) * kTile + warp * 32; };
+  auto look_up = [&](int i) { page = i < end ? page_of(p, b, first_key(i) + lane) : p.num_pages; };
+  auto locate = [&](int i) {
+    if (i >= end) return;
+    const int key = first_key(i) + lane, slot = key & (p.page_size - 1);
+    const bool mine = page < p.num_pages && ((key < kt.hi && key >= kt.lo) || key < kt.sink_hi);
+    there = __ballot_sync(0xffffffffu, mine);
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) pages[j] = __shfl_sync(0xffffffffu, page, j * kRowsAtOnce);
+    const int64_t at = cache.scales.at(mine ? page : 0, kvh, slot);
+    scale[0] = mine ? __ldg(cache.scales.k + at) : 0.f;
+    scale[1] = mine ? __ldg(cache.scales.v + at) : 0.f;
+  };
+  auto load_data = [&](int i, int kv) {
+    if (i >= end) return;
+    const int key0 = first_key(i) + in_step;
+    const uint8_t* from = (kv == 0 ? cache.k : cache.v) + (int64_t)kvh * cache.head_stride + 16 * chunk;
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
-      const int64_t at = __shfl_sync(0xffffffffu, row_at, j * kRowsAtOnce + in_step);
-      data[kv][j] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(from + at)) : make_uint4(0, 0, 0, 0);
+      const int slot = (key0 + j * kRowsAtOnce) & (p.page_size - 1);
+      data[kv][j] = load_if(from + (int64_t)pages[j] * cache.page_stride + (int64_t)slot * cache.slot_stride, (there >> (j * kRowsAtOnce + in_step)) & 1u);
     }
   };
-  auto look_up = [&](int i) {  // the tile's rows and scales
-    const int key = kt.tile_index(i) * kTile + warp * 32 + lane, slot = key & (p.page_size - 1);
-    const int page = page_of(p, b, key);
-    const bool there = page < p.num_pages && ((key < kt.hi && key >= kt.lo) || key < kt.sink_hi);
-    row_at = there ? (int64_t)page * cache.page_stride + (int64_t)slot * cache.slot_stride + (int64_t)kvh * cache.head_stride : -1;
-    scale[0] = there ? __ldg(cache.scales.k + cache.scales.at(page, kvh, slot)) : 0.f;
-    scale[1] = there ? __ldg(cache.scales.v + cache.scales.at(page, kvh, slot)) : 0.f;
-  };
-  if (p.withhold_loads || begin >= end) return;
-  look_up(begin);
-  load_data(0);
-  load_data(1);
-  int n = 0;
-  for (int i = begin; i < end; ++i) {
-    // ---- the group's factors, and what is left for its keys
-    uint32_t pair[2];     // this lane's key: its scale over the group's factor, high and low fp16
-    bool uniform[2];
+  // The factors of tile i's group, and what is left for its keys: this lane's key's scale over the factor, as high and low fp16.
+  uint32_t pair[2];
+  bool uniform[2], no_values = false;
+  auto factor_out = [&](int i) {
+    if (i >= end) return;
     float factor[2];
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
       const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(scale[kv]));
-      uniform[kv] = __all_sync(0xffffffffu, row_at < 0 || __float_as_uint(scale[kv]) == most);
+      uniform[kv] = __all_sync(0xffffffffu, !((there >> lane) & 1u) || __float_as_uint(scale[kv]) == most);
       const uint32_t exponent = min(max(most >> 23, 1u), 253u);
       factor[kv] = uniform[kv] ? __uint_as_float(most) : __uint_as_float(exponent << 23);
       const float rest = scale[kv] * __uint_as_float((254u - exponent) << 23);  // below 2
       const __half high = __float2half_rn(rest), low = __float2half_rn(rest - __half2float(high));
       pair[kv] = (uint32_t)__half_as_ushort(high) | (uint32_t)__half_as_ushort(low) << 16;
     }
+    no_values = factor[1] == 0.f;  // a scale of zero: zeros, whatever is stored
     if (lane == 0) {
       const uint32_t to = factors + 32u * ((i - begin) & 3) + 4u * warp;
       st_shared_f32(to, factor[0]);
       st_shared_f32(to + 16u, log2f(factor[1]));
     }
-    const bool no_values = factor[1] == 0.f;  // a scale of zero: zeros, whatever is stored
-    if (i + 1 < end) look_up(i + 1);
+  };
+  if (p.withhold_loads || begin >= end) return;
+  look_up(begin);
+  locate(begin);
+  look_up(begin + 1);
+  load_data(begin, 0);
+  load_data(begin, 1);
+  factor_out(begin);
+  locate(begin + 1);
+  look_up(begin + 2);
+  int n = 0;
+  for (int i = begin; i < end; ++i) {
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv, ++n) {
       const int stage = n % kStages;
@@ -267,11 +300,16 @@ __device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& 
           store(j, out);
         }
       }
+      load_data(i + 1, kv);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(full(stage));
-      if (i + 1 < end) load_data(kv);
     }
+    // What needs an answer from the shared-memory pipe (it works through the stores above first, between the products' reads)
+    // comes once a tile, here.
+    factor_out(i + 1);
+    locate(i + 2);
+    look_up(i + 3);
   }
 }
 
