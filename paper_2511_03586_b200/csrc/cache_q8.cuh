@@ -74,6 +74,11 @@ __device__ __forceinline__ void q8_word_to_half(uint32_t w, uint32_t& even, uint
   }
 }
 
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
 // ---- host side -----------------------------------------------------------------------
 inline bool q8_dtype(pd_dtype t) { return t == PD_I8 || t == PD_E4M3; }
 // A power of two that divides the page.

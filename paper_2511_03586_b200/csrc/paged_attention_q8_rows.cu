@@ -21,8 +21,6 @@
 // scales with one 4-byte copy per block; all arrive on the stage's barrier.  Of the four consumer warps two share a tile, 32 keys
 // each, and the two pairs take tiles in turn (up to 32 rows), or each pair has its 32 of 64 rows.  A warp keeps a reference maximum
 // of its own, raised when a score exceeds it by 2^4; the warps' results meet at the end of a piece.
-#include <cuda_fp16.h>
-
 #include "cache_q8.cuh"
 #include "paged_rows.cuh"
 
@@ -69,10 +67,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
-}
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ void copy_async_4(uint32_t dst, const float* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");

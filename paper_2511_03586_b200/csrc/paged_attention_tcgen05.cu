@@ -61,13 +61,13 @@ __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu 
 
 // Where keys and values come from.  A bf16 cache: by TMA.
 struct TiledCache {
-  static constexpr bool kBytes = false;
+  static constexpr bool kBytes = false, kSwapped = false;
   CUtensorMap k, v;
 };
 // An 8-bit cache: by plain loads of four warps, which make fp16 of it; Q and P are fp16 then, too.
 template <pd_dtype TYPE>
 struct ByteCache {
-  static constexpr bool kBytes = true;
+  static constexpr bool kBytes = true, kSwapped = TYPE == PD_I8;  // elements 1 and 2 of every four in the tiles
   static constexpr pd_dtype T = TYPE;
   const uint8_t *k, *v;
   int64_t page_stride, slot_stride, head_stride;
@@ -101,11 +101,13 @@ struct SlotView {
 
 // The output of a warp's 32 rows, one per lane: row (token t of the sequence, head), its reference m, sum l and accumulator (at
 // t_o, in units of `unit`, once `any` product has gone into it).  `stage`: shared memory that the warp may use, 32 lines of 128 bytes for every
-// 64 columns (its rows of the Q tile, which every product has read by then).
-template <int D>
+// 64 columns (its rows of the Q tile, which every product has read by then).  SWAPPED: elements 1 and 2 of every four have
+// changed places in the accumulator.
+template <int D, bool SWAPPED>
 __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq, int split, int t, int head, bool valid, bool any,
                                            float m, float l, float unit, uint32_t t_o, uint32_t stage) {
   const int lane = threadIdx.x & 31;
+  auto place = [](int i) { return SWAPPED && (i % 4 == 1 || i % 4 == 2) ? i ^ 3 : i; };
   tcgen05_fence_after_sync();
   const float inv = l > 0.f ? unit / l : 0.f;  // nothing seen: zeros
   const int64_t at = ((int64_t)split * p.part_tokens + seq.part0 + t) * p.heads_q + head;
@@ -123,7 +125,7 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          w[j] = any ? pack_bf16(__uint_as_float(o[8 * u + 2 * j]) * inv, __uint_as_float(o[8 * u + 2 * j + 1]) * inv) : 0u;
+          w[j] = any ? pack_bf16(__uint_as_float(o[place(8 * u + 2 * j)]) * inv, __uint_as_float(o[place(8 * u + 2 * j + 1)]) * inv) : 0u;
         const int chunk = c / 8 + u;
         st_shared_v4(stage + (chunk >> 3) * kHalf + (uint32_t)lane * 128u + (uint32_t)(((chunk & 7) ^ (lane & 7)) << 4),
                      make_uint4(w[0], w[1], w[2], w[3]));
@@ -151,8 +153,8 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
         float4* dst = reinterpret_cast<float4*>(p.part_o + at * D + c);
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-          dst[u] = make_float4(__uint_as_float(o[4 * u]) * inv, __uint_as_float(o[4 * u + 1]) * inv,
-                               __uint_as_float(o[4 * u + 2]) * inv, __uint_as_float(o[4 * u + 3]) * inv);
+          dst[u] = make_float4(__uint_as_float(o[4 * u]) * inv, __uint_as_float(o[place(4 * u + 1)]) * inv,
+                               __uint_as_float(o[place(4 * u + 2)]) * inv, __uint_as_float(o[4 * u + 3]) * inv);
       }
     }
   }
@@ -163,7 +165,8 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
 // 16 elements of a key at a time and loads a whole tile's worth of them ahead, while the tile before is converted.  Keys in
 // nobody's view, and ones without a page, become zeros.
 //
-// A stored byte is exact in fp16.  Where the warp's 32 keys share a scale (blocks of 32 tokens and more, usually) that is what goes
+// A stored byte is exact in fp16.  (Of int8, bytes 0 and 2 of a word become one register and 1 and 3 the other: elements 1 and 2 of
+// every four change places, in K as in Q, and in V as in O, where they change back.)  Where the warp's 32 keys share a scale (blocks of 32 tokens and more, usually) that is what goes
 // into the product, and the scale goes with the group of 32 keys: to the softmax, which multiplies the group's scores by it, and for
 // values adds its logarithm to the exponents and takes it out of the sums.  Where they have several, the elements are
 // multiplied by their scale over the power of two below the largest one (as a high and a low fp16, so that the product is
@@ -172,19 +175,10 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
 //   scales in fp32, rounded to bf16, took 1800, and 4 x 2048 tokens over up to 16384 keys 2033 us.)
 // factors: of the last four tiles, each 4 scales of keys and 4 logarithms of scales of values, as floats.
 
-// 16 bytes, or zeros; a load that stays where it is written (the compiler moves a plain one to where its result is used).
-__device__ __forceinline__ uint4 load_if(const uint8_t* from, bool there) {
+// 16 bytes; a load that stays where it is written (the compiler moves a plain one to where its result is used).
+__device__ __forceinline__ uint4 load_now(const uint8_t* from) {
   uint4 v;
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "setp.ne.u32 p, %5, 0;\n"
-      "mov.b32 %0, 0; mov.b32 %1, 0; mov.b32 %2, 0; mov.b32 %3, 0;\n"
-      "@p ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];\n"
-      "}\n"
-      : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
-      : "l"(from), "r"((uint32_t)there)
-      : "memory");
+  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(from) : "memory");
   return v;
 }
 template <pd_dtype T>
@@ -192,44 +186,70 @@ __device__ __forceinline__ void convert_16(uint4 v, uint32_t (&out)[8]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    if constexpr (T == PD_I8) q8_word_to_half<T, false>(__byte_perm(w[c], 0, 0x3120), out[2 * c], out[2 * c + 1]);
-    else q8_word_to_half<T, true>(w[c], out[2 * c], out[2 * c + 1]);
+    q8_word_to_half<T, T != PD_I8>(w[c], out[2 * c], out[2 * c + 1]);
   }
 }
 template <int D, typename Cache>
 __device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& p, const KeyTiles& kt, int kvh, int b, int begin, int end,
                                               int warp, uint32_t ring, uint32_t bars, uint32_t factors, volatile int* abort_flag) {
   constexpr int kLanes = D / 16, kRowsAtOnce = 32 / kLanes, kSteps = 32 / kRowsAtOnce, kTensor = kTile * D * 2;
-  const int lane = threadIdx.x & 31, chunk = lane % kLanes, in_step = lane / kLanes;
+  // Eight lanes, whose 16-byte stores go together, have half of two neighbouring lines: the swizzle puts these into different banks.
+  const int lane = threadIdx.x & 31, chunk = D == 128 ? (lane & 3) | (lane >> 4) << 2 : lane & 3, in_step = D == 128 ? (lane >> 2) & 3 : lane >> 2;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 32u + 8u * s; };
   uint4 data[2][kSteps];
   // Of the next tile: the page of every step's keys (pages hold eight slots at least, a step's four or eight keys share one),
   // which keys there are, and this lane's key's scales (0 where there is none); of the one behind it this lane's key's page.
+  // Pages of 32 slots and more: the group has one page, and the lanes all look that up; blocks of 32 tokens and more: one scale.
   int pages[kSteps], page;
   uint32_t there;
   float scale[2];
+  const bool one_page = p.page_size >= 32, one_scale = cache.scales.shift >= 5;
   auto first_key = [&](int i) { return kt.tile_index(i) * kTile + warp * 32; };
-  auto look_up = [&](int i) { page = i < end ? page_of(p, b, first_key(i) + lane) : p.num_pages; };
+  auto look_up = [&](int i) {  // (the entry as it is: to look at it is to wait for it)
+    const int entry = i < end ? (first_key(i) + (one_page ? 0 : lane)) >> p.page_shift : p.max_pages;
+    page = -1;
+    if (entry < p.max_pages) page = __ldg(p.block_table + (int64_t)b * p.max_pages + entry);
+  };
   auto locate = [&](int i) {
     if (i >= end) return;
-    const int key = first_key(i) + lane, slot = key & (p.page_size - 1);
-    const bool mine = page < p.num_pages && ((key < kt.hi && key >= kt.lo) || key < kt.sink_hi);
-    there = __ballot_sync(0xffffffffu, mine);
+    const int key0 = first_key(i), slot = (key0 + (one_scale ? 0 : lane)) & (p.page_size - 1);
+    there = 0xffffffffu;
+    if (key0 < kt.lo || key0 + 32 > kt.hi) there = below(kt.hi - key0) & (~below(kt.lo - key0) | below(kt.sink_hi - key0));
+    const bool valid = (unsigned)page < (unsigned)p.num_pages;
+    if (one_page) {
+      pages[0] = page;
+      if (!valid) there = 0;
+    } else {
+      there &= __ballot_sync(0xffffffffu, valid);
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) pages[j] = __shfl_sync(0xffffffffu, page, j * kRowsAtOnce);
-    const int64_t at = cache.scales.at(mine ? page : 0, kvh, slot);
-    scale[0] = mine ? __ldg(cache.scales.k + at) : 0.f;
-    scale[1] = mine ? __ldg(cache.scales.v + at) : 0.f;
+      for (int j = 0; j < kSteps; ++j) pages[j] = __shfl_sync(0xffffffffu, page, j * kRowsAtOnce);
+    }
+    const bool mine = one_scale ? there != 0 : (there >> lane) & 1u;
+    scale[0] = scale[1] = 0.f;
+    if (mine) {
+      const int64_t at = cache.scales.at(page, kvh, slot);
+      scale[0] = __ldg(cache.scales.k + at);
+      scale[1] = __ldg(cache.scales.v + at);
+    }
   };
+  const int64_t lane_at = (int64_t)kvh * cache.head_stride + 16 * chunk;
   auto load_data = [&](int i, int kv) {
     if (i >= end) return;
     const int key0 = first_key(i) + in_step;
-    const uint8_t* from = (kv == 0 ? cache.k : cache.v) + (int64_t)kvh * cache.head_stride + 16 * chunk;
+    const uint8_t* from = (kv == 0 ? cache.k : cache.v) + lane_at;
+    if (one_page && there == 0xffffffffu) {
+      from += (int64_t)pages[0] * cache.page_stride + (int64_t)(key0 & (p.page_size - 1)) * cache.slot_stride;
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const int slot = (key0 + j * kRowsAtOnce) & (p.page_size - 1);
-      data[kv][j] = load_if(from + (int64_t)pages[j] * cache.page_stride + (int64_t)slot * cache.slot_stride, (there >> (j * kRowsAtOnce + in_step)) & 1u);
+      for (int j = 0; j < kSteps; ++j, from += kRowsAtOnce * cache.slot_stride) data[kv][j] = load_now(from);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        const int slot = (key0 + j * kRowsAtOnce) & (p.page_size - 1);
+        data[kv][j] = make_uint4(0, 0, 0, 0);
+        if ((there >> (j * kRowsAtOnce + in_step)) & 1u)
+          data[kv][j] = load_now(from + (int64_t)(one_page ? pages[0] : pages[j]) * cache.page_stride + (int64_t)slot * cache.slot_stride);
+      }
     }
   };
   // The factors of tile i's group, and what is left for its keys: this lane's key's scale over the factor, as high and low fp16.
@@ -237,22 +257,25 @@ __device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& 
   bool uniform[2], no_values = false;
   auto factor_out = [&](int i) {
     if (i >= end) return;
-    float factor[2];
+    float factor[2] = {scale[0], scale[1]};
+    uniform[0] = uniform[1] = true;
+    if (!one_scale) {
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(scale[kv]));
-      uniform[kv] = __all_sync(0xffffffffu, !((there >> lane) & 1u) || __float_as_uint(scale[kv]) == most);
-      const uint32_t exponent = min(max(most >> 23, 1u), 253u);
-      factor[kv] = uniform[kv] ? __uint_as_float(most) : __uint_as_float(exponent << 23);
-      const float rest = scale[kv] * __uint_as_float((254u - exponent) << 23);  // below 2
-      const __half high = __float2half_rn(rest), low = __float2half_rn(rest - __half2float(high));
-      pair[kv] = (uint32_t)__half_as_ushort(high) | (uint32_t)__half_as_ushort(low) << 16;
+      for (int kv = 0; kv < 2; ++kv) {
+        const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(scale[kv]));
+        uniform[kv] = __all_sync(0xffffffffu, !((there >> lane) & 1u) || __float_as_uint(scale[kv]) == most);
+        const uint32_t exponent = min(max(most >> 23, 1u), 253u);
+        factor[kv] = uniform[kv] ? __uint_as_float(most) : __uint_as_float(exponent << 23);
+        const float rest = scale[kv] * __uint_as_float((254u - exponent) << 23);  // below 2
+        const __half high = __float2half_rn(rest), low = __float2half_rn(rest - __half2float(high));
+        pair[kv] = (uint32_t)__half_as_ushort(high) | (uint32_t)__half_as_ushort(low) << 16;
+      }
     }
     no_values = factor[1] == 0.f;  // a scale of zero: zeros, whatever is stored
     if (lane == 0) {
       const uint32_t to = factors + 32u * ((i - begin) & 3) + 4u * warp;
       st_shared_f32(to, factor[0]);
-      st_shared_f32(to + 16u, log2f(factor[1]));
+      st_shared_f32(to + 16u, __log2f(factor[1]));
     }
   };
   if (p.withhold_loads || begin >= end) return;
@@ -413,11 +436,12 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
         for (int c = 0; c < D / 8; ++c) {
           uint4 v = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
           if constexpr (Cache::kBytes) {
-            auto half = [&](uint32_t two) {
-              const __half2 h = __floats2half2_rn(__uint_as_float(two << 16) * up, __uint_as_float(two & 0xffff0000u) * up);
-              return *reinterpret_cast<const uint32_t*>(&h);
-            };
-            v = make_uint4(half(v.x), half(v.y), half(v.z), half(v.w));
+            auto low = [&](uint32_t two) { return __uint_as_float(two << 16) * up; };
+            auto high = [&](uint32_t two) { return __uint_as_float(two & 0xffff0000u) * up; };
+            if constexpr (Cache::kSwapped)
+              v = make_uint4(pack_half(low(v.x), low(v.y)), pack_half(high(v.x), high(v.y)), pack_half(low(v.z), low(v.w)), pack_half(high(v.z), high(v.w)));
+            else
+              v = make_uint4(pack_half(low(v.x), high(v.x)), pack_half(low(v.y), high(v.y)), pack_half(low(v.z), high(v.z)), pack_half(low(v.w), high(v.w)));
           }
           st_shared_v4(dst + (c >> 3) * kHalf + (uint32_t)(((c & 7) ^ (r & 7)) << 4), v);
         }
@@ -541,8 +565,7 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
             uint64_t& sum = sum2[Cache::kBytes ? j >> 5 : 0][(j >> 1) & 1];
             sum = add_f32x2(sum, pack_b32x2(v[j & 31], v[(j & 31) + 1]));
             if constexpr (Cache::kBytes) {
-              const __half2 h = __floats2half2_rn(__uint_as_float(v[j & 31]), __uint_as_float(v[(j & 31) + 1]));
-              pk[j / 2] = *reinterpret_cast<const uint32_t*>(&h);
+              pk[j / 2] = pack_half(__uint_as_float(v[j & 31]), __uint_as_float(v[(j & 31) + 1]));
             } else {
               pk[j / 2] = pack_bf16(__uint_as_float(v[j & 31]), __uint_as_float(v[(j & 31) + 1]));
             }
@@ -575,7 +598,7 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
       // ---- the row's output
       if (ok && done > 0) ok = mbar_wait_warp(o_full(s, (done - 1) & 1), ((done - 1) >> 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns);
       if (ok && view.active && *abort_flag == 0) {
-        write_rows<D>(p, seq, split, t, head, valid, done > 0, Cache::kBytes ? m - kOffset : m, l, Cache::kBytes ? ex2(unit) : 1.f, t_o,
+        write_rows<D, Cache::kSwapped>(p, seq, split, t, head, valid, done > 0, Cache::kBytes ? m - kOffset : m, l, Cache::kBytes ? ex2(unit) : 1.f, t_o,
                       sQ + s * C::kTensor + (uint32_t)(quarter * 32) * 128u);
       }
     } else if (warp >= kProducer) {
@@ -894,7 +917,7 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
       if (ok && blocks > 0)
         ok = mbar_wait_warp(o_full, (blocks - 1) & 1u, abort_flag, p.status, kTimeoutChunkSoftmax, p.wait_limit_ns);
       if (ok && *abort_flag == 0)
-        write_rows<D>(p, seq, split, t, head, valid, blocks > 0, m, l, 1.f, t_o, sQ + (uint32_t)(warp * 32) * 128u);
+        write_rows<D, false>(p, seq, split, t, head, valid, blocks > 0, m, l, 1.f, t_o, sQ + (uint32_t)(warp * 32) * 128u);
     } else {
       // ------------------------------------------- producer and issuer of both products
       const int box = min(p.page_size, kBlock);
