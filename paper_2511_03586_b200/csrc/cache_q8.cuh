@@ -92,24 +92,27 @@ inline Scales make_scales(const pd_cache_scales& s, int heads_kv, int page_size)
   return r;
 }
 
-// Tensor map of one cache: {head_dim, page_size, heads_kv, num_pages} bytes, boxes of a head's elements x `box_rows` slots.
-inline bool make_cache_map_q8(CUtensorMap* map, const void* cache, const pd_paged_attention_desc& d, int box_rows) {
+// Tensor map of one cache: {head_dim, page_size, heads_kv, num_pages} bytes, boxes of `box_rows` slots of `box_heads` heads.  What
+// is fetched beside a box's rows belongs to other heads, which other CTAs read at other times: promotion to 256 bytes fetched
+// twice what rows of 128 need (64 x 1 tokens: 150 against 140 us).
+inline bool make_cache_map_q8(CUtensorMap* map, const void* cache, const pd_paged_attention_desc& d, int box_rows, int box_heads) {
   gemm::EncodeTiledFn fn = gemm::encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t dims[4] = {(cuuint64_t)d.head_dim, (cuuint64_t)d.page_size, (cuuint64_t)d.heads_kv, (cuuint64_t)d.num_pages};
   const cuuint64_t strides[3] = {(cuuint64_t)d.slot_stride, (cuuint64_t)d.head_stride, (cuuint64_t)d.page_stride};
-  const cuuint32_t box[4] = {(cuuint32_t)d.head_dim, (cuuint32_t)box_rows, 1, 1};
+  const cuuint32_t box[4] = {(cuuint32_t)d.head_dim, (cuuint32_t)box_rows, (cuuint32_t)box_heads, 1};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(cache), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            d.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            d.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+            d.head_dim == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_64B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Launchers (each in its own file).  `rows_per_tile` of the row kernel: 8, 16, 32 or 64.
+// Launchers (each in its own file).
 pd_status launch_chunk_q8(const pd_paged_attention_desc& d, const Params& p, pd_dtype type, const Scales& scales, const void* k_cache,
                           const void* v_cache, cudaStream_t s);
-pd_status launch_rows_q8(const pd_paged_attention_desc& d, Params& p, pd_dtype type, const Scales& scales, const void* k_cache,
-                         const void* v_cache, int rows_per_tile, cudaStream_t s);
+pd_status launch_rows_q8(const pd_paged_attention_desc& d, const Params& p, const Plan& plan, pd_dtype type, const Scales& scales,
+                         const void* k_cache, const void* v_cache, cudaStream_t s);
 
 }  // namespace paged
 }  // namespace pd

@@ -6,7 +6,23 @@ namespace pd {
 namespace paged {
 namespace {
 
-Plan plan_q8(const pd_paged_attention_desc& d) { return plan(d, 8, true); }
+// Row kernel: up to four warps beside each other take cache heads (the rows of a slot that lie beside each other in the usual
+// layout), as many as divide the heads; the rest of the four share keys, or rows.
+Plan plan_q8(const pd_paged_attention_desc& d) {
+  Plan pl{};
+  const int64_t rows = plan_rows(d);
+  pl.rows_per_tile = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
+  if (pl.rows_per_tile > 64) {
+    plan_splits(d, pl);
+    return pl;
+  }
+  const int warps = 4 * 16 / std::max(pl.rows_per_tile, 16);  // that have different heads or keys
+  pl.heads_per_item = warps;
+  while (d.heads_kv % pl.heads_per_item != 0) pl.heads_per_item /= 2;
+  pl.tile = 32 * warps / pl.heads_per_item;
+  plan_shares(d, pl);
+  return pl;
+}
 
 }  // namespace
 }  // namespace paged
@@ -49,7 +65,7 @@ extern "C" pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* de
   const paged::Scales sc = paged::make_scales(*scales, d.heads_kv, d.page_size);
   logf("paged attention (%s) batch %d tokens %d (max %d) heads %d/%d x %d: tiles of %d rows, %s %d", scales->dtype == PD_I8 ? "int8" : "e4m3",
        d.batch, d.tokens, d.max_q_len, d.heads_q, d.heads_kv, d.head_dim, pl.rows_per_tile, pl.rows_per_tile > 64 ? "key splits" : "CTAs", pl.splits);
-  if (pl.rows_per_tile <= 64) return paged::launch_rows_q8(d, p, scales->dtype, sc, k_cache, v_cache, pl.rows_per_tile, stream);
+  if (pl.rows_per_tile <= 64) return paged::launch_rows_q8(d, p, pl, scales->dtype, sc, k_cache, v_cache, stream);
   if (pd_status st = paged::launch_chunk_q8(d, p, scales->dtype, sc, k_cache, v_cache, stream); st != PD_OK) return st;
   return pl.splits > 1 ? paged::launch_join(d, p, stream) : PD_OK;
 }

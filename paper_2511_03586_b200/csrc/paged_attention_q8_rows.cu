@@ -17,10 +17,12 @@
 //      2^-26 and less of the largest is off by up to 2^-36 of that).  The power follows the largest vs_j that the warp has met.
 //   O: fp32 sums.  The row sums of the exponentials are fp32, too, and of the unrounded ones.
 //
-// A producer warp copies key tiles of 64 keys, K and V of one tile to a stage, by TMA, one box per page and tensor, and their
-// scales with one 4-byte copy per block; all arrive on the stage's barrier.  Of the four consumer warps two share a tile, 32 keys
-// each, and the two pairs take tiles in turn (up to 32 rows), or each pair has its 32 of 64 rows.  A warp keeps a reference maximum
-// of its own, raised when a score exceeds it by 2^4; the warps' results meet at the end of a piece.
+// A producer warp copies key tiles by TMA, one box per page and tensor, and their scales with one 4-byte copy per block; K (with
+// all scales) and V of a tile are a stage of the ring each.  Four consumer warps take 32 keys of a tile each.  In the usual layout a
+// slot's heads lie beside each other, 64 or 128 bytes each, and a tile of one head would take that much of every slot: DRAM
+// delivered 4.2 TB/s so.  So the warps take up to four neighbouring heads, and a box has the rows of all of them; where there are fewer
+// heads, warps share the keys of a tile, and more than 16 rows are shared by two or four warps.  A warp keeps a reference maximum of its
+// own, raised when a score exceeds it by 2^4; warps with the same rows meet at the end of a piece.
 #include "cache_q8.cuh"
 #include "paged_rows.cuh"
 
@@ -28,34 +30,27 @@ namespace pd {
 namespace paged {
 namespace {
 
-constexpr int kTile = 64;        // keys per stage
 constexpr int kKeys = 32;        // of a tile, per warp
 constexpr int kConsumers = 4;    // warps
 constexpr int kThreads = 32 * (kConsumers + 1);
 constexpr float kRaise = 4.f;    // powers of two by which a score may exceed the reference
 constexpr float kTopP = 2048.f;  // 2^(15 - kRaise): the largest vs_j times the power of two that goes with P
 
-template <int D, int NR, int WR>
+// H cache heads side by side, WK warps that share a tile's keys, WR that share the rows; NR groups of 8 rows to a warp.
+template <int D, int NR, int H, int WK, int WR>
 struct Q8Config {
-  static constexpr int kWK = WR < 4 ? kTile / kKeys : 1; // warps that share a tile's keys
-  static constexpr int kWT = kConsumers / (kWK * WR);   // groups of warps that take tiles in turn
+  static_assert(H * WK * WR == kConsumers);
+  static constexpr int kTile = kKeys * WK;              // keys
   static constexpr int kGroupRows = 8 * NR;             // rows of a warp
   static constexpr int kRows = kGroupRows * WR;
-  static constexpr int kTensorBytes = kTile * D;        // K or V of a tile
-  static constexpr int kScaleBytes = 2 * kTile * 4;     // a scale per key at most, for K and for V
-  static constexpr int kStageBytes = 2 * kTensorBytes;
-  static constexpr int kParts = kConsumers / WR;        // warps with the same rows
-  static constexpr int kMergeStride = D + 2;
-  static constexpr int kExchange = WR * (kParts / 2) * 512 * NR * (D / 16 + 1);  // half the warps' results, 16 bytes per lane and step
-  static constexpr int kRowsOut = kRows * kMergeStride * 4;
-  static constexpr int kMerge = kExchange > kRowsOut ? kExchange : kRowsOut;
-  static constexpr int kPerCta = 112 * 1024 - 2048;     // two CTAs per SM
-  static constexpr int kFit = (kPerCta - kMerge) / (kStageBytes + kScaleBytes);
-  // A multiple of kWT: the tile that was in a stage before is then the same warps' tile.  They have seen it complete, which a
-  // wait by parity relies on: two phases ahead of an incomplete one it would find the parity of the one before that.
-  static constexpr int kStages = (kFit > 8 ? 8 : kFit) / kWT * kWT;
-  static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kMerge + 256 /*barriers*/ + 1024 /*alignment*/;
-  static_assert(2 * (kSmem + 1024) <= 228 * 1024 && kStages >= 3);
+  static constexpr int kStageBytes = H * kTile * D;     // K or V of a tile
+  static constexpr int kScaleBytes = 2 * H * kTile * 4; // a scale per key at most, for K and for V
+  static constexpr int kExchange = WK > 1 ? H * WR * (WK / 2) * 512 * (D / 16 + 1) : 0;  // half the warps' results for 8 rows
+  static constexpr int kPerCta = 113 * 1024 - 256 /*barriers*/ - 1024 /*alignment*/;     // two CTAs per SM
+  static constexpr int kFit = (kPerCta - kExchange) / (kStageBytes + kScaleBytes);
+  static constexpr int kStages = kFit > 8 ? 8 : kFit;
+  static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kExchange + 256 + 1024;
+  static_assert(2 * (kSmem + 1024) <= 228 * 1024 && kStages >= 4);
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -76,24 +71,25 @@ __device__ __forceinline__ void arrive_after_copies(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-template <pd_dtype T, int D, int NR, int WR>
+template <pd_dtype T, int D, int NR, int H, int WK, int WR>
 __global__ void __launch_bounds__(kThreads, 2)
 paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const Params p,
                                const Scales scales) {
-  using C = Q8Config<D, NR, WR>;
+  using C = Q8Config<D, NR, H, WK, WR>;
+  constexpr int kTile = C::kTile, kTileShift = kTile == 32 ? 5 : kTile == 64 ? 6 : 7;
   constexpr bool kAdjacent = T != PD_I8;  // K's words: bytes 0 and 1 together, else 0 and 2
   extern __shared__ uint8_t smem_raw[];
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t scale_ring = ring + C::kStages * C::kStageBytes, merge_at = scale_ring + C::kStages * C::kScaleBytes;
-  float* merge = reinterpret_cast<float*>(smem_raw + (merge_at - smem_u32(smem_raw)));
-  const uint32_t bars = merge_at + C::kMerge;
+  const uint32_t scale_ring = ring + C::kStages * C::kStageBytes, exchange_at = scale_ring + C::kStages * C::kScaleBytes;
+  float* exchange = reinterpret_cast<float*>(smem_raw + (exchange_at - smem_u32(smem_raw)));
+  const uint32_t bars = exchange_at + C::kExchange;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 64u + 8u * s; };
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + (bars - smem_u32(smem_raw)) + 128);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::kStages; ++s) { mbar_init(full(s), 1 + 32); mbar_init(empty(s), kConsumers / C::kWT); }
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(full(s), 1 + 32); mbar_init(empty(s), kConsumers); }
     *abort_flag = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
@@ -103,58 +99,69 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
   griddep_wait();
   griddep_launch_dependents();
 
-  Piece w;
+  Piece w;  // (w.kvh counts groups of H cache heads)
   int start, stop, share;
-  if (!first_piece<kThreads>(p, blockIdx.x, w, start, stop, share)) return;
-  const int scale_shift = min(scales.shift, 6);  // blocks of 64 tokens and more: one scale per tile
+  if (!first_piece<kThreads, kTile>(p, blockIdx.x, w, start, stop, share)) return;
+  const int box_shift = min(p.page_shift, kTileShift);      // slots of a page's box
+  const int scale_shift = min(scales.shift, kTileShift), blocks = kTile >> scale_shift;  // scales of a tile and head
 
   if (warp == kConsumers) {
     // ------------------------------------------------------------------ producer
-    // Per stage: 64 / page_size pages (or a part of one), each a box of `box` slots.  The lanes hold the pages of the next
-    // `per_batch` tiles.
-    const int box = min(p.page_size, kTile);
-    const int per_tile = kTile / box;
-    const int per_batch = 32 / per_tile;
-    const int blocks = kTile >> scale_shift;
+    // Per stage: kTile / page_size pages (or a part of one), each a box of slots of H heads that a lane of its own requests.  The
+    // lanes hold the pages of `per_batch` tiles, and the table's entries for as many behind them.
+    const int tile_shift = kTileShift - box_shift, batch_shift = 5 - tile_shift;
+    const int in_tile = lane & ((1 << tile_shift) - 1);
     bool ok = !p.withhold_loads;
-    int n = 0;  // stages requested so far
+    int stage = 0, n = 0;  // stages requested so far
+    uint32_t phase = 1;
+    auto request = [&](const CUtensorMap* map, int slot, int pg) {  // waits for the stage, and asks for one of the tensors
+      if (!mbar_wait_warp(empty(stage), phase, abort_flag, p.status, kTimeoutRowsProducer, p.wait_limit_ns)) return false;
+      if (lane == 0) mbar_arrive_expect_tx(full(stage), C::kStageBytes);
+      __syncwarp();
+      if (lane < (1 << tile_shift))
+        tma_load_4d(ring + stage * C::kStageBytes + (uint32_t)(lane << box_shift) * (H * D), map, full(stage), 0, slot, w.kvh * H, pg);
+      return true;
+    };
+    auto advance = [&]() {
+      arrive_after_copies(full(stage));
+      ++n;
+      if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+    };
     while (ok) {
       const int end = min(w.end, w.tiles.n);
-      int page = 0;
-      for (int i = w.begin; i < end; ++i, ++n) {
-        const int in_batch = (i - w.begin) % per_batch;
+      auto entry_of = [&](int i) {  // of the lane's tile and page in the batch that begins with tile i; -1: none
+        const int ti = i + (lane >> tile_shift);
+        const int at = ti < end ? (w.tiles.tile_index(ti) * kTile + (in_tile << box_shift)) >> p.page_shift : p.max_pages;
+        int e = -1;
+        if (at < p.max_pages) e = __ldg(p.block_table + (int64_t)w.b * p.max_pages + at);
+        return e;
+      };
+      int ahead = entry_of(w.begin), page = 0;
+      for (int i = w.begin; i < end; ++i) {
+        const int in_batch = (i - w.begin) & ((1 << batch_shift) - 1);
         if (in_batch == 0) {
-          const int ti = i + lane / per_tile;
-          page = ti < end ? page_of(p, w.b, w.tiles.tile_index(ti) * kTile + (lane % per_tile) * box) : 0;
+          page = (unsigned)ahead < (unsigned)p.num_pages ? ahead : p.num_pages;
+          ahead = entry_of(i + (1 << batch_shift));
         }
         const int slot = (w.tiles.tile_index(i) * kTile) & (p.page_size - 1);  // 0 unless a page holds several tiles
-        const int stage = n % C::kStages;
-        if (!mbar_wait_warp(empty(stage), ((n / C::kStages) & 1u) ^ 1u, abort_flag, p.status, kTimeoutRowsProducer, p.wait_limit_ns)) { ok = false; break; }
-        if (elect_one()) mbar_arrive_expect_tx(full(stage), C::kStageBytes);
-        __syncwarp();
-        const uint32_t to = ring + stage * C::kStageBytes;
-        for (int j = 0; j < per_tile; ++j) {
-          const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + j);
-          if (elect_one()) {
-            tma_load_4d(to + (uint32_t)(j * box * D), &tmap_k, full(stage), 0, slot, w.kvh, pg);
-            tma_load_4d(to + C::kTensorBytes + (uint32_t)(j * box * D), &tmap_v, full(stage), 0, slot, w.kvh, pg);
-          }
-          __syncwarp();
-        }
-        for (int e0 = 0; e0 < blocks; e0 += 32) {
-          const int e = e0 + lane, key = e << scale_shift;  // of the tile
-          const int pg = __shfl_sync(0xffffffffu, page, in_batch * per_tile + min(key, kTile - 1) / box);
-          if (e < blocks) {
-            const bool there = pg < p.num_pages;
-            const int64_t at = there ? scales.at(pg, w.kvh, slot + key % box) : 0;
+        const int pg = __shfl_sync(0xffffffffu, page, (in_batch << tile_shift) + in_tile);
+        if (!request(&tmap_k, slot, pg)) { ok = false; break; }
+        for (int e0 = 0; e0 < H * blocks; e0 += 32) {
+          const int e = e0 + lane, h = e / blocks, key = (e - h * blocks) << scale_shift;  // (a power of two)
+          const int mine = __shfl_sync(0xffffffffu, page, (in_batch << tile_shift) + (key >> box_shift));
+          if (e < H * blocks) {
+            const bool there = mine < p.num_pages;
+            const int64_t at = there ? scales.at(mine, w.kvh * H + h, slot + (key & ((1 << box_shift) - 1))) : 0;
             const uint32_t dst = scale_ring + stage * C::kScaleBytes + 4u * e;
             copy_async_4(dst, scales.k + at, there);
-            copy_async_4(dst + 4u * kTile, scales.v + at, there);
+            copy_async_4(dst + 4u * H * kTile, scales.v + at, there);
           }
         }
-        arrive_after_copies(full(stage));
+        advance();
+        if (!request(&tmap_v, slot, pg)) { ok = false; break; }
+        advance();
       }
-      if (!ok || !next_piece(p, w, stop)) break;
+      if (!ok || !next_piece<kTile>(p, w, stop)) break;
     }
     // Leave no copy in flight, whichever warp gives up: the last request of every stage gets a short time to land.
     volatile int never = 0;
@@ -164,18 +171,30 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
   }
 
   // ------------------------------------------------------------------- consumers
-  const int wk = warp % C::kWK, wr = WR > 1 ? warp / C::kWK : 0, wt = WR > 1 ? 0 : warp / C::kWK;
+  const int hs = warp % H, wk = warp / H % WK, wr = warp / (H * WK);
   constexpr int KS = D / 16, MT = D / 16;  // steps of 16 elements; tiles of 16 elements
   const int g = lane >> 2, i4 = lane & 3;
-  // this lane's ldmatrix row: key within 16, and which of two neighbouring 16-byte chunks
-  const int mat_key = lane & 15, mat_chunk = lane >> 4;
-  auto chunk_at = [&](uint32_t tensor, int key, int chunk) {
-    if constexpr (D == 128) return tensor + (uint32_t)key * 128u + (uint32_t)((chunk ^ (key & 7)) << 4);
-    else return tensor + (uint32_t)key * 64u + (uint32_t)((chunk ^ ((key >> 1) & 3)) << 4);
+  // this lane's ldmatrix rows (a key of either 16 of the warp's) within a stage, and which of two neighbouring 16-byte chunks
+  const int mat_chunk = lane >> 4;
+  uint32_t mat_row[2];
+  int mat_swizzle[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int key = wk * kKeys + 16 * h + (lane & 15);
+    mat_row[h] = (uint32_t)(((((key >> box_shift) * H + hs) << box_shift) + (key & ((1 << box_shift) - 1))) * D);
+    mat_swizzle[h] = D == 128 ? key & 7 : (key >> 1) & 3;
+  }
+  auto chunk_at = [&](uint32_t tensor, int h, int chunk) { return tensor + mat_row[h] + (uint32_t)((chunk ^ mat_swizzle[h]) << 4); };
+  int stage = 0;
+  uint32_t phase = 0;
+  auto advance = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(empty(stage));
+    if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
   };
-  int n = 0;  // stages so far, of all warps
   for (int piece = 0;; ++piece) {
     const int first_pos = w.seq.pos0, last_pos = w.seq.pos0 + w.seq.n - 1;
+    const int kvh = w.kvh * H + hs;
     const KeyTiles& kt = w.tiles;
     // ---- queries: row 8 r + g of the warp's, elements 16 k + 4 i ... + 3 of it
     uint32_t qf[NR][KS][2];
@@ -187,7 +206,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
       for (int r = 0; r < NR; ++r) {
         const int row = min(wr * C::kGroupRows + 8 * r + g, w.rows - 1);  // (rows beyond the last repeat it and are not stored)
         const int t = row / p.group;
-        const __nv_bfloat16* src = p.q + (int64_t)(w.seq.q0 + t) * p.ld_q + (int64_t)(w.kvh * p.group + row % p.group) * D + 4 * i4;
+        const __nv_bfloat16* src = p.q + (int64_t)(w.seq.q0 + t) * p.ld_q + (int64_t)(kvh * p.group + row % p.group) * D + 4 * i4;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           raw[r][k] = __ldg(reinterpret_cast<const uint2*>(src + 16 * k));
@@ -227,262 +246,277 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
 
     bool failed = false;
     const int end = min(w.end, kt.n);
-    for (int i = w.begin; i < end; ++i, ++n) {
-      if (C::kWT > 1 && n % C::kWT != wt) continue;
-      const int stage = n % C::kStages;
-      // (a warp that gives up goes on to the barrier below, which tells the others)
-      if (!mbar_wait_warp(full(stage), (n / C::kStages) & 1u, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
-      const uint32_t sk = ring + stage * C::kStageBytes, sv = sk + C::kTensorBytes, sc = scale_ring + stage * C::kScaleBytes;
-#pragma unroll 1
-      for (int in_tile = wk * kKeys; in_tile < kTile; in_tile += C::kWK * kKeys) {
-        const int key0 = kt.tile_index(i) * kTile + in_tile;
-        // ---- S^T = K Q^T, two tiles of 16 keys
-        float s[2][NR][4];
+    for (int i = w.begin; i < end; ++i) {
+      // (a warp that gives up goes on to the barrier below, if there is one, which tells the others)
+      if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
+      const uint32_t sk = ring + stage * C::kStageBytes, sc = scale_ring + stage * C::kScaleBytes + 4u * (uint32_t)(hs * blocks);
+      const int key0 = kt.tile_index(i) * kTile + wk * kKeys;
+      // ---- S^T = K Q^T, two tiles of 16 keys
+      float s[2][NR][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-          for (int r = 0; r < NR; ++r) s[h][r][0] = s[h][r][1] = s[h][r][2] = s[h][r][3] = 0.f;
+        for (int r = 0; r < NR; ++r) s[h][r][0] = s[h][r][1] = s[h][r][2] = s[h][r][3] = 0.f;
 #pragma unroll
-          for (int k = 0; k < KS; k += 2) {
-            uint32_t kw[4];  // words of keys 0-7 and 8-15, of this step's 16 elements and the next one's
-            ldmatrix_x4(chunk_at(sk, in_tile + 16 * h + mat_key, k + mat_chunk), kw);
+        for (int k = 0; k < KS; k += 2) {
+          uint32_t kw[4];  // words of keys 0-7 and 8-15, of this step's 16 elements and the next one's
+          ldmatrix_x4(chunk_at(sk, h, k + mat_chunk), kw);
 #pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
-              uint32_t a0, a1, a2, a3;
-              q8_word_to_half<T, kAdjacent>(kw[2 * k2], a0, a2);
-              q8_word_to_half<T, kAdjacent>(kw[2 * k2 + 1], a1, a3);
+          for (int k2 = 0; k2 < 2; ++k2) {
+            uint32_t a0, a1, a2, a3;
+            q8_word_to_half<T, kAdjacent>(kw[2 * k2], a0, a2);
+            q8_word_to_half<T, kAdjacent>(kw[2 * k2 + 1], a1, a3);
 #pragma unroll
-              for (int r = 0; r < NR; ++r) mma_f16(s[h][r], a0, a1, a2, a3, qf[r][k + k2][0], qf[r][k + k2][1]);
-            }
+            for (int r = 0; r < NR; ++r) mma_f16(s[h][r], a0, a1, a2, a3, qf[r][k + k2][0], qf[r][k + k2][1]);
           }
         }
-        // ---- scales of this lane's keys 16 h + 8 e + g
-        float ks[2][2], vs[2][2];
+      }
+      // ---- scales of this lane's keys 16 h + 8 e + g
+      float ks[2][2], vs[2][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t at = sc + 4u * (uint32_t)((in_tile + 16 * h + 8 * e + g) >> scale_shift);
-            ks[h][e] = ld_shared_f32(at) * score_scale;
-            vs[h][e] = ld_shared_f32(at + 4u * kTile);
-          }
-        // keys outside a row's view; whole tiles in everybody's view skip this
-        const int last_key = key0 + kKeys - 1;
-        const bool whole = last_key <= first_pos && last_key < w.seq.length && (p.window == 0 || key0 > last_pos - p.window || last_key < p.sinks);
-        auto in_view = [&](int key) { return (key < kt.hi && key >= kt.lo) || key < kt.sink_hi; };  // of some row
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int r = 0; r < NR; ++r)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[h][r][e] *= ks[h][e >> 1];
-        if (!whole) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int key = key0 + 16 * h + 8 * (e >> 1) + g;
-#pragma unroll
-              for (int r = 0; r < NR; ++r) {
-                const int at = pos[r][e & 1];
-                const bool seen = key <= at && key < w.seq.length && (p.window == 0 || key > at - p.window || key < p.sinks);
-                if (!seen) s[h][r][e] = -INFINITY;
-              }
-              if (!in_view(key)) vs[h][e >> 1] = 0.f;
-            }
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t at = sc + 4u * (uint32_t)((wk * kKeys + 16 * h + 8 * e + g) >> scale_shift);
+          ks[h][e] = ld_shared_f32(at) * score_scale;
+          vs[h][e] = ld_shared_f32(at + 4u * H * kTile);
         }
-        // ---- references
-        const float v_most = fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[1][0], vs[1][1]));
-        float mx[NR][2];
-        bool raise = v_most > v_top;
+      advance();
+      // keys outside a row's view; whole tiles in everybody's view skip this
+      const int last_key = key0 + kKeys - 1;
+      const bool whole = last_key <= first_pos && last_key < w.seq.length && (p.window == 0 || key0 > last_pos - p.window || last_key < p.sinks);
+      auto in_view = [&](int key) { return (key < kt.hi && key >= kt.lo) || key < kt.sink_hi; };  // of some row
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            mx[r][e] = fmaxf(fmaxf(s[0][r][e], s[0][r][e + 2]), fmaxf(s[1][r][e], s[1][r][e + 2]));
-            raise |= mx[r][e] > m[r][e] + kRaise;  // also the first finite score of a row (m = -inf)
-          }
-        if (__any_sync(0xffffffffu, raise)) {
-          const float most = warp_max(v_most);
-          float down = 1.f;
-          if (most > v_top) {
-            // the next power of two, within what fp32 has as a power of two times kTopP
-            const float top = __uint_as_float(min(max((__float_as_uint(most) >> 23) + 1u, 27u), 254u) << 23);
-            down = v_top / top;
-            v_top = top;
-          }
+          for (int e = 0; e < 4; ++e) s[h][r][e] *= ks[h][e >> 1];
+      if (!whole) {
 #pragma unroll
-          for (int r = 0; r < NR; ++r) {
-            float alpha[2];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float top = mx[r][e];
+          for (int e = 0; e < 4; ++e) {
+            const int key = key0 + 16 * h + 8 * (e >> 1) + g;
 #pragma unroll
-              for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-              const bool up = top > m[r][e] + kRaise;
-              alpha[e] = up ? ex2(m[r][e] - top) : 1.f;
-              if (up) m[r][e] = top;
-              l[r][e] *= alpha[e];
-              alpha[e] *= down;
+            for (int r = 0; r < NR; ++r) {
+              const int at = pos[r][e & 1];
+              const bool seen = key <= at && key < w.seq.length && (p.window == 0 || key > at - p.window || key < p.sinks);
+              if (!seen) s[h][r][e] = -INFINITY;
             }
-#pragma unroll
-            for (int d = 0; d < MT; ++d) {
-              o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
-            }
+            if (!in_view(key)) vs[h][e >> 1] = 0.f;
           }
-        }
-        // ---- P^T: exponentials, and times vs_j in fp16
-        const float v_unit = kTopP / v_top;
-        uint32_t pf[2][NR][2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float v0 = v_top > 0.f ? vs[h][0] * v_unit : 0.f, v1 = v_top > 0.f ? vs[h][1] * v_unit : 0.f;
-#pragma unroll
-          for (int r = 0; r < NR; ++r) {
-            // a row that has seen nothing yet is referred to 0: its exponentials are 2^-inf = 0
-            const float r0 = m[r][0] == -INFINITY ? 0.f : m[r][0], r1 = m[r][1] == -INFINITY ? 0.f : m[r][1];
-            const float e0 = ex2(s[h][r][0] - r0), e1 = ex2(s[h][r][1] - r1), e2 = ex2(s[h][r][2] - r0), e3 = ex2(s[h][r][3] - r1);
-            l[r][0] += e0 + e2;
-            l[r][1] += e1 + e3;
-            pf[h][r][0] = transpose_8x8(pack_half(e0 * v0, e1 * v0));
-            pf[h][r][1] = transpose_8x8(pack_half(e2 * v1, e3 * v1));
-          }
-        }
-        // ---- O^T += V^T P^T
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          // Values of keys in nobody's view may be any bits, NaN among them: zeroed, since 0 * NaN is NaN.  A word holds two
-          // elements of key 2 i (of eight) and two of key 2 i + 1.
-          uint32_t mask0 = 0xffffffffu, mask1 = 0xffffffffu;
-          if (!whole) {
-            auto half = [&](int key) { return in_view(key) ? 0xffffu : 0u; };
-            const int key = key0 + 16 * h + 2 * i4;
-            mask0 = half(key) | half(key + 1) << 16;
-            mask1 = half(key + 8) | half(key + 9) << 16;
-          }
-#pragma unroll
-          for (int d = 0; d < MT; d += 2) {
-            uint32_t vw[4];  // words of keys 0-7 and 8-15, of these 16 elements and the next ones
-            ldmatrix_x4_trans(chunk_at(sv, in_tile + 16 * h + mat_key, d + mat_chunk), vw);
-            if (!whole) { vw[0] &= mask0; vw[1] &= mask1; vw[2] &= mask0; vw[3] &= mask1; }
-#pragma unroll
-            for (int d2 = 0; d2 < 2; ++d2) {
-              uint32_t a0, a1, a2, a3;
-              q8_word_to_half<T, false>(vw[2 * d2], a0, a1);
-              q8_word_to_half<T, false>(vw[2 * d2 + 1], a2, a3);
-#pragma unroll
-              for (int r = 0; r < NR; ++r) mma_f16(o[d + d2][r], a0, a1, a2, a3, pf[h][r][0], pf[h][r][1]);
-            }
-          }
-        }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(empty(stage));
-    }
-    const float unit = v_top * (1.f / kTopP);
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int x = 4; x < 32; x *= 2) l[r][e] += __shfl_xor_sync(0xffffffffu, l[r][e], x);
-#pragma unroll
-      for (int d = 0; d < MT; ++d) { o[d][r][0] *= unit; o[d][r][1] *= unit; o[d][r][2] *= unit; o[d][r][3] *= unit; }
-    }
-    // (the last piece's exchange has been read by then)
-    if (barrier_any<32 * kConsumers>(failed)) break;
-    // The warps with the same rows: the upper half's results go, lane by lane, into the lower half's registers, until one is left.
-    const int part = wt * C::kWK + wk;
-#pragma unroll
-    for (int half = C::kParts / 2; half > 0; half /= 2) {
-      const int step = WR * half * 32 * 4;  // floats
-      float* mine = merge + ((wr * half + part % half) * 32 + lane) * 4;
-      if (part >= half && part < 2 * half) {
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-#pragma unroll
-          for (int d = 0; d < MT; ++d)
-            *reinterpret_cast<float4*>(mine + (r * MT + d) * step) = make_float4(o[d][r][0], o[d][r][1], o[d][r][2], o[d][r][3]);
-          *reinterpret_cast<float4*>(mine + (NR * MT + r) * step) = make_float4(m[r][0], m[r][1], l[r][0], l[r][1]);
-        }
-      }
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * kConsumers) : "memory");
-      if (part < half) {
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          const float4 other = *reinterpret_cast<const float4*>(mine + (NR * MT + r) * step);
-          const float om[2] = {other.x, other.y}, ol[2] = {other.z, other.w};
-          float a[2], b[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float top = fmaxf(m[r][e], om[e]);
-            a[e] = m[r][e] == -INFINITY ? 0.f : ex2(m[r][e] - top);
-            b[e] = om[e] == -INFINITY ? 0.f : ex2(om[e] - top);
-            m[r][e] = top;
-            l[r][e] = l[r][e] * a[e] + ol[e] * b[e];
-          }
-#pragma unroll
-          for (int d = 0; d < MT; ++d) {
-            const float4 v = *reinterpret_cast<const float4*>(mine + (r * MT + d) * step);
-            o[d][r][0] = o[d][r][0] * a[0] + v.x * b[0];
-            o[d][r][1] = o[d][r][1] * a[1] + v.y * b[1];
-            o[d][r][2] = o[d][r][2] * a[0] + v.z * b[0];
-            o[d][r][3] = o[d][r][3] * a[1] + v.w * b[1];
-          }
-        }
-      }
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * kConsumers) : "memory");
-    }
-    if (part == 0) {
+      // ---- references
+      const float v_most = fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[1][0], vs[1][1]));
+      float mx[NR][2];
+      bool raise = v_most > v_top;
 #pragma unroll
       for (int r = 0; r < NR; ++r)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float* row = merge + (wr * C::kGroupRows + 8 * r + 2 * i4 + e) * C::kMergeStride;
-#pragma unroll
-          for (int d = 0; d < MT; ++d) *reinterpret_cast<float2*>(row + 16 * d + 2 * g) = make_float2(o[d][r][e], o[d][r][2 + e]);
-          if (g == 0) { row[D] = m[r][e]; row[D + 1] = l[r][e]; }
+          mx[r][e] = fmaxf(fmaxf(s[0][r][e], s[0][r][e + 2]), fmaxf(s[1][r][e], s[1][r][e + 2]));
+          raise |= mx[r][e] > m[r][e] + kRaise;  // also the first finite score of a row (m = -inf)
         }
+      if (__any_sync(0xffffffffu, raise)) {
+        const float most = warp_max(v_most);
+        float down = 1.f;
+        if (most > v_top) {
+          // the next power of two, within what fp32 has as a power of two times kTopP
+          const float top = __uint_as_float(min(max((__float_as_uint(most) >> 23) + 1u, 27u), 254u) << 23);
+          down = v_top / top;
+          v_top = top;
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          float alpha[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float top = mx[r][e];
+#pragma unroll
+            for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            const bool up = top > m[r][e] + kRaise;
+            alpha[e] = up ? ex2(m[r][e] - top) : 1.f;
+            if (up) m[r][e] = top;
+            l[r][e] *= alpha[e];
+            alpha[e] *= down;
+          }
+#pragma unroll
+          for (int d = 0; d < MT; ++d) {
+            o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
+          }
+        }
+      }
+      // ---- P^T: exponentials, and times vs_j in fp16
+      const float v_unit = kTopP / v_top;
+      uint32_t pf[2][NR][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float v0 = v_top > 0.f ? vs[h][0] * v_unit : 0.f, v1 = v_top > 0.f ? vs[h][1] * v_unit : 0.f;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          // a row that has seen nothing yet is referred to 0: its exponentials are 2^-inf = 0
+          const float r0 = m[r][0] == -INFINITY ? 0.f : m[r][0], r1 = m[r][1] == -INFINITY ? 0.f : m[r][1];
+          const float e0 = ex2(s[h][r][0] - r0), e1 = ex2(s[h][r][1] - r1), e2 = ex2(s[h][r][2] - r0), e3 = ex2(s[h][r][3] - r1);
+          l[r][0] += e0 + e2;
+          l[r][1] += e1 + e3;
+          pf[h][r][0] = transpose_8x8(pack_half(e0 * v0, e1 * v0));
+          pf[h][r][1] = transpose_8x8(pack_half(e2 * v1, e3 * v1));
+        }
+      }
+      // ---- O^T += V^T P^T
+      if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
+      const uint32_t sv = ring + stage * C::kStageBytes;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // Values of keys in nobody's view may be any bits, NaN among them: zeroed, since 0 * NaN is NaN.  A word holds two
+        // elements of key 2 i (of eight) and two of key 2 i + 1.
+        uint32_t mask0 = 0xffffffffu, mask1 = 0xffffffffu;
+        if (!whole) {
+          auto half = [&](int key) { return in_view(key) ? 0xffffu : 0u; };
+          const int key = key0 + 16 * h + 2 * i4;
+          mask0 = half(key) | half(key + 1) << 16;
+          mask1 = half(key + 8) | half(key + 9) << 16;
+        }
+#pragma unroll
+        for (int d = 0; d < MT; d += 2) {
+          uint32_t vw[4];  // words of keys 0-7 and 8-15, of these 16 elements and the next ones
+          ldmatrix_x4_trans(chunk_at(sv, h, d + mat_chunk), vw);
+          if (!whole) { vw[0] &= mask0; vw[1] &= mask1; vw[2] &= mask0; vw[3] &= mask1; }
+#pragma unroll
+          for (int d2 = 0; d2 < 2; ++d2) {
+            uint32_t a0, a1, a2, a3;
+            q8_word_to_half<T, false>(vw[2 * d2], a0, a1);
+            q8_word_to_half<T, false>(vw[2 * d2 + 1], a2, a3);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) mma_f16(o[d + d2][r], a0, a1, a2, a3, pf[h][r][0], pf[h][r][1]);
+          }
+        }
+      }
+      advance();
     }
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * kConsumers) : "memory");
-    write_piece<D, C::kGroupRows, 1, C::kRows, 32 * kConsumers>(p, w, piece, share, merge);
-    if (!next_piece(p, w, stop)) break;
+    float unit = v_top * (1.f / kTopP);
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int x = 4; x < 32; x *= 2) l[r][e] += __shfl_xor_sync(0xffffffffu, l[r][e], x);
+    if constexpr (WK == 1) {
+      if (failed) break;
+    } else {
+      // (the last piece's exchange has been read by then)
+      if (barrier_any<32 * kConsumers>(failed)) break;
+      // The warps with the same rows: the upper half's results go, lane by lane and 8 rows at a time, into the lower half's registers,
+      // until one is left.
+#pragma unroll
+      for (int half = WK / 2; half > 0; half /= 2) {
+        const int step = H * WR * half * 32 * 4;  // floats
+        float* mine = exchange + (((wr * H + hs) * half + wk % half) * 32 + lane) * 4;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          if (wk >= half && wk < 2 * half) {
+#pragma unroll
+            for (int d = 0; d < MT; ++d)
+              *reinterpret_cast<float4*>(mine + d * step) = make_float4(o[d][r][0] * unit, o[d][r][1] * unit, o[d][r][2] * unit, o[d][r][3] * unit);
+            *reinterpret_cast<float4*>(mine + MT * step) = make_float4(m[r][0], m[r][1], l[r][0], l[r][1]);
+          }
+          asm volatile("bar.sync 1, %0;" ::"n"(32 * kConsumers) : "memory");
+          if (wk < half) {
+            const float4 other = *reinterpret_cast<const float4*>(mine + MT * step);
+            const float om[2] = {other.x, other.y}, ol[2] = {other.z, other.w};
+            float a[2], b[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float top = fmaxf(m[r][e], om[e]);
+              a[e] = m[r][e] == -INFINITY ? 0.f : ex2(m[r][e] - top);
+              b[e] = om[e] == -INFINITY ? 0.f : ex2(om[e] - top);
+              m[r][e] = top;
+              l[r][e] = l[r][e] * a[e] + ol[e] * b[e];
+              a[e] *= unit;
+            }
+#pragma unroll
+            for (int d = 0; d < MT; ++d) {
+              const float4 v = *reinterpret_cast<const float4*>(mine + d * step);
+              o[d][r][0] = o[d][r][0] * a[0] + v.x * b[0];
+              o[d][r][1] = o[d][r][1] * a[1] + v.y * b[1];
+              o[d][r][2] = o[d][r][2] * a[0] + v.z * b[0];
+              o[d][r][3] = o[d][r][3] * a[1] + v.w * b[1];
+            }
+          }
+          asm volatile("bar.sync 1, %0;" ::"n"(32 * kConsumers) : "memory");
+        }
+        unit = 1.f;
+      }
+    }
+    // ---- the rows 8 r + 2 i and + 1, elements 16 d + 2 g and + 1: to the output, or to the workspace
+    const bool complete = w.begin == 0 && w.end == w.weight;
+    const int part = 2 * blockIdx.x + (piece > 0 ? 1 : 0);  // a piece that is neither the CTA's first nor its last is complete
+    if (wk == 0) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int row = wr * C::kGroupRows + 8 * r + 2 * i4 + e;
+          const float inv = l[r][e] > 0.f ? unit / l[r][e] : 0.f;  // nothing seen: zeros
+          if (row < w.rows) {
+            if (complete) {
+              const int t = row / p.group;
+              __nv_bfloat16* to = p.out + (int64_t)(w.seq.q0 + t) * p.ld_out + (int64_t)(kvh * p.group + row - t * p.group) * D + 2 * g;
+#pragma unroll
+              for (int d = 0; d < MT; ++d) *reinterpret_cast<uint32_t*>(to + 16 * d) = pack_bf16(o[d][r][e] * inv, o[d][r][2 + e] * inv);
+            } else {
+              const int64_t at = ((int64_t)part * H + hs) * C::kRows + row;
+              if (l[r][e] > 0.f) {
+#pragma unroll
+                for (int d = 0; d < MT; ++d) *reinterpret_cast<float2*>(p.part_o + at * D + 16 * d + 2 * g) = make_float2(o[d][r][e] * inv, o[d][r][2 + e] * inv);
+              }
+              if (g == 0) p.part_lse[at] = l[r][e] > 0.f ? m[r][e] + log2f(l[r][e]) : -INFINITY;
+            }
+          }
+        }
+      if (wr == 0 && lane == 0 && w.begin == 0)  // where the item's pieces are: its first one, and the CTA of its last
+        p.pieces[(int64_t)w.b * p.heads_kv + kvh] = complete ? make_int2(-1, 0) : make_int2(part, (w.base + w.weight - 1) / share);
+    }
+    if (!next_piece<kTile>(p, w, stop)) break;
   }
 }
 
-template <pd_dtype T, int D, int NR, int WR>
-pd_status launch(const pd_paged_attention_desc& d, const Params& p, const Scales& scales, const CUtensorMap& tk, const CUtensorMap& tv,
+template <pd_dtype T, int D, int NR, int H, int WK, int WR>
+pd_status launch(const pd_paged_attention_desc& d, const Params& p, const Scales& scales, const void* k_cache, const void* v_cache,
                  cudaStream_t s) {
-  using C = Q8Config<D, NR, WR>;
+  using C = Q8Config<D, NR, H, WK, WR>;
+  CUtensorMap tk, tv;
+  const int box = d.page_size < C::kTile ? d.page_size : C::kTile;
+  if (!make_cache_map_q8(&tk, k_cache, d, box, H) || !make_cache_map_q8(&tv, v_cache, d, box, H)) return PD_ERR_UNSUPPORTED;
   static PerDeviceFlag smem_allowed;
-  if (pd_status st = allow_dynamic_smem(paged_attention_q8_rows_kernel<T, D, NR, WR>, C::kSmem, smem_allowed); st != PD_OK) return st;
-  launch_pdl(paged_attention_q8_rows_kernel<T, D, NR, WR>, dim3(p.splits), dim3(kThreads), C::kSmem, s, tk, tv, p, scales);
+  if (pd_status st = allow_dynamic_smem(paged_attention_q8_rows_kernel<T, D, NR, H, WK, WR>, C::kSmem, smem_allowed); st != PD_OK) return st;
+  launch_pdl(paged_attention_q8_rows_kernel<T, D, NR, H, WK, WR>, dim3(p.splits), dim3(kThreads), C::kSmem, s, tk, tv, p, scales);
   if (pd_status st = check_launch(); st != PD_OK || p.whole_items) return st;
   const int rows = (int)std::min<int64_t>((int64_t)p.max_q_len * p.group, C::kRows);
-  launch_pdl(paged_attention_join_rows<D>, dim3(d.heads_kv, d.batch, (rows + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p, C::kRows);
+  launch_pdl(paged_attention_join_rows<D>, dim3(d.heads_kv, d.batch, (rows + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p, C::kRows, H);
   return check_launch();
 }
 template <pd_dtype T, int D>
-pd_status launch_rows_of(const pd_paged_attention_desc& d, const Params& p, const Scales& scales, const CUtensorMap& tk, const CUtensorMap& tv,
-                         int rows_per_tile, cudaStream_t s) {
-  if (rows_per_tile == 8) return launch<T, D, 1, 1>(d, p, scales, tk, tv, s);
-  if (rows_per_tile == 16) return launch<T, D, 2, 1>(d, p, scales, tk, tv, s);
-  if (rows_per_tile == 32) return launch<T, D, 2, 2>(d, p, scales, tk, tv, s);
-  return launch<T, D, 2, 4>(d, p, scales, tk, tv, s);
+pd_status launch_plan(const pd_paged_attention_desc& d, const Params& p, const Plan& plan, const Scales& scales, const void* k, const void* v,
+                      cudaStream_t s) {
+  const int h = plan.heads_per_item;
+  if (plan.rows_per_tile == 8)
+    return h == 4 ? launch<T, D, 1, 4, 1, 1>(d, p, scales, k, v, s) : h == 2 ? launch<T, D, 1, 2, 2, 1>(d, p, scales, k, v, s) : launch<T, D, 1, 1, 4, 1>(d, p, scales, k, v, s);
+  if (plan.rows_per_tile == 16)
+    return h == 4 ? launch<T, D, 2, 4, 1, 1>(d, p, scales, k, v, s) : h == 2 ? launch<T, D, 2, 2, 2, 1>(d, p, scales, k, v, s) : launch<T, D, 2, 1, 4, 1>(d, p, scales, k, v, s);
+  if (plan.rows_per_tile == 32)
+    return h == 2 ? launch<T, D, 2, 2, 1, 2>(d, p, scales, k, v, s) : launch<T, D, 2, 1, 2, 2>(d, p, scales, k, v, s);
+  return launch<T, D, 2, 1, 1, 4>(d, p, scales, k, v, s);
 }
 
 }  // namespace
 
-pd_status launch_rows_q8(const pd_paged_attention_desc& d, Params& p, pd_dtype type, const Scales& scales, const void* k_cache,
-                         const void* v_cache, int rows_per_tile, cudaStream_t s) {
-  CUtensorMap tk, tv;
-  const int box = d.page_size < kTile ? d.page_size : kTile;
-  if (!make_cache_map_q8(&tk, k_cache, d, box) || !make_cache_map_q8(&tv, v_cache, d, box)) return PD_ERR_UNSUPPORTED;
+pd_status launch_rows_q8(const pd_paged_attention_desc& d, const Params& p, const Plan& plan, pd_dtype type, const Scales& scales,
+                         const void* k_cache, const void* v_cache, cudaStream_t s) {
   if (d.head_dim == 64)
-    return type == PD_I8 ? launch_rows_of<PD_I8, 64>(d, p, scales, tk, tv, rows_per_tile, s)
-                         : launch_rows_of<PD_E4M3, 64>(d, p, scales, tk, tv, rows_per_tile, s);
-  return type == PD_I8 ? launch_rows_of<PD_I8, 128>(d, p, scales, tk, tv, rows_per_tile, s)
-                       : launch_rows_of<PD_E4M3, 128>(d, p, scales, tk, tv, rows_per_tile, s);
+    return type == PD_I8 ? launch_plan<PD_I8, 64>(d, p, plan, scales, k_cache, v_cache, s) : launch_plan<PD_E4M3, 64>(d, p, plan, scales, k_cache, v_cache, s);
+  return type == PD_I8 ? launch_plan<PD_I8, 128>(d, p, plan, scales, k_cache, v_cache, s) : launch_plan<PD_E4M3, 128>(d, p, plan, scales, k_cache, v_cache, s);
 }
 
 }  // namespace paged

@@ -74,7 +74,7 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
 
   Piece w;
   int start, stop, share;
-  if (!first_piece<C::kThreads>(p, blockIdx.x, w, start, stop, share)) return;
+  if (!first_piece<C::kThreads, kTile>(p, blockIdx.x, w, start, stop, share)) return;
 
   if (warp == C::kConsumers) {
     // ------------------------------------------------------------------ producer
@@ -112,7 +112,7 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
           }
         }
       }
-      if (!ok || !next_piece(p, w, stop)) break;
+      if (!ok || !next_piece<kTile>(p, w, stop)) break;
     }
     // Leave no copy in flight, whichever warp gives up: the last request of every stage gets a short time to land.
     volatile int never = 0;
@@ -266,7 +266,7 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
     }
     asm volatile("bar.sync 1, %0;" ::"n"(32 * C::kConsumers) : "memory");
     write_piece<D, 16, WK, C::kRows, 32 * C::kConsumers>(p, w, piece, share, merge);
-    if (!next_piece(p, w, stop)) break;
+    if (!next_piece<kTile>(p, w, stop)) break;
   }
 }
 
@@ -278,7 +278,7 @@ pd_status launch(const pd_paged_attention_desc& d, const Params& p, const CUtens
   if (pd_status st = allow_dynamic_smem(paged_attention_rows_kernel<D, WR, WK>, C::kSmem, smem_allowed); st != PD_OK) return st;
   launch_pdl(paged_attention_rows_kernel<D, WR, WK>, dim3(p.splits), dim3(C::kThreads), C::kSmem, s, tk, tv, p);
   if (pd_status st = check_launch(); st != PD_OK || p.whole_items) return st;
-  launch_pdl(paged_attention_join_rows<D>, dim3(d.heads_kv, d.batch, (min(p.max_q_len * p.group, C::kRows) + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p, C::kRows);
+  launch_pdl(paged_attention_join_rows<D>, dim3(d.heads_kv, d.batch, (min(p.max_q_len * p.group, C::kRows) + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p, C::kRows, 1);
   return check_launch();
 }
 

@@ -34,6 +34,7 @@ struct Params {
   // Tokens that can have partial results in the chunk kernel: all rows of the token tensors, or, where these are padded to
   // more than max_q_len for each sequence, that many places a sequence.
   int part_tokens, part_by_sequence;
+  int items;            // of a sequence in the row kernels: cache heads, or groups of them
   int splits;           // of the keys of every row tile (chunk kernel), CTAs in all (row kernel)
   int min_split_tiles;  // the smallest share of key tiles (chunk kernel)
   int whole_items;      // row kernel: no item is shared out (short contexts: nothing to join)
@@ -170,36 +171,43 @@ inline bool supported(const pd_paged_attention_desc& d) {
 
 struct Plan {
   int rows_per_tile;            // up to 64: row kernel; 128, 256: chunk kernel
+  int heads_per_item, tile;     // row kernel: cache heads that a CTA works on side by side; keys per tile
   int splits, min_split_tiles;  // in key tiles of the kernel (64, 128); the latter of the chunk kernels alone
   bool whole_items;
 };
 
-// Depends on the desc alone (the workspace size follows from it).  `smallest`: rows of the smallest tile;
-// `wide`: chunks take 256 rows and key tiles of 128 whatever the head_dim.
-inline Plan plan(const pd_paged_attention_desc& d, int smallest = 16, bool wide = false) {
-  constexpr int kSms = 148;  // (not asked of the device: the workspace follows from the desc alone)
-  Plan pl{};
-  const bool narrow = d.head_dim == 64 && !wide;
-  const int64_t group = d.heads_q / d.heads_kv, rows = std::min(d.max_q_len, d.tokens) * group;
-  pl.rows_per_tile = rows <= smallest ? smallest : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : narrow ? 128 : 256;
-  const bool chunk = pl.rows_per_tile > 64;
-  const int64_t row_tiles = (rows + pl.rows_per_tile - 1) / pl.rows_per_tile;
-  const int64_t items = row_tiles * d.heads_kv * d.batch;  // CTAs without splitting
-  int64_t keys = d.max_kv_len;
-  if (d.window > 0) keys = std::min<int64_t>(keys, (int64_t)d.window + d.sinks + d.max_q_len);
-  const int64_t tile = !chunk || narrow ? 64 : 128, tiles = (keys + tile - 1) / tile;
-  if (!chunk) {
-    // two CTAs per SM share all key tiles evenly; fewer when there are not enough tiles for that
-    pl.whole_items = tiles <= 2;
-    const int64_t all = std::max<int64_t>(tiles, 1) * d.heads_kv * d.batch;  // (not 0: an empty batch launches nothing)
-    pl.splits = (int)std::min<int64_t>(2 * kSms, all);
-    return pl;
-  }
-  // One or four CTAs per SM, and splits only to fill the SMs, none below min_split_tiles.
-  pl.min_split_tiles = narrow ? 8 : 4;
-  int64_t want = items > 0 ? kSms * (narrow ? 4 : 1) / items : 1;
+constexpr int kSms = 148;  // (not asked of the device: the workspace follows from the desc alone)
+
+inline int64_t plan_rows(const pd_paged_attention_desc& d) { return (int64_t)std::min(d.max_q_len, d.tokens) * (d.heads_q / d.heads_kv); }
+inline int64_t plan_keys(const pd_paged_attention_desc& d) {
+  return d.window > 0 ? std::min<int64_t>(d.max_kv_len, (int64_t)d.window + d.sinks + d.max_q_len) : d.max_kv_len;
+}
+// Row kernel: two CTAs per SM share all key tiles evenly; fewer when there are not enough tiles for that.
+inline void plan_shares(const pd_paged_attention_desc& d, Plan& pl) {
+  const int64_t tiles = (plan_keys(d) + pl.tile - 1) / pl.tile;
+  pl.whole_items = tiles * pl.tile <= 128;
+  const int64_t all = std::max<int64_t>(tiles, 1) * (d.heads_kv / pl.heads_per_item) * d.batch;  // (not 0: an empty batch launches nothing)
+  pl.splits = (int)std::min<int64_t>(2 * kSms, all);
+}
+// Chunk kernel: one (wide) or four CTAs per SM, and splits only to fill the SMs, none below min_split_tiles.
+inline void plan_splits(const pd_paged_attention_desc& d, Plan& pl) {
+  const bool wide = pl.rows_per_tile == 256;
+  const int64_t tile = wide ? 128 : 64, tiles = (plan_keys(d) + tile - 1) / tile;
+  const int64_t items = (plan_rows(d) + pl.rows_per_tile - 1) / pl.rows_per_tile * d.heads_kv * d.batch;  // CTAs without splitting
+  pl.min_split_tiles = wide ? 4 : 8;
+  int64_t want = items > 0 ? kSms * (wide ? 1 : 4) / items : 1;
   want = std::min<int64_t>(want, (tiles + pl.min_split_tiles - 1) / pl.min_split_tiles);
   pl.splits = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 256);
+}
+// For a bf16 cache.  Depends on the desc alone (the workspace size follows from it).
+inline Plan plan(const pd_paged_attention_desc& d) {
+  Plan pl{};
+  const int64_t rows = plan_rows(d);
+  pl.rows_per_tile = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : d.head_dim == 64 ? 128 : 256;
+  pl.heads_per_item = 1;
+  pl.tile = 64;
+  if (pl.rows_per_tile <= 64) plan_shares(d, pl);
+  else plan_splits(d, pl);
   return pl;
 }
 
@@ -210,7 +218,7 @@ inline int64_t partial_tokens(const pd_paged_attention_desc& d) {
 // Rows of partial results in the workspace, and entries of the piece table behind them.
 inline size_t partial_rows(const pd_paged_attention_desc& d, const Plan& pl) {
   if (pl.rows_per_tile > 64) return pl.splits > 1 ? (size_t)pl.splits * partial_tokens(d) * d.heads_q : 0;
-  return (size_t)2 * pl.splits * pl.rows_per_tile;
+  return (size_t)2 * pl.splits * pl.heads_per_item * pl.rows_per_tile;
 }
 inline size_t table_entries(const pd_paged_attention_desc& d, const Plan& pl) {
   return pl.rows_per_tile > 64 ? 0 : (size_t)d.batch * d.heads_kv;
@@ -234,7 +242,7 @@ inline Params make_params(const pd_paged_attention_desc& d, const Plan& pl, cons
   while ((1 << p.page_shift) < d.page_size) ++p.page_shift;
   p.max_q_len = std::min(d.max_q_len, d.tokens); p.window = std::min(d.window, kMaxPositions); p.sinks = d.sinks;
   p.part_tokens = (int)partial_tokens(d); p.part_by_sequence = p.part_tokens < d.tokens;
-  p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles; p.whole_items = pl.whole_items;
+  p.items = pl.heads_per_item > 0 ? d.heads_kv / pl.heads_per_item : 0; p.splits = pl.splits; p.min_split_tiles = pl.min_split_tiles; p.whole_items = pl.whole_items;
   p.scale_log2e = base2_scale(d.scale);
   if (workspace && workspace_bytes(d, pl) > 0) {
     const size_t rows = partial_rows(d, pl);  // (an even number in the row kernel: the table is aligned)

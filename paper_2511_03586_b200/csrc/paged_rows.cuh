@@ -9,7 +9,8 @@ namespace pd {
 namespace paged {
 namespace {
 
-// One item, or a part of one: cache head and sequence, its key tiles, and the tiles [begin, end) of `weight` that are meant.
+// One item, or a part of one: sequence and cache head (or group of them), its key tiles, and the tiles [begin, end) of `weight`
+// that are meant.
 struct Piece {
   Sequence seq;
   KeyTiles tiles;
@@ -19,21 +20,23 @@ struct Piece {
   int begin, end;
 };
 
+template <int TILE>
 __device__ __forceinline__ void set_sequence(const Params& p, int b, Piece& w) {
   w.b = b;
   w.seq = load_sequence(p, b);
   w.rows = w.seq.n * p.group;
-  w.tiles = key_tiles(p, w.seq.pos0, w.seq.pos0 + w.seq.n - 1, w.seq.length, 64);
+  w.tiles = key_tiles(p, w.seq.pos0, w.seq.pos0 + w.seq.n - 1, w.seq.length, TILE);
   w.weight = w.rows > 0 ? max(w.tiles.n, 1) : 0;
 }
 
 // On to the next item; false when the share ends.
+template <int TILE>
 __device__ __forceinline__ bool next_piece(const Params& p, Piece& w, int stop) {
   w.base += w.weight;
   if (w.base >= stop) return false;
-  if (++w.kvh == p.heads_kv) {
+  if (++w.kvh == p.items) {
     w.kvh = 0;
-    do set_sequence(p, w.b + 1, w); while (w.weight == 0);  // (there is one: the share goes on)
+    do set_sequence<TILE>(p, w.b + 1, w); while (w.weight == 0);  // (there is one: the share goes on)
   }
   w.begin = 0;
   w.end = p.whole_items ? w.weight : min(w.weight, stop - w.base);
@@ -42,7 +45,7 @@ __device__ __forceinline__ bool next_piece(const Params& p, Piece& w, int stop) 
 
 // The share of CTA `cta`: [start, stop) of all tiles, and in `w` the item that `start` lies in.  Collective over the block
 // (THREADS threads); false if the share is empty.
-template <int THREADS>
+template <int THREADS, int TILE>
 __device__ __forceinline__ bool first_piece(const Params& p, int cta, Piece& w, int& start, int& stop, int& share) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int found_b, found_base, total;
@@ -64,8 +67,8 @@ __device__ __forceinline__ bool first_piece(const Params& p, int cta, Piece& w, 
   if (p.batch <= 32) {  // every warp for itself
     int mine = 0;
     if (lane < p.batch) {
-      set_sequence(p, lane, w);
-      mine = w.weight * p.heads_kv;
+      set_sequence<TILE>(p, lane, w);
+      mine = w.weight * p.items;
     }
     const int upto = scan(mine);
     total = __shfl_sync(0xffffffffu, upto, 31);
@@ -77,8 +80,8 @@ __device__ __forceinline__ bool first_piece(const Params& p, int cta, Piece& w, 
     const int per = (p.batch + THREADS - 1) / THREADS, b0 = threadIdx.x * per;
     int mine = 0;
     for (int b = b0; b < min(b0 + per, p.batch); ++b) {
-      set_sequence(p, b, w);
-      mine += w.weight * p.heads_kv;
+      set_sequence<TILE>(p, b, w);
+      mine += w.weight * p.items;
     }
     int upto = scan(mine);
     if (lane == 31) warp_sums[warp] = upto;
@@ -93,8 +96,8 @@ __device__ __forceinline__ bool first_piece(const Params& p, int cta, Piece& w, 
     int base = upto - mine;
     if (base <= start && start < upto) {
       for (int b = b0;; ++b) {
-        set_sequence(p, b, w);
-        const int next = base + w.weight * p.heads_kv;
+        set_sequence<TILE>(p, b, w);
+        const int next = base + w.weight * p.items;
         if (start < next) {
           found[0] = b;
           found[1] = base;
@@ -107,13 +110,13 @@ __device__ __forceinline__ bool first_piece(const Params& p, int cta, Piece& w, 
     found_b = found[0];
     found_base = found[1];
   }
-  set_sequence(p, found_b, w);
+  set_sequence<TILE>(p, found_b, w);
   w.kvh = (start - found_base) / w.weight;
   w.base = found_base + w.kvh * w.weight;
   w.begin = start - w.base;
   w.end = p.whole_items ? w.weight : min(w.weight, stop - w.base);
   // (whole items: they are the CTA's in whose share they begin)
-  return !p.whole_items || w.begin == 0 || next_piece(p, w, stop);
+  return !p.whole_items || w.begin == 0 || next_piece<TILE>(p, w, stop);
 }
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
@@ -188,8 +191,9 @@ __device__ __forceinline__ void write_piece(const Params& p, const Piece& w, int
 // every so-manieth piece.
 // Latency-bound: the loads of a warp's pieces are in flight together (one at a time, 37 pieces of a long context took 12 us).
 constexpr int kJoinWarps = 8;
+// `group`: cache heads to an item; their partial results lie behind one another.
 template <int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) paged_attention_join_rows(const Params p, int rows_per_tile) {
+__global__ void __launch_bounds__(32 * kJoinWarps) paged_attention_join_rows(const Params p, int rows_per_tile, int group) {
   __shared__ float part[kJoinWarps][D + 2];
   griddep_wait();
   griddep_launch_dependents();
@@ -207,7 +211,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) paged_attention_join_rows(con
   constexpr int kCols = D / 32;
   {
     const int r = blockIdx.z * kJoinWarps + warp / per_row, z0 = warp % per_row;
-    auto at = [&](int z) { return (int64_t)(z == 0 ? pieces.x : 2 * (first_cta + z)) * rows_per_tile + r; };
+    auto at = [&](int z) { return ((int64_t)(z == 0 ? pieces.x : 2 * (first_cta + z)) * group + kvh % group) * rows_per_tile + r; };
     float top = -INFINITY, sum = 0.f, acc[kCols];
 #pragma unroll
     for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
