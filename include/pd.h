@@ -597,7 +597,7 @@ pd_status pd_sample(const void* logits, pd_dtype dtype, int64_t rows, int64_t vo
  *    of which the first prompt_len[i] are the prompt (NULL: none).  Entries outside
  *    [0, vocab) do not count.
  *  - repetition, frequency, presence: fp32 [rows], or NULL for none.  A repetition that is
- *    not positive and finite counts as 1.
+ *    not positive and finite, or whose reciprocal is not finite, counts as 1.
  *  - bias_tokens (int32), bias_values (fp32): [rows, bias_cols], dense.  Entries whose token
  *    lies outside [0, vocab) do not count; of several for one token the last does.  -inf is
  *    a value like any other.  bias_cols = 0: none.

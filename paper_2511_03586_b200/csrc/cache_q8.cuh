@@ -111,8 +111,10 @@ inline bool make_cache_map_q8(CUtensorMap* map, const void* cache, const pd_page
 // Launchers (each in its own file).
 pd_status launch_chunk_q8(const pd_paged_attention_desc& d, const Params& p, pd_dtype type, const Scales& scales, const void* k_cache,
                           const void* v_cache, cudaStream_t s);
-pd_status launch_rows_q8(const pd_paged_attention_desc& d, const Params& p, const Plan& plan, pd_dtype type, const Scales& scales,
-                         const void* k_cache, const void* v_cache, cudaStream_t s);
+pd_status launch_rows_i8(const pd_paged_attention_desc& d, const Params& p, const Plan& plan, const Scales& scales, const void* k_cache,
+                         const void* v_cache, cudaStream_t s);
+pd_status launch_rows_e4m3(const pd_paged_attention_desc& d, const Params& p, const Plan& plan, const Scales& scales, const void* k_cache,
+                           const void* v_cache, cudaStream_t s);
 
 }  // namespace paged
 }  // namespace pd

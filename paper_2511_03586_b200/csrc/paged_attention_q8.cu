@@ -11,12 +11,12 @@ namespace {
 Plan plan_q8(const pd_paged_attention_desc& d) {
   Plan pl{};
   const int64_t rows = plan_rows(d);
-  pl.rows_per_tile = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
+  pl.rows_per_tile = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 24 ? 24 : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
   if (pl.rows_per_tile > 64) {
     plan_splits(d, pl);
     return pl;
   }
-  const int warps = 4 * 16 / std::max(pl.rows_per_tile, 16);  // that have different heads or keys
+  const int warps = rows <= 24 ? 4 : rows <= 32 ? 2 : 1;  // that have different heads or keys
   pl.heads_per_item = warps;
   while (d.heads_kv % pl.heads_per_item != 0) pl.heads_per_item /= 2;
   pl.tile = 32 * warps / pl.heads_per_item;
@@ -65,7 +65,8 @@ extern "C" pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* de
   const paged::Scales sc = paged::make_scales(*scales, d.heads_kv, d.page_size);
   logf("paged attention (%s) batch %d tokens %d (max %d) heads %d/%d x %d: tiles of %d rows, %s %d", scales->dtype == PD_I8 ? "int8" : "e4m3",
        d.batch, d.tokens, d.max_q_len, d.heads_q, d.heads_kv, d.head_dim, pl.rows_per_tile, pl.rows_per_tile > 64 ? "key splits" : "CTAs", pl.splits);
-  if (pl.rows_per_tile <= 64) return paged::launch_rows_q8(d, p, pl, scales->dtype, sc, k_cache, v_cache, stream);
+  if (pl.rows_per_tile <= 64)
+    return scales->dtype == PD_I8 ? paged::launch_rows_i8(d, p, pl, sc, k_cache, v_cache, stream) : paged::launch_rows_e4m3(d, p, pl, sc, k_cache, v_cache, stream);
   if (pd_status st = paged::launch_chunk_q8(d, p, scales->dtype, sc, k_cache, v_cache, stream); st != PD_OK) return st;
   return pl.splits > 1 ? paged::launch_join(d, p, stream) : PD_OK;
 }

@@ -23,6 +23,8 @@
 // delivered 4.2 TB/s so.  So the warps take up to four neighbouring heads, and a box has the rows of all of them; where there are fewer
 // heads, warps share the keys of a tile, and more than 16 rows are shared by two or four warps.  A warp keeps a reference maximum of its
 // own, raised when a score exceeds it by 2^4; warps with the same rows meet at the end of a piece.
+#pragma once
+
 #include "cache_q8.cuh"
 #include "paged_rows.cuh"
 
@@ -45,11 +47,15 @@ struct Q8Config {
   static constexpr int kRows = kGroupRows * WR;
   static constexpr int kStageBytes = H * kTile * D;     // K or V of a tile
   static constexpr int kScaleBytes = 2 * H * kTile * 4; // a scale per key at most, for K and for V
+  // From 24 rows on the queries' fragments stay in shared memory, and a warp takes its 32 keys 16 at a time: 168 registers a thread
+  // hold the accumulators of 24 rows and little else.
+  static constexpr bool kLean = NR > 2;
+  static constexpr int kQ = kLean ? kConsumers * NR * (D / 16) * 256 : 0;
   static constexpr int kExchange = WK > 1 ? H * WR * (WK / 2) * 512 * (D / 16 + 1) : 0;  // half the warps' results for 8 rows
   static constexpr int kPerCta = 113 * 1024 - 256 /*barriers*/ - 1024 /*alignment*/;     // two CTAs per SM
-  static constexpr int kFit = (kPerCta - kExchange) / (kStageBytes + kScaleBytes);
+  static constexpr int kFit = (kPerCta - kExchange - kQ) / (kStageBytes + kScaleBytes);
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
-  static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kExchange + 256 + 1024;
+  static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kExchange + kQ + 256 + 1024;
   static_assert(2 * (kSmem + 1024) <= 228 * 1024 && kStages >= 4);
 };
 
@@ -82,7 +88,8 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t scale_ring = ring + C::kStages * C::kStageBytes, exchange_at = scale_ring + C::kStages * C::kScaleBytes;
   float* exchange = reinterpret_cast<float*>(smem_raw + (exchange_at - smem_u32(smem_raw)));
-  const uint32_t bars = exchange_at + C::kExchange;
+  const uint32_t sq = exchange_at + C::kExchange + (threadIdx.x >> 5) * (C::kQ / kConsumers) + (threadIdx.x & 31) * 8;  // this lane's queries
+  const uint32_t bars = exchange_at + C::kExchange + C::kQ;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 64u + 8u * s; };
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + (bars - smem_u32(smem_raw)) + 128);
@@ -173,6 +180,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
   // ------------------------------------------------------------------- consumers
   const int hs = warp % H, wk = warp / H % WK, wr = warp / (H * WK);
   constexpr int KS = D / 16, MT = D / 16;  // steps of 16 elements; tiles of 16 elements
+  constexpr int HB = C::kLean ? 1 : 2;     // tiles of 16 keys at a time
   const int g = lane >> 2, i4 = lane & 3;
   // this lane's ldmatrix rows (a key of either 16 of the warp's) within a stage, and which of two neighbouring 16-byte chunks
   const int mat_chunk = lane >> 4;
@@ -197,20 +205,23 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
     const int kvh = w.kvh * H + hs;
     const KeyTiles& kt = w.tiles;
     // ---- queries: row 8 r + g of the warp's, elements 16 k + 4 i ... + 3 of it
-    uint32_t qf[NR][KS][2];
+    uint32_t qf[C::kLean ? 1 : NR][KS][2];
     float score_scale;
     {
-      uint2 raw[NR][KS];
       uint32_t most = 0;
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
+      auto source = [&](int r) {
         const int row = min(wr * C::kGroupRows + 8 * r + g, w.rows - 1);  // (rows beyond the last repeat it and are not stored)
         const int t = row / p.group;
-        const __nv_bfloat16* src = p.q + (int64_t)(w.seq.q0 + t) * p.ld_q + (int64_t)(kvh * p.group + row % p.group) * D + 4 * i4;
+        return p.q + (int64_t)(w.seq.q0 + t) * p.ld_q + (int64_t)(kvh * p.group + row % p.group) * D + 4 * i4;
+      };
+      auto load = [&](const __nv_bfloat16* src, int k) { return __ldg(reinterpret_cast<const uint2*>(src + 16 * k)); };
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const __nv_bfloat16* src = source(r);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          raw[r][k] = __ldg(reinterpret_cast<const uint2*>(src + 16 * k));
-          most = max(most, max(max(raw[r][k].x & 0x7fff0000u, raw[r][k].x << 16 & 0x7fff0000u), max(raw[r][k].y & 0x7fff0000u, raw[r][k].y << 16 & 0x7fff0000u)));
+          const uint2 v = load(src, k);
+          most = max(most, max(max(v.x & 0x7fff0000u, v.x << 16 & 0x7fff0000u), max(v.y & 0x7fff0000u, v.y << 16 & 0x7fff0000u)));
         }
       }
       most = __reduce_max_sync(0xffffffffu, most);
@@ -219,14 +230,22 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
       const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
       score_scale = p.scale_log2e * __uint_as_float((uint32_t)(127 - shift) << 23);
 #pragma unroll
-      for (int r = 0; r < NR; ++r)
+      for (int r = 0; r < NR; ++r) {
+        const __nv_bfloat16* src = source(r);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          const float x0 = __uint_as_float(raw[r][k].x << 16) * up, x1 = __uint_as_float(raw[r][k].x & 0xffff0000u) * up;
-          const float x2 = __uint_as_float(raw[r][k].y << 16) * up, x3 = __uint_as_float(raw[r][k].y & 0xffff0000u) * up;
-          qf[r][k][0] = kAdjacent ? pack_half(x0, x1) : pack_half(x0, x2);
-          qf[r][k][1] = kAdjacent ? pack_half(x2, x3) : pack_half(x1, x3);
+          const uint2 v = load(src, k);
+          const float x0 = __uint_as_float(v.x << 16) * up, x1 = __uint_as_float(v.x & 0xffff0000u) * up;
+          const float x2 = __uint_as_float(v.y << 16) * up, x3 = __uint_as_float(v.y & 0xffff0000u) * up;
+          const uint32_t b0 = kAdjacent ? pack_half(x0, x1) : pack_half(x0, x2), b1 = kAdjacent ? pack_half(x2, x3) : pack_half(x1, x3);
+          if constexpr (C::kLean) {
+            asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(sq + (uint32_t)((r * KS + k) * 256)), "r"(b0), "r"(b1) : "memory");
+          } else {
+            qf[r][k][0] = b0;
+            qf[r][k][1] = b1;
+          }
         }
+      }
     }
     // positions of the rows 8 r + 2 i and + 1, which this lane has scores of
     int pos[NR][2];
@@ -251,148 +270,172 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
       if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
       const uint32_t sk = ring + stage * C::kStageBytes, sc = scale_ring + stage * C::kScaleBytes + 4u * (uint32_t)(hs * blocks);
       const int key0 = kt.tile_index(i) * kTile + wk * kKeys;
-      // ---- S^T = K Q^T, two tiles of 16 keys
-      float s[2][NR][4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int r = 0; r < NR; ++r) s[h][r][0] = s[h][r][1] = s[h][r][2] = s[h][r][3] = 0.f;
-#pragma unroll
-        for (int k = 0; k < KS; k += 2) {
-          uint32_t kw[4];  // words of keys 0-7 and 8-15, of this step's 16 elements and the next one's
-          ldmatrix_x4(chunk_at(sk, h, k + mat_chunk), kw);
-#pragma unroll
-          for (int k2 = 0; k2 < 2; ++k2) {
-            uint32_t a0, a1, a2, a3;
-            q8_word_to_half<T, kAdjacent>(kw[2 * k2], a0, a2);
-            q8_word_to_half<T, kAdjacent>(kw[2 * k2 + 1], a1, a3);
-#pragma unroll
-            for (int r = 0; r < NR; ++r) mma_f16(s[h][r], a0, a1, a2, a3, qf[r][k + k2][0], qf[r][k + k2][1]);
-          }
-        }
+      uint32_t sv = 0;
+      if constexpr (HB == 1) {  // both at once, and both are given back at the end
+        const bool wraps = stage + 1 == C::kStages;
+        sv = ring + (wraps ? 0 : stage + 1) * C::kStageBytes;
+        if (!mbar_wait_warp(full(wraps ? 0 : stage + 1), wraps ? phase ^ 1u : phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
       }
-      // ---- scales of this lane's keys 16 h + 8 e + g
-      float ks[2][2], vs[2][2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t at = sc + 4u * (uint32_t)((wk * kKeys + 16 * h + 8 * e + g) >> scale_shift);
-          ks[h][e] = ld_shared_f32(at) * score_scale;
-          vs[h][e] = ld_shared_f32(at + 4u * H * kTile);
-        }
-      advance();
       // keys outside a row's view; whole tiles in everybody's view skip this
       const int last_key = key0 + kKeys - 1;
       const bool whole = last_key <= first_pos && last_key < w.seq.length && (p.window == 0 || key0 > last_pos - p.window || last_key < p.sinks);
       auto in_view = [&](int key) { return (key < kt.hi && key >= kt.lo) || key < kt.sink_hi; };  // of some row
+#pragma unroll 1
+      for (int h0 = 0; h0 < 2; h0 += HB) {
+        // ---- S^T = K Q^T, one or two tiles of 16 keys
+        float s[HB][NR][4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < HB; ++h) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) s[h][r][0] = s[h][r][1] = s[h][r][2] = s[h][r][3] = 0.f;
+#pragma unroll
+          for (int k = 0; k < KS; k += 2) {
+            uint32_t kw[4];  // words of keys 0-7 and 8-15, of this step's 16 elements and the next one's
+            ldmatrix_x4(chunk_at(sk, h0 + h, k + mat_chunk), kw);
+#pragma unroll
+            for (int k2 = 0; k2 < 2; ++k2) {
+              uint32_t a0, a1, a2, a3;
+              q8_word_to_half<T, kAdjacent>(kw[2 * k2], a0, a2);
+              q8_word_to_half<T, kAdjacent>(kw[2 * k2 + 1], a1, a3);
+#pragma unroll
+              for (int r = 0; r < NR; ++r) {
+                uint32_t b0, b1;
+                if constexpr (C::kLean) {
+                  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(b0), "=r"(b1) : "r"(sq + (uint32_t)((r * KS + k + k2) * 256)));
+                } else {
+                  b0 = qf[r][k + k2][0];
+                  b1 = qf[r][k + k2][1];
+                }
+                mma_f16(s[h][r], a0, a1, a2, a3, b0, b1);
+              }
+            }
+          }
+        }
+        // ---- scales of this lane's keys 16 h + 8 e + g
+        float ks[HB][2], vs[HB][2];
+#pragma unroll
+        for (int h = 0; h < HB; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t at = sc + 4u * (uint32_t)((wk * kKeys + 16 * (h0 + h) + 8 * e + g) >> scale_shift);
+            ks[h][e] = ld_shared_f32(at) * score_scale;
+            vs[h][e] = ld_shared_f32(at + 4u * H * kTile);
+          }
+        if constexpr (HB == 2) advance();
+#pragma unroll
+        for (int h = 0; h < HB; ++h)
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[h][r][e] *= ks[h][e >> 1];
+        if (!whole) {
+#pragma unroll
+          for (int h = 0; h < HB; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = key0 + 16 * (h0 + h) + 8 * (e >> 1) + g;
+#pragma unroll
+              for (int r = 0; r < NR; ++r) {
+                const int at = pos[r][e & 1];
+                const bool seen = key <= at && key < w.seq.length && (p.window == 0 || key > at - p.window || key < p.sinks);
+                if (!seen) s[h][r][e] = -INFINITY;
+              }
+              if (!in_view(key)) vs[h][e >> 1] = 0.f;
+            }
+        }
+        // ---- references
+        float v_most = fmaxf(vs[0][0], vs[0][1]);
+        if constexpr (HB == 2) v_most = fmaxf(v_most, fmaxf(vs[1][0], vs[1][1]));
+        float mx[NR][2];
+        bool raise = v_most > v_top;
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[h][r][e] *= ks[h][e >> 1];
-      if (!whole) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int key = key0 + 16 * h + 8 * (e >> 1) + g;
-#pragma unroll
-            for (int r = 0; r < NR; ++r) {
-              const int at = pos[r][e & 1];
-              const bool seen = key <= at && key < w.seq.length && (p.window == 0 || key > at - p.window || key < p.sinks);
-              if (!seen) s[h][r][e] = -INFINITY;
-            }
-            if (!in_view(key)) vs[h][e >> 1] = 0.f;
-          }
-      }
-      // ---- references
-      const float v_most = fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[1][0], vs[1][1]));
-      float mx[NR][2];
-      bool raise = v_most > v_top;
-#pragma unroll
-      for (int r = 0; r < NR; ++r)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          mx[r][e] = fmaxf(fmaxf(s[0][r][e], s[0][r][e + 2]), fmaxf(s[1][r][e], s[1][r][e + 2]));
-          raise |= mx[r][e] > m[r][e] + kRaise;  // also the first finite score of a row (m = -inf)
-        }
-      if (__any_sync(0xffffffffu, raise)) {
-        const float most = warp_max(v_most);
-        float down = 1.f;
-        if (most > v_top) {
-          // the next power of two, within what fp32 has as a power of two times kTopP
-          const float top = __uint_as_float(min(max((__float_as_uint(most) >> 23) + 1u, 27u), 254u) << 23);
-          down = v_top / top;
-          v_top = top;
-        }
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          float alpha[2];
-#pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float top = mx[r][e];
-#pragma unroll
-            for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-            const bool up = top > m[r][e] + kRaise;
-            alpha[e] = up ? ex2(m[r][e] - top) : 1.f;
-            if (up) m[r][e] = top;
-            l[r][e] *= alpha[e];
-            alpha[e] *= down;
+            mx[r][e] = fmaxf(s[0][r][e], s[0][r][e + 2]);
+            if constexpr (HB == 2) mx[r][e] = fmaxf(mx[r][e], fmaxf(s[1][r][e], s[1][r][e + 2]));
+            raise |= mx[r][e] > m[r][e] + kRaise;  // also the first finite score of a row (m = -inf)
+          }
+        if (__any_sync(0xffffffffu, raise)) {
+          const float most = warp_max(v_most);
+          float down = 1.f;
+          if (most > v_top) {
+            // the next power of two, within what fp32 has as a power of two times kTopP
+            const float top = __uint_as_float(min(max((__float_as_uint(most) >> 23) + 1u, 27u), 254u) << 23);
+            down = v_top / top;
+            v_top = top;
           }
 #pragma unroll
-          for (int d = 0; d < MT; ++d) {
-            o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
+          for (int r = 0; r < NR; ++r) {
+            float alpha[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float top = mx[r][e];
+#pragma unroll
+              for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+              const bool up = top > m[r][e] + kRaise;
+              alpha[e] = up ? ex2(m[r][e] - top) : 1.f;
+              if (up) m[r][e] = top;
+              l[r][e] *= alpha[e];
+              alpha[e] *= down;
+            }
+#pragma unroll
+            for (int d = 0; d < MT; ++d) {
+              o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
+            }
+          }
+        }
+        // ---- P^T: exponentials, and times vs_j in fp16
+        const float v_unit = kTopP / v_top;
+        uint32_t pf[HB][NR][2];
+#pragma unroll
+        for (int h = 0; h < HB; ++h) {
+          const float v0 = v_top > 0.f ? vs[h][0] * v_unit : 0.f, v1 = v_top > 0.f ? vs[h][1] * v_unit : 0.f;
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            // a row that has seen nothing yet is referred to 0: its exponentials are 2^-inf = 0
+            const float r0 = m[r][0] == -INFINITY ? 0.f : m[r][0], r1 = m[r][1] == -INFINITY ? 0.f : m[r][1];
+            const float e0 = ex2(s[h][r][0] - r0), e1 = ex2(s[h][r][1] - r1), e2 = ex2(s[h][r][2] - r0), e3 = ex2(s[h][r][3] - r1);
+            l[r][0] += e0 + e2;
+            l[r][1] += e1 + e3;
+            pf[h][r][0] = transpose_8x8(pack_half(e0 * v0, e1 * v0));
+            pf[h][r][1] = transpose_8x8(pack_half(e2 * v1, e3 * v1));
+          }
+        }
+        // ---- O^T += V^T P^T
+        if constexpr (HB == 2) {
+          if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
+          sv = ring + stage * C::kStageBytes;
+        }
+#pragma unroll
+        for (int h = 0; h < HB; ++h) {
+          // Values of keys in nobody's view may be any bits, NaN among them: zeroed, since 0 * NaN is NaN.  A word holds two
+          // elements of key 2 i (of eight) and two of key 2 i + 1.
+          uint32_t mask0 = 0xffffffffu, mask1 = 0xffffffffu;
+          if (!whole) {
+            auto half = [&](int key) { return in_view(key) ? 0xffffu : 0u; };
+            const int key = key0 + 16 * (h0 + h) + 2 * i4;
+            mask0 = half(key) | half(key + 1) << 16;
+            mask1 = half(key + 8) | half(key + 9) << 16;
+          }
+#pragma unroll
+          for (int d = 0; d < MT; d += 2) {
+            uint32_t vw[4];  // words of keys 0-7 and 8-15, of these 16 elements and the next ones
+            ldmatrix_x4_trans(chunk_at(sv, h0 + h, d + mat_chunk), vw);
+            if (!whole) { vw[0] &= mask0; vw[1] &= mask1; vw[2] &= mask0; vw[3] &= mask1; }
+#pragma unroll
+            for (int d2 = 0; d2 < 2; ++d2) {
+              uint32_t a0, a1, a2, a3;
+              q8_word_to_half<T, false>(vw[2 * d2], a0, a1);
+              q8_word_to_half<T, false>(vw[2 * d2 + 1], a2, a3);
+#pragma unroll
+              for (int r = 0; r < NR; ++r) mma_f16(o[d + d2][r], a0, a1, a2, a3, pf[h][r][0], pf[h][r][1]);
+            }
           }
         }
       }
-      // ---- P^T: exponentials, and times vs_j in fp16
-      const float v_unit = kTopP / v_top;
-      uint32_t pf[2][NR][2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float v0 = v_top > 0.f ? vs[h][0] * v_unit : 0.f, v1 = v_top > 0.f ? vs[h][1] * v_unit : 0.f;
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          // a row that has seen nothing yet is referred to 0: its exponentials are 2^-inf = 0
-          const float r0 = m[r][0] == -INFINITY ? 0.f : m[r][0], r1 = m[r][1] == -INFINITY ? 0.f : m[r][1];
-          const float e0 = ex2(s[h][r][0] - r0), e1 = ex2(s[h][r][1] - r1), e2 = ex2(s[h][r][2] - r0), e3 = ex2(s[h][r][3] - r1);
-          l[r][0] += e0 + e2;
-          l[r][1] += e1 + e3;
-          pf[h][r][0] = transpose_8x8(pack_half(e0 * v0, e1 * v0));
-          pf[h][r][1] = transpose_8x8(pack_half(e2 * v1, e3 * v1));
-        }
-      }
-      // ---- O^T += V^T P^T
-      if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
-      const uint32_t sv = ring + stage * C::kStageBytes;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // Values of keys in nobody's view may be any bits, NaN among them: zeroed, since 0 * NaN is NaN.  A word holds two
-        // elements of key 2 i (of eight) and two of key 2 i + 1.
-        uint32_t mask0 = 0xffffffffu, mask1 = 0xffffffffu;
-        if (!whole) {
-          auto half = [&](int key) { return in_view(key) ? 0xffffu : 0u; };
-          const int key = key0 + 16 * h + 2 * i4;
-          mask0 = half(key) | half(key + 1) << 16;
-          mask1 = half(key + 8) | half(key + 9) << 16;
-        }
-#pragma unroll
-        for (int d = 0; d < MT; d += 2) {
-          uint32_t vw[4];  // words of keys 0-7 and 8-15, of these 16 elements and the next ones
-          ldmatrix_x4_trans(chunk_at(sv, h, d + mat_chunk), vw);
-          if (!whole) { vw[0] &= mask0; vw[1] &= mask1; vw[2] &= mask0; vw[3] &= mask1; }
-#pragma unroll
-          for (int d2 = 0; d2 < 2; ++d2) {
-            uint32_t a0, a1, a2, a3;
-            q8_word_to_half<T, false>(vw[2 * d2], a0, a1);
-            q8_word_to_half<T, false>(vw[2 * d2 + 1], a2, a3);
-#pragma unroll
-            for (int r = 0; r < NR; ++r) mma_f16(o[d + d2][r], a0, a1, a2, a3, pf[h][r][0], pf[h][r][1]);
-          }
-        }
-      }
+      if (failed) break;
+      if constexpr (HB == 1) advance();
       advance();
     }
     float unit = v_top * (1.f / kTopP);
@@ -505,19 +548,13 @@ pd_status launch_plan(const pd_paged_attention_desc& d, const Params& p, const P
     return h == 4 ? launch<T, D, 1, 4, 1, 1>(d, p, scales, k, v, s) : h == 2 ? launch<T, D, 1, 2, 2, 1>(d, p, scales, k, v, s) : launch<T, D, 1, 1, 4, 1>(d, p, scales, k, v, s);
   if (plan.rows_per_tile == 16)
     return h == 4 ? launch<T, D, 2, 4, 1, 1>(d, p, scales, k, v, s) : h == 2 ? launch<T, D, 2, 2, 2, 1>(d, p, scales, k, v, s) : launch<T, D, 2, 1, 4, 1>(d, p, scales, k, v, s);
+  if (plan.rows_per_tile == 24)
+    return h == 4 ? launch<T, D, 3, 4, 1, 1>(d, p, scales, k, v, s) : h == 2 ? launch<T, D, 3, 2, 2, 1>(d, p, scales, k, v, s) : launch<T, D, 3, 1, 4, 1>(d, p, scales, k, v, s);
   if (plan.rows_per_tile == 32)
     return h == 2 ? launch<T, D, 2, 2, 1, 2>(d, p, scales, k, v, s) : launch<T, D, 2, 1, 2, 2>(d, p, scales, k, v, s);
   return launch<T, D, 2, 1, 1, 4>(d, p, scales, k, v, s);
 }
 
 }  // namespace
-
-pd_status launch_rows_q8(const pd_paged_attention_desc& d, const Params& p, const Plan& plan, pd_dtype type, const Scales& scales,
-                         const void* k_cache, const void* v_cache, cudaStream_t s) {
-  if (d.head_dim == 64)
-    return type == PD_I8 ? launch_plan<PD_I8, 64>(d, p, plan, scales, k_cache, v_cache, s) : launch_plan<PD_E4M3, 64>(d, p, plan, scales, k_cache, v_cache, s);
-  return type == PD_I8 ? launch_plan<PD_I8, 128>(d, p, plan, scales, k_cache, v_cache, s) : launch_plan<PD_E4M3, 128>(d, p, plan, scales, k_cache, v_cache, s);
-}
-
 }  // namespace paged
 }  // namespace pd

@@ -6,12 +6,15 @@
 //   z = z + bias_ij                                      the last entry of row i's list that names j
 //   z = -inf                                             where row i's mask has bit j cleared
 //
-// Bound: HBM, every logit read once and written once.  A CTA takes 16 logits a thread of one row and loads them first; while
-// they are under way it counts the row's history in shared memory, one word for each of its tokens:
+// Bound: HBM, every logit read once and written once.  A CTA takes 16 logits a thread of one row and has them copied to shared
+// memory (every thread its own, asynchronously); while they are under way it counts the row's history in shared memory, one word for each of its tokens:
 //   bit 31: occurs in the history;  bits 11 ... 30: times behind the prompt;  bits 0 ... 10: 1 + entry of the bias list
 // The counts are integer sums, the entries a maximum, so neither depends on the order in which threads get there.  Every CTA of
-// a row reads the whole history (from the L2 cache, 16 times 32 KB for 8000 tokens of a row of 128000 logits) instead of exchanging
-// parts of it; a row that changes nothing skips the counting.
+// a row reads the whole history (from the L2 cache, 16 times 32 KB for 8000 tokens of a row of 128000 logits), 16 tokens a thread at
+// a time; a row that changes nothing skips the counting.
+//   256 x 128000 fp32 with up to 8000 tokens a row: 91 us with the logits in registers and four tokens at a time, 150 with the
+//   history shared out over a cluster (half of a text's tokens belong to few slices, and additions to another CTA's shared memory
+//   queue there).
 #include "pd_common.cuh"
 
 namespace pd {
@@ -40,17 +43,12 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162f
 __device__ __forceinline__ void put(float* to, float v) { *to = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* to, float v) { *to = __float2bfloat16_rn(v); }
 
-// Four neighbouring logits.
-__device__ __forceinline__ float4 load4(const float* from) { return __ldcs(reinterpret_cast<const float4*>(from)); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* from) {
-  const uint2 v = __ldcs(reinterpret_cast<const uint2*>(from));
-  return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
-}
-
 template <typename In, typename Out, int THREADS>
-__global__ void __launch_bounds__(THREADS) penalize_logits_kernel(const PenaltyParams p) {
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) penalize_logits_kernel(const PenaltyParams p) {
   constexpr int kSlice = THREADS * kEach;
-  __shared__ __align__(16) uint32_t words[kSlice];
+  constexpr int kQuad = 4 * sizeof(In);
+  extern __shared__ __align__(16) uint32_t words[];
+  In* logits = reinterpret_cast<In*>(words + kSlice);
   griddep_wait();
   griddep_launch_dependents();
   const int row = blockIdx.x / p.slices, first = (blockIdx.x % p.slices) * kSlice;
@@ -59,20 +57,15 @@ __global__ void __launch_bounds__(THREADS) penalize_logits_kernel(const PenaltyP
   Out* dst = static_cast<Out*>(p.out) + (int64_t)row * p.ld_out + first;
 
   // this thread's logits: four at a time, THREADS * 4 apart
-  float z[kEach];
 #pragma unroll
   for (int k = 0; k < kEach / 4; ++k) {
     const int j = (k * THREADS + threadIdx.x) * 4;
-    if (p.vectors && j + 4 <= n) {
-      const float4 v = load4(src + j);
-      z[4 * k] = v.x; z[4 * k + 1] = v.y; z[4 * k + 2] = v.z; z[4 * k + 3] = v.w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[4 * k + e] = j + e < n ? as_float(src[j + e]) : 0.f;
-    }
+    if (p.vectors && j + 4 <= n)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(logits + j)), "l"(src + j), "n"(kQuad) : "memory");
   }
   float r = p.repetition ? p.repetition[row] : 1.f;
-  if (!(r > 0.f && r <= 3.402823466e38f)) r = 1.f;
+  if (!(r > 0.f && r <= 3.402823466e38f && 1.f / r <= 3.402823466e38f)) r = 1.f;
+  const float inv = 1.f / r;
   const float f = p.frequency ? p.frequency[row] : 0.f, g = p.presence ? p.presence[row] : 0.f;
   const int length = p.history ? min(max(p.history_len ? p.history_len[row] : p.history_cols, 0), p.history_cols) : 0;
   const int prompt = p.prompt_len ? p.prompt_len[row] : 0;
@@ -93,35 +86,49 @@ __global__ void __launch_bounds__(THREADS) penalize_logits_kernel(const PenaltyP
     }
     if (counts) {
       const int32_t* history = p.history + (int64_t)row * p.ld_history;
-#pragma unroll 4
-      for (int h = threadIdx.x; h < length; h += THREADS) {
-        const uint32_t at = (uint32_t)history[h] - (uint32_t)first;
-        if (at < (uint32_t)n) {
-          if (h >= prompt) atomicAdd(words + at, kOnce);
-          else atomicOr(words + at, kOccurs);
+      constexpr int kAhead = 16;
+      for (int h0 = threadIdx.x; h0 < length; h0 += kAhead * THREADS) {
+        int32_t token[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) token[k] = h0 + k * THREADS < length ? history[h0 + k * THREADS] : -1;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const uint32_t at = (uint32_t)token[k] - (uint32_t)first;
+          if (at < (uint32_t)n) {
+            if (h0 + k * THREADS >= prompt) atomicAdd(words + at, kOnce);
+            else atomicOr(words + at, kOccurs);
+          }
         }
       }
       __syncthreads();
     }
   }
   const uint32_t* mask = p.mask + (int64_t)mask_row * p.ld_mask;
+  asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
   for (int k = 0; k < kEach / 4; ++k) {
     const int j = (k * THREADS + threadIdx.x) * 4;
     if (j >= n) break;
+    const bool quad = p.vectors && j + 4 <= n;
+    float z[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = quad ? as_float(logits[j + e]) : j + e < n ? as_float(src[j + e]) : 0.f;
     if (changes) {
       const uint4 w4 = *reinterpret_cast<const uint4*>(words + j);
       if (w4.x | w4.y | w4.z | w4.w) {
         const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+        // (few instructions and one branch: in a row with a history most warps come through here.  With a division, and a branch for
+        // every case, this took 30 of 89 us.)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float& v = z[4 * k + e];
-          const uint32_t times = (w[e] & ~kOccurs) / kOnce, entry = w[e] & kBiasBits;
-          if (w[e] >= kOnce) {
-            if (r != 1.f) v = v > 0.f ? v / r : v * r;
-            if (times > 0) v = v - f * (float)times - g;
-          }
-          if (entry > 0) v += p.bias_values[(int64_t)row * p.bias_cols + entry - 1];
+          const uint32_t times = (w[e] & ~kOccurs) / kOnce;
+          z[e] *= w[e] < kOnce ? 1.f : z[e] > 0.f ? inv : r;
+          z[e] = times > 0 ? fmaf(-f, (float)times, z[e]) - g : z[e];
+        }
+        if ((w[0] | w[1] | w[2] | w[3]) & kBiasBits) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (w[e] & kBiasBits) z[e] += p.bias_values[(int64_t)row * p.bias_cols + (w[e] & kBiasBits) - 1];
         }
       }
     }
@@ -129,14 +136,14 @@ __global__ void __launch_bounds__(THREADS) penalize_logits_kernel(const PenaltyP
       const uint32_t allowed = __ldg(mask + (first + j) / 32) >> (j % 32);  // (the four lie in one word)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (!((allowed >> e) & 1u)) z[4 * k + e] = -INFINITY;
+        if (!((allowed >> e) & 1u)) z[e] = -INFINITY;
     }
-    if (p.vectors && j + 4 <= n) {
-      store_out4(dst, j / 4, make_float4(z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]));
+    if (quad) {
+      store_out4(dst, j / 4, make_float4(z[0], z[1], z[2], z[3]));
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (j + e < n) put(dst + j + e, z[4 * k + e]);
+        if (j + e < n) put(dst + j + e, z[e]);
     }
   }
 }
@@ -149,8 +156,14 @@ pd_status launch(PenaltyParams& p, int64_t rows, cudaStream_t s) {
   p.slices = (p.vocab + slice - 1) / slice;
   if (rows * p.slices > 0x7fffffff) return PD_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)(rows * p.slices));
-  if (narrow) launch_pdl(penalize_logits_kernel<In, Out, 128>, grid, dim3(128), 0, s, p);
-  else launch_pdl(penalize_logits_kernel<In, Out, 512>, grid, dim3(512), 0, s, p);
+  const size_t smem = (size_t)slice * (4 + sizeof(In));
+  if (narrow) {
+    launch_pdl(penalize_logits_kernel<In, Out, 128>, grid, dim3(128), smem, s, p);
+  } else {
+    static PerDeviceFlag smem_allowed;
+    if (pd_status st = allow_dynamic_smem(penalize_logits_kernel<In, Out, 512>, (int)smem, smem_allowed); st != PD_OK) return st;
+    launch_pdl(penalize_logits_kernel<In, Out, 512>, grid, dim3(512), smem, s, p);
+  }
   return check_launch();
 }
 
