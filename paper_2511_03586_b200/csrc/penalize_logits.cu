@@ -6,21 +6,20 @@
 //   z = z + bias_ij                                      the last entry of row i's list that names j
 //   z = -inf                                             where row i's mask has bit j cleared
 //
-// Bound: HBM, every logit read once and written once.  A CTA takes 16 logits a thread of one row and has them copied to shared
-// memory (every thread its own, asynchronously); while they are under way it counts the row's history in shared memory, one word for each of its tokens:
+// Bound: HBM, every logit read once and written once.  A CTA takes a slice of 32 logits a thread of one row, which it loads first; while
+// they are under way it counts the row's history, in a word of shared memory for each of the slice's tokens:
 //   bit 31: occurs in the history;  bits 11 ... 30: times behind the prompt;  bits 0 ... 10: 1 + entry of the bias list
-// The counts are integer sums, the entries a maximum, so neither depends on the order in which threads get there.  Every CTA of
-// a row reads the whole history (from the L2 cache, 16 times 32 KB for 8000 tokens of a row of 128000 logits), 16 tokens a thread at
-// a time; a row that changes nothing skips the counting.
-//   256 x 128000 fp32 with up to 8000 tokens a row: 91 us with the logits in registers and four tokens at a time, 150 with the
-//   history shared out over a cluster (half of a text's tokens belong to few slices, and additions to another CTA's shared memory
-//   queue there).
+// The counts are integer sums, the entries a maximum, so neither depends on the order in which threads get there.  Every CTA of a
+// row reads the whole history, from the L2 cache.  A row that changes nothing skips the counting.
+//   256 x 128000 fp32, up to 8000 tokens a row, half of the rows masked: 76 us, 45 without histories and biases.  Other forms: slices half as
+//   long (twice as many looks at the history) 82; several slices to a CTA, their logits copied ahead, 80; a plain copy first
+//   and the named tokens mended one by one after it 100; the history shared out over a cluster 150 (half of a text's tokens
+//   belong to few slices, and additions to another CTA's shared memory queue there).
 #include "pd_common.cuh"
 
 namespace pd {
 namespace {
 
-constexpr int kEach = 16;  // logits per thread
 constexpr uint32_t kOccurs = 0x80000000u, kOnce = 1u << 11, kBiasBits = kOnce - 1;
 
 struct PenaltyParams {
@@ -35,7 +34,7 @@ struct PenaltyParams {
   int64_t ld, ld_out, ld_history, ld_mask;
   int vocab, history_cols, bias_cols, mask_rows;
   int slices;  // CTAs of a row
-  int vectors; // rows of logits and of results begin on 16-byte boundaries
+  int vectors;  // rows of logits and of results begin where four elements may be accessed at once
 };
 
 __device__ __forceinline__ float as_float(float v) { return v; }
@@ -43,54 +42,78 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162f
 __device__ __forceinline__ void put(float* to, float v) { *to = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* to, float v) { *to = __float2bfloat16_rn(v); }
 
-template <typename In, typename Out, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS) penalize_logits_kernel(const PenaltyParams p) {
-  constexpr int kSlice = THREADS * kEach;
-  constexpr int kQuad = 4 * sizeof(In);
+// Four neighbouring logits.
+__device__ __forceinline__ void load4(const float* from, float* z) {
+  const float4 v = __ldcs(reinterpret_cast<const float4*>(from));
+  z[0] = v.x; z[1] = v.y; z[2] = v.z; z[3] = v.w;
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* from, float* z) {
+  const uint2 v = __ldcs(reinterpret_cast<const uint2*>(from));
+  z[0] = __uint_as_float(v.x << 16); z[1] = __uint_as_float(v.x & 0xffff0000u);
+  z[2] = __uint_as_float(v.y << 16); z[3] = __uint_as_float(v.y & 0xffff0000u);
+}
+
+// EACH logits per thread.
+template <typename In, typename Out, int THREADS, int EACH>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) penalize_logits_kernel(const PenaltyParams p) {
+  constexpr int kSlice = THREADS * EACH, kAhead = 8;
   extern __shared__ __align__(16) uint32_t words[];
-  In* logits = reinterpret_cast<In*>(words + kSlice);
   griddep_wait();
   griddep_launch_dependents();
   const int row = blockIdx.x / p.slices, first = (blockIdx.x % p.slices) * kSlice;
   const int n = min(kSlice, p.vocab - first);
   const In* src = static_cast<const In*>(p.logits) + (int64_t)row * p.ld + first;
   Out* dst = static_cast<Out*>(p.out) + (int64_t)row * p.ld_out + first;
-
-  // this thread's logits: four at a time, THREADS * 4 apart
-#pragma unroll
-  for (int k = 0; k < kEach / 4; ++k) {
-    const int j = (k * THREADS + threadIdx.x) * 4;
-    if (p.vectors && j + 4 <= n)
-      asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(logits + j)), "l"(src + j), "n"(kQuad) : "memory");
-  }
+  // Everything that is read is asked for before anything is waited for, but the history, which waits for its length.
   float r = p.repetition ? p.repetition[row] : 1.f;
-  if (!(r > 0.f && r <= 3.402823466e38f && 1.f / r <= 3.402823466e38f)) r = 1.f;
-  const float inv = 1.f / r;
   const float f = p.frequency ? p.frequency[row] : 0.f, g = p.presence ? p.presence[row] : 0.f;
-  const int length = p.history ? min(max(p.history_len ? p.history_len[row] : p.history_cols, 0), p.history_cols) : 0;
+  int length = 0;
+  if (p.history) length = p.history_len ? p.history_len[row] : p.history_cols;
   const int prompt = p.prompt_len ? p.prompt_len[row] : 0;
   const int mask_row = !p.mask ? -1 : p.mask_row ? p.mask_row[row] : row;
+  const int32_t* history = p.history + (int64_t)row * p.ld_history;
+  const int32_t* bias_tokens = p.bias_tokens + (int64_t)row * p.bias_cols;
+  const int32_t bias_token = (int)threadIdx.x < p.bias_cols ? bias_tokens[threadIdx.x] : -1;
+  // this thread's logits: four at a time, THREADS * 4 apart
+  float z[EACH];
+  auto place = [&](int k) { return (k * THREADS + (int)threadIdx.x) * 4; };
+#pragma unroll
+  for (int k = 0; k < EACH / 4; ++k) {
+    const int j = place(k);
+    if (p.vectors && j + 4 <= n) {
+      load4(src + j, z + 4 * k);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[4 * k + e] = j + e < n ? as_float(src[j + e]) : 0.f;
+    }
+  }
+  if (!(r > 0.f && r <= 3.402823466e38f && 1.f / r <= 3.402823466e38f)) r = 1.f;
+  const float inv = 1.f / r;
+  length = min(max(length, 0), p.history_cols);
   const bool masked = mask_row >= 0 && mask_row < p.mask_rows;
   const bool counts = length > 0 && (r != 1.f || f != 0.f || g != 0.f);
   const bool changes = counts || p.bias_cols > 0;  // (the same for all threads)
   if (changes) {
+    int32_t token[kAhead];
+    auto load = [&](int h0) {
 #pragma unroll
-    for (int k = 0; k < kEach / 4; ++k) *reinterpret_cast<uint4*>(words + (k * THREADS + threadIdx.x) * 4) = make_uint4(0, 0, 0, 0);
+      for (int k = 0; k < kAhead; ++k) token[k] = h0 + k * THREADS < length ? history[h0 + k * THREADS] : -1;
+    };
+    if (counts) load(threadIdx.x);
+#pragma unroll
+    for (int k = 0; k < EACH / 4; ++k) *reinterpret_cast<uint4*>(words + place(k)) = make_uint4(0, 0, 0, 0);
     __syncthreads();
     if (p.bias_cols > 0) {
-      for (int e = threadIdx.x; e < p.bias_cols; e += THREADS) {
-        const uint32_t at = (uint32_t)p.bias_tokens[(int64_t)row * p.bias_cols + e] - (uint32_t)first;
+      auto set_bias = [&](int32_t t, int e) {
+        const uint32_t at = (uint32_t)t - (uint32_t)first;
         if (at < (uint32_t)n) atomicMax(words + at, (uint32_t)e + 1u);
-      }
+      };
+      set_bias(bias_token, threadIdx.x);
+      for (int e = THREADS + threadIdx.x; e < p.bias_cols; e += THREADS) set_bias(bias_tokens[e], e);
       __syncthreads();
     }
     if (counts) {
-      const int32_t* history = p.history + (int64_t)row * p.ld_history;
-      constexpr int kAhead = 16;
       for (int h0 = threadIdx.x; h0 < length; h0 += kAhead * THREADS) {
-        int32_t token[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) token[k] = h0 + k * THREADS < length ? history[h0 + k * THREADS] : -1;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
           const uint32_t at = (uint32_t)token[k] - (uint32_t)first;
@@ -99,36 +122,34 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) penalize_logits_kerne
             else atomicOr(words + at, kOccurs);
           }
         }
+        load(h0 + kAhead * THREADS);
       }
       __syncthreads();
     }
   }
   const uint32_t* mask = p.mask + (int64_t)mask_row * p.ld_mask;
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  const float* bias_values = p.bias_values + (int64_t)row * p.bias_cols;
 #pragma unroll
-  for (int k = 0; k < kEach / 4; ++k) {
-    const int j = (k * THREADS + threadIdx.x) * 4;
+  for (int k = 0; k < EACH / 4; ++k) {
+    const int j = place(k);
     if (j >= n) break;
-    const bool quad = p.vectors && j + 4 <= n;
-    float z[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = quad ? as_float(logits[j + e]) : j + e < n ? as_float(src[j + e]) : 0.f;
+    float* v = z + 4 * k;
     if (changes) {
       const uint4 w4 = *reinterpret_cast<const uint4*>(words + j);
       if (w4.x | w4.y | w4.z | w4.w) {
+        // (few instructions and one branch: in a row with a history most warps come through here; with a division, and a branch for
+        // every case, this took 10 us more)
         const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-        // (few instructions and one branch: in a row with a history most warps come through here.  With a division, and a branch for
-        // every case, this took 30 of 89 us.)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t times = (w[e] & ~kOccurs) / kOnce;
-          z[e] *= w[e] < kOnce ? 1.f : z[e] > 0.f ? inv : r;
-          z[e] = times > 0 ? fmaf(-f, (float)times, z[e]) - g : z[e];
+          v[e] *= w[e] < kOnce ? 1.f : v[e] > 0.f ? inv : r;
+          v[e] = times > 0 ? fmaf(-f, (float)times, v[e]) - g : v[e];
         }
         if ((w[0] | w[1] | w[2] | w[3]) & kBiasBits) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (w[e] & kBiasBits) z[e] += p.bias_values[(int64_t)row * p.bias_cols + (w[e] & kBiasBits) - 1];
+            if (w[e] & kBiasBits) v[e] += bias_values[(w[e] & kBiasBits) - 1];
         }
       }
     }
@@ -136,33 +157,33 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) penalize_logits_kerne
       const uint32_t allowed = __ldg(mask + (first + j) / 32) >> (j % 32);  // (the four lie in one word)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (!((allowed >> e) & 1u)) z[e] = -INFINITY;
+        if (!((allowed >> e) & 1u)) v[e] = -INFINITY;
     }
-    if (quad) {
-      store_out4(dst, j / 4, make_float4(z[0], z[1], z[2], z[3]));
+    if (p.vectors && j + 4 <= n) {
+      store_out4(dst, j / 4, make_float4(v[0], v[1], v[2], v[3]));
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (j + e < n) put(dst + j + e, z[e]);
+        if (j + e < n) put(dst + j + e, v[e]);
     }
   }
 }
 
 template <typename In, typename Out>
 pd_status launch(PenaltyParams& p, int64_t rows, cudaStream_t s) {
-  // 512 threads, 8192 logits per CTA; 128 and 2048 where that would leave SMs without work
-  const bool narrow = rows * ((p.vocab + 8191) / 8192) < 2 * 148;
-  const int slice = narrow ? 2048 : 8192;
+  // 512 threads, 16384 logits to a slice; 128 and 2048 where that would leave SMs without work.
+  const bool narrow = rows * ((p.vocab + 16383) / 16384) < 2 * 148;
+  const int slice = narrow ? 2048 : 16384;
   p.slices = (p.vocab + slice - 1) / slice;
   if (rows * p.slices > 0x7fffffff) return PD_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)(rows * p.slices));
-  const size_t smem = (size_t)slice * (4 + sizeof(In));
+  const size_t smem = (size_t)slice * 4;
   if (narrow) {
-    launch_pdl(penalize_logits_kernel<In, Out, 128>, grid, dim3(128), smem, s, p);
+    launch_pdl(penalize_logits_kernel<In, Out, 128, 16>, grid, dim3(128), smem, s, p);
   } else {
     static PerDeviceFlag smem_allowed;
-    if (pd_status st = allow_dynamic_smem(penalize_logits_kernel<In, Out, 512>, (int)smem, smem_allowed); st != PD_OK) return st;
-    launch_pdl(penalize_logits_kernel<In, Out, 512>, grid, dim3(512), smem, s, p);
+    if (pd_status st = allow_dynamic_smem(penalize_logits_kernel<In, Out, 512, 32>, (int)smem, smem_allowed); st != PD_OK) return st;
+    launch_pdl(penalize_logits_kernel<In, Out, 512, 32>, grid, dim3(512), smem, s, p);
   }
   return check_launch();
 }
