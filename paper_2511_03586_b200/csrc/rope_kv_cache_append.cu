@@ -13,10 +13,11 @@
 // a decode batch is one launch and a chain of four dependent loads.
 //
 // The 8-bit cache: a block's scale is its largest magnitude over the top of the type, so all of its new tokens have to be seen
-// before the first is rounded.  A CTA takes one block of one sequence, a warp one head of K or V of it: the warp's share is held
-// in registers between the two passes as long as it has at most 512 units of 8 elements (32 tokens of 128), and read again, from
-// the L2 cache, beyond that.  Values are rounded once, from the rotated fp32 ones.  A block that held older tokens keeps its scale
-// unless a new token exceeds it; then the older values are rounded again, to the larger step.
+// before the first is rounded.  A CTA takes one block of one sequence and up to eight heads of K or of V of it, a warp or, for blocks
+// of more than 256 units of 8 elements (16 tokens of 128), several to a head; they hold the block in registers between the two passes as
+// long as it has at most 2048 units, and read it again, from the L2 cache, beyond that.  Values are rounded once, from the rotated fp32
+// ones.  A block that held older tokens keeps its scale unless a new token exceeds it; then the older values are rounded again,
+// to the larger step.
 #include "cache_q8.cuh"
 
 namespace pd {
@@ -25,8 +26,8 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnit = 8;         // elements that one lane handles at a time: four pairs, or eight elements that are not rotated
-constexpr int kHeld = 16;        // units a lane holds between the passes of the 8-bit form
-constexpr int kGroup = 32 * kHeld;
+constexpr int kHeld = 8;         // units a lane holds between the passes of the 8-bit form
+constexpr int kGroup = 32 * kHeld;  // and a warp
 constexpr int kMaxDim = 256;
 constexpr int kMaxPairs = kMaxDim / 2;
 constexpr int kMaxIndex = 1 << 30;
@@ -45,7 +46,8 @@ struct RopeParams {
   int batch, tokens, heads_q, heads_kv, head_dim;
   int num_pages, page_size, max_pages;
   int parts;           // warps that share a token
-  int rounds;          // 8-bit form: CTAs that share a block, each up to kWarps heads of K or of V
+  int warps_a_head;    // 8-bit form: warps that share a head of a block
+  int rounds;          // 8-bit form: CTAs that share a block, each up to kWarps / warps_a_head heads of K or of V
   int64_t block_ctas;  // 8-bit form: CTAs in front of the ones that rotate queries
 };
 
@@ -115,12 +117,58 @@ __device__ __forceinline__ void store_unit(__nv_bfloat16* head, const Place& at,
 struct NewTokens {
   int q0, n, pos0;
 };
-__device__ __forceinline__ NewTokens new_tokens(const RopeParams& p, int b) {
+__device__ __forceinline__ NewTokens new_tokens(const RopeParams& p, int from, int to, int length) {
   NewTokens s;
-  s.q0 = min(max(__ldg(p.cu_q + b), 0), p.tokens);
-  s.n = min(max(__ldg(p.cu_q + b + 1), s.q0), p.tokens) - s.q0;
-  s.pos0 = max(__ldg(p.kv_len + b), 0) - s.n;
+  s.q0 = min(max(from, 0), p.tokens);
+  s.n = min(max(to, s.q0), p.tokens) - s.q0;
+  s.pos0 = max(length, 0) - s.n;
   return s;
+}
+// The number of sequences b >= 0 in front of the first one for which inside(b, cu_q[b], cu_q[b + 1]) is false (it holds for leading
+// ones only), and in `s` the tokens of sequence `that number - back`.  A warp.  Up to 128 sequences are looked at at once, with
+// their lengths, so that a decode batch waits for one round of loads instead of three.
+template <typename F>
+__device__ __forceinline__ int find_tokens(const RopeParams& p, int back, NewTokens& s, F inside) {
+  const int lane = threadIdx.x & 31;
+  int b;
+  if (p.batch <= 128) {
+    int from[4], to[4], length[4], n = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = lane + 32 * k;
+      const bool there = i < p.batch;
+      from[k] = there ? __ldg(p.cu_q + i) : 0;
+      to[k] = there ? __ldg(p.cu_q + i + 1) : 0;
+      length[k] = there ? __ldg(p.kv_len + i) : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) n += __popc(__ballot_sync(0xffffffffu, lane + 32 * k < p.batch && inside(lane + 32 * k, from[k], to[k])));
+    b = n;
+    const int at = min(max(b - back, 0), 127);
+    int f = 0, e = 0, l = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int f1 = __shfl_sync(0xffffffffu, from[k], at & 31), e1 = __shfl_sync(0xffffffffu, to[k], at & 31), l1 = __shfl_sync(0xffffffffu, length[k], at & 31);
+      if (at >> 5 == k) { f = f1; e = e1; l = l1; }
+    }
+    s = new_tokens(p, f, e, l);
+    return b;
+  }
+  int lo = 0, hi = p.batch;  // the answer lies in [lo, hi]
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32;
+    const int i = lo + lane * step;
+    const unsigned yes = __ballot_sync(0xffffffffu, i < hi && inside(i, __ldg(p.cu_q + min(i, p.batch - 1)), __ldg(p.cu_q + min(i, p.batch - 1) + 1)));
+    const int k = __popc(yes);
+    if (k == 0) break;
+    const int next = lo + (k - 1) * step + 1;
+    hi = min(lo + k * step, hi);
+    lo = next;
+  }
+  b = lo;
+  const int at = min(max(b - back, 0), p.batch - 1);
+  s = new_tokens(p, __ldg(p.cu_q + at), __ldg(p.cu_q + at + 1), __ldg(p.kv_len + at));
+  return b;
 }
 __device__ __forceinline__ int page_at(const RopeParams& p, int b, int pos) {
   const int i = pos / p.page_size;
@@ -137,9 +185,9 @@ __device__ __forceinline__ int page_at(const RopeParams& p, int b, int pos) {
 template <bool CACHE, int AHEAD>
 __device__ __forceinline__ void rotate_token(const RopeParams& p, int t, int part, float2* turns) {
   const int lane = threadIdx.x & 31;
-  const int b = paged::find_sequence(p.cu_q, p.batch, t);
-  if (b >= p.batch || t < __ldg(p.cu_q + b)) return;  // padding behind the last sequence
-  const NewTokens s = new_tokens(p, b);
+  NewTokens s;
+  const int b = find_tokens(p, 0, s, [&](int, int, int to) { return to <= t; });
+  if (b >= p.batch || t < s.q0) return;  // padding behind the last sequence
   const int pos = s.pos0 + (t - s.q0);
   if (pos < 0) return;
   const int page = CACHE ? page_at(p, b, pos) : -1;
@@ -206,32 +254,21 @@ __device__ __forceinline__ void rotate_token(const RopeParams& p, int t, int par
 
 // Where the blocks of sequence b begin in the count of places for blocks: as many as its new tokens can touch, and no more
 // than one and two halves of them, so that a place's sequence is found from cu_q alone.
-__device__ __forceinline__ int64_t first_block_place(const RopeParams& p, int b) {
-  return (int64_t)(min(max(__ldg(p.cu_q + b), 0), p.tokens) >> p.scales.shift) + 2 * (int64_t)b;
+__device__ __forceinline__ int64_t first_block_place(const RopeParams& p, int b, int from) {
+  return (int64_t)(min(max(from, 0), p.tokens) >> p.scales.shift) + 2 * (int64_t)b;
 }
 
-// One block of one sequence, and up to kWarps heads of K or of V of it.  A CTA.
+// One block of one sequence, and some heads of K or of V of it.  A CTA.
 template <pd_dtype T>
-__device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t place, int round, float2* turns) {
+__device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t place, int round, float2* turns, float* largest) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  // the last sequence whose places begin at or in front of `place`: a 32-way search by every warp for itself
-  int lo = 0, hi = p.batch - 1;
-  while (lo < hi) {
-    const int step = (hi - lo + 31) / 32;
-    const int i = lo + 1 + lane * step;
-    const unsigned le = __ballot_sync(0xffffffffu, i <= hi && first_block_place(p, i) <= place);
-    const int k = __popc(le);
-    if (k == 0) { hi = lo; break; }
-    const int next = lo + 1 + (k - 1) * step;
-    hi = min(lo + k * step, hi);
-    lo = next;
-  }
-  const int b = lo;
-  const NewTokens s = new_tokens(p, b);
+  // the last sequence whose places begin at or in front of `place`
+  NewTokens s;
+  const int b = max(find_tokens(p, 1, s, [&](int i, int from, int) { return first_block_place(p, i, from) <= place; }) - 1, 0);
   const int shift = p.scales.shift;
   const int from = max(s.pos0, 0), to = s.pos0 + s.n;  // positions of the new tokens that have one
   if (from >= to) return;
-  const int64_t index = (from >> shift) + (place - first_block_place(p, b));
+  const int64_t index = (from >> shift) + (place - first_block_place(p, b, s.q0));
   if (index > ((to - 1) >> shift)) return;
   const int start = (int)index << shift;
   const int page = page_at(p, b, start);
@@ -240,20 +277,21 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
   const int old = first - start;  // older tokens of the block
   const int slot0 = start % p.page_size;
 
-  const int rounds_k = (p.heads_kv + kWarps - 1) / kWarps;
+  const int heads_a_cta = kWarps / p.warps_a_head, part = warp % p.warps_a_head;
+  const int rounds_k = p.rounds / 2;
   const bool keys = round < rounds_k;
-  const int head = (keys ? round : round - rounds_k) * kWarps + warp;
+  const int head = (keys ? round : round - rounds_k) * heads_a_cta + warp / p.warps_a_head;
   const bool mine = head < p.heads_kv;
   const int units = p.head_dim / kUnit;
   const int shift_u = 31 - __clz(units);
   const bool power = (units & (units - 1)) == 0;
-  auto token_of = [&](int i) { return power ? i >> shift_u : i / units; };  // of a unit in the group
+  auto token_of = [&](int i) { return power ? i >> shift_u : i / units; };  // of a unit in the warp's share
   const __nv_bfloat16* src = (keys ? p.k_new : p.v_new) + (int64_t)(s.q0 + first - s.pos0) * p.ld_new + (int64_t)head * p.head_dim;
   uint8_t* dst = (keys ? p.k_cache : p.v_cache) + (int64_t)page * p.page_stride + (int64_t)slot0 * p.slot_stride + (int64_t)head * p.head_stride;
   float* scale_at = (keys ? p.k_scale : p.v_scale) + p.scales.at(page, head, slot0);
   const float before = mine && old > 0 ? *scale_at : 0.f;
 
-  const int per_group = kGroup / units;  // tokens
+  const int per_warp = kGroup / units, per_group = per_warp * p.warps_a_head;  // tokens
   const int tokens = last - first, groups = (tokens + per_group - 1) / per_group;
   const int pairs = p.rotary / 2;
   auto place_in = [&](int u) {
@@ -261,15 +299,18 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
     if (!keys) { at.rotated = at.split = false; at.first = u * kUnit; at.second = at.first + 4; }
     return at;
   };
+  // this warp's tokens of group g: from t0 of the block's new ones on, n units
+  auto first_token = [&](int g) { return g * per_group + part * per_warp; };
+  auto units_in = [&](int g) { return mine ? max(min(per_warp, tokens - first_token(g)), 0) * units : 0; };
   uint4 held[kHeld];
   auto load_group = [&](int g) {
-    const int n = min(per_group, tokens - g * per_group) * units;
+    const int n = units_in(g);
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
       const int i = lane + 32 * j;
-      if (mine && i < n) {
+      if (i < n) {
         const int t = token_of(i);
-        held[j] = load_unit(src + (int64_t)(g * per_group + t) * p.ld_new, place_in(i - t * units));
+        held[j] = load_unit(src + (int64_t)(first_token(g) + t) * p.ld_new, place_in(i - t * units));
       }
     }
   };
@@ -283,24 +324,30 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
     }
     __syncthreads();
   };
+  const float2* my_turns = turns + part * per_warp * pairs;
   float most = 0.f;
   for (int g = 0; g < groups; ++g) {
     load_group(g);
     turn_group(g);
-    const int n = mine ? min(per_group, tokens - g * per_group) * units : 0;
+    const int n = units_in(g);
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
       const int i = lane + 32 * j;
       if (i < n) {
         const int t = token_of(i), u = i - t * units;
         float x[8];
-        rotate_unit(held[j], place_in(u), turns + t * pairs + 4 * u, x);
+        rotate_unit(held[j], place_in(u), my_turns + t * pairs + 4 * u, x);
 #pragma unroll
         for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[k]));
       }
     }
   }
   most = warp_max(most);
+  if (p.warps_a_head > 1) {
+    if (lane == 0) largest[warp] = most;
+    __syncthreads();
+    for (int k = 0; k < p.warps_a_head; ++k) most = fmaxf(most, largest[warp - part + k]);
+  }
   // (a scale below the normal range would have no reciprocal)
   const float need = most > 0.f ? fmaxf(most / paged::q8_top<T>(), 1.17549435e-38f) : 0.f;
   const float scale = fmaxf(before, need), inv = scale > 0.f ? 1.f / scale : 0.f;
@@ -309,7 +356,7 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
       load_group(g);
       turn_group(g);
     }
-    const int n = mine ? min(per_group, tokens - g * per_group) * units : 0;
+    const int n = units_in(g);
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
       const int i = lane + 32 * j;
@@ -317,13 +364,13 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
         const int t = token_of(i), u = i - t * units;
         const Place at = place_in(u);
         float x[8];
-        rotate_unit(held[j], at, turns + t * pairs + 4 * u, x);
+        rotate_unit(held[j], at, my_turns + t * pairs + 4 * u, x);
         uint32_t w[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           w[k] = paged::q8_pair_from_float<T>(x[4 * k] * inv, x[4 * k + 1] * inv) |
                  paged::q8_pair_from_float<T>(x[4 * k + 2] * inv, x[4 * k + 3] * inv) << 16;
-        uint8_t* row = dst + (int64_t)(old + g * per_group + t) * p.slot_stride;
+        uint8_t* row = dst + (int64_t)(old + first_token(g) + t) * p.slot_stride;
         if (at.split) {
           *reinterpret_cast<uint32_t*>(row + at.first) = w[0];
           *reinterpret_cast<uint32_t*>(row + at.second) = w[1];
@@ -335,21 +382,34 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
   }
   if (!mine) return;
   if (old > 0 && scale > before) {
-    const float ratio = before / scale;
-    for (int i = lane; i < old * units; i += 32) {
-      const int t = i / units;
-      uint2* at = reinterpret_cast<uint2*>(dst + (int64_t)t * p.slot_stride + (i - t * units) * kUnit);
-      const uint2 v = *at;
-      uint32_t w[2] = {v.x, v.y};
+    // older values, to the larger step; the products in 64 bits, since 8 bits times the ratio of two scales can lie next to a border
+    const double ratio = (double)before / (double)scale;
+    constexpr int kAhead = 4;
+    const int n = old * units, stride = 32 * p.warps_a_head;
+    for (int i0 = part * 32 + lane; i0 < n; i0 += kAhead * stride) {
+      uint2 v[kAhead];
+      uint2* at[kAhead];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const float2 a = paged::q8_pair_to_float<T>(w[k]), c = paged::q8_pair_to_float<T>(w[k] >> 16);
-        w[k] = paged::q8_pair_from_float<T>(a.x * ratio, a.y * ratio) | paged::q8_pair_from_float<T>(c.x * ratio, c.y * ratio) << 16;
+      for (int a = 0; a < kAhead; ++a) {
+        const int i = min(i0 + a * stride, n - 1), t = token_of(i);
+        at[a] = reinterpret_cast<uint2*>(dst + (int64_t)t * p.slot_stride + (i - t * units) * kUnit);
+        v[a] = *at[a];
       }
-      *at = make_uint2(w[0], w[1]);
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        if (i0 + a * stride >= n) break;
+        uint32_t w[2] = {v[a].x, v[a].y};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float2 x = paged::q8_pair_to_float<T>(w[k]), y = paged::q8_pair_to_float<T>(w[k] >> 16);
+          w[k] = paged::q8_pair_from_float<T>((float)(x.x * ratio), (float)(x.y * ratio)) |
+                 paged::q8_pair_from_float<T>((float)(y.x * ratio), (float)(y.y * ratio)) << 16;
+        }
+        *at[a] = make_uint2(w[0], w[1]);
+      }
     }
   }
-  if (lane == 0) *scale_at = scale;
+  if (lane == 0 && part == 0) *scale_at = scale;
 }
 
 // bf16 cache: a warp for every part of a token.
@@ -365,19 +425,20 @@ __global__ void __launch_bounds__(kThreads) rope_kv_cache_append_kernel(const Ro
 
 // 8-bit cache: the first CTAs take blocks of keys and values, the others parts of tokens' queries.
 template <pd_dtype T>
-__global__ void __launch_bounds__(kThreads, 2) rope_kv_cache_append_q8_kernel(const RopeParams p) {
-  __shared__ float2 turns[kGroup * 4];  // of a group's tokens: 512 units, at most four pairs each
+__global__ void __launch_bounds__(kThreads, 4) rope_kv_cache_append_q8_kernel(const RopeParams p) {
+  extern __shared__ float2 turns[];  // of a group's tokens: at most four pairs to a unit, kGroup units to each of warps_a_head warps
+  __shared__ float largest[kWarps];
   static_assert(kWarps * kMaxPairs <= kGroup * 4);
   griddep_wait();
   griddep_launch_dependents();
   if ((int64_t)blockIdx.x < p.block_ctas) {
-    quantise_block<T>(p, blockIdx.x / p.rounds, blockIdx.x % p.rounds, turns);
+    quantise_block<T>(p, blockIdx.x / p.rounds, blockIdx.x % p.rounds, turns, largest);
     return;
   }
   const int warp = threadIdx.x >> 5;
   const int64_t w = ((int64_t)blockIdx.x - p.block_ctas) * kWarps + warp;
   const int64_t t = w / p.parts;
-  if (t < p.tokens) rotate_token<false, 8>(p, (int)t, (int)(w - t * p.parts), turns + warp * kMaxPairs);
+  if (t < p.tokens) rotate_token<false, 4>(p, (int)t, (int)(w - t * p.parts), turns + warp * kMaxPairs);
 }
 
 }  // namespace
@@ -439,7 +500,11 @@ extern "C" pd_status pd_rope_kv_cache_append(const pd_paged_attention_desc* desc
   if (scales) {
     p.scales = paged::make_scales(*scales, d.heads_kv, d.page_size);
     p.k_scale = scales->k_scale; p.v_scale = scales->v_scale;
-    p.rounds = 2 * ((d.heads_kv + kWarps - 1) / kWarps);
+    // as many warps to a head as hold a block's units, while there are heads and tokens for the other warps
+    p.warps_a_head = 1;
+    while (p.warps_a_head < kWarps && (int64_t)scales->block * (d.head_dim / kUnit) > (int64_t)kGroup * p.warps_a_head) p.warps_a_head *= 2;
+    const int heads_a_cta = kWarps / p.warps_a_head;
+    p.rounds = 2 * ((d.heads_kv + heads_a_cta - 1) / heads_a_cta);
     p.block_ctas = (((int64_t)d.tokens >> p.scales.shift) + 2 * (int64_t)d.batch) * p.rounds;
   }
   const int64_t ctas = p.block_ctas + token_ctas;
@@ -447,8 +512,15 @@ extern "C" pd_status pd_rope_kv_cache_append(const pd_paged_attention_desc* desc
   if (pd_status st = require_sm100(); st != PD_OK) return st;
   logf("rope kv cache append: %d tokens of %d sequences, %s cache, %lld + %lld CTAs", d.tokens, d.batch,
        !scales ? "bf16" : scales->dtype == PD_I8 ? "int8" : "e4m3", (long long)p.block_ctas, (long long)token_ctas);
-  auto kernel = !scales ? rope_kv_cache_append_kernel
-                        : scales->dtype == PD_I8 ? rope_kv_cache_append_q8_kernel<PD_I8> : rope_kv_cache_append_q8_kernel<PD_E4M3>;
-  launch_pdl(kernel, dim3((unsigned)ctas), dim3(kThreads), 0, stream, p);
+  const dim3 grid((unsigned)ctas), block(kThreads);
+  if (!scales) {
+    launch_pdl(rope_kv_cache_append_kernel, grid, block, 0, stream, p);
+    return check_launch();
+  }
+  auto kernel = scales->dtype == PD_I8 ? rope_kv_cache_append_q8_kernel<PD_I8> : rope_kv_cache_append_q8_kernel<PD_E4M3>;
+  static PerDeviceFlag smem_allowed[2];
+  const size_t turn_bytes = (size_t)p.warps_a_head * kGroup * 4 * sizeof(float2);
+  if (pd_status st = allow_dynamic_smem(kernel, kWarps * kGroup * 4 * (int)sizeof(float2), smem_allowed[scales->dtype == PD_I8]); st != PD_OK) return st;
+  launch_pdl(kernel, grid, block, turn_bytes, stream, p);
   return check_launch();
 }
