@@ -288,26 +288,34 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
         for (int h = 0; h < HB; ++h) {
 #pragma unroll
           for (int r = 0; r < NR; ++r) s[h][r][0] = s[h][r][1] = s[h][r][2] = s[h][r][3] = 0.f;
+          // words of keys 0-7 and 8-15, of two steps' 16 elements each; lean: these and the queries are asked for a step ahead
+          uint32_t kw[2][4], qb[2][NR][2];
+          auto keys_of = [&](int k) { ldmatrix_x4(chunk_at(sk, h0 + h, k + mat_chunk), kw[(k >> 1) & 1]); };
+          auto queries_of = [&](int k) {
 #pragma unroll
-          for (int k = 0; k < KS; k += 2) {
-            uint32_t kw[4];  // words of keys 0-7 and 8-15, of this step's 16 elements and the next one's
-            ldmatrix_x4(chunk_at(sk, h0 + h, k + mat_chunk), kw);
+            for (int r = 0; r < NR; ++r)
+              asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(qb[k & 1][r][0]), "=r"(qb[k & 1][r][1]) : "r"(sq + (uint32_t)((r * KS + k) * 256)));
+          };
+          if constexpr (C::kLean) {
+            keys_of(0);
+            queries_of(0);
+          }
 #pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
-              uint32_t a0, a1, a2, a3;
-              q8_word_to_half<T, kAdjacent>(kw[2 * k2], a0, a2);
-              q8_word_to_half<T, kAdjacent>(kw[2 * k2 + 1], a1, a3);
+          for (int k = 0; k < KS; ++k) {
+            if constexpr (C::kLean) {
+              if (k % 2 == 0 && k + 2 < KS) keys_of(k + 2);
+              if (k + 1 < KS) queries_of(k + 1);
+            } else if (k % 2 == 0) {
+              keys_of(k);
+            }
+            const uint32_t* words = kw[(k >> 1) & 1] + 2 * (k & 1);
+            uint32_t a0, a1, a2, a3;
+            q8_word_to_half<T, kAdjacent>(words[0], a0, a2);
+            q8_word_to_half<T, kAdjacent>(words[1], a1, a3);
 #pragma unroll
-              for (int r = 0; r < NR; ++r) {
-                uint32_t b0, b1;
-                if constexpr (C::kLean) {
-                  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(b0), "=r"(b1) : "r"(sq + (uint32_t)((r * KS + k + k2) * 256)));
-                } else {
-                  b0 = qf[r][k + k2][0];
-                  b1 = qf[r][k + k2][1];
-                }
-                mma_f16(s[h][r], a0, a1, a2, a3, b0, b1);
-              }
+            for (int r = 0; r < NR; ++r) {
+              if constexpr (C::kLean) mma_f16(s[h][r], a0, a1, a2, a3, qb[k & 1][r][0], qb[k & 1][r][1]);
+              else mma_f16(s[h][r], a0, a1, a2, a3, qf[r][k][0], qf[r][k][1]);
             }
           }
         }
@@ -418,16 +426,19 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
             mask0 = half(key) | half(key + 1) << 16;
             mask1 = half(key + 8) | half(key + 9) << 16;
           }
+          uint32_t vw[2][4];  // words of keys 0-7 and 8-15, of 16 elements and the next ones
+          auto values_of = [&](int d) { ldmatrix_x4_trans(chunk_at(sv, h0 + h, d + mat_chunk), vw[(d >> 1) & 1]); };
+          values_of(0);
 #pragma unroll
           for (int d = 0; d < MT; d += 2) {
-            uint32_t vw[4];  // words of keys 0-7 and 8-15, of these 16 elements and the next ones
-            ldmatrix_x4_trans(chunk_at(sv, h0 + h, d + mat_chunk), vw);
-            if (!whole) { vw[0] &= mask0; vw[1] &= mask1; vw[2] &= mask0; vw[3] &= mask1; }
+            if (d + 2 < MT) values_of(d + 2);
+            uint32_t(&words)[4] = vw[(d >> 1) & 1];
+            if (!whole) { words[0] &= mask0; words[1] &= mask1; words[2] &= mask0; words[3] &= mask1; }
 #pragma unroll
             for (int d2 = 0; d2 < 2; ++d2) {
               uint32_t a0, a1, a2, a3;
-              q8_word_to_half<T, false>(vw[2 * d2], a0, a1);
-              q8_word_to_half<T, false>(vw[2 * d2 + 1], a2, a3);
+              q8_word_to_half<T, false>(words[2 * d2], a0, a1);
+              q8_word_to_half<T, false>(words[2 * d2 + 1], a2, a3);
 #pragma unroll
               for (int r = 0; r < NR; ++r) mma_f16(o[d + d2][r], a0, a1, a2, a3, pf[h][r][0], pf[h][r][1]);
             }

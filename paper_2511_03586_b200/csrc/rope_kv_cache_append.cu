@@ -258,8 +258,8 @@ __device__ __forceinline__ int64_t first_block_place(const RopeParams& p, int b,
   return (int64_t)(min(max(from, 0), p.tokens) >> p.scales.shift) + 2 * (int64_t)b;
 }
 
-// One block of one sequence, and some heads of K or of V of it.  A CTA.
-template <pd_dtype T>
+// One block of one sequence, and some heads of K (KEYS) or of V of it.  A CTA.
+template <pd_dtype T, bool KEYS>
 __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t place, int round, float2* turns, float* largest) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // the last sequence whose places begin at or in front of `place`
@@ -279,16 +279,15 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
 
   const int heads_a_cta = kWarps / p.warps_a_head, part = warp % p.warps_a_head;
   const int rounds_k = p.rounds / 2;
-  const bool keys = round < rounds_k;
-  const int head = (keys ? round : round - rounds_k) * heads_a_cta + warp / p.warps_a_head;
+  const int head = (KEYS ? round : round - rounds_k) * heads_a_cta + warp / p.warps_a_head;
   const bool mine = head < p.heads_kv;
   const int units = p.head_dim / kUnit;
   const int shift_u = 31 - __clz(units);
   const bool power = (units & (units - 1)) == 0;
   auto token_of = [&](int i) { return power ? i >> shift_u : i / units; };  // of a unit in the warp's share
-  const __nv_bfloat16* src = (keys ? p.k_new : p.v_new) + (int64_t)(s.q0 + first - s.pos0) * p.ld_new + (int64_t)head * p.head_dim;
-  uint8_t* dst = (keys ? p.k_cache : p.v_cache) + (int64_t)page * p.page_stride + (int64_t)slot0 * p.slot_stride + (int64_t)head * p.head_stride;
-  float* scale_at = (keys ? p.k_scale : p.v_scale) + p.scales.at(page, head, slot0);
+  const __nv_bfloat16* src = (KEYS ? p.k_new : p.v_new) + (int64_t)(s.q0 + first - s.pos0) * p.ld_new + (int64_t)head * p.head_dim;
+  uint8_t* dst = (KEYS ? p.k_cache : p.v_cache) + (int64_t)page * p.page_stride + (int64_t)slot0 * p.slot_stride + (int64_t)head * p.head_stride;
+  float* scale_at = (KEYS ? p.k_scale : p.v_scale) + p.scales.at(page, head, slot0);
   const float before = mine && old > 0 ? *scale_at : 0.f;
 
   const int per_warp = kGroup / units, per_group = per_warp * p.warps_a_head;  // tokens
@@ -296,7 +295,7 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
   const int pairs = p.rotary / 2;
   auto place_in = [&](int u) {
     Place at = place_of(p, u);
-    if (!keys) { at.rotated = at.split = false; at.first = u * kUnit; at.second = at.first + 4; }
+    if (!KEYS) { at.rotated = at.split = false; at.first = u * kUnit; at.second = at.first + 4; }
     return at;
   };
   // this warp's tokens of group g: from t0 of the block's new ones on, n units
@@ -315,7 +314,7 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
     }
   };
   auto turn_group = [&](int g) {  // cos and sin of the group's tokens; collective over the CTA
-    if (!keys || pairs == 0) return;
+    if (!KEYS || pairs == 0) return;
     __syncthreads();
     const int n = min(per_group, tokens - g * per_group) * pairs;
     for (int i = threadIdx.x; i < n; i += kThreads) {
@@ -326,6 +325,7 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
   };
   const float2* my_turns = turns + part * per_warp * pairs;
   float most = 0.f;
+  uint32_t most2 = 0;
   for (int g = 0; g < groups; ++g) {
     load_group(g);
     turn_group(g);
@@ -334,14 +334,21 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
     for (int j = 0; j < kHeld; ++j) {
       const int i = lane + 32 * j;
       if (i < n) {
-        const int t = token_of(i), u = i - t * units;
-        float x[8];
-        rotate_unit(held[j], place_in(u), my_turns + t * pairs + 4 * u, x);
+        if constexpr (KEYS) {
+          const int t = token_of(i), u = i - t * units;
+          float x[8];
+          rotate_unit(held[j], place_in(u), my_turns + t * pairs + 4 * u, x);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[k]));
+          for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[k]));
+        } else {  // (bf16 magnitudes are in the order of their bits)
+          const uint32_t w[4] = {held[j].x, held[j].y, held[j].z, held[j].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) most2 = __vmaxu2(most2, w[k] & 0x7fff7fffu);
+        }
       }
     }
   }
+  if constexpr (!KEYS) most = __uint_as_float(max(most2 << 16, most2 & 0xffff0000u));
   most = warp_max(most);
   if (p.warps_a_head > 1) {
     if (lane == 0) largest[warp] = most;
@@ -432,7 +439,9 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kv_cache_append_q8_kernel(co
   griddep_wait();
   griddep_launch_dependents();
   if ((int64_t)blockIdx.x < p.block_ctas) {
-    quantise_block<T>(p, blockIdx.x / p.rounds, blockIdx.x % p.rounds, turns, largest);
+    const int round = blockIdx.x % p.rounds;
+    if (round < p.rounds / 2) quantise_block<T, true>(p, blockIdx.x / p.rounds, round, turns, largest);
+    else quantise_block<T, false>(p, blockIdx.x / p.rounds, round, turns, largest);
     return;
   }
   const int warp = threadIdx.x >> 5;
