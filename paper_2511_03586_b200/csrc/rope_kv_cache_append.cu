@@ -177,11 +177,35 @@ __device__ __forceinline__ int page_at(const RopeParams& p, int b, int pos) {
   return (unsigned)page < (unsigned)p.num_pages ? page : -1;
 }
 
-// `part` of the heads of token t: queries to q_out and, for a bf16 cache (CACHE), keys and values to their slot.  A warp, which takes
-// 32 units at a time, AHEAD times ahead.
-//   Where the units of a head divide 32 (head_dim 32, 64, 128 or 256) a lane has the same unit of every head it comes to: its turns
-//   stay in registers, and from step to step only the head changes.  (With units found by division for every step, and turns read
-//   from shared memory, 8 x 2048 tokens took 76 us.)
+// Units of a token's heads, `steps` of them for this lane, src_step and dst_step elements apart: read, rotated by the turns of its
+// unit (ROTATE; else copied), and written.  AHEAD loads are under way together.
+template <bool ROTATE, int AHEAD>
+__device__ __forceinline__ void turn_units(const __nv_bfloat16* src, int src_step, __nv_bfloat16* dst, int64_t dst_step, int steps, const Place& at,
+                                           const float2 (&turn)[4]) {
+  for (; steps > 0; steps -= AHEAD, src += AHEAD * src_step, dst += AHEAD * dst_step) {
+    uint4 raw[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (j < steps) raw[j] = load_unit(src + j * src_step, at);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (j < steps) {
+        if (ROTATE && at.rotated) {
+          float x[8];
+          rotate_unit(raw[j], at, turn, x);
+          store_unit(dst + j * dst_step, at, x);
+        } else {
+          *reinterpret_cast<uint4*>(dst + j * dst_step + at.first) = raw[j];
+        }
+      }
+    }
+  }
+}
+
+// `part` of the heads of token t: queries to q_out and, for a bf16 cache (CACHE), keys and values to their slot.  A warp.
+//   Where the units of a head divide 32 (head_dim 32, 64, 128 or 256) a lane has the same unit of every head it comes to: its place and
+//   its turns stay in registers, and from step to step only the head changes.  (With units found by division for every step, and
+//   turns read from shared memory, 8 x 2048 tokens took 76 us single; now 65, where more loads ahead cost more than they bring, 88 with six.)
 template <bool CACHE, int AHEAD>
 __device__ __forceinline__ void rotate_token(const RopeParams& p, int t, int part, float2* turns) {
   const int lane = threadIdx.x & 31;
@@ -192,62 +216,48 @@ __device__ __forceinline__ void rotate_token(const RopeParams& p, int t, int par
   if (pos < 0) return;
   const int page = CACHE ? page_at(p, b, pos) : -1;
   const int units = p.head_dim / kUnit;
-  // steps of 32 units: those of the queries, then the keys', then the values'
-  const int steps_q = (p.heads_q * units + 31) / 32, steps_kv = page >= 0 ? (p.heads_kv * units + 31) / 32 : 0;
+  const bool fixed = 32 % units == 0;
+  // steps: of 32 / units heads, or of one head (taken by as many lanes as it has units, in turns of 32)
+  const int heads_a_step = fixed ? 32 / units : 1;
+  const int steps_q = (p.heads_q + heads_a_step - 1) / heads_a_step, steps_kv = page >= 0 ? (p.heads_kv + heads_a_step - 1) / heads_a_step : 0;
   const int all = steps_q + 2 * steps_kv, per = (all + p.parts - 1) / p.parts;
   const int begin = part * per, end = min(begin + per, all);
   if (begin >= end) return;
-  const bool fixed = 32 % units == 0;
   const int pairs = p.rotary / 2;
   for (int i = lane; i < pairs; i += 32) turns[i] = turn_of(p, pos, i);
   __syncwarp();
-  float2 mine[4];
-  const int my_unit = lane % units, my_head = lane / units, heads_a_step = 32 / units;
-  const Place my_place = place_of(p, my_unit), my_plain{my_unit * kUnit, my_unit * kUnit + 4, false, false};
-  if (fixed && my_place.rotated) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) mine[i] = turns[4 * my_unit + i];
-  }
   const int64_t slot = page < 0 ? 0 : (int64_t)page * p.page_stride + (int64_t)(pos % p.page_size) * p.slot_stride;
-  for (int s0 = begin; s0 < end; s0 += AHEAD) {
-    uint4 raw[AHEAD];
+  const int my_head = fixed ? lane / units : 0;
+  for (int u = fixed ? lane % units : lane; u < units; u += 32) {  // (once where the unit is fixed)
+    const Place at = place_of(p, u), plain{u * kUnit, u * kUnit + 4, false, false};
+    float2 turn[4];
 #pragma unroll
-    for (int k = 0; k < 2 * AHEAD; ++k) {  // AHEAD loads, then AHEAD stores
-      const int j = k % AHEAD, step = s0 + j;
-      if (step >= end) continue;
-      const int which = step < steps_q ? 0 : step < steps_q + steps_kv ? 1 : 2;  // (the same for the warp)
-      const int in = which == 0 ? step : which == 1 ? step - steps_q : step - steps_q - steps_kv;
-      const int heads = which == 0 ? p.heads_q : p.heads_kv;
-      int head, u;
-      Place at;
-      if (fixed) {
-        head = in * heads_a_step + my_head;
-        u = my_unit;
-        at = which == 2 ? my_plain : my_place;
-      } else {
-        head = (in * 32 + lane) / units;
-        u = in * 32 + lane - head * units;
-        at = place_of(p, u);
-        if (which == 2) at = Place{u * kUnit, u * kUnit + 4, false, false};
-      }
-      if (head >= heads) continue;
-      if (k < AHEAD) {
-        const __nv_bfloat16* src = which == 0 ? p.q + (int64_t)t * p.ld_q : (which == 1 ? p.k_new : p.v_new) + (int64_t)t * p.ld_new;
-        raw[j] = load_unit(src + head * p.head_dim, at);
-      } else {
-        __nv_bfloat16* dst = which == 0 ? p.q_out + (int64_t)t * p.ld_q_out + head * p.head_dim
-                                        : reinterpret_cast<__nv_bfloat16*>(which == 1 ? p.k_cache : p.v_cache) + slot + (int64_t)head * p.head_stride;
-        if (!at.rotated) {
-          *reinterpret_cast<uint4*>(dst + at.first) = raw[j];
-        } else {
-          float x[8];
-          float2 turn[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) turn[i] = fixed ? mine[i] : turns[4 * u + i];
-          rotate_unit(raw[j], at, turn, x);
-          store_unit(dst, at, x);
-        }
-      }
+    for (int i = 0; i < 4; ++i) turn[i] = at.rotated ? turns[4 * u + i] : make_float2(1.f, 0.f);
+    // the share of the steps [from, from + steps) of `heads` heads that is this part's: first step, and steps of this lane
+    auto share = [&](int from, int steps, int heads, int& first) {
+      first = max(begin - from, 0);
+      const int last = min(end - from, steps);
+      return min(last - first, (heads - my_head - first * heads_a_step + heads_a_step - 1) / heads_a_step);
+    };
+    int first;
+    const int src_step = heads_a_step * p.head_dim;
+    int n = share(0, steps_q, p.heads_q, first);
+    if (n > 0) {
+      const int head = first * heads_a_step + my_head;
+      turn_units<true, AHEAD>(p.q + (int64_t)t * p.ld_q + head * p.head_dim, src_step, p.q_out + (int64_t)t * p.ld_q_out + head * p.head_dim, src_step, n, at, turn);
+    }
+    if (CACHE && page >= 0) {
+      const int64_t dst_step = heads_a_step * p.head_stride;
+      n = share(steps_q, steps_kv, p.heads_kv, first);
+      int head = first * heads_a_step + my_head;
+      if (n > 0)
+        turn_units<true, AHEAD>(p.k_new + (int64_t)t * p.ld_new + head * p.head_dim, src_step, reinterpret_cast<__nv_bfloat16*>(p.k_cache) + slot + head * p.head_stride,
+                                dst_step, n, at, turn);
+      n = share(steps_q + steps_kv, steps_kv, p.heads_kv, first);
+      head = first * heads_a_step + my_head;
+      if (n > 0)
+        turn_units<false, AHEAD>(p.v_new + (int64_t)t * p.ld_new + head * p.head_dim, src_step, reinterpret_cast<__nv_bfloat16*>(p.v_cache) + slot + head * p.head_stride,
+                                 dst_step, n, plain, turn);
     }
   }
 }
@@ -258,8 +268,9 @@ __device__ __forceinline__ int64_t first_block_place(const RopeParams& p, int b,
   return (int64_t)(min(max(from, 0), p.tokens) >> p.scales.shift) + 2 * (int64_t)b;
 }
 
-// One block of one sequence, and some heads of K (KEYS) or of V of it.  A CTA.
-template <pd_dtype T, bool KEYS>
+// One block of one sequence, and some heads of K (KEYS) or of V of it.  A CTA.  FIXED: the units of a head divide 32, so that a lane has
+// the same unit of every token it comes to.
+template <pd_dtype T, bool KEYS, bool FIXED>
 __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t place, int round, float2* turns, float* largest) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // the last sequence whose places begin at or in front of `place`
@@ -282,9 +293,7 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
   const int head = (KEYS ? round : round - rounds_k) * heads_a_cta + warp / p.warps_a_head;
   const bool mine = head < p.heads_kv;
   const int units = p.head_dim / kUnit;
-  const int shift_u = 31 - __clz(units);
-  const bool power = (units & (units - 1)) == 0;
-  auto token_of = [&](int i) { return power ? i >> shift_u : i / units; };  // of a unit in the warp's share
+  auto token_of = [&](int i) { return i / units; };  // of a unit in the warp's share
   const __nv_bfloat16* src = (KEYS ? p.k_new : p.v_new) + (int64_t)(s.q0 + first - s.pos0) * p.ld_new + (int64_t)head * p.head_dim;
   uint8_t* dst = (KEYS ? p.k_cache : p.v_cache) + (int64_t)page * p.page_stride + (int64_t)slot0 * p.slot_stride + (int64_t)head * p.head_stride;
   float* scale_at = (KEYS ? p.k_scale : p.v_scale) + p.scales.at(page, head, slot0);
@@ -298,6 +307,20 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
     if (!KEYS) { at.rotated = at.split = false; at.first = u * kUnit; at.second = at.first + 4; }
     return at;
   };
+  // unit j of this lane: its token in the warp's share, its unit of the head and its place in it
+  const int my_token = lane / units, my_unit = lane % units, tokens_a_step = 32 / units;
+  const Place my_place = place_in(my_unit);
+  auto unit_j = [&](int j, int& t, int& u, Place& at) {
+    if constexpr (FIXED) {
+      t = my_token + j * tokens_a_step;
+      u = my_unit;
+      at = my_place;
+    } else {
+      t = token_of(lane + 32 * j);
+      u = lane + 32 * j - t * units;
+      at = place_in(u);
+    }
+  };
   // this warp's tokens of group g: from t0 of the block's new ones on, n units
   auto first_token = [&](int g) { return g * per_group + part * per_warp; };
   auto units_in = [&](int g) { return mine ? max(min(per_warp, tokens - first_token(g)), 0) * units : 0; };
@@ -308,8 +331,10 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
     for (int j = 0; j < kHeld; ++j) {
       const int i = lane + 32 * j;
       if (i < n) {
-        const int t = token_of(i);
-        held[j] = load_unit(src + (int64_t)(first_token(g) + t) * p.ld_new, place_in(i - t * units));
+        int t, u;
+        Place at;
+        unit_j(j, t, u, at);
+        held[j] = load_unit(src + (int64_t)(first_token(g) + t) * p.ld_new, at);
       }
     }
   };
@@ -335,9 +360,11 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
       const int i = lane + 32 * j;
       if (i < n) {
         if constexpr (KEYS) {
-          const int t = token_of(i), u = i - t * units;
+          int t, u;
+          Place at;
+          unit_j(j, t, u, at);
           float x[8];
-          rotate_unit(held[j], place_in(u), my_turns + t * pairs + 4 * u, x);
+          rotate_unit(held[j], at, my_turns + t * pairs + 4 * u, x);
 #pragma unroll
           for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[k]));
         } else {  // (bf16 magnitudes are in the order of their bits)
@@ -368,8 +395,9 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
     for (int j = 0; j < kHeld; ++j) {
       const int i = lane + 32 * j;
       if (i < n) {
-        const int t = token_of(i), u = i - t * units;
-        const Place at = place_in(u);
+        int t, u;
+        Place at;
+        unit_j(j, t, u, at);
         float x[8];
         rotate_unit(held[j], at, my_turns + t * pairs + 4 * u, x);
         uint32_t w[2];
@@ -440,8 +468,14 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kv_cache_append_q8_kernel(co
   griddep_launch_dependents();
   if ((int64_t)blockIdx.x < p.block_ctas) {
     const int round = blockIdx.x % p.rounds;
-    if (round < p.rounds / 2) quantise_block<T, true>(p, blockIdx.x / p.rounds, round, turns, largest);
-    else quantise_block<T, false>(p, blockIdx.x / p.rounds, round, turns, largest);
+    const int64_t place = blockIdx.x / p.rounds;
+    if (32 % (p.head_dim / kUnit) == 0) {
+      if (round < p.rounds / 2) quantise_block<T, true, true>(p, place, round, turns, largest);
+      else quantise_block<T, false, true>(p, place, round, turns, largest);
+    } else {
+      if (round < p.rounds / 2) quantise_block<T, true, false>(p, place, round, turns, largest);
+      else quantise_block<T, false, false>(p, place, round, turns, largest);
+    }
     return;
   }
   const int warp = threadIdx.x >> 5;
