@@ -500,7 +500,7 @@ typedef struct {
  *    (PD_E4M3): scale = m / Q, or the scale that is there if that is larger and the
  *    block holds tokens in front of the new ones already.  Where it grew, the older
  *    tokens' elements e become round(e * old / new); the new ones' are round(x / scale),
- *    both to nearest.  x / scale is formed in fp32: where it lies within 2^-20 of itself
+ *    both to nearest.  x / scale is formed in fp32 (as x Q / m where the scale is new): where it lies within 2^-20 of itself
  *    (for a rotated element, of its pair's magnitudes over the scale) of a border between
  *    two bytes, it may go to either.  So a block that is filled token by token has lost at
  *    most half a step of its last scale for every time that it grew, and one that is

@@ -384,7 +384,16 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
   }
   // (a scale below the normal range would have no reciprocal)
   const float need = most > 0.f ? fmaxf(most / paged::q8_top<T>(), 1.17549435e-38f) : 0.f;
-  const float scale = fmaxf(before, need), inv = scale > 0.f ? 1.f / scale : 0.f;
+  const float scale = fmaxf(before, need);
+  // x / scale, as x Q / m where the scale m / Q is new: keys and values are multiples of each other by small fractions often enough that
+  // quotients lie on the border between two bytes, and m / Q rounded to fp32 would take them all to the same side of it.  One
+  // refinement by the residual makes the product with the reciprocal as good as a division.
+  const bool fresh = need >= before && most > 0x1p-100f && most < 0x1p100f;
+  const float times = fresh ? paged::q8_top<T>() : 1.f, by = fresh ? most : scale, inv = by > 0.f ? 1.f / by : 0.f;
+  auto quotient = [&](float x) {
+    const float n = x * times, y = n * inv;
+    return fmaf(fmaf(-y, by, n), inv, y);
+  };
   for (int g = 0; g < groups; ++g) {
     if (groups > 1) {
       load_group(g);
@@ -403,8 +412,8 @@ __device__ __forceinline__ void quantise_block(const RopeParams& p, int64_t plac
         uint32_t w[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          w[k] = paged::q8_pair_from_float<T>(x[4 * k] * inv, x[4 * k + 1] * inv) |
-                 paged::q8_pair_from_float<T>(x[4 * k + 2] * inv, x[4 * k + 3] * inv) << 16;
+          w[k] = paged::q8_pair_from_float<T>(quotient(x[4 * k]), quotient(x[4 * k + 1])) |
+                 paged::q8_pair_from_float<T>(quotient(x[4 * k + 2]), quotient(x[4 * k + 3])) << 16;
         uint8_t* row = dst + (int64_t)(old + first_token(g) + t) * p.slot_stride;
         if (at.split) {
           *reinterpret_cast<uint32_t*>(row + at.first) = w[0];
