@@ -522,9 +522,15 @@ pd_status pd_rope_kv_cache_append(const pd_paged_attention_desc* desc, const pd_
 /* pd_attention_paged_fwd over an 8-bit cache:
  *   out[t, h] = sum_j softmax_j(scale * ks_j * (q[t, h] . k[j])) * vs_j * v[j]
  * with k[j], v[j] the stored elements and ks_j, vs_j the scales of their blocks.  Arguments,
- * limits, errors, workspace and what may lie in slots and entries out of view as there;
- * scales out of view may be anything, too.  The dequantised keys and values that a query
- * sees have to be finite. */
+ * limits (but batch * heads_kv * max_pages * page_size / 32 is what is at most 2^30), errors,
+ * workspace and what may lie in slots and entries out of view as there; scales out of view may
+ * be anything, too.  The keys and values that a query sees have to be finite, with their scales.
+ * Arithmetic: stored elements are exact, queries are taken to fp16 after a multiplication by
+ * a power of two, scores, softmax statistics and sums are fp32; the exponentials (with the
+ * scales of the values) are rounded to fp16 for the second product, and so are, where chunks of
+ * many rows meet several scales within 32 tokens, the elements times their scales.  A value's
+ * share of a result is exact to fp16's 2^-11 as long as its weight times its scale is above
+ * 2^-21 of the largest scale of a value in view, and off by 2^-30 of the largest value below. */
 size_t pd_attention_paged_q8_workspace_bytes(const pd_paged_attention_desc* desc);
 pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* desc, const pd_cache_scales* scales, const void* q,
                                     const void* k_cache, const void* v_cache, const int32_t* block_table,

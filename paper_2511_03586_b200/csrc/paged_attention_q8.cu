@@ -6,6 +6,11 @@ namespace pd {
 namespace paged {
 namespace {
 
+// (the row kernel's tiles can be of 32 keys, and all of a batch's are counted in 32 bits)
+bool supported_q8(const pd_paged_attention_desc& d) {
+  return supported(d) && (int64_t)d.batch * d.heads_kv * (((int64_t)d.max_pages * d.page_size + 31) / 32) <= kMaxPositions;
+}
+
 // Row kernel: up to four warps beside each other take cache heads (the rows of a slot that lie beside each other in the usual
 // layout), as many as divide the heads; the rest of the four share keys, or rows.
 Plan plan_q8(const pd_paged_attention_desc& d) {
@@ -29,7 +34,7 @@ Plan plan_q8(const pd_paged_attention_desc& d) {
 }  // namespace pd
 
 extern "C" size_t pd_attention_paged_q8_workspace_bytes(const pd_paged_attention_desc* desc) {
-  if (!desc || !pd::paged::valid(*desc) || !pd::paged::supported(*desc)) return 0;
+  if (!desc || !pd::paged::valid(*desc) || !pd::paged::supported_q8(*desc)) return 0;
   if (desc->batch == 0 || desc->tokens == 0 || desc->max_q_len == 0) return 0;
   return pd::paged::workspace_bytes(*desc, pd::paged::plan_q8(*desc));
 }
@@ -42,7 +47,7 @@ extern "C" pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* de
   if (!desc || !scales) return PD_ERR_NULL_POINTER;
   const pd_paged_attention_desc& d = *desc;
   if (!paged::valid(d) || !paged::q8_dtype(scales->dtype) || !paged::q8_block_valid(scales->block, d.page_size)) return PD_ERR_BAD_SHAPE;
-  if (!paged::supported(d)) return PD_ERR_UNSUPPORTED;
+  if (!paged::supported_q8(d)) return PD_ERR_UNSUPPORTED;
   const int64_t row = (int64_t)d.heads_q * d.head_dim;
   if (d.ld_q < row || d.ld_out < row || d.page_stride <= 0 || d.slot_stride <= 0 || d.head_stride <= 0) return PD_ERR_BAD_SHAPE;
   if (d.batch == 0 || d.tokens == 0 || d.max_q_len == 0) return PD_OK;

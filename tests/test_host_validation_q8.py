@@ -143,3 +143,17 @@ def test_binding_wants_cuda_tensors():
         api.pd_attention_paged_q8_fwd(t, c, c, t, t, t, t, t, max_q_len=1, max_kv_len=1)
     with pytest.raises(TypeError):
         api.pd_penalize_logits(t[0])
+
+
+@pytest.mark.parametrize("batch,max_pages,tiles,ok", [
+    (64, 1 << 16, 1 << 26, True),
+    (64, (1 << 16) + 1, (1 << 26) + 1024, True),      # 64 * 8 heads * 2 tiles of 32 keys a page more
+    (1024, 1 << 16, 1 << 30, True),
+    (1024, (1 << 16) + 1, (1 << 30) + 16384, False),
+])
+def test_extents_beyond_the_kernels_index_types(batch, max_pages, tiles, ok):
+    kw = dict(batch=batch, heads_kv=8, max_pages=max_pages, page_size=64)
+    assert batch * 8 * max_pages * 64 // 32 == tiles and (tiles <= 1 << 30) == ok
+    assert (lib.pd_attention_paged_q8_workspace_bytes(ctypes.byref(paged(**kw))) > 0) == ok
+    if not ok:
+        assert attend(**kw) == UNSUP
