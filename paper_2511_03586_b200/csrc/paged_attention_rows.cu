@@ -278,7 +278,7 @@ pd_status launch(const pd_paged_attention_desc& d, const Params& p, const CUtens
   if (pd_status st = allow_dynamic_smem(paged_attention_rows_kernel<D, WR, WK>, C::kSmem, smem_allowed); st != PD_OK) return st;
   launch_pdl(paged_attention_rows_kernel<D, WR, WK>, dim3(p.splits), dim3(C::kThreads), C::kSmem, s, tk, tv, p);
   if (pd_status st = check_launch(); st != PD_OK || p.whole_items) return st;
-  launch_pdl(paged_attention_join_rows<D>, dim3(d.heads_kv, d.batch, (min(p.max_q_len * p.group, C::kRows) + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p, C::kRows, 1);
+  launch_pdl(paged_attention_join_rows<D>, dim3(d.heads_kv, d.batch, (min(p.max_q_len * p.group, C::kRows) + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p, C::kRows, 1, false);
   return check_launch();
 }
 

@@ -192,8 +192,12 @@ __device__ __forceinline__ void write_piece(const Params& p, const Piece& w, int
 // Latency-bound: the loads of a warp's pieces are in flight together (one at a time, 37 pieces of a long context took 12 us).
 constexpr int kJoinWarps = 8;
 // `group`: cache heads to an item; their partial results lie behind one another.
+// `spread`: the grid has a CTA for every row, which all of its warps work on where there are kSpread pieces and more.
+//   (One sequence of 16384 keys, 4 cache heads, 8 rows, 256 pieces: 20 us for the call, with a warp to a row 41.  Joins of fewer pieces have
+//   loads enough in flight either way: 16 sequences of 2048 keys, 16 rows, 18 pieces: 37 spread, 29 not.)
+constexpr int kSpread = 32;
 template <int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) paged_attention_join_rows(const Params p, int rows_per_tile, int group) {
+__global__ void __launch_bounds__(32 * kJoinWarps) paged_attention_join_rows(const Params p, int rows_per_tile, int group, bool spread) {
   __shared__ float part[kJoinWarps][D + 2];
   griddep_wait();
   griddep_launch_dependents();
@@ -201,16 +205,18 @@ __global__ void __launch_bounds__(32 * kJoinWarps) paged_attention_join_rows(con
   const int2 pieces = p.pieces[(int64_t)b * p.heads_kv + kvh];
   const Sequence seq = load_sequence(p, b);
   const int rows = seq.n * p.group;
-  if (rows <= (int)blockIdx.z * kJoinWarps || pieces.x < 0) return;  // (no CTA had this item and wrote its entry; or one CTA had all of it)
+  if (rows <= (int)blockIdx.z || pieces.x < 0) return;  // (no CTA had this item and wrote its entry; or one CTA had all of it)
   const int first_cta = pieces.x >> 1, n = pieces.y - first_cta + 1;
+  const int rows_a_cta = spread && n >= kSpread ? 1 : kJoinWarps, r0 = blockIdx.z * rows_a_cta;
+  if (rows <= r0) return;
   // (a CTA whose wait for a key tile ran out has left the entry as it was in the workspace)
   if (first_cta >= p.splits || pieces.y >= p.splits || pieces.y < first_cta) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int per_row = 1;
-  while (2 * per_row * rows <= kJoinWarps) per_row *= 2;
+  while (2 * per_row * min(rows, rows_a_cta) <= kJoinWarps) per_row *= 2;
   constexpr int kCols = D / 32;
   {
-    const int r = blockIdx.z * kJoinWarps + warp / per_row, z0 = warp % per_row;
+    const int r = r0 + warp / per_row, z0 = warp % per_row;
     auto at = [&](int z) { return ((int64_t)(z == 0 ? pieces.x : 2 * (first_cta + z)) * group + kvh % group) * rows_per_tile + r; };
     float top = -INFINITY, sum = 0.f, acc[kCols];
 #pragma unroll

@@ -548,7 +548,9 @@ pd_status launch(const pd_paged_attention_desc& d, const Params& p, const Scales
   launch_pdl(paged_attention_q8_rows_kernel<T, D, NR, H, WK, WR>, dim3(p.splits), dim3(kThreads), C::kSmem, s, tk, tv, p, scales);
   if (pd_status st = check_launch(); st != PD_OK || p.whole_items) return st;
   const int rows = (int)std::min<int64_t>((int64_t)p.max_q_len * p.group, C::kRows);
-  launch_pdl(paged_attention_join_rows<D>, dim3(d.heads_kv, d.batch, (rows + kJoinWarps - 1) / kJoinWarps), dim3(32 * kJoinWarps), 0, s, p, C::kRows, H);
+  const bool spread = (int64_t)d.heads_kv * d.batch * rows <= 4 * kSms;  // (more CTAs keep the loads coming)
+  const dim3 grid(d.heads_kv, d.batch, spread ? rows : (rows + kJoinWarps - 1) / kJoinWarps);
+  launch_pdl(paged_attention_join_rows<D>, grid, dim3(32 * kJoinWarps), 0, s, p, C::kRows, H, spread);
   return check_launch();
 }
 template <pd_dtype T, int D>

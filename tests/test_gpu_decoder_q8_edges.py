@@ -148,3 +148,12 @@ def test_penalties_in_place_in_a_wider_tensor(vocab, offset, dtype):
         bound = 5 * 2 ** -24 * (want.abs() + 300 * 0.25 + 0.5) + (2 ** -8 * want.abs() if dtype == torch.bfloat16 else 0)
         assert bool(((z[i].cpu().double() - want).abs() <= bound).all())
     assert torch.equal(wide[:, :offset], before[:, :offset]) and torch.equal(wide[:, offset + vocab:], before[:, offset + vocab:])
+
+
+@both
+@pytest.mark.parametrize("heads,group,tokens,d", [(4, 4, 1, 128), (4, 8, 1, 64), (1, 8, 1, 128), (2, 5, 1, 128), (1, 16, 4, 64), (8, 4, 5, 128), (3, 8, 3, 128)])
+def test_one_long_context(heads, group, tokens, d, dtype):
+    """An item's keys over most of the CTAs, so that its join has hundreds of pieces; alone, and beside short ones."""
+    for lens in ([(tokens, 20000)], [(1, 40), (tokens, 16400), (tokens, tokens)]):
+        p = PagedQ8(lens, heads * group, heads, d, 16, seed=heads + d, dtype=dtype)
+        p.check(p.attend())
