@@ -405,7 +405,8 @@ pd_status pd_encoder_layer_fwd_profiled(const pd_encoder_layer_desc* desc,
  *    of the window, may hold anything, NaN included.  An entry outside
  *    [0, num_pages) is never followed: keys and values there count as zeros.
  *  - What is visible to any query of a sequence has to be finite, and so have the
- *    scores q . k in fp32; scaled, they stay below 2^127 in size.
+ *    scores q . k in fp32; scaled, they stay below 2^28 in size (2^22 over an 8-bit
+ *    cache), where fp32 still tells them apart by what the exponentials can hold.
  *  - The sequences' pages may be shared for reading (a common prefix). */
 typedef struct {
   int32_t batch, tokens;               /* sequences; rows of the token tensors */
