@@ -527,7 +527,8 @@ pd_status pd_rope_kv_cache_append(const pd_paged_attention_desc* desc, const pd_
  * workspace and what may lie in slots and entries out of view as there; scales out of view may
  * be anything, too.  The keys and values that a query sees have to be finite, with their scales.
  * Arithmetic: stored elements are exact, queries are taken to fp16 after a multiplication by
- * a power of two, scores, softmax statistics and sums are fp32; the exponentials (with the
+ * a power of two (off by at most 2^-27 of the query's largest element, whatever the others
+ * hold), scores, softmax statistics and sums are fp32; the exponentials (with the
  * scales of the values) are rounded to fp16 for the second product, and so are, where chunks of
  * many rows meet several scales within 32 tokens, the elements times their scales.  A value's
  * share of a result is exact to fp16's 2^-11 as long as its weight times its scale is above

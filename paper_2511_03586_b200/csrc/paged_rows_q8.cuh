@@ -10,8 +10,9 @@
 // columns.  A tile of up to 8 rows, the usual single token, then costs half of what it does with the rows along the 16.  A byte
 // is converted once per warp, however many rows the warp has; words are taken as ldmatrix delivers them, bytes 0 and 2 as one
 // operand register and 1 and 3 as the other, which permutes the elements of a head alike in K and Q, and in O.
-//   Q: multiplied by a power of two that takes the tile's largest magnitude to [2^14, 2^15), which is exact in fp16 down to 2^-28
-//      of it (and off by 2^-40 of it below); the power is taken back in the scale of the scores.
+//   Q: multiplied by a power of two that takes the largest magnitude of a warp's rows to [2^14, 2^15), which is exact in fp16 down to 2^-28
+//      of it (and off by 2^-40 of it below); the power is taken back in the scale of the scores.  Rows that are more than 2^12 apart
+//      have a power each, so that a row's queries are off by 2^-28 of its own largest at most, whatever the others hold.
 //   S: fp32, times ks_j.
 //   P: exponentials, fp32, times vs_j and a power of two that keeps them below 2^15, rounded to fp16 (2^-11 of each; what is
 //      2^-26 and less of the largest is off by up to 2^-36 of that).  The power follows the largest vs_j that the warp has met.
@@ -27,6 +28,8 @@
 //   97 to 99.  16 x 5 tokens over up to 8192 keys, e4m3: 73 us; there the warps' chains of conversions, products and softmax are what
 //   takes the time, loads alone take 38.
 #pragma once
+
+#include <type_traits>
 
 #include "cache_q8.cuh"
 #include "paged_rows.cuh"
@@ -55,10 +58,12 @@ struct Q8Config {
   static constexpr bool kLean = NR > 2;
   static constexpr int kQ = kLean ? kConsumers * NR * (D / 16) * 256 : 0;
   static constexpr int kExchange = WK > 1 ? H * WR * (WK / 2) * 512 * (D / 16 + 1) : 0;  // half the warps' results for 8 rows
-  static constexpr int kPerCta = 113 * 1024 - 256 /*barriers*/ - 1024 /*alignment*/;     // two CTAs per SM
+  static constexpr int kRowBytes = kGroupRows * 4;      // a float for each of a warp's rows
+  static constexpr int kControl = 256 /*barriers*/ + kConsumers * kRowBytes;
+  static constexpr int kPerCta = 113 * 1024 - kControl - 1024 /*alignment*/;             // two CTAs per SM
   static constexpr int kFit = (kPerCta - kExchange - kQ) / (kStageBytes + kScaleBytes);
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
-  static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kExchange + kQ + 256 + 1024;
+  static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kExchange + kQ + kControl + 1024;
   static_assert(2 * (kSmem + 1024) <= 228 * 1024 && kStages >= 4);
 };
 
@@ -97,6 +102,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
   auto empty = [&](int s) { return bars + 64u + 8u * s; };
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + (bars - smem_u32(smem_raw)) + 128);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto row_power = [&](int r) { return bars + 256u + (uint32_t)(warp * C::kRowBytes + 4 * r); };  // of a consumer warp's row: what its scores still need
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) { mbar_init(full(s), 1 + 32); mbar_init(empty(s), kConsumers); }
@@ -210,31 +216,55 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
     // ---- queries: row 8 r + g of the warp's, elements 16 k + 4 i ... + 3 of it
     uint32_t qf[C::kLean ? 1 : NR][KS][2];
     float score_scale;
+    bool apart;
     {
-      uint32_t most = 0;
       auto source = [&](int r) {
         const int row = min(wr * C::kGroupRows + 8 * r + g, w.rows - 1);  // (rows beyond the last repeat it and are not stored)
         const int t = row / p.group;
         return p.q + (int64_t)(w.seq.q0 + t) * p.ld_q + (int64_t)(kvh * p.group + row % p.group) * D + 4 * i4;
       };
       auto load = [&](const __nv_bfloat16* src, int k) { return __ldg(reinterpret_cast<const uint2*>(src + 16 * k)); };
+      // The largest exponent e of the rows goes to 14: times 2^(14 - e), within what fp32 has as a power of two and its reciprocal.  Rows
+      // more than 2^kNear apart (one that is infinite or not a number, too) each get a power of their own: the middle one of the
+      // reciprocals goes with the scale of the scores, the rest is taken back in each row's scores.
+      constexpr int kNear = 12, kNone = 127;  // (rows of zeros take whatever the others have)
+      uint32_t most[NR];
 #pragma unroll
-      for (int r = 0; r < NR; ++r) {
+      for (int r = 0; r < NR; ++r) {  // (all loads before the first exchange)
         const __nv_bfloat16* src = source(r);
+        most[r] = 0;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           const uint2 v = load(src, k);
-          most = max(most, max(max(v.x & 0x7fff0000u, v.x << 16 & 0x7fff0000u), max(v.y & 0x7fff0000u, v.y << 16 & 0x7fff0000u)));
+          most[r] = max(most[r], max(max(v.x & 0x7fff0000u, v.x << 16 & 0x7fff0000u), max(v.y & 0x7fff0000u, v.y << 16 & 0x7fff0000u)));
         }
       }
-      most = __reduce_max_sync(0xffffffffu, most);
-      // the largest exponent e goes to 14: times 2^(14 - e), within what fp32 has as a power of two and its reciprocal
-      const int shift = min(max(14 + 127 - (int)(most >> 23), -126), 126);
-      const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
-      score_scale = p.scale_log2e * __uint_as_float((uint32_t)(127 - shift) << 23);
+      int shift[NR], least = kNone, largest = -126;
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        most[r] = max(most[r], __shfl_xor_sync(0xffffffffu, most[r], 1));
+        most[r] = max(most[r], __shfl_xor_sync(0xffffffffu, most[r], 2));
+        shift[r] = most[r] == 0 ? kNone : min(max(14 + 127 - (int)(most[r] >> 23), -126), 126);
+        least = min(least, shift[r]);
+        if (most[r] != 0) largest = max(largest, shift[r]);
+      }
+      least = __reduce_min_sync(0xffffffffu, least);
+      largest = __reduce_max_sync(0xffffffffu, largest);
+      apart = largest - least > kNear;
+      const int middle = least == kNone ? 0 : apart ? (least + largest) >> 1 : least;
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+        if (!apart || shift[r] == kNone) shift[r] = middle;
+      score_scale = p.scale_log2e * __uint_as_float((uint32_t)(127 - middle) << 23);
+      __syncwarp();
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+        if (i4 == 0) st_shared_f32(row_power(8 * r + g), __uint_as_float((uint32_t)(127 + middle - shift[r]) << 23));
+      __syncwarp();
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
         const __nv_bfloat16* src = source(r);
+        const float up = __uint_as_float((uint32_t)(127 + shift[r]) << 23);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           const uint2 v = load(src, k);
@@ -268,190 +298,209 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
 
     bool failed = false;
     const int end = min(w.end, kt.n);
-    for (int i = w.begin; i < end; ++i) {
-      // (a warp that gives up goes on to the barrier below, if there is one, which tells the others)
-      if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
-      const uint32_t sk = ring + stage * C::kStageBytes, sc = scale_ring + stage * C::kScaleBytes + 4u * (uint32_t)(hs * blocks);
-      const int key0 = kt.tile_index(i) * kTile + wk * kKeys;
-      uint32_t sv = 0;
-      if constexpr (HB == 1) {  // both at once, and both are given back at the end
-        const bool wraps = stage + 1 == C::kStages;
-        sv = ring + (wraps ? 0 : stage + 1) * C::kStageBytes;
-        if (!mbar_wait_warp(full(wraps ? 0 : stage + 1), wraps ? phase ^ 1u : phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
-      }
-      // keys outside a row's view; whole tiles in everybody's view skip this
-      const int last_key = key0 + kKeys - 1;
-      const bool whole = last_key <= first_pos && last_key < w.seq.length && (p.window == 0 || key0 > last_pos - p.window || last_key < p.sinks);
-      auto in_view = [&](int key) { return (key < kt.hi && key >= kt.lo) || key < kt.sink_hi; };  // of some row
-#pragma unroll 1
-      for (int h0 = 0; h0 < 2; h0 += HB) {
-        // ---- S^T = K Q^T, one or two tiles of 16 keys
-        float s[HB][NR][4];
-#pragma unroll
-        for (int h = 0; h < HB; ++h) {
-#pragma unroll
-          for (int r = 0; r < NR; ++r) s[h][r][0] = s[h][r][1] = s[h][r][2] = s[h][r][3] = 0.f;
-          // words of keys 0-7 and 8-15, of two steps' 16 elements each; lean: these and the queries are asked for a step ahead
-          uint32_t kw[2][4], qb[2][NR][2];
-          auto keys_of = [&](int k) { ldmatrix_x4(chunk_at(sk, h0 + h, k + mat_chunk), kw[(k >> 1) & 1]); };
-          auto queries_of = [&](int k) {
-#pragma unroll
-            for (int r = 0; r < NR; ++r)
-              asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(qb[k & 1][r][0]), "=r"(qb[k & 1][r][1]) : "r"(sq + (uint32_t)((r * KS + k) * 256)));
-          };
-          if constexpr (C::kLean) {
-            keys_of(0);
-            queries_of(0);
-          }
-#pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            if constexpr (C::kLean) {
-              if (k % 2 == 0 && k + 2 < KS) keys_of(k + 2);
-              if (k + 1 < KS) queries_of(k + 1);
-            } else if (k % 2 == 0) {
-              keys_of(k);
-            }
-            const uint32_t* words = kw[(k >> 1) & 1] + 2 * (k & 1);
-            uint32_t a0, a1, a2, a3;
-            q8_word_to_half<T, kAdjacent>(words[0], a0, a2);
-            q8_word_to_half<T, kAdjacent>(words[1], a1, a3);
-#pragma unroll
-            for (int r = 0; r < NR; ++r) {
-              if constexpr (C::kLean) mma_f16(s[h][r], a0, a1, a2, a3, qb[k & 1][r][0], qb[k & 1][r][1]);
-              else mma_f16(s[h][r], a0, a1, a2, a3, qf[r][k][0], qf[r][k][1]);
-            }
-          }
+    // Compiled twice, so that rows that are not apart, as they hardly ever are, have no instruction for it: in one, 64 x 4096 keys took
+    // 141 us against 135 with 16 rows of 128, 240 against 232 with 32.
+    auto walk = [&](auto own_powers) {
+      for (int i = w.begin; i < end; ++i) {
+        // (a warp that gives up goes on to the barrier below, if there is one, which tells the others)
+        if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
+        const uint32_t sk = ring + stage * C::kStageBytes, sc = scale_ring + stage * C::kScaleBytes + 4u * (uint32_t)(hs * blocks);
+        const int key0 = kt.tile_index(i) * kTile + wk * kKeys;
+        uint32_t sv = 0;
+        if constexpr (HB == 1) {  // both at once, and both are given back at the end
+          const bool wraps = stage + 1 == C::kStages;
+          sv = ring + (wraps ? 0 : stage + 1) * C::kStageBytes;
+          if (!mbar_wait_warp(full(wraps ? 0 : stage + 1), wraps ? phase ^ 1u : phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
         }
-        // ---- scales of this lane's keys 16 h + 8 e + g
-        float ks[HB][2], vs[HB][2];
+        // keys outside a row's view; whole tiles in everybody's view skip this
+        const int last_key = key0 + kKeys - 1;
+        const bool whole = last_key <= first_pos && last_key < w.seq.length && (p.window == 0 || key0 > last_pos - p.window || last_key < p.sinks);
+        auto in_view = [&](int key) { return (key < kt.hi && key >= kt.lo) || key < kt.sink_hi; };  // of some row
+#pragma unroll 1
+        for (int h0 = 0; h0 < 2; h0 += HB) {
+          // ---- S^T = K Q^T, one or two tiles of 16 keys
+          float s[HB][NR][4];
 #pragma unroll
-        for (int h = 0; h < HB; ++h)
+          for (int h = 0; h < HB; ++h) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t at = sc + 4u * (uint32_t)((wk * kKeys + 16 * (h0 + h) + 8 * e + g) >> scale_shift);
-            ks[h][e] = ld_shared_f32(at) * score_scale;
-            vs[h][e] = ld_shared_f32(at + 4u * H * kTile);
+            for (int r = 0; r < NR; ++r) s[h][r][0] = s[h][r][1] = s[h][r][2] = s[h][r][3] = 0.f;
+            // words of keys 0-7 and 8-15, of two steps' 16 elements each; lean: these and the queries are asked for a step ahead
+            uint32_t kw[2][4], qb[2][NR][2];
+            auto keys_of = [&](int k) { ldmatrix_x4(chunk_at(sk, h0 + h, k + mat_chunk), kw[(k >> 1) & 1]); };
+            auto queries_of = [&](int k) {
+#pragma unroll
+              for (int r = 0; r < NR; ++r)
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(qb[k & 1][r][0]), "=r"(qb[k & 1][r][1]) : "r"(sq + (uint32_t)((r * KS + k) * 256)));
+            };
+            if constexpr (C::kLean) {
+              keys_of(0);
+              queries_of(0);
+            }
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              if constexpr (C::kLean) {
+                if (k % 2 == 0 && k + 2 < KS) keys_of(k + 2);
+                if (k + 1 < KS) queries_of(k + 1);
+              } else if (k % 2 == 0) {
+                keys_of(k);
+              }
+              const uint32_t* words = kw[(k >> 1) & 1] + 2 * (k & 1);
+              uint32_t a0, a1, a2, a3;
+              q8_word_to_half<T, kAdjacent>(words[0], a0, a2);
+              q8_word_to_half<T, kAdjacent>(words[1], a1, a3);
+#pragma unroll
+              for (int r = 0; r < NR; ++r) {
+                if constexpr (C::kLean) mma_f16(s[h][r], a0, a1, a2, a3, qb[k & 1][r][0], qb[k & 1][r][1]);
+                else mma_f16(s[h][r], a0, a1, a2, a3, qf[r][k][0], qf[r][k][1]);
+              }
+            }
           }
-        if constexpr (HB == 2) advance();
-#pragma unroll
-        for (int h = 0; h < HB; ++h)
-#pragma unroll
-          for (int r = 0; r < NR; ++r)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[h][r][e] *= ks[h][e >> 1];
-        if (!whole) {
+          // ---- scales of this lane's keys 16 h + 8 e + g
+          float ks[HB][2], vs[HB][2];
 #pragma unroll
           for (int h = 0; h < HB; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int key = key0 + 16 * (h0 + h) + 8 * (e >> 1) + g;
-#pragma unroll
-              for (int r = 0; r < NR; ++r) {
-                const int at = pos[r][e & 1];
-                const bool seen = key <= at && key < w.seq.length && (p.window == 0 || key > at - p.window || key < p.sinks);
-                if (!seen) s[h][r][e] = -INFINITY;
-              }
-              if (!in_view(key)) vs[h][e >> 1] = 0.f;
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t at = sc + 4u * (uint32_t)((wk * kKeys + 16 * (h0 + h) + 8 * e + g) >> scale_shift);
+              ks[h][e] = ld_shared_f32(at) * score_scale;
+              vs[h][e] = ld_shared_f32(at + 4u * H * kTile);
             }
-        }
-        // ---- references
-        float v_most = fmaxf(vs[0][0], vs[0][1]);
-        if constexpr (HB == 2) v_most = fmaxf(v_most, fmaxf(vs[1][0], vs[1][1]));
-        float mx[NR][2];
-        bool raise = v_most > v_top;
+          if constexpr (HB == 2) advance();
 #pragma unroll
-        for (int r = 0; r < NR; ++r)
+          for (int h = 0; h < HB; ++h)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            mx[r][e] = fmaxf(s[0][r][e], s[0][r][e + 2]);
-            if constexpr (HB == 2) mx[r][e] = fmaxf(mx[r][e], fmaxf(s[1][r][e], s[1][r][e + 2]));
-            raise |= mx[r][e] > m[r][e] + kRaise;  // also the first finite score of a row (m = -inf)
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[h][r][e] *= ks[h][e >> 1];
+          if (!whole) {
+#pragma unroll
+            for (int h = 0; h < HB; ++h)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int key = key0 + 16 * (h0 + h) + 8 * (e >> 1) + g;
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                  const int at = pos[r][e & 1];
+                  const bool seen = key <= at && key < w.seq.length && (p.window == 0 || key > at - p.window || key < p.sinks);
+                  if (!seen) s[h][r][e] = -INFINITY;
+                }
+                if (!in_view(key)) vs[h][e >> 1] = 0.f;
+              }
           }
-        if (__any_sync(0xffffffffu, raise)) {
-          const float most = warp_max(v_most);
-          float down = 1.f;
-          if (most > v_top) {
-            // the next power of two, within what fp32 has as a power of two times kTopP
-            const float top = __uint_as_float(min(max((__float_as_uint(most) >> 23) + 1u, 27u), 254u) << 23);
-            down = v_top / top;
-            v_top = top;
-          }
+          if constexpr (own_powers.value) {
 #pragma unroll
-          for (int r = 0; r < NR; ++r) {
-            float alpha[2];
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float power = ld_shared_f32(row_power(8 * r + 2 * i4 + e));
+#pragma unroll
+                for (int h = 0; h < HB; ++h) {
+                  s[h][r][e] *= power;
+                  s[h][r][e + 2] *= power;
+                }
+              }
+          }
+          // ---- references
+          float v_most = fmaxf(vs[0][0], vs[0][1]);
+          if constexpr (HB == 2) v_most = fmaxf(v_most, fmaxf(vs[1][0], vs[1][1]));
+          float mx[NR][2];
+          bool raise = v_most > v_top;
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float top = mx[r][e];
-#pragma unroll
-              for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-              const bool up = top > m[r][e] + kRaise;
-              alpha[e] = up ? ex2(m[r][e] - top) : 1.f;
-              if (up) m[r][e] = top;
-              l[r][e] *= alpha[e];
-              alpha[e] *= down;
+              mx[r][e] = fmaxf(s[0][r][e], s[0][r][e + 2]);
+              if constexpr (HB == 2) mx[r][e] = fmaxf(mx[r][e], fmaxf(s[1][r][e], s[1][r][e + 2]));
+              raise |= mx[r][e] > m[r][e] + kRaise;  // also the first finite score of a row (m = -inf)
+            }
+          if (__any_sync(0xffffffffu, raise)) {
+            const float most = warp_max(v_most);
+            float down = 1.f;
+            if (most > v_top) {
+              // the next power of two, within what fp32 has as a power of two times kTopP
+              const float top = __uint_as_float(min(max((__float_as_uint(most) >> 23) + 1u, 27u), 254u) << 23);
+              down = v_top / top;
+              v_top = top;
             }
 #pragma unroll
-            for (int d = 0; d < MT; ++d) {
-              o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
+            for (int r = 0; r < NR; ++r) {
+              float alpha[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                float top = mx[r][e];
+#pragma unroll
+                for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                const bool up = top > m[r][e] + kRaise;
+                alpha[e] = up ? ex2(m[r][e] - top) : 1.f;
+                if (up) m[r][e] = top;
+                l[r][e] *= alpha[e];
+                alpha[e] *= down;
+              }
+#pragma unroll
+              for (int d = 0; d < MT; ++d) {
+                o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
+              }
+            }
+          }
+          // ---- P^T: exponentials, and times vs_j in fp16
+          const float v_unit = kTopP / v_top;
+          uint32_t pf[HB][NR][2];
+#pragma unroll
+          for (int h = 0; h < HB; ++h) {
+            const float v0 = v_top > 0.f ? vs[h][0] * v_unit : 0.f, v1 = v_top > 0.f ? vs[h][1] * v_unit : 0.f;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+              // a row that has seen nothing yet is referred to 0: its exponentials are 2^-inf = 0
+              const float r0 = m[r][0] == -INFINITY ? 0.f : m[r][0], r1 = m[r][1] == -INFINITY ? 0.f : m[r][1];
+              const float e0 = ex2(s[h][r][0] - r0), e1 = ex2(s[h][r][1] - r1), e2 = ex2(s[h][r][2] - r0), e3 = ex2(s[h][r][3] - r1);
+              l[r][0] += e0 + e2;
+              l[r][1] += e1 + e3;
+              pf[h][r][0] = transpose_8x8(pack_half(e0 * v0, e1 * v0));
+              pf[h][r][1] = transpose_8x8(pack_half(e2 * v1, e3 * v1));
+            }
+          }
+          // ---- O^T += V^T P^T
+          if constexpr (HB == 2) {
+            if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
+            sv = ring + stage * C::kStageBytes;
+          }
+#pragma unroll
+          for (int h = 0; h < HB; ++h) {
+            // Values of keys in nobody's view may be any bits, NaN among them: zeroed, since 0 * NaN is NaN.  A word holds two
+            // elements of key 2 i (of eight) and two of key 2 i + 1.
+            uint32_t mask0 = 0xffffffffu, mask1 = 0xffffffffu;
+            if (!whole) {
+              auto half = [&](int key) { return in_view(key) ? 0xffffu : 0u; };
+              const int key = key0 + 16 * (h0 + h) + 2 * i4;
+              mask0 = half(key) | half(key + 1) << 16;
+              mask1 = half(key + 8) | half(key + 9) << 16;
+            }
+            uint32_t vw[2][4];  // words of keys 0-7 and 8-15, of 16 elements and the next ones
+            auto values_of = [&](int d) { ldmatrix_x4_trans(chunk_at(sv, h0 + h, d + mat_chunk), vw[(d >> 1) & 1]); };
+            values_of(0);
+#pragma unroll
+            for (int d = 0; d < MT; d += 2) {
+              if (d + 2 < MT) values_of(d + 2);
+              uint32_t(&words)[4] = vw[(d >> 1) & 1];
+              if (!whole) { words[0] &= mask0; words[1] &= mask1; words[2] &= mask0; words[3] &= mask1; }
+#pragma unroll
+              for (int d2 = 0; d2 < 2; ++d2) {
+                uint32_t a0, a1, a2, a3;
+                q8_word_to_half<T, false>(words[2 * d2], a0, a1);
+                q8_word_to_half<T, false>(words[2 * d2 + 1], a2, a3);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) mma_f16(o[d + d2][r], a0, a1, a2, a3, pf[h][r][0], pf[h][r][1]);
+              }
             }
           }
         }
-        // ---- P^T: exponentials, and times vs_j in fp16
-        const float v_unit = kTopP / v_top;
-        uint32_t pf[HB][NR][2];
-#pragma unroll
-        for (int h = 0; h < HB; ++h) {
-          const float v0 = v_top > 0.f ? vs[h][0] * v_unit : 0.f, v1 = v_top > 0.f ? vs[h][1] * v_unit : 0.f;
-#pragma unroll
-          for (int r = 0; r < NR; ++r) {
-            // a row that has seen nothing yet is referred to 0: its exponentials are 2^-inf = 0
-            const float r0 = m[r][0] == -INFINITY ? 0.f : m[r][0], r1 = m[r][1] == -INFINITY ? 0.f : m[r][1];
-            const float e0 = ex2(s[h][r][0] - r0), e1 = ex2(s[h][r][1] - r1), e2 = ex2(s[h][r][2] - r0), e3 = ex2(s[h][r][3] - r1);
-            l[r][0] += e0 + e2;
-            l[r][1] += e1 + e3;
-            pf[h][r][0] = transpose_8x8(pack_half(e0 * v0, e1 * v0));
-            pf[h][r][1] = transpose_8x8(pack_half(e2 * v1, e3 * v1));
-          }
-        }
-        // ---- O^T += V^T P^T
-        if constexpr (HB == 2) {
-          if (!mbar_wait_warp(full(stage), phase, abort_flag, p.status, kTimeoutRowsConsumer, p.wait_limit_ns)) { failed = true; break; }
-          sv = ring + stage * C::kStageBytes;
-        }
-#pragma unroll
-        for (int h = 0; h < HB; ++h) {
-          // Values of keys in nobody's view may be any bits, NaN among them: zeroed, since 0 * NaN is NaN.  A word holds two
-          // elements of key 2 i (of eight) and two of key 2 i + 1.
-          uint32_t mask0 = 0xffffffffu, mask1 = 0xffffffffu;
-          if (!whole) {
-            auto half = [&](int key) { return in_view(key) ? 0xffffu : 0u; };
-            const int key = key0 + 16 * (h0 + h) + 2 * i4;
-            mask0 = half(key) | half(key + 1) << 16;
-            mask1 = half(key + 8) | half(key + 9) << 16;
-          }
-          uint32_t vw[2][4];  // words of keys 0-7 and 8-15, of 16 elements and the next ones
-          auto values_of = [&](int d) { ldmatrix_x4_trans(chunk_at(sv, h0 + h, d + mat_chunk), vw[(d >> 1) & 1]); };
-          values_of(0);
-#pragma unroll
-          for (int d = 0; d < MT; d += 2) {
-            if (d + 2 < MT) values_of(d + 2);
-            uint32_t(&words)[4] = vw[(d >> 1) & 1];
-            if (!whole) { words[0] &= mask0; words[1] &= mask1; words[2] &= mask0; words[3] &= mask1; }
-#pragma unroll
-            for (int d2 = 0; d2 < 2; ++d2) {
-              uint32_t a0, a1, a2, a3;
-              q8_word_to_half<T, false>(words[2 * d2], a0, a1);
-              q8_word_to_half<T, false>(words[2 * d2 + 1], a2, a3);
-#pragma unroll
-              for (int r = 0; r < NR; ++r) mma_f16(o[d + d2][r], a0, a1, a2, a3, pf[h][r][0], pf[h][r][1]);
-            }
-          }
-        }
+        if (failed) break;
+        if constexpr (HB == 1) advance();
+        advance();
       }
-      if (failed) break;
-      if constexpr (HB == 1) advance();
-      advance();
-    }
+    };
+    if (!apart) walk(std::false_type{});
+    else walk(std::true_type{});
     float unit = v_top * (1.f / kTopP);
 #pragma unroll
     for (int r = 0; r < NR; ++r)

@@ -1,0 +1,111 @@
+"""Attention over an 8-bit cache where the rows that a kernel computes together have little in common: a query that is infinite or not a
+number, queries of very different magnitudes.  What a row gets follows from its own query.
+
+The tolerance is that of the operator's own test (test_gpu_paged_attention_q8.py), with the largest value of the keys in the view of
+each query in place of the largest of the sequence."""
+import math
+
+import pytest
+import torch
+
+import decoder_reference as ref
+from test_gpu_paged_attention_q8 import PagedQ8, both
+
+pytestmark = pytest.mark.gpu
+
+# new tokens and keys of the sequences, query heads, cache heads, head_dim: 4 to 64 rows to a cache head, and chunks
+FORMS = [([(1, 300), (1, 77)], 8, 2, 128), ([(1, 900), (1, 77)], 8, 4, 64), ([(2, 300), (2, 77)], 16, 2, 128), ([(3, 700), (2, 77)], 8, 1, 64),
+         ([(3, 700), (3, 77)], 32, 4, 64), ([(5, 700), (2, 77)], 24, 4, 128), ([(4, 300), (4, 77)], 16, 2, 64), ([(5, 400), (3, 90)], 20, 2, 128),
+         ([(16, 300), (9, 77)], 8, 2, 128), ([(40, 300), (33, 77)], 8, 2, 128), ([(70, 300), (33, 77)], 8, 2, 64)]
+forms = pytest.mark.parametrize("form", FORMS, ids=str)
+
+
+def rows_of(p):
+    """Sequence, first row and new tokens."""
+    at = 0
+    for b, (n, kv) in enumerate(p.lens):
+        yield b, at, n, kv
+        at += n
+
+
+def check(p, out, rows=None):
+    """rows: of tokens and heads, the ones to look at."""
+    from paper_2511_03586_b200 import api
+    assert api.pd_get_device_status() == 0
+    for b, at, n, kv in rows_of(p):
+        q, k, v = p.q[at:at + n], p.k_seq[b], p.v_seq[b]
+        heads, d = q.shape[1:]
+        group = heads // k.shape[1]
+        scale = d ** -0.5
+        want, mag = ref.attention(q, k, v, kv - n, window=p.window, sinks=p.sinks)
+        pos, key = torch.arange(kv - n, kv, device="cuda")[:, None], torch.arange(kv, device="cuda")[None, :]
+        seen = key <= pos
+        if p.window:
+            seen &= (key > pos - p.window) | (key < p.sinks)
+        # the largest value, and the largest key element by element, of what each query sees
+        v_most = torch.where(seen[:, :, None], v.abs().amax(2)[None], 0.0).amax(1).repeat_interleave(group, 1)[:, :, None]
+        e = torch.zeros(n, heads, 1, dtype=torch.float64, device="cuda")
+        for t in range(n):
+            most = torch.where(seen[t][:, None, None], k.abs(), 0.0).amax(0).repeat_interleave(group, 0)
+            e[t] = 6 * 2 ** -11 / 3 ** 0.5 * (q[t].double() * most).pow(2).sum(-1, keepdim=True).sqrt() * scale
+        count = (seen.sum(1).double() + 1)[:, None, None]
+        bound = (2 * 2 ** -11 + 2 ** -10) * mag + 2 ** -8 * want.abs() + e * (mag + want.abs()) + 2 ** -30 * count * v_most + 1e-30
+        off = (out[at:at + n].double() - want).abs() / bound
+        if rows is not None:
+            off = off[rows[at:at + n]]
+        assert bool((off <= 1.0).all()), (b, n, kv, off.nan_to_num(math.inf).max().item())
+
+
+@both
+@forms
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan, 3e38], ids=str)
+def test_a_query_that_is_not_finite_harms_its_own_row_only(value, form, dtype):
+    """Bit for bit: nothing that the others' results are made of may know of it.  (3e38: finite, its scores are not.)"""
+    lens, *heads = form
+    p = PagedQ8(lens, *heads, 16, seed=31, dtype=dtype)
+    want = p.attend()
+    p.check(want)
+    bad = torch.zeros(p.q.shape[:2], dtype=torch.bool, device="cuda")
+    bad[0, 1] = True
+    if len(p.q) > 2:
+        bad[-1, 0] = bad[len(p.q) // 2, -1] = True
+    p.q[bad] = torch.where(torch.arange(heads[2], device="cuda") % 7 == 3, value, p.q[bad].float()).bfloat16()
+    got = p.attend()
+    assert torch.equal(got[~bad], want[~bad])
+
+
+@both
+@forms
+@pytest.mark.parametrize("power", [28, 40, 100])
+def test_queries_of_different_magnitudes(power, form, dtype):
+    """One row 2^power times as large as the others, and one as much smaller.  (The large one's scores are beyond what the operator takes: nothing is
+    asked of its own result.)"""
+    lens, *heads = form
+    p = PagedQ8(lens, *heads, 16, seed=32, dtype=dtype)
+    large = torch.zeros(p.q.shape[:2], dtype=torch.bool, device="cuda")
+    large[0, 0] = True
+    p.q[0, 0] *= 2.0 ** power
+    p.q[-1, -1] *= 2.0 ** -power
+    check(p, p.attend(), ~large)
+
+
+@both
+@forms
+def test_queries_of_zero_beside_others(form, dtype):
+    lens, *heads = form
+    p = PagedQ8(lens, *heads, 16, seed=33, dtype=dtype)
+    p.q[0, 0] = 0
+    p.q[-1, 1:] = 0
+    check(p, p.attend())
+
+
+@both
+@forms
+@pytest.mark.parametrize("factor", [2.0 ** -60, 2.0 ** 60])
+def test_scales_of_keys_far_from_one(factor, form, dtype):
+    lens, *heads = form
+    for block in (4, 16):
+        p = PagedQ8(lens, *heads, 16, block=block, seed=38, dtype=dtype, q_gain=1 / factor)
+        p.k_scale *= factor
+        p.k_seq = [k * factor for k in p.k_seq]
+        check(p, p.attend())
