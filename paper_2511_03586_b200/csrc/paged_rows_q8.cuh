@@ -15,7 +15,7 @@
 //      have a power each, so that a row's queries are off by 2^-28 of its own largest at most, whatever the others hold.
 //   S: fp32, times ks_j.
 //   P: exponentials, fp32, times vs_j and a power of two that keeps them below 2^15, rounded to fp16 (2^-11 of each; what is
-//      2^-26 and less of the largest is off by up to 2^-36 of that).  The power follows the largest vs_j that the warp has met.
+//      2^-24 and less of the largest is off by up to 2^-35 of that).  The power follows the largest vs_j that the row has seen.
 //   O: fp32 sums.  The row sums of the exponentials are fp32, too, and of the unrounded ones.
 //
 // A producer warp copies key tiles by TMA, one box per page and tensor, and their scales with one 4-byte copy per block; K (with
@@ -42,6 +42,7 @@ constexpr int kKeys = 32;        // of a tile, per warp
 constexpr int kConsumers = 4;    // warps
 constexpr int kThreads = 32 * (kConsumers + 1);
 constexpr float kRaise = 4.f;    // powers of two by which a score may exceed the reference
+constexpr float kLift = 90.f;    // 2^(kRaise + kLift) times the keys that there can be is in fp32's range
 constexpr float kTopP = 2048.f;  // 2^(15 - kRaise): the largest vs_j times the power of two that goes with P
 
 // H cache heads side by side, WK warps that share a tile's keys, WR that share the rows; NR groups of 8 rows to a warp.
@@ -58,7 +59,7 @@ struct Q8Config {
   static constexpr bool kLean = NR > 2;
   static constexpr int kQ = kLean ? kConsumers * NR * (D / 16) * 256 : 0;
   static constexpr int kExchange = WK > 1 ? H * WR * (WK / 2) * 512 * (D / 16 + 1) : 0;  // half the warps' results for 8 rows
-  static constexpr int kRowBytes = kGroupRows * 4;      // a float for each of a warp's rows
+  static constexpr int kRowBytes = 2 * kGroupRows * 4;  // two floats for each of a warp's rows
   static constexpr int kControl = 256 /*barriers*/ + kConsumers * kRowBytes;
   static constexpr int kPerCta = 113 * 1024 - kControl - 1024 /*alignment*/;             // two CTAs per SM
   static constexpr int kFit = (kPerCta - kExchange - kQ) / (kStageBytes + kScaleBytes);
@@ -85,6 +86,15 @@ __device__ __forceinline__ void arrive_after_copies(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// The power of two above v, within what fp32 has as a power of two times kTopP; 0 for 0.
+__device__ __forceinline__ float power_above(float v) {
+  return v > 0.f ? __uint_as_float(min(max((__float_as_uint(v) >> 23) + 1u, 27u), 254u) << 23) : 0.f;
+}
+// How many powers of two `own` is below `top`, as far as a sum of exponentials can be raised by; all of them for 0.
+__device__ __forceinline__ float lift(float top, float own) {
+  return own > 0.f ? fminf((float)((int)(__float_as_uint(top) >> 23) - (int)(__float_as_uint(own) >> 23)), kLift) : kLift;
+}
+
 template <pd_dtype T, int D, int NR, int H, int WK, int WR>
 __global__ void __launch_bounds__(kThreads, 2)
 paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const Params p,
@@ -103,6 +113,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + (bars - smem_u32(smem_raw)) + 128);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto row_power = [&](int r) { return bars + 256u + (uint32_t)(warp * C::kRowBytes + 4 * r); };  // of a consumer warp's row: what its scores still need
+  auto row_top = [&](int r) { return row_power(C::kGroupRows + r); };  // a power of two, at least the largest vs_j that it has seen
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) { mbar_init(full(s), 1 + 32); mbar_init(empty(s), kConsumers); }
@@ -259,7 +270,10 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
       __syncwarp();
 #pragma unroll
       for (int r = 0; r < NR; ++r)
-        if (i4 == 0) st_shared_f32(row_power(8 * r + g), __uint_as_float((uint32_t)(127 + middle - shift[r]) << 23));
+        if (i4 == 0) {
+          st_shared_f32(row_power(8 * r + g), __uint_as_float((uint32_t)(127 + middle - shift[r]) << 23));
+          st_shared_f32(row_top(8 * r + g), 0.f);
+        }
       __syncwarp();
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
@@ -294,7 +308,10 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
     float m[NR][2], l[NR][2];  // references (in powers of two), this lane's part of the sums
 #pragma unroll
     for (int r = 0; r < NR; ++r) { m[r][0] = m[r][1] = -INFINITY; l[r][0] = l[r][1] = 0.f; }
-    float v_top = 0.f;  // a power of two, at least the largest vs_j so far; O is in units of v_top / kTopP
+    // O is in units of 1 / v_unit: kTopP over a power of two that is at least the largest vs_j that a row has seen so far (0: none).  Rows
+    // differ in what they see, so each has such a power of its own (row_top, in shared memory; their smallest: least_top), and its reference
+    // lies below its largest score by what its own is below the warp's: the products then fill fp16's range for every row.
+    float v_unit = 0.f, least_top = 0.f;
 
     bool failed = false;
     const int end = min(w.end, kt.n);
@@ -404,7 +421,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
           float v_most = fmaxf(vs[0][0], vs[0][1]);
           if constexpr (HB == 2) v_most = fmaxf(v_most, fmaxf(vs[1][0], vs[1][1]));
           float mx[NR][2];
-          bool raise = v_most > v_top;
+          bool raise = v_most > least_top;
 #pragma unroll
           for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -414,27 +431,38 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
               raise |= mx[r][e] > m[r][e] + kRaise;  // also the first finite score of a row (m = -inf)
             }
           if (__any_sync(0xffffffffu, raise)) {
-            const float most = warp_max(v_most);
-            float down = 1.f;
-            if (most > v_top) {
-              // the next power of two, within what fp32 has as a power of two times kTopP
-              const float top = __uint_as_float(min(max((__float_as_uint(most) >> 23) + 1u, 27u), 254u) << 23);
-              down = v_top / top;
-              v_top = top;
-            }
+            const float top0 = v_unit > 0.f ? kTopP / v_unit : 0.f, top1 = fmaxf(top0, power_above(warp_max(v_most)));
+            const float down = top1 > 0.f ? top0 / top1 : 1.f;
+            v_unit = top1 > 0.f ? kTopP / top1 : 0.f;
+            least_top = INFINITY;
+            __syncwarp();  // (what was written here the last time is there)
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
               float alpha[2];
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                float top = mx[r][e];
+                float top = mx[r][e], seen = 0.f;
 #pragma unroll
-                for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                const bool up = top > m[r][e] + kRaise;
-                alpha[e] = up ? ex2(m[r][e] - top) : 1.f;
-                if (up) m[r][e] = top;
+                for (int h = 0; h < HB; ++h)
+#pragma unroll
+                  for (int x = 0; x < 2; ++x) seen = s[h][r][e + 2 * x] > -INFINITY ? fmaxf(seen, vs[h][x]) : seen;
+#pragma unroll
+                for (int x = 4; x < 32; x *= 2) {
+                  top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                  seen = fmaxf(seen, __shfl_xor_sync(0xffffffffu, seen, x));
+                }
+                const uint32_t at = row_top(8 * r + 2 * i4 + e);
+                const float own0 = ld_shared_f32(at), own1 = fmaxf(own0, power_above(seen));
+                const float lift0 = lift(top0, own0), lift1 = lift(top1, own1), peak = m[r][e] + lift0;
+                float ref = lift1 == lift0 ? m[r][e] : peak - lift1;
+                if (top > peak + kRaise) ref = top - lift1;
+                alpha[e] = ref == m[r][e] ? 1.f : ex2(m[r][e] - ref);
+                m[r][e] = ref;
                 l[r][e] *= alpha[e];
                 alpha[e] *= down;
+                least_top = fminf(least_top, own1);
+                __syncwarp();
+                if (g == 0) st_shared_f32(at, own1);
               }
 #pragma unroll
               for (int d = 0; d < MT; ++d) {
@@ -443,11 +471,10 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
             }
           }
           // ---- P^T: exponentials, and times vs_j in fp16
-          const float v_unit = kTopP / v_top;
           uint32_t pf[HB][NR][2];
 #pragma unroll
           for (int h = 0; h < HB; ++h) {
-            const float v0 = v_top > 0.f ? vs[h][0] * v_unit : 0.f, v1 = v_top > 0.f ? vs[h][1] * v_unit : 0.f;
+            const float v0 = vs[h][0] * v_unit, v1 = vs[h][1] * v_unit;
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
               // a row that has seen nothing yet is referred to 0: its exponentials are 2^-inf = 0
@@ -501,7 +528,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
     };
     if (!apart) walk(std::false_type{});
     else walk(std::true_type{});
-    float unit = v_top * (1.f / kTopP);
+    float unit = v_unit > 0.f ? 1.f / v_unit : 0.f;
 #pragma unroll
     for (int r = 0; r < NR; ++r)
 #pragma unroll

@@ -1,8 +1,9 @@
 """Attention over an 8-bit cache where the rows that a kernel computes together have little in common: a query that is infinite or not a
-number, queries of very different magnitudes.  What a row gets follows from its own query.
+number, queries of very different magnitudes, values of very different magnitudes that only some of the rows see.  What a row gets follows
+from its own query and from the keys in its own view.
 
 The tolerance is that of the operator's own test (test_gpu_paged_attention_q8.py), with the largest value of the keys in the view of
-each query in place of the largest of the sequence."""
+each query in place of the largest of the sequence; in the kernel for chunks, where keys of several scales share 32 positions, of those 32."""
 import math
 
 import pytest
@@ -18,6 +19,7 @@ FORMS = [([(1, 300), (1, 77)], 8, 2, 128), ([(1, 900), (1, 77)], 8, 4, 64), ([(2
          ([(3, 700), (3, 77)], 32, 4, 64), ([(5, 700), (2, 77)], 24, 4, 128), ([(4, 300), (4, 77)], 16, 2, 64), ([(5, 400), (3, 90)], 20, 2, 128),
          ([(16, 300), (9, 77)], 8, 2, 128), ([(40, 300), (33, 77)], 8, 2, 128), ([(70, 300), (33, 77)], 8, 2, 64)]
 forms = pytest.mark.parametrize("form", FORMS, ids=str)
+row_forms = pytest.mark.parametrize("form", FORMS[:9], ids=str)
 
 
 def rows_of(p):
@@ -28,8 +30,8 @@ def rows_of(p):
         at += n
 
 
-def check(p, out, rows=None):
-    """rows: of tokens and heads, the ones to look at."""
+def check(p, out, rows=None, around=1):
+    """rows: of tokens and heads, the ones to look at.  around: aligned positions that share their largest key and value."""
     from paper_2511_03586_b200 import api
     assert api.pd_get_device_status() == 0
     for b, at, n, kv in rows_of(p):
@@ -42,11 +44,16 @@ def check(p, out, rows=None):
         seen = key <= pos
         if p.window:
             seen &= (key > pos - p.window) | (key < p.sinks)
+        near = seen
+        if around > 1:
+            whole = torch.zeros(n, -(-kv // around) * around, dtype=torch.bool, device="cuda")
+            whole[:, :kv] = seen
+            near = whole.unflatten(1, (-1, around)).any(-1).repeat_interleave(around, 1)[:, :kv]
         # the largest value, and the largest key element by element, of what each query sees
-        v_most = torch.where(seen[:, :, None], v.abs().amax(2)[None], 0.0).amax(1).repeat_interleave(group, 1)[:, :, None]
+        v_most = torch.where(near[:, :, None], v.abs().amax(2)[None], 0.0).amax(1).repeat_interleave(group, 1)[:, :, None]
         e = torch.zeros(n, heads, 1, dtype=torch.float64, device="cuda")
         for t in range(n):
-            most = torch.where(seen[t][:, None, None], k.abs(), 0.0).amax(0).repeat_interleave(group, 0)
+            most = torch.where(near[t][:, None, None], k.abs(), 0.0).amax(0).repeat_interleave(group, 0)
             e[t] = 6 * 2 ** -11 / 3 ** 0.5 * (q[t].double() * most).pow(2).sum(-1, keepdim=True).sqrt() * scale
         count = (seen.sum(1).double() + 1)[:, None, None]
         bound = (2 * 2 ** -11 + 2 ** -10) * mag + 2 ** -8 * want.abs() + e * (mag + want.abs()) + 2 ** -30 * count * v_most + 1e-30
@@ -109,3 +116,56 @@ def test_scales_of_keys_far_from_one(factor, form, dtype):
         p.k_scale *= factor
         p.k_seq = [k * factor for k in p.k_seq]
         check(p, p.attend())
+
+
+def scale_values(p, b, first, last, factor):
+    """The values of the blocks of sequence b that lie in [first, last) times `factor`."""
+    for blk in range(first // p.block, -(-last // p.block)):
+        page, in_page = int(p.table[b, blk * p.block // p.page]), blk % (p.page // p.block)
+        p.v_scale[page, :, in_page] *= factor
+        p.v_seq[b][blk * p.block:(blk + 1) * p.block] *= factor
+
+
+def later_values(form, block, dtype):
+    """The last token's values are 2^30 times the others': no token in front of it sees them."""
+    lens, *heads = form
+    p = PagedQ8(lens, *heads, 32, block=block, seed=34, dtype=dtype)
+    for b, _, n, kv in rows_of(p):
+        scale_values(p, b, kv - 1, kv, 2.0 ** 30)
+    return p
+
+
+def earlier_values(form, block, window, sinks, factor, dtype):
+    """Values `factor` times the others' that the first new tokens see and that have left the window of the last ones."""
+    lens, *heads = form
+    p = PagedQ8(lens, *heads, 32, block=block, seed=35, window=window, sinks=sinks, dtype=dtype)
+    for b, _, n, kv in rows_of(p):
+        first = max(kv - n - window + 1, 0)     # of the first new token's window
+        last = max(kv - window + 1, 0)          # of the last one's
+        if last - first > block:
+            scale_values(p, b, first, first + (last - first) // 2, factor)
+        elif last > first and block == 1:
+            scale_values(p, b, first, first + 1, factor)
+    return p
+
+
+blocks = pytest.mark.parametrize("block", [1, 16, 32])
+windows = pytest.mark.parametrize("block,window,sinks", [(1, 64, 0), (1, 40, 3), (16, 100, 0), (32, 64, 5), (32, 200, 0)])
+factors = pytest.mark.parametrize("factor", [2.0 ** 30, 2.0 ** 90])
+
+
+@both
+@row_forms
+@blocks
+def test_values_that_later_tokens_bring(block, form, dtype):
+    p = later_values(form, block, dtype)
+    check(p, p.attend())
+
+
+@both
+@row_forms
+@windows
+@factors
+def test_values_in_front_of_later_tokens_windows(factor, block, window, sinks, form, dtype):
+    p = earlier_values(form, block, window, sinks, factor, dtype)
+    check(p, p.attend())
