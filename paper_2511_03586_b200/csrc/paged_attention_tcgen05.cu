@@ -454,8 +454,8 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
       const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16);
       const uint32_t t_o = t_lane + C::kColO + s * D;
       float m = -INFINITY, l = 0.f;
-      // 8-bit caches: O is in units of 2^unit, at least the largest scale of values so far; P carries kOffset powers of two more,
-      // so that what fp16 loses of small exponentials is below 2^-32 of the largest
+      // 8-bit caches: O is in units of 2^unit, more than the largest scale of values that the row has seen so far; P carries kOffset powers of
+      // two more, so that what fp16 loses of small exponentials is below 2^-30 of the largest
       float unit = -1e30f;
       uint32_t done = 0;  // blocks of this slot
       bool ok = true;
@@ -502,9 +502,10 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
           scale[0] = fmaxf(k.x * row_scale, 1.17549435e-38f);  // (-inf times it stays -inf)
           scale[1] = fmaxf(k.y * row_scale, 1.17549435e-38f);
           mx = fmaxf(fmaxf(mx4[0], mx4[1]) * scale[0], fmaxf(mx4[2], mx4[3]) * scale[1]);
-          shift[0] = v.x;
-          shift[1] = v.y;
-          grown = fmaxf(v.x, v.y) > unit;
+          // (a half that this row sees nothing of does not count)
+          shift[0] = fmaxf(mx4[0], mx4[1]) > -INFINITY ? v.x : -INFINITY;
+          shift[1] = fmaxf(mx4[2], mx4[3]) > -INFINITY ? v.y : -INFINITY;
+          grown = fmaxf(shift[0], shift[1]) > unit;
         } else {
           mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * p.scale_log2e;
         }
@@ -513,7 +514,7 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
           float alpha = raise ? ex2(m - mx) : 1.f;
           if (raise) m = mx;
           l *= alpha;
-          if (grown) {  // (all rows alike)
+          if (grown) {
             const float larger = ceilf(fmaxf(shift[0], shift[1])) + 1.f;
             alpha *= ex2(unit - larger);
             unit = larger;

@@ -169,3 +169,23 @@ def test_values_that_later_tokens_bring(block, form, dtype):
 def test_values_in_front_of_later_tokens_windows(factor, block, window, sinks, form, dtype):
     p = earlier_values(form, block, window, sinks, factor, dtype)
     check(p, p.attend())
+
+
+chunk_forms = pytest.mark.parametrize("form", FORMS[9:] + [([(200, 1000), (70, 99)], 8, 1, 128), ([(300, 700), (129, 129), (1, 40)], 4, 4, 64)], ids=str)
+
+
+@both
+@chunk_forms
+@blocks
+def test_values_that_later_tokens_of_a_chunk_bring(block, form, dtype):
+    p = later_values(form, block, dtype)
+    check(p, p.attend(), around=32 if block < 32 else 1)
+
+
+@both
+@chunk_forms
+@windows
+@factors
+def test_values_in_front_of_the_windows_of_a_chunks_last_tokens(factor, block, window, sinks, form, dtype):
+    p = earlier_values(form, block, window, sinks, factor, dtype)
+    check(p, p.attend(), around=32 if block < 32 else 1)
