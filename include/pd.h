@@ -530,9 +530,11 @@ pd_status pd_rope_kv_cache_append(const pd_paged_attention_desc* desc, const pd_
  * a power of two (off by at most 2^-27 of the query's largest element, whatever the others
  * hold), scores, softmax statistics and sums are fp32; the exponentials (with the
  * scales of the values) are rounded to fp16 for the second product, and so are, where chunks of
- * many rows meet several scales within 32 tokens, the elements times their scales.  A value's
- * share of a result is exact to fp16's 2^-11 as long as its weight times its scale is above
- * 2^-21 of the largest scale of a value in view, and off by 2^-30 of the largest value below. */
+ * many rows meet several scales within 32 tokens, the elements times their scales: by 2^-11 of themselves,
+ * or 2^-31 of the largest key or value that any query of the call sees among the 32.
+ * A value's share of a result is exact to fp16's 2^-11 as long as its weight times its scale is above
+ * 2^-19 of the largest scale of a value in its query's view (and, there, in the same 32 tokens as one in view),
+ * and off by 2^-30 of the largest value below. */
 size_t pd_attention_paged_q8_workspace_bytes(const pd_paged_attention_desc* desc);
 pd_status pd_attention_paged_q8_fwd(const pd_paged_attention_desc* desc, const pd_cache_scales* scales, const void* q,
                                     const void* k_cache, const void* v_cache, const int32_t* block_table,

@@ -170,9 +170,10 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
 // A stored byte is exact in fp16.  (Of int8, bytes 0 and 2 of a word become one register and 1 and 3 the other: elements 1 and 2 of
 // every four change places, in K as in Q, and in V as in O, where they change back.)  Where the warp's 32 keys share a scale (blocks of 32 tokens and more, usually) that is what goes
 // into the product, and the scale goes with the group of 32 keys: to the softmax, which multiplies the group's scores by it, and for
-// values adds its logarithm to the exponents and takes it out of the sums.  Where they have several, the elements are
-// multiplied by their scale over the power of two below the largest one (as a high and a low fp16, so that the product is
-// rounded once, 2^-12 of it at most), and the power of two goes with the group.
+// values adds its logarithm to the exponents and takes it out of the sums.  Where they have several (blocks of 16 tokens and less), the
+// elements are multiplied by their scale over the power of two below the largest one that any row sees (as a high and a low fp16, so that
+// the product is rounded once, by 2^-11 of it at most), and the power of two goes with the group.  The products take up fp16's range to
+// the top, 448 x 128: a scale that is a small part of the group's largest is then off by 2^-31 of that.
 //   Instructions per tile and warp: 600 or 1000, where the softmax of the two slots takes 3300 of a scheduler's.  (Elements times their
 //   scales in fp32, rounded to bf16, took 1800, and 4 x 2048 tokens over up to 16384 keys 2033 us.)
 // factors: of the last four tiles, each 4 scales of keys and 4 logarithms of scales of values, as floats.
@@ -191,6 +192,7 @@ __device__ __forceinline__ void convert_16(uint4 v, uint32_t (&out)[8]) {
     q8_word_to_half<T, T != PD_I8>(w[c], out[2 * c], out[2 * c + 1]);
   }
 }
+constexpr uint32_t kHeadroom = 6;  // powers of two: the largest element times 2^(1 + 6) is in fp16's range
 template <int D, typename Cache>
 __device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& p, const KeyTiles& kt, int kvh, int b, int begin, int end,
                                               int warp, uint32_t ring, uint32_t bars, uint32_t factors, volatile int* abort_flag) {
@@ -265,10 +267,10 @@ __device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& 
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(scale[kv]));
-        uniform[kv] = __all_sync(0xffffffffu, !((there >> lane) & 1u) || __float_as_uint(scale[kv]) == most);
-        const uint32_t exponent = min(max(most >> 23, 1u), 253u);
-        factor[kv] = uniform[kv] ? __uint_as_float(most) : __uint_as_float(exponent << 23);
-        const float rest = scale[kv] * __uint_as_float((254u - exponent) << 23);  // below 2
+        uniform[kv] = most == 0;
+        const uint32_t exponent = min(max(most >> 23, 1u + kHeadroom), 253u);
+        factor[kv] = uniform[kv] ? 0.f : __uint_as_float((exponent - kHeadroom) << 23);
+        const float rest = scale[kv] * __uint_as_float((254u + kHeadroom - exponent) << 23);  // below 2^(kHeadroom + 1)
         const __half high = __float2half_rn(rest), low = __float2half_rn(rest - __half2float(high));
         pair[kv] = (uint32_t)__half_as_ushort(high) | (uint32_t)__half_as_ushort(low) << 16;
       }

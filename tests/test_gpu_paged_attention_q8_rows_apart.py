@@ -10,7 +10,7 @@ import pytest
 import torch
 
 import decoder_reference as ref
-from test_gpu_paged_attention_q8 import PagedQ8, both
+from test_gpu_paged_attention_q8 import PagedQ8, both, quantised
 
 pytestmark = pytest.mark.gpu
 
@@ -30,8 +30,9 @@ def rows_of(p):
         at += n
 
 
-def check(p, out, rows=None, around=1):
-    """rows: of tokens and heads, the ones to look at.  around: aligned positions that share their largest key and value."""
+def check(p, out, rows=None, around=1, each_key=True):
+    """rows: of tokens and heads, the ones to look at.  around: aligned positions that share their largest key and value.  each_key: what a
+    key may be off by below fp16's normal numbers counts for every key; else once, where the other keys' products are below it."""
     from paper_2511_03586_b200 import api
     assert api.pd_get_device_status() == 0
     for b, at, n, kv in rows_of(p):
@@ -55,7 +56,7 @@ def check(p, out, rows=None, around=1):
         for t in range(n):
             most = torch.where(near[t][:, None, None], k.abs(), 0.0).amax(0).repeat_interleave(group, 0)
             e[t] = 6 * 2 ** -11 / 3 ** 0.5 * (q[t].double() * most).pow(2).sum(-1, keepdim=True).sqrt() * scale
-        count = (seen.sum(1).double() + 1)[:, None, None]
+        count = (seen.sum(1).double() + 1)[:, None, None] if each_key else 1.0
         bound = (2 * 2 ** -11 + 2 ** -10) * mag + 2 ** -8 * want.abs() + e * (mag + want.abs()) + 2 ** -30 * count * v_most + 1e-30
         off = (out[at:at + n].double() - want).abs() / bound
         if rows is not None:
@@ -189,3 +190,30 @@ def test_values_that_later_tokens_of_a_chunk_bring(block, form, dtype):
 def test_values_in_front_of_the_windows_of_a_chunks_last_tokens(factor, block, window, sinks, form, dtype):
     p = earlier_values(form, block, window, sinks, factor, dtype)
     check(p, p.attend(), around=32 if block < 32 else 1)
+
+
+@both
+@forms
+@pytest.mark.parametrize("block", [8, 16])
+def test_weights_on_the_smaller_scales_of_32_keys(block, form, dtype):
+    """Every other block's values are 2^24 times smaller, and its keys get all of the weight: their scores are at least 32 and the others' at
+    most -32, so that these, 2^24 times as large and e^-64 < 2^-92 times as heavy, add less than 2^-68 of the result.  What fp16 loses is then
+    that of a few keys of weight one, not of every key."""
+    lens, *heads = form
+    p = PagedQ8(lens, *heads, 32, block=block, seed=36, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(37)
+    d, hk = heads[2], heads[1]
+    for b, _, n, kv in rows_of(p):
+        small = (torch.arange(kv, device="cuda") // block % 2 == 0)[:, None, None]    # (every query sees the first block)
+        keys = torch.where(small, 1.0, -1.0) * (torch.rand(kv, hk, d, generator=g, device="cuda") * 0.5 + 0.75)
+        values = torch.where(small, 2.0 ** -24, 1.0) * torch.randn(kv, hk, d, generator=g, device="cuda")
+        for x, seq, cache, scales in ((keys, p.k_seq, p.k_cache, p.k_scale), (values, p.v_seq, p.v_cache, p.v_scale)):
+            y, scale, seq[b] = quantised(x, block, dtype)
+            for i in range(-(-kv // p.page)):
+                lo, hi, pg = i * p.page, min(kv, (i + 1) * p.page), int(p.table[b, i])
+                cache[pg, :hi - lo] = y[lo:hi]
+                blocks = scale[lo // block:-(-hi // block)]
+                scales[pg, :, :len(blocks)] = blocks.T
+    # scores at most -32 and at least 32: |q k| = sum of d products of at least 0.75 x, divided by sqrt(d)
+    p.q = (torch.rand(p.q.shape, generator=g, device="cuda") * 0.5 + 1.0).bfloat16() * (32 / (0.7 * d ** 0.5))
+    check(p, p.attend(), each_key=False)
