@@ -145,8 +145,8 @@ paged_attention_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const __
       const __nv_bfloat16* qr = p.q + (int64_t)(w.seq.q0 + t) * p.ld_q + (int64_t)(w.kvh * p.group + r % p.group) * D;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        qf[k][i] = __ldg(reinterpret_cast<const uint32_t*>(qr + 16 * k + c2));
-        qf[k][2 + i] = __ldg(reinterpret_cast<const uint32_t*>(qr + 16 * k + 8 + c2));
+        qf[k][i] = *reinterpret_cast<const uint32_t*>(qr + 16 * k + c2);
+        qf[k][2 + i] = *reinterpret_cast<const uint32_t*>(qr + 16 * k + 8 + c2);
       }
     }
     float o[D / 8][4];

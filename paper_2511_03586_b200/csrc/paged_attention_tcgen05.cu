@@ -178,10 +178,16 @@ __device__ __forceinline__ void write_rows(const Params& p, const Sequence& seq,
 //   scales in fp32, rounded to bf16, took 1800, and 4 x 2048 tokens over up to 16384 keys 2033 us.)
 // factors: of the last four tiles, each 4 scales of keys and 4 logarithms of scales of values, as floats.
 
-// 16 bytes; a load that stays where it is written (the compiler moves a plain one to where its result is used).
+// 16 bytes; a load that stays where it is written (the compiler moves a plain one to where its result is used).  Not a non-coherent one: the
+// kernel that appends to the cache may have been running when this one started.
 __device__ __forceinline__ uint4 load_now(const uint8_t* from) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(from) : "memory");
+  asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(from) : "memory");
+  return v;
+}
+__device__ __forceinline__ float load_now(const float* from) {
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(from));
   return v;
 }
 template <pd_dtype T>
@@ -233,8 +239,8 @@ __device__ __forceinline__ void convert_tiles(const Cache& cache, const Params& 
     scale[0] = scale[1] = 0.f;
     if (mine) {
       const int64_t at = cache.scales.at(page, kvh, slot);
-      scale[0] = __ldg(cache.scales.k + at);
-      scale[1] = __ldg(cache.scales.v + at);
+      scale[0] = load_now(cache.scales.k + at);
+      scale[1] = load_now(cache.scales.v + at);
     }
   };
   const int64_t lane_at = (int64_t)kvh * cache.head_stride + 16 * chunk;
@@ -428,7 +434,7 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
           uint32_t most = 0;
 #pragma unroll
           for (int c = 0; c < D / 8; ++c) {
-            const uint4 v = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+            const uint4 v = valid ? src[c] : make_uint4(0, 0, 0, 0);
             most = max(most, max(max((v.x << 16) & 0x7fffffffu, v.x & 0x7fff0000u), max((v.y << 16) & 0x7fffffffu, v.y & 0x7fff0000u)));
             most = max(most, max(max((v.z << 16) & 0x7fffffffu, v.z & 0x7fff0000u), max((v.w << 16) & 0x7fffffffu, v.w & 0x7fff0000u)));
           }
@@ -437,17 +443,23 @@ paged_attention_chunk_kernel(const __grid_constant__ Cache cache, const Params p
           row_scale *= __uint_as_float((uint32_t)(127 - shift) << 23);
         }
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          uint4 v = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-          if constexpr (Cache::kBytes) {
-            auto low = [&](uint32_t two) { return __uint_as_float(two << 16) * up; };
-            auto high = [&](uint32_t two) { return __uint_as_float(two & 0xffff0000u) * up; };
-            if constexpr (Cache::kSwapped)
-              v = make_uint4(pack_half(low(v.x), low(v.y)), pack_half(high(v.x), high(v.y)), pack_half(low(v.z), low(v.w)), pack_half(high(v.z), high(v.w)));
-            else
-              v = make_uint4(pack_half(low(v.x), high(v.x)), pack_half(low(v.y), high(v.y)), pack_half(low(v.z), high(v.z)), pack_half(low(v.w), high(v.w)));
+        for (int c0 = 0; c0 < D / 8; c0 += 8) {
+          uint4 raw[8];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) raw[c] = valid ? src[c0 + c] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            uint4 v = raw[c];
+            if constexpr (Cache::kBytes) {
+              auto low = [&](uint32_t two) { return __uint_as_float(two << 16) * up; };
+              auto high = [&](uint32_t two) { return __uint_as_float(two & 0xffff0000u) * up; };
+              if constexpr (Cache::kSwapped)
+                v = make_uint4(pack_half(low(v.x), low(v.y)), pack_half(high(v.x), high(v.y)), pack_half(low(v.z), low(v.w)), pack_half(high(v.z), high(v.w)));
+              else
+                v = make_uint4(pack_half(low(v.x), high(v.x)), pack_half(low(v.y), high(v.y)), pack_half(low(v.z), high(v.z)), pack_half(low(v.w), high(v.w)));
+            }
+            st_shared_v4(dst + (c0 >> 3) * kHalf + (uint32_t)((c ^ (r & 7)) << 4), v);
           }
-          st_shared_v4(dst + (c >> 3) * kHalf + (uint32_t)(((c & 7) ^ (r & 7)) << 4), v);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -827,9 +839,11 @@ paged_attention_chunk_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, 
       const int t = valid ? row / p.group : 0, head = kvh * p.group + (valid ? row % p.group : 0);
       const int pos = seq.pos0 + t;
       const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)(seq.q0 + t) * p.ld_q + (int64_t)head * D);
+      uint4 raw[D / 8];
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c)
-        st_shared_v4(sQ + (uint32_t)r * 128u + (uint32_t)((c ^ (r & 7)) << 4), valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0));
+      for (int c = 0; c < D / 8; ++c) raw[c] = valid ? src[c] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) st_shared_v4(sQ + (uint32_t)r * 128u + (uint32_t)((c ^ (r & 7)) << 4), raw[c]);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);

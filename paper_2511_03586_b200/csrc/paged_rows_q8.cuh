@@ -234,7 +234,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
         const int t = row / p.group;
         return p.q + (int64_t)(w.seq.q0 + t) * p.ld_q + (int64_t)(kvh * p.group + row % p.group) * D + 4 * i4;
       };
-      auto load = [&](const __nv_bfloat16* src, int k) { return __ldg(reinterpret_cast<const uint2*>(src + 16 * k)); };
+      auto load = [&](const __nv_bfloat16* src, int k) { return *reinterpret_cast<const uint2*>(src + 16 * k); };
       // The largest exponent e of the rows goes to 14: times 2^(14 - e), within what fp32 has as a power of two and its reciprocal.  Rows
       // more than 2^kNear apart (one that is infinite or not a number, too) each get a power of their own: the middle one of the
       // reciprocals goes with the scale of the scores, the rest is taken back in each row's scores.
