@@ -24,3 +24,10 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+@pytest.fixture(autouse=True)
+def same_draws_every_time():
+    """Tests that draw from torch's own generator get the same numbers in every run, whatever ran before them."""
+    import torch
+    torch.manual_seed(0)
