@@ -270,10 +270,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
       __syncwarp();
 #pragma unroll
       for (int r = 0; r < NR; ++r)
-        if (i4 == 0) {
-          st_shared_f32(row_power(8 * r + g), __uint_as_float((uint32_t)(127 + middle - shift[r]) << 23));
-          st_shared_f32(row_top(8 * r + g), 0.f);
-        }
+        if (i4 == 0) st_shared_f32(row_power(8 * r + g), __uint_as_float((uint32_t)(127 + middle - shift[r]) << 23));
       __syncwarp();
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
@@ -316,7 +313,12 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
     bool failed = false;
     const int end = min(w.end, kt.n);
     // Compiled twice, so that rows that are not apart, as they hardly ever are, have no instruction for it: in one, 64 x 4096 keys took
-    // 141 us against 135 with 16 rows of 128, 240 against 232 with 32.
+    // 141 us against 135 with 16 rows of 128, 240 against 232 with 32.  Up to 8 rows have the registers for it, and the longer way to the
+    // code costs a first call 2 us.
+    constexpr bool kTwice = NR > 1;
+    // Rows of one power are raised in a path of their own, which is most of what short walks see of it (16 x 2048 keys, 20 rows of 64: 30 against
+    // 32 us); the form of 24 rows of 128, for long walks alone, has no registers to spare (64 x 4096: 203 against 196).
+    constexpr bool kLevel = !(C::kLean && D == 128);
     auto walk = [&](auto own_powers) {
       for (int i = w.begin; i < end; ++i) {
         // (a warp that gives up goes on to the barrier below, if there is one, which tells the others)
@@ -404,7 +406,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
                 if (!in_view(key)) vs[h][e >> 1] = 0.f;
               }
           }
-          if constexpr (own_powers.value) {
+          if (kTwice ? own_powers.value : apart) {
 #pragma unroll
             for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -431,42 +433,66 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
               raise |= mx[r][e] > m[r][e] + kRaise;  // also the first finite score of a row (m = -inf)
             }
           if (__any_sync(0xffffffffu, raise)) {
-            const float top0 = v_unit > 0.f ? kTopP / v_unit : 0.f, top1 = fmaxf(top0, power_above(warp_max(v_most)));
+            const float most = warp_max(v_most), top0 = v_unit > 0.f ? kTopP / v_unit : 0.f, top1 = fmaxf(top0, power_above(most));
             const float down = top1 > 0.f ? top0 / top1 : 1.f;
+            const bool level = __all_sync(0xffffffffu, least_top == top0);  // all rows' powers are the warp's
             v_unit = top1 > 0.f ? kTopP / top1 : 0.f;
-            least_top = INFINITY;
-            __syncwarp();  // (what was written here the last time is there)
+            if (kLevel && __builtin_expect(level && (top1 == top0 || whole || first_pos == last_pos), 1)) {  // and stay so: all see what there is to see here
+              least_top = top1;
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-              float alpha[2];
+              for (int r = 0; r < NR; ++r) {
+                float alpha[2];
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                float top = mx[r][e], seen = 0.f;
+                for (int e = 0; e < 2; ++e) {
+                  float top = mx[r][e];
 #pragma unroll
-                for (int h = 0; h < HB; ++h)
-#pragma unroll
-                  for (int x = 0; x < 2; ++x) seen = s[h][r][e + 2 * x] > -INFINITY ? fmaxf(seen, vs[h][x]) : seen;
-#pragma unroll
-                for (int x = 4; x < 32; x *= 2) {
-                  top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                  seen = fmaxf(seen, __shfl_xor_sync(0xffffffffu, seen, x));
+                  for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                  const bool up = top > m[r][e] + kRaise;
+                  alpha[e] = up ? ex2(m[r][e] - top) : 1.f;
+                  if (up) m[r][e] = top;
+                  l[r][e] *= alpha[e];
+                  alpha[e] *= down;
                 }
-                const uint32_t at = row_top(8 * r + 2 * i4 + e);
-                const float own0 = ld_shared_f32(at), own1 = fmaxf(own0, power_above(seen));
-                const float lift0 = lift(top0, own0), lift1 = lift(top1, own1), peak = m[r][e] + lift0;
-                float ref = lift1 == lift0 ? m[r][e] : peak - lift1;
-                if (top > peak + kRaise) ref = top - lift1;
-                alpha[e] = ref == m[r][e] ? 1.f : ex2(m[r][e] - ref);
-                m[r][e] = ref;
-                l[r][e] *= alpha[e];
-                alpha[e] *= down;
-                least_top = fminf(least_top, own1);
-                __syncwarp();
-                if (g == 0) st_shared_f32(at, own1);
-              }
 #pragma unroll
-              for (int d = 0; d < MT; ++d) {
-                o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
+                for (int d = 0; d < MT; ++d) {
+                  o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
+                }
+              }
+            } else {
+              least_top = INFINITY;
+              __syncwarp();  // (what was written here the last time is there)
+#pragma unroll
+              for (int r = 0; r < NR; ++r) {
+                float alpha[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  float top = mx[r][e], seen = 0.f;
+#pragma unroll
+                  for (int h = 0; h < HB; ++h)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) seen = s[h][r][e + 2 * x] > -INFINITY ? fmaxf(seen, vs[h][x]) : seen;
+#pragma unroll
+                  for (int x = 4; x < 32; x *= 2) {
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                    seen = fmaxf(seen, __shfl_xor_sync(0xffffffffu, seen, x));
+                  }
+                  const uint32_t at = row_top(8 * r + 2 * i4 + e);
+                  const float own0 = level ? top0 : ld_shared_f32(at), own1 = fmaxf(own0, power_above(seen));
+                  const float lift0 = level ? 0.f : lift(top0, own0), lift1 = lift(top1, own1), peak = m[r][e] + lift0;
+                  float ref = lift1 == lift0 ? m[r][e] : peak - lift1;
+                  if (top > peak + kRaise) ref = top - lift1;
+                  alpha[e] = ref == m[r][e] ? 1.f : ex2(m[r][e] - ref);
+                  m[r][e] = ref;
+                  l[r][e] *= alpha[e];
+                  alpha[e] *= down;
+                  least_top = fminf(least_top, own1);
+                  __syncwarp();
+                  if (g == 0) st_shared_f32(at, own1);
+                }
+#pragma unroll
+                for (int d = 0; d < MT; ++d) {
+                  o[d][r][0] *= alpha[0]; o[d][r][1] *= alpha[1]; o[d][r][2] *= alpha[0]; o[d][r][3] *= alpha[1];
+                }
               }
             }
           }
@@ -526,7 +552,7 @@ paged_attention_q8_rows_kernel(const __grid_constant__ CUtensorMap tmap_k, const
         advance();
       }
     };
-    if (!apart) walk(std::false_type{});
+    if (!kTwice || __builtin_expect(!apart, 1)) walk(std::false_type{});
     else walk(std::true_type{});
     float unit = v_unit > 0.f ? 1.f / v_unit : 0.f;
 #pragma unroll
