@@ -14,16 +14,19 @@ bool supported_q8(const pd_paged_attention_desc& d) {
 // Row kernel: up to four warps beside each other take cache heads (the rows of a slot that lie beside each other in the usual
 // layout), as many as divide the heads; the rest of the four share keys, or rows.
 //   17 to 24 rows: tiles of 24 have a quarter less to compute than tiles of 32, but twice the heads to an item, so twice the
-//   partial results at the ends of a CTA's share.  At head_dim 64 they never lose (8 heads, 32 sequences of 4096 keys: 70 against 81 us); at 128
-//   they win where a CTA has some 20 tiles of 128 keys and heads (64 x 4096: 212 against 235 us; 32 x 4096, 28 tiles: 123 against
-//   129; 32 x 2048, 14 tiles: 82 against 78; 16 x 2048: 55 against 47).  Lengths are usually well below max_kv_len, so 32 by that.
-//   65 rows and more: the chunk kernel (64 x 4096 keys, 8 heads of 128: 463 us for anything up to 256 rows, where tiles of
-//   64 rows take 445, of 32 rows 243; 32 x 700: 66 against 73 and 46).
+//   partial results at the ends of a CTA's share.  So 24 where shares are long, counted in tiles of 128 keys and heads (20 rows, 8 heads,
+//   tiles of 24 against 32):
+//     head_dim 64, from 12 on:  64 x 4096 keys (55) 107 against 133 us, 64 x 1024 (14) 45 and 49, 8 x 8192 (14) 42 and 45; but 16 x 2048 (7)
+//       30 and 29, 8 x 1024 (2) 18 and 16
+//     head_dim 128, from 32 on: 64 x 4096 (55) 199 against 222, 32 x 4096 (28) 115 and 121; but 32 x 2048 (14) 76 and 72, 16 x 2048 (7) 53 and 43.
+//       Lengths are usually well below max_kv_len, which alone is known here: hence 32, although 28 full tiles would do.
+//   65 rows and more: the chunk kernel (64 x 4096 keys, 8 heads of 128: 450 us for 68 rows, 476 for 256, where tiles of 64 rows take 428
+//   for 64, of 32 rows 231 for 32).
 Plan plan_q8(const pd_paged_attention_desc& d) {
   Plan pl{};
   const int64_t rows = plan_rows(d);
-  const bool long_shares = plan_keys(d) * d.heads_kv * d.batch >= (int64_t)32 * 128 * 2 * kSms;
-  const bool rows24 = rows > 16 && rows <= 24 && (d.head_dim == 64 || long_shares);
+  const bool long_shares = plan_keys(d) * d.heads_kv * d.batch >= (int64_t)(d.head_dim == 64 ? 12 : 32) * 128 * 2 * kSms;
+  const bool rows24 = rows > 16 && rows <= 24 && long_shares;
   pl.rows_per_tile = rows <= 8 ? 8 : rows <= 16 ? 16 : rows24 ? 24 : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
   if (pl.rows_per_tile > 64) {
     plan_splits(d, pl);
