@@ -94,7 +94,7 @@ inline Scales make_scales(const pd_cache_scales& s, int heads_kv, int page_size)
 
 // Tensor map of one cache: {head_dim, page_size, heads_kv, num_pages} bytes, boxes of `box_rows` slots of `box_heads` heads.  What
 // is fetched beside a box's rows belongs to other heads, which other CTAs read at other times: promotion to 256 bytes fetched
-// twice what rows of 128 need (64 x 1 tokens: 150 against 140 us).
+// twice what rows of 128 need (64 x 1 tokens: 150 us, where the same kernel took 140 without it).
 inline bool make_cache_map_q8(CUtensorMap* map, const void* cache, const pd_paged_attention_desc& d, int box_rows, int box_heads) {
   gemm::EncodeTiledFn fn = gemm::encode_tiled_fn();
   if (!fn) return false;

@@ -21,8 +21,9 @@
 //   warp 12        : producer: looks the pages up and copies K and V tiles by TMA, one box per page, into a ring of four
 //                    32 KiB stages, K and V in turn.
 //   8-bit caches     : warps 12-15 in its place, which load, convert and write the same tiles (convert_tiles).
-//                    (4 chunks of up to 2048 tokens over up to 16384 keys, 32/8 heads of 128, int8: 1141 us, 980 with the
-//                    conversions for free; 8 prompts of up to 2048, 16 heads of 64, window 1024, e4m3: 187 and 173.)
+//                    (4 chunks of up to 2048 tokens over up to 16384 keys, 32/8 heads of 128, int8: 1137 us a single call, 1238 in long
+//                    runs, where the board's power limits the clock; single with the conversions for free 980.  8 prompts of up to 2048,
+//                    16 heads of 64, window 1024, e4m3: 186 single, 178 in long runs, 173 with the conversions for free.)
 // Tensor memory: per slot two score buffers of 64 columns and an output of 128; that is all of it.  Two
 // buffers let the scores of the next block be formed while the current ones are exponentiated: the buffer they take was
 // last read by the product of the block before.  (With one buffer of 128 columns the softmax warps of a slot waited half

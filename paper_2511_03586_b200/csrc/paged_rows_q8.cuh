@@ -24,9 +24,9 @@
 // delivered 4.2 TB/s so.  So the warps take up to four neighbouring heads, and a box has the rows of all of them; where there are fewer
 // heads, warps share the keys of a tile, and more than 16 rows are shared by two or four warps.  A warp keeps a reference maximum of its
 // own, raised when a score exceeds it by 2^4; warps with the same rows meet at the end of a piece.
-//   64 single tokens over 200 to 8192 keys, 32/8 heads of 128, int8: 105 us, 82 % of the copy rate (bf16 cache: 186); the loads alone
-//   97 to 99.  16 x 5 tokens over up to 8192 keys, e4m3: 73 us; there the warps' chains of conversions, products and softmax are what
-//   takes the time, loads alone take 38.
+//   64 single tokens over 200 to 8192 keys, 32/8 heads of 128, int8: 104 us, 81 % of the copy rate (bf16 cache: 186); the loads alone
+//   97 to 99.  16 x 5 tokens over up to 8192 keys, e4m3: 69 us, where the loads alone take 38.  No unit is full there (issue slots 42 %,
+//   tensor cores 32 %, DRAM 29 %): eight warps to an SM do not hide a warp's chain of conversions, products and softmax.
 #pragma once
 
 #include <type_traits>

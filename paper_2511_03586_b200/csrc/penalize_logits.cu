@@ -6,13 +6,13 @@
 //   z = z + bias_ij                                      the last entry of row i's list that names j
 //   z = -inf                                             where row i's mask has bit j cleared
 //
-// Bound: HBM, every logit read once and written once.  A CTA takes a slice of 32 logits a thread of one row, which it loads first; while
-// they are under way it counts the row's history, in a word of shared memory for each of the slice's tokens:
+// Bound: HBM, every logit read once and written once.  A CTA takes a slice of one row, 32 logits a thread (16 where there are few rows), which
+// it loads first; while they are under way it counts the row's history, in a word of shared memory for each of the slice's tokens:
 //   bit 31: occurs in the history;  bits 11 ... 30: times behind the prompt;  bits 0 ... 10: 1 + entry of the bias list
 // The counts are integer sums, the entries a maximum, so neither depends on the order in which threads get there.  Every CTA of a
 // row reads the whole history, from the L2 cache.  A row that changes nothing skips the counting.
-//   256 x 128000 fp32, up to 8000 tokens a row, half of the rows masked: 74 us (3.7 TB/s), 45 without histories and biases.  Other forms: slices half as
-//   long (twice as many looks at the history) 82; several slices to a CTA, their logits copied ahead, 80; a plain copy first
+//   256 x 128000 fp32, up to 8000 tokens a row, half of the rows masked: 68 us in long runs (3.9 TB/s), 45 to 49 without histories and biases.
+//   A single call takes 75.  Other forms, single, when this one took 76: slices half as long (twice as many looks at the history) 82; several slices to a CTA, their logits copied ahead, 80; a plain copy first
 //   and the named tokens mended one by one after it 100; the history shared out over a cluster 150 (half of a text's tokens
 //   belong to few slices, and additions to another CTA's shared memory queue there).
 #include "pd_common.cuh"

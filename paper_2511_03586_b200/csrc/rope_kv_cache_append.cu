@@ -18,7 +18,8 @@
 // long as it has at most 2048 units, and read it again, from the L2 cache, beyond that.  Values are rounded once, from the rotated fp32
 // ones.  A block that held older tokens keeps its scale unless a new token exceeds it; then the older values are rounded again,
 // to the larger step.
-//   8 x up to 2048 tokens, 32/8 heads of 128: 65 us into a bf16 cache (75 % of the copy rate), 76 into an e4m3 cache with blocks of 32 (59 %).
+//   8 x up to 2048 tokens, 32/8 heads of 128, in long runs: 67 us into a bf16 cache (73 % of the copy rate), 73 into an e4m3 cache with blocks
+//   of 32 (61 %).
 #include "cache_q8.cuh"
 
 namespace pd {
@@ -553,7 +554,8 @@ extern "C" pd_status pd_rope_kv_cache_append(const pd_paged_attention_desc* desc
   if (scales) {
     p.scales = paged::make_scales(*scales, d.heads_kv, d.page_size);
     p.k_scale = scales->k_scale; p.v_scale = scales->v_scale;
-    // as many warps to a head as hold a block's units, while there are heads and tokens for the other warps
+    // as many warps to a head as hold a whole block's units between the two passes (by the block alone: with few heads and short blocks, or
+    // few new tokens in long ones, some of a CTA's warps have nothing to do)
     p.warps_a_head = 1;
     while (p.warps_a_head < kWarps && (int64_t)scales->block * (d.head_dim / kUnit) > (int64_t)kGroup * p.warps_a_head) p.warps_a_head *= 2;
     const int heads_a_cta = kWarps / p.warps_a_head;
